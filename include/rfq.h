@@ -464,6 +464,142 @@ RFQ_API rfq_status rfq_linear_noalloc(const rfq_qtensor *xq, const rfq_qtensor *
  * RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
 RFQ_API rfq_status rfq_dequant(const rfq_qtensor *q, void *out, int32_t out_dtype, void *stream);
 
+/* ---- Serving: one attention step on a 4-bit cache ------------------------
+ * The entry points below carry a decoding step next to the linear layers
+ * above: slots for the new tokens (rfq_slot_map), rotary positions
+ * (rfq_rope), keys and values into a paged cache in MXFP4 or HiF4
+ * (rfq_kv_append, rfq_kv_read), attention over that cache
+ * (rfq_kv_attention), and products of a few tokens with a 4-bit weight
+ * (rfq_matvec).  The paper's linear layer has no counterpart for them; the
+ * formats are its own (Sec. 3.2.2, Sec. 3.3).  Arrays of int32, int64 and
+ * fp32 need their natural alignment only; every other device pointer must be
+ * 16-byte aligned, as above. */
+
+/* Block tables, slot maps and positions of one serving step, built on the
+ * GPU from the requests' lengths in one launch.  A cache is split into pages
+ * of page_size tokens; request r holds its tokens in the pages
+ * block_table[r][0 .. ceil(cached[r] / page_size)).  Free pages are a stack,
+ * free_pages[0 .. *free_in).
+ *   cached, added: device int32 [requests]: tokens in the cache, and tokens to
+ *     add (> 0) or to drop from the end (< 0; more than cached drops all).
+ *     after = max(cached + added, 0).
+ *   1. Pages given back (those past ceil(after / page_size)) go on top of the
+ *      stack, requests in order, each request's in the order of its table.
+ *      Their table entries stay as they were.
+ *   2. Pages wanted are taken from the top, requests in order.  The first
+ *      request whose pages are not all there, and every later one that wants
+ *      any, gets none: it is not served.  Requests that want none are served.
+ *      A request whose pages exceed table_width (or whose cached is negative
+ *      or exceeds it) is not served either, takes and gives nothing, and the
+ *      device status becomes RFQ_ERR_SHAPE.
+ *   3. block_table (device int32 [requests][table_width], in place) gets the
+ *      pages taken; free_out the stack's new height; lengths [requests] after,
+ *      or cached where a request was not served.
+ *   4. token_start [requests + 1]: prefix sums of max(added, 0), the rows of
+ *      the step's tokens.  For token t = token_start[r] + i, positions[t] =
+ *      cached[r] + i, and slots[t] = page * page_size + position % page_size,
+ *      or -1 where request r was not served.  slots and positions hold
+ *      `tokens` entries; those past token_start[requests] are -1 and 0 (a
+ *      fixed-size step for a CUDA graph), and more tokens than that set the
+ *      device status RFQ_ERR_SHAPE.
+ * free_pages holds free_capacity entries; pages given back past it are
+ * dropped (device status RFQ_ERR_SHAPE).  free_out may be free_in and lengths
+ * may be cached; no other arrays overlap.  0 <= requests <= 8192,
+ * page_size >= 1, table_width >= 1, tokens >= 0.  workspace: device, 256
+ * bytes zeroed by the caller once, for the device status
+ * (rfq_workspace_status).
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_slot_map(const int32_t *cached, const int32_t *added, int32_t requests, int32_t page_size,
+                                int32_t *block_table, int32_t table_width, int32_t *free_pages,
+                                int32_t free_capacity, const int32_t *free_in, int32_t *free_out, int32_t *lengths,
+                                int32_t *token_start, int64_t *slots, int32_t *positions, int64_t tokens,
+                                void *workspace, void *stream);
+
+/* How the two elements of a rotary pair i of P lie in a head:
+ *   RFQ_ROPE_HALF         elements i and i + P
+ *   RFQ_ROPE_INTERLEAVED  elements 2i and 2i + 1 */
+typedef enum { RFQ_ROPE_HALF = 0, RFQ_ROPE_INTERLEAVED = 1 } rfq_rope_pairing;
+
+/* Rotary positions with several axes (time, height, width of images and
+ * video; one axis for text).  For token t and pair i of every head,
+ *     angle = positions[axis_of[i]][t] * inv_freq[i]
+ *     (a, b) -> (a cos angle - b sin angle, b cos angle + a sin angle)
+ * and with inverse != 0 by -angle: the gradient of the rotation.  Elements
+ * past 2 pairs pass through unchanged, as does a pair whose axis_of is not in
+ * [0, axes).
+ *   x, out: device [tokens][heads][head_dim] of dtype (RFQ_OUT_F32 or
+ *     RFQ_OUT_BF16) with the given strides in elements between tokens and
+ *     heads (so queries and keys of a packed projection need no copy); out may
+ *     be x with the same strides, and does not overlap it otherwise.  Strides
+ *     and head_dim that are multiples of 16 bytes are read and written 16
+ *     bytes at a time, others element by element.
+ *   positions: device int32 [axes][tokens]; inv_freq: device fp32 [pairs];
+ *   axis_of: device int32 [pairs].  The angle is reduced in fp64, so any
+ *     int32 position keeps fp32 accuracy; the rotation is fp32, rounded once.
+ * 1 <= head_dim <= 1024, 1 <= pairs <= head_dim / 2, axes >= 1, tokens >= 0,
+ * heads >= 1.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_rope(const void *x, int64_t x_token_stride, int64_t x_head_stride, void *out,
+                            int64_t out_token_stride, int64_t out_head_stride, int32_t dtype, int64_t tokens,
+                            int32_t heads, int32_t head_dim, const int32_t *positions, int32_t axes,
+                            const float *inv_freq, const int32_t *axis_of, int32_t pairs, int32_t pairing,
+                            int32_t inverse, void *stream);
+
+/* A paged cache of keys and values in 4 bits, quantized along head_dim.
+ * Each (page, head) holds page_size tokens, and its bytes are contiguous:
+ *   k_codes [pages][heads][page_size][head_dim / 2]: a token's row, its
+ *     4-byte words transposed: the codes of elements 32 b + 8 c .. + 7 (element
+ *     2j in the low nibble of byte j) are word c (head_dim / 32) + b.
+ *   v_codes [pages][heads][page_size / 16][2][8][4][2][head_dim / 16]: token
+ *     16 i + 8 h + 2 c + j of a page holds its elements g head_dim / 8 .. at
+ *     [i][h][g][c][j].
+ *   k_scales, v_scales: MXFP4 [pages][heads][page_size][head_dim / 32] E8M0
+ *     bytes; HiF4 [pages][heads][page_size][head_dim / 64] metadata words.
+ * This is the order in which the tensor cores' operands are loaded;
+ * rfq_kv_read gives the values back in plain order.
+ * fmt: RFQ_FMT_MXFP4 or RFQ_FMT_HIF4; head_dim: 64 or 128; page_size: a
+ * multiple of 16 up to 4096.  Slot s is token s % page_size of page
+ * s / page_size. */
+typedef struct {
+    int32_t fmt;       /* rfq_format */
+    int32_t heads;     /* key / value heads */
+    int32_t head_dim;
+    int32_t page_size; /* tokens of a page */
+    int64_t pages;
+    void *k_codes;     /* device, see above */
+    void *k_scales;
+    void *v_codes;
+    void *v_scales;
+} rfq_kv_cache;
+
+/* Byte sizes of each codes array and each scales array of a cache (host only).
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_UNSUPPORTED (head_dim). */
+RFQ_API rfq_status rfq_kv_cache_bytes(int32_t fmt, int32_t heads, int32_t head_dim, int32_t page_size, int64_t pages,
+                                      size_t *code_bytes, size_t *scale_bytes);
+
+/* Quantizes the keys and values of `tokens` new tokens into the cache at
+ * their slots, exactly as rfq_quantize_act would quantize the rows of one head
+ * (RFQ_FALLBACK_NONE).  k, v: device bf16 [tokens][heads][head_dim] with
+ * strides in elements (multiples of 8, so that every head starts on 16 bytes).
+ * slots: device int64 [tokens]; a slot outside the cache (-1 of a token that
+ * was not served) is skipped, and a slot given twice gets either token.
+ * Non-finite inputs give unspecified codes.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
+ * RFQ_ERR_UNSUPPORTED, RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_kv_append(const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                                 int64_t v_token_stride, int64_t v_head_stride, int64_t tokens, const int64_t *slots,
+                                 const rfq_kv_cache *cache, void *stream);
+
+/* The values of the cache's tokens at `slots` (device int64 [tokens]), keys
+ * to k and values to v: device [tokens][heads][head_dim], fp32 or bf16 by
+ * out_dtype (rounded to nearest even where bf16 does not hold a value: below
+ * its normal range).  Rows of slots outside the cache are zero.
+ * Errors: as rfq_kv_append. */
+RFQ_API rfq_status rfq_kv_read(const rfq_kv_cache *cache, const int64_t *slots, int64_t tokens, void *k, void *v,
+                               int32_t out_dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

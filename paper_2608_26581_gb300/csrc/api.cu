@@ -35,6 +35,8 @@ PFN_encodeTiled get_encode()
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+} // namespace
+
 rfq_status check_device()
 {
     int dev = 0;
@@ -52,6 +54,8 @@ rfq_status check_device()
     }
     return cache[dev] == 1 ? RFQ_OK : RFQ_ERR_DEVICE;
 }
+
+namespace {
 
 rfq_status from_cuda(cudaError_t e) { return e == cudaSuccess ? RFQ_OK : RFQ_ERR_CUDA; }
 
@@ -83,6 +87,8 @@ int64_t k_granule(int32_t fmt, int32_t layout)
     return layout == RFQ_SCALE_MMA ? 128 : 32;
 }
 
+} // namespace
+
 rfq_status check_qtensor(const rfq_qtensor *q, int64_t rows, int64_t k)
 {
     if (!q || !fmt_ok(q->fmt) || !layout_ok(q->scale_layout))
@@ -96,8 +102,6 @@ rfq_status check_qtensor(const rfq_qtensor *q, int64_t rows, int64_t k)
         return RFQ_ERR_ALIGNMENT;
     return RFQ_OK;
 }
-
-} // namespace
 
 int num_sms()
 {

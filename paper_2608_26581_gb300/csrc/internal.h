@@ -52,7 +52,8 @@ int debug_word_gemm_mxf4_pair(int clear);
 // Device status word values written into a workspace by kernels.
 constexpr int32_t kDevOk = 0;
 constexpr int32_t kDevTimeout = 1;
-constexpr int32_t kDevBadGroups = 2;   // grouped GEMM: device-side row offsets break the contract
+constexpr int32_t kDevBadGroups = 2;   // device-side sizes break the contract (grouped GEMM row offsets, request
+                                       // lengths, page numbers)
 constexpr int32_t kDevNonFinite = 3;   // rfq_check_finite found an Inf or NaN
 
 // Bounded waits in the GEMM give up after this many nanoseconds.
@@ -211,6 +212,93 @@ cudaError_t launch_fp4_mma_peak(int pair, int64_t iters, int32_t *status, double
 rfq_status linear_check(const rfq_qtensor *xq, const rfq_qtensor *xr, const uint8_t *phi, int32_t phi_r_s,
                         const rfq_qtensor *wq, void *y, int32_t out_dtype, void *workspace, bool *launch,
                         bool check_ws);
+
+// Host checks shared by the entry points (api.cu): the current device is an
+// sm_103 one; a quantized matrix of rows x k is well formed.
+rfq_status check_device();
+rfq_status check_qtensor(const rfq_qtensor *q, int64_t rows, int64_t k);
+
+// ---- block tables and slot maps (slot_map.cu)
+constexpr int kSlotMapRequests = 8192;   // requests of one call
+struct SlotMapArgs {
+    const int32_t *cached, *added;
+    int32_t requests, page_size;
+    int32_t *table;
+    int32_t width;
+    int32_t *free_pages;
+    int32_t free_capacity;
+    const int32_t *free_in;
+    int32_t *free_out, *lengths, *token_start;
+    int64_t *slots;
+    int32_t *positions;
+    int64_t tokens;
+    int32_t *status;
+};
+cudaError_t launch_slot_map(const SlotMapArgs &a, cudaStream_t st);
+
+// ---- rotary positions (rope.cu); strides in elements
+struct RopeArgs {
+    const void *x;
+    int64_t x_token, x_head;
+    void *out;
+    int64_t out_token, out_head;
+    bool bf16;
+    int64_t tokens;
+    int32_t heads, head_dim;
+    const int32_t *positions;
+    int32_t axes;
+    const float *inv_freq;
+    const int32_t *axis_of;
+    int32_t pairs;
+    bool interleaved, inverse;
+};
+cudaError_t launch_rope(const RopeArgs &a, cudaStream_t st);
+
+// ---- the paged 4-bit cache (kv_cache.cu)
+struct KvAppendArgs {
+    const void *k;
+    int64_t k_token, k_head;
+    const void *v;
+    int64_t v_token, v_head;
+    int64_t tokens;
+    const int64_t *slots;
+    rfq_kv_cache cache;
+};
+cudaError_t launch_kv_append(const KvAppendArgs &a, cudaStream_t st);
+cudaError_t launch_kv_read(const rfq_kv_cache &cache, const int64_t *slots, int64_t tokens, void *k, void *v, bool bf16,
+                           cudaStream_t st);
+
+// ---- attention over the paged 4-bit cache (kv_attention.cu)
+struct KvAttentionArgs {
+    const void *q;
+    int64_t q_token, q_head;
+    int64_t tokens;
+    int32_t heads;
+    const int32_t *q_start, *lengths;
+    int32_t requests;
+    rfq_kv_cache cache;
+    const int32_t *table;
+    int32_t width;
+    float scale;
+    int32_t window;
+    void *out;
+    float *lse;
+    void *workspace;
+};
+size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim);
+cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st);
+
+// ---- matrix-vector products with 4-bit weights (matvec.cu)
+constexpr int kMatvecRows = 32;          // rows of x of one call
+struct MatvecArgs {
+    const void *x;
+    int64_t x_row;
+    int32_t M;
+    rfq_qtensor w;
+    void *y;
+    bool bf16;
+};
+cudaError_t launch_matvec(const MatvecArgs &a, cudaStream_t st);
 
 // Blocks of `threads` threads (and `smem` dynamic shared bytes) of `kern`
 // resident on one SM at once (cached per kernel): grid-stride kernels launch

@@ -21,6 +21,7 @@ RFQ_FMT_MXFP4, RFQ_FMT_HIF4, RFQ_FMT_BF16, RFQ_FMT_MXFP8 = 0, 1, 2, 3
 RFQ_SCALE_ROWMAJOR, RFQ_SCALE_MMA = 0, 1
 RFQ_FALLBACK_NONE, RFQ_FALLBACK_ALL, RFQ_FALLBACK_AMAX = 0, 1, 2
 RFQ_OUT_F32, RFQ_OUT_BF16 = 0, 1
+RFQ_ROPE_HALF, RFQ_ROPE_INTERLEAVED = 0, 1
 (RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_UNSUPPORTED, RFQ_ERR_CUDA, RFQ_ERR_TIMEOUT,
  RFQ_ERR_DEVICE, RFQ_ERR_NONFINITE) = range(1, 9)
 STATUS_NAMES = {0: "RFQ_OK", 1: "RFQ_ERR_INVALID_ARG", 2: "RFQ_ERR_SHAPE", 3: "RFQ_ERR_ALIGNMENT",
@@ -31,7 +32,8 @@ EXPORTED = ("rfq_status_string", "rfq_qtensor_bytes", "rfq_quantize_weight", "rf
             "rfq_linear_workspace_bytes", "rfq_linear", "rfq_workspace_status", "rfq_dequant",
             "rfq_linear_noalloc", "rfq_linear_fused", "rfq_convert", "rfq_linear_grouped", "rfq_check_finite",
             "rfq_quantize_act_expand", "rfq_fp4_mma_peak", "rfq_linear_fused_workspace_bytes",
-            "rfq_linear_profile", "rfq_debug_bounds", "rfq_linear_mixed", "rfq_linear_host")
+            "rfq_linear_profile", "rfq_debug_bounds", "rfq_linear_mixed", "rfq_linear_host",
+            "rfq_slot_map", "rfq_rope", "rfq_kv_cache_bytes", "rfq_kv_append", "rfq_kv_read")
 
 
 class RFQError(RuntimeError):
@@ -48,6 +50,12 @@ class _QT(ctypes.Structure):
 class _FB(ctypes.Structure):
     _fields_ = [("mode", ctypes.c_int32), ("tau", ctypes.c_float), ("p_s", ctypes.c_int32),
                 ("r_s", ctypes.c_int32)]
+
+
+class _KV(ctypes.Structure):
+    _fields_ = [("fmt", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("pages", ctypes.c_int64), ("k_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 _lib = None
@@ -102,6 +110,17 @@ def load_library(path: str = LIB_PATH):
         lib.rfq_linear_profile.argtypes = [QTP, QTP, QTP, P, I32, P, P]
         lib.rfq_fp4_mma_peak.restype = I32
         lib.rfq_fp4_mma_peak.argtypes = [I32, I64, P, ctypes.POINTER(ctypes.c_double), P]
+        KVP, F32 = ctypes.POINTER(_KV), ctypes.c_float
+        lib.rfq_slot_map.restype = I32
+        lib.rfq_slot_map.argtypes = [P, P, I32, I32, P, I32, P, I32, P, P, P, P, P, P, I64, P, P]
+        lib.rfq_rope.restype = I32
+        lib.rfq_rope.argtypes = [P, I64, I64, P, I64, I64, I32, I64, I32, I32, P, I32, P, P, I32, I32, I32, P]
+        lib.rfq_kv_cache_bytes.restype = I32
+        lib.rfq_kv_cache_bytes.argtypes = [I32, I32, I32, I32, I64, ctypes.POINTER(SZ), ctypes.POINTER(SZ)]
+        lib.rfq_kv_append.restype = I32
+        lib.rfq_kv_append.argtypes = [P, I64, I64, P, I64, I64, I64, P, KVP, P]
+        lib.rfq_kv_read.restype = I32
+        lib.rfq_kv_read.argtypes = [KVP, P, I64, P, P, I32, P]
         _lib = lib
     return _lib
 
@@ -352,3 +371,139 @@ def rfq_debug_bounds(clear: bool = False) -> tuple[int, int]:
     line = ctypes.c_int32(0)
     st = load_library().rfq_debug_bounds(ctypes.byref(line), 1 if clear else 0)
     return st, line.value
+
+
+# ---- serving: slot maps, rotary positions, the 4-bit cache ------------------
+
+def _raw_stream(stream, t: torch.Tensor) -> int:
+    """The CUDA stream handle of a call: `stream`, or the current stream of the tensor's device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _want(ok: bool, call: str, what: str):
+    if not ok:
+        raise ValueError(f"{call}: {what}")
+
+
+_DTYPES = {torch.float32: RFQ_OUT_F32, torch.bfloat16: RFQ_OUT_BF16}
+
+
+def rfq_slot_map(cached: torch.Tensor, added: torch.Tensor, page_size: int, block_table: torch.Tensor,
+                 free_pages: torch.Tensor, free_in: torch.Tensor, free_out: torch.Tensor, lengths: torch.Tensor,
+                 token_start: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor,
+                 stream=None):
+    """Block tables, slots and positions of one serving step from the
+    requests' lengths (see include/rfq.h).  block_table [requests, width] and
+    free_pages are updated in place; free_in, free_out: int32 tensors of one
+    element (may be the same); lengths may be `cached`; slots is int64, every
+    other tensor int32, all contiguous.  workspace: 256 bytes, zeroed once."""
+    R, width = block_table.shape
+    T = slots.numel()
+    i32 = torch.int32
+    _want(cached.dtype is i32 and added.dtype is i32 and block_table.dtype is i32 and free_pages.dtype is i32 and
+          free_in.dtype is i32 and free_out.dtype is i32 and lengths.dtype is i32 and token_start.dtype is i32 and
+          positions.dtype is i32 and slots.dtype is torch.int64, "rfq_slot_map", "slots is int64, the others int32")
+    _want(cached.numel() == R and added.numel() == R and lengths.numel() == R and token_start.numel() == R + 1 and
+          positions.numel() == T, "rfq_slot_map", "sizes do not match the block table's requests or the slots")
+    _want(block_table.is_contiguous() and cached.is_contiguous() and added.is_contiguous() and
+          free_pages.is_contiguous() and lengths.is_contiguous() and token_start.is_contiguous() and
+          slots.is_contiguous() and positions.is_contiguous(), "rfq_slot_map", "tensors must be contiguous")
+    _check(load_library().rfq_slot_map(
+        cached.data_ptr(), added.data_ptr(), R, page_size, block_table.data_ptr(), width, free_pages.data_ptr(),
+        free_pages.numel(), free_in.data_ptr(), free_out.data_ptr(), lengths.data_ptr(), token_start.data_ptr(),
+        slots.data_ptr(), positions.data_ptr(), T, workspace.data_ptr(), _raw_stream(stream, block_table)),
+        "rfq_slot_map")
+
+
+def rfq_rope(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor,
+             axis_of: torch.Tensor, pairing: int = RFQ_ROPE_HALF, inverse: bool = False, stream=None):
+    """Rotary positions with several axes: x, out [tokens, heads, head_dim]
+    (fp32 or bf16, any strides with unit stride in the head; out may be x);
+    positions int32 [axes, tokens]; inv_freq fp32 [pairs]; axis_of int32
+    [pairs].  inverse: the gradient (see include/rfq.h)."""
+    T, H, D = x.shape
+    dtype = _DTYPES.get(x.dtype)
+    _want(dtype is not None and out.dtype is x.dtype and positions.dtype is torch.int32 and
+          inv_freq.dtype is torch.float32 and axis_of.dtype is torch.int32, "rfq_rope",
+          "x and out are fp32 or bf16 alike, positions and axis_of int32, inv_freq fp32")
+    _want(out.shape == x.shape and positions.dim() == 2 and positions.shape[1] == T and
+          axis_of.numel() == inv_freq.numel(), "rfq_rope", "sizes do not match")
+    (xt, xh, xd), (ot, oh, od) = x.stride(), out.stride()
+    _want((xd == 1 and od == 1) or D == 1, "rfq_rope", "the elements of a head must be contiguous")
+    _want(positions.is_contiguous() and inv_freq.is_contiguous() and axis_of.is_contiguous(), "rfq_rope",
+          "positions, inv_freq and axis_of must be contiguous")
+    _check(load_library().rfq_rope(x.data_ptr(), xt, xh, out.data_ptr(), ot, oh, dtype, T, H, D, positions.data_ptr(),
+                                   positions.shape[0], inv_freq.data_ptr(), axis_of.data_ptr(), inv_freq.numel(),
+                                   pairing, 1 if inverse else 0, _raw_stream(stream, x)), "rfq_rope")
+
+
+@dataclass
+class KVCache:
+    """A paged 4-bit cache of keys and values (layout in include/rfq.h); the
+    tensors are uint8 and stay the same for the cache's life."""
+    fmt: int
+    heads: int
+    head_dim: int
+    page_size: int
+    pages: int
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+    def __post_init__(self):
+        cb, sb = rfq_kv_cache_bytes(self.fmt, self.heads, self.head_dim, self.page_size, self.pages)
+        for t, n in ((self.k_codes, cb), (self.k_scales, sb), (self.v_codes, cb), (self.v_scales, sb)):
+            _want(t.dtype is torch.uint8 and t.is_contiguous() and t.numel() >= n, "KVCache",
+                  "codes and scales are contiguous uint8 tensors of rfq_kv_cache_bytes bytes")
+        self._c = _KV(self.fmt, self.heads, self.head_dim, self.page_size, self.pages, self.k_codes.data_ptr(),
+                      self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr())
+
+    def c(self) -> _KV:
+        return self._c
+
+
+def rfq_kv_cache_bytes(fmt: int, heads: int, head_dim: int, page_size: int, pages: int):
+    cb, sb = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load_library().rfq_kv_cache_bytes(fmt, heads, head_dim, page_size, pages, ctypes.byref(cb),
+                                             ctypes.byref(sb)), "rfq_kv_cache_bytes")
+    return cb.value, sb.value
+
+
+def empty_kv_cache(fmt: int, heads: int, head_dim: int, page_size: int, pages: int, device="cuda") -> KVCache:
+    """Allocate (with torch) a cache of `pages` pages."""
+    cb, sb = rfq_kv_cache_bytes(fmt, heads, head_dim, page_size, pages)
+    new = lambda n: torch.empty(max(n, 16), dtype=torch.uint8, device=device)  # noqa: E731
+    return KVCache(fmt, heads, head_dim, page_size, pages, new(cb), new(sb), new(cb), new(sb))
+
+
+def rfq_kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: KVCache, stream=None):
+    """Quantize keys and values (bf16 [tokens, heads, head_dim], strided) into
+    the cache at `slots` (int64 [tokens]; see include/rfq.h)."""
+    T, H, D = k.shape
+    _want(k.dtype is torch.bfloat16 and v.dtype is torch.bfloat16 and slots.dtype is torch.int64, "rfq_kv_append",
+          "k and v are bf16, slots int64")
+    _want(v.shape == k.shape and H == cache.heads and D == cache.head_dim and slots.numel() == T, "rfq_kv_append",
+          "sizes do not match the cache")
+    (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
+    _want(kd == 1 and vd == 1 and slots.is_contiguous(), "rfq_kv_append",
+          "the elements of a head and the slots must be contiguous")
+    _check(load_library().rfq_kv_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, slots.data_ptr(), cache._c,
+                                        _raw_stream(stream, k)), "rfq_kv_append")
+
+
+def rfq_kv_read(cache: KVCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None):
+    """The cached keys and values at `slots`, into k and v (fp32 or bf16
+    [tokens, heads, head_dim], contiguous; see include/rfq.h)."""
+    T, H, D = k.shape
+    dtype = _DTYPES.get(k.dtype)
+    _want(dtype is not None and v.dtype is k.dtype and slots.dtype is torch.int64, "rfq_kv_read",
+          "k and v are fp32 or bf16 alike, slots int64")
+    _want(v.shape == k.shape and H == cache.heads and D == cache.head_dim and slots.numel() == T, "rfq_kv_read",
+          "sizes do not match the cache")
+    _want(k.is_contiguous() and v.is_contiguous() and slots.is_contiguous(), "rfq_kv_read",
+          "tensors must be contiguous")
+    _check(load_library().rfq_kv_read(cache._c, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(), dtype,
+                                      _raw_stream(stream, k)), "rfq_kv_read")
