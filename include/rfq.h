@@ -600,6 +600,62 @@ RFQ_API rfq_status rfq_kv_append(const void *k, int64_t k_token_stride, int64_t 
 RFQ_API rfq_status rfq_kv_read(const rfq_kv_cache *cache, const int64_t *slots, int64_t tokens, void *k, void *v,
                                int32_t out_dtype, void *stream);
 
+/* Bytes of device workspace rfq_kv_attention needs on the current device for
+ * `heads` query heads of head_dim (whatever the lengths and requests). */
+RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim);
+
+/* Attention over the paged 4-bit cache, in one launch:
+ *     o = softmax(scale q k^T) v
+ * for the last tokens of every request over its cached keys (causal).
+ *   q: device bf16 [tokens][heads][head_dim], strides in elements (multiples
+ *     of 8).  heads is a multiple of cache->heads: query head i reads key head
+ *     i / (heads / cache->heads).
+ *   q_start: device int32 [requests + 1]: rows q_start[r] .. q_start[r + 1] of
+ *     q are the last tokens of request r (their keys are in the cache), or
+ *     NULL: one token a request (tokens == requests).
+ *   lengths: device int32 [requests]: keys of each request, its new tokens
+ *     included.  Token i of n sees keys j <= length - n + i, and with
+ *     window > 0 only j > length - n + i - window (window 0: all).  A row
+ *     that sees no key gets o = 0 and lse = -inf.
+ *   block_table: device int32 [requests][table_width] pages of each request.
+ *   out: device bf16 [tokens][heads][head_dim], contiguous.
+ *   lse: device fp32 [tokens][heads], the logarithm of the sum of
+ *     exp(scale q k), or NULL.
+ *   workspace: rfq_kv_attention_workspace_bytes bytes, zeroed by the caller
+ *     once; calls that overlap on the GPU must not share it.
+ * Scores, their maximum and sum and the accumulators are fp32; the codes enter
+ * the tensor cores exactly, q as f16 scaled by a power of two per row, and the
+ * softmax weights rounded to f16.  Values whose block scale lies more than
+ * 2^24 below the largest of the same head and dimensions in that request are
+ * taken as zero.  q must be finite.  The same inputs give the same bits.
+ * Lengths past table_width pages, rows outside q and pages outside the cache
+ * set the device status RFQ_ERR_SHAPE (rfq_workspace_status); such requests'
+ * rows are unspecified.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
+ * RFQ_ERR_UNSUPPORTED, RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens,
+                                    int32_t heads, const int32_t *q_start, const int32_t *lengths, int32_t requests,
+                                    const rfq_kv_cache *cache, const int32_t *block_table, int32_t table_width,
+                                    float scale, int32_t window, void *out, float *lse, void *workspace,
+                                    void *stream);
+
+/* y = x W~^T for a few rows of x, x kept in bf16: the linear layer of a
+ * decoding step, where the bytes of W~ bound the time (rfq_linear quantizes x
+ * and is the call for more rows).
+ *   x: device bf16 [rows][wq->k], x_row_stride in elements (a multiple of 8);
+ *     0 <= rows <= 32.  x must be finite.
+ *   wq: device, MXFP4 or HiF4 with either scale layout, any number of rows up
+ *     to 2^21 (as rfq_quantize_weight writes it).
+ *   y: device [rows][wq->rows], fp32 or bf16 by out_dtype.
+ * Products and sums are fp32; W~ enters the tensor cores exactly and x as f16
+ * scaled by a power of two per row and stretch of k, which keeps every bf16
+ * bit down to 2^-28 of the stretch's maximum.  The same inputs give the same
+ * bits.  Should a bounded wait run out, y is NaN.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
+ * RFQ_ERR_UNSUPPORTED (other formats), RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows, const rfq_qtensor *wq, void *y,
+                              int32_t out_dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

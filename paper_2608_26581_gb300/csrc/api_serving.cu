@@ -158,4 +158,63 @@ rfq_status rfq_kv_read(const rfq_kv_cache *cache, const int64_t *slots, int64_t 
                                     static_cast<cudaStream_t>(stream)));
 }
 
+size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
+{
+    if (heads < 1 || (head_dim != 64 && head_dim != 128))
+        return 0;
+    return kv_attention_workspace_bytes(heads, head_dim);
+}
+
+rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens,
+                            int32_t heads, const int32_t *q_start, const int32_t *lengths, int32_t requests,
+                            const rfq_kv_cache *cache, const int32_t *block_table, int32_t table_width, float scale,
+                            int32_t window, void *out, float *lse, void *workspace, void *stream)
+{
+    rfq_status s = check_kv_cache(cache);
+    if (s != RFQ_OK)
+        return s;
+    if (tokens < 0 || tokens > INT32_MAX || requests < 0 || heads < 1 || heads % cache->heads != 0 ||
+        table_width < 1 || window < 0 || q_token_stride < 0 || q_head_stride < 0 ||
+        (!q_start && tokens != requests) || (int64_t)table_width * cache->page_size > INT32_MAX - 4096)
+        return RFQ_ERR_SHAPE;
+    if (!workspace || !(scale == scale) ||
+        (tokens > 0 && requests > 0 && (!q || !out || !lengths || !block_table)))
+        return RFQ_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(q_start, 4) ||
+        !aligned(lengths, 4) || !aligned(block_table, 4) || !aligned(lse, 4) ||
+        (q_token_stride | q_head_stride) % 8 != 0)
+        return RFQ_ERR_ALIGNMENT;
+    if ((s = check_device()) != RFQ_OK)
+        return s;
+    if (tokens == 0 || requests == 0)
+        return RFQ_OK;
+    return from_cuda(launch_kv_attention({q, q_token_stride, q_head_stride, tokens, heads, q_start, lengths, requests,
+                                          *cache, block_table, table_width, scale, window, out, lse, workspace},
+                                         static_cast<cudaStream_t>(stream)));
+}
+
+rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows, const rfq_qtensor *wq, void *y,
+                      int32_t out_dtype, void *stream)
+{
+    if (!wq || (out_dtype != RFQ_OUT_F32 && out_dtype != RFQ_OUT_BF16))
+        return RFQ_ERR_INVALID_ARG;
+    rfq_status s = check_qtensor(wq, wq->rows, wq->k);
+    if (s != RFQ_OK)
+        return s;
+    if (wq->fmt != RFQ_FMT_MXFP4 && wq->fmt != RFQ_FMT_HIF4)
+        return RFQ_ERR_UNSUPPORTED;
+    if (rows < 0 || rows > kMatvecRows || x_row_stride < 0 || wq->rows > kMatvecWeightRows || wq->k > INT32_MAX)
+        return RFQ_ERR_SHAPE;
+    if (rows > 0 && wq->rows > 0 && (!x || !y))
+        return RFQ_ERR_INVALID_ARG;
+    if (!aligned(x, 16) || !aligned(y, 16) || x_row_stride % 8 != 0)
+        return RFQ_ERR_ALIGNMENT;
+    if ((s = check_device()) != RFQ_OK)
+        return s;
+    if (rows == 0 || wq->rows == 0)
+        return RFQ_OK;
+    return from_cuda(launch_matvec({x, x_row_stride, (int32_t)rows, *wq, y, out_dtype == RFQ_OUT_BF16},
+                                   static_cast<cudaStream_t>(stream)));
+}
+
 } // extern "C"

@@ -289,7 +289,8 @@ size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim);
 cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st);
 
 // ---- matrix-vector products with 4-bit weights (matvec.cu)
-constexpr int kMatvecRows = 32;          // rows of x of one call
+constexpr int kMatvecRows = 32;                   // rows of x of one call
+constexpr int64_t kMatvecWeightRows = 1ll << 21;  // (64 of them a CTA; the grid's y holds 65535)
 struct MatvecArgs {
     const void *x;
     int64_t x_row;

@@ -33,7 +33,8 @@ EXPORTED = ("rfq_status_string", "rfq_qtensor_bytes", "rfq_quantize_weight", "rf
             "rfq_linear_noalloc", "rfq_linear_fused", "rfq_convert", "rfq_linear_grouped", "rfq_check_finite",
             "rfq_quantize_act_expand", "rfq_fp4_mma_peak", "rfq_linear_fused_workspace_bytes",
             "rfq_linear_profile", "rfq_debug_bounds", "rfq_linear_mixed", "rfq_linear_host",
-            "rfq_slot_map", "rfq_rope", "rfq_kv_cache_bytes", "rfq_kv_append", "rfq_kv_read")
+            "rfq_slot_map", "rfq_rope", "rfq_kv_cache_bytes", "rfq_kv_append", "rfq_kv_read",
+            "rfq_kv_attention_workspace_bytes", "rfq_kv_attention", "rfq_matvec")
 
 
 class RFQError(RuntimeError):
@@ -121,6 +122,12 @@ def load_library(path: str = LIB_PATH):
         lib.rfq_kv_append.argtypes = [P, I64, I64, P, I64, I64, I64, P, KVP, P]
         lib.rfq_kv_read.restype = I32
         lib.rfq_kv_read.argtypes = [KVP, P, I64, P, P, I32, P]
+        lib.rfq_kv_attention_workspace_bytes.restype = SZ
+        lib.rfq_kv_attention_workspace_bytes.argtypes = [I32, I32]
+        lib.rfq_kv_attention.restype = I32
+        lib.rfq_kv_attention.argtypes = [P, I64, I64, I64, I32, P, P, I32, KVP, P, I32, F32, I32, P, P, P, P]
+        lib.rfq_matvec.restype = I32
+        lib.rfq_matvec.argtypes = [P, I64, I64, QTP, P, I32, P]
         _lib = lib
     return _lib
 
@@ -460,9 +467,17 @@ class KVCache:
                   "codes and scales are contiguous uint8 tensors of rfq_kv_cache_bytes bytes")
         self._c = _KV(self.fmt, self.heads, self.head_dim, self.page_size, self.pages, self.k_codes.data_ptr(),
                       self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr())
+        self._ws = None
 
     def c(self) -> _KV:
         return self._c
+
+    def attention_workspace_bytes(self, heads: int) -> int:
+        """rfq_kv_attention_workspace_bytes, asked once for a cache's device."""
+        if self._ws is None:
+            with torch.cuda.device(self.k_codes.device):
+                self._ws = rfq_kv_attention_workspace_bytes(heads, self.head_dim)
+        return self._ws
 
 
 def rfq_kv_cache_bytes(fmt: int, heads: int, head_dim: int, page_size: int, pages: int):
@@ -507,3 +522,56 @@ def rfq_kv_read(cache: KVCache, slots: torch.Tensor, k: torch.Tensor, v: torch.T
           "tensors must be contiguous")
     _check(load_library().rfq_kv_read(cache._c, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(), dtype,
                                       _raw_stream(stream, k)), "rfq_kv_read")
+
+
+def rfq_kv_attention_workspace_bytes(heads: int, head_dim: int) -> int:
+    return load_library().rfq_kv_attention_workspace_bytes(heads, head_dim)
+
+
+def kv_attention_workspace(heads: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A zeroed workspace for rfq_kv_attention (int32 words)."""
+    n = rfq_kv_attention_workspace_bytes(heads, head_dim)
+    _want(n > 0, "kv_attention_workspace", "head_dim is 64 or 128")
+    return torch.zeros((n + 3) // 4, dtype=torch.int32, device=device)
+
+
+def rfq_kv_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
+                     out: torch.Tensor, workspace: torch.Tensor, lse: torch.Tensor | None = None,
+                     q_start: torch.Tensor | None = None, scale: float | None = None, window: int = 0, stream=None):
+    """Attention of the requests' last tokens over the 4-bit cache: q bf16
+    [tokens, heads, head_dim] (strided), block_table int32 [requests, width],
+    lengths int32 [requests], out bf16 and lse fp32 contiguous; q_start int32
+    [requests + 1], or None for one token a request; scale defaults to
+    head_dim ** -0.5 (see include/rfq.h)."""
+    T, Hq, D = q.shape
+    R, width = block_table.shape
+    i32 = torch.int32
+    _want(q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and block_table.dtype is i32 and
+          lengths.dtype is i32 and (lse is None or lse.dtype is torch.float32) and
+          (q_start is None or q_start.dtype is i32), "rfq_kv_attention",
+          "q and out are bf16, lse fp32, block_table, lengths and q_start int32")
+    _want(D == cache.head_dim and out.shape == q.shape and lengths.numel() == R and
+          (lse is None or lse.numel() == T * Hq) and (T == R if q_start is None else q_start.numel() == R + 1),
+          "rfq_kv_attention", "sizes do not match")
+    qt, qh, qd = q.stride()
+    _want(qd == 1 and out.is_contiguous() and block_table.is_contiguous() and lengths.is_contiguous() and
+          (lse is None or lse.is_contiguous()) and (q_start is None or q_start.is_contiguous()), "rfq_kv_attention",
+          "the elements of a head and every other tensor must be contiguous")
+    _want(workspace.numel() * workspace.element_size() >= cache.attention_workspace_bytes(Hq), "rfq_kv_attention",
+          "the workspace is smaller than rfq_kv_attention_workspace_bytes")
+    _check(load_library().rfq_kv_attention(
+        q.data_ptr(), qt, qh, T, Hq, None if q_start is None else q_start.data_ptr(), lengths.data_ptr(), R, cache._c,
+        block_table.data_ptr(), width, D ** -0.5 if scale is None else scale, window, out.data_ptr(),
+        None if lse is None else lse.data_ptr(), workspace.data_ptr(), _raw_stream(stream, q)), "rfq_kv_attention")
+
+
+def rfq_matvec(x: torch.Tensor, wq: QTensor, y: torch.Tensor, stream=None):
+    """y = x W~^T for up to 32 rows of x (bf16 [rows, k], rows strided); wq
+    MXFP4 or HiF4; y fp32 or bf16 [rows, n], contiguous (see include/rfq.h)."""
+    M, K = x.shape
+    dtype = _DTYPES.get(y.dtype)
+    _want(x.dtype is torch.bfloat16 and dtype is not None, "rfq_matvec", "x is bf16, y fp32 or bf16")
+    _want(K == wq.k and y.shape == (M, wq.rows), "rfq_matvec", "sizes do not match")
+    _want(x.stride(1) == 1 and y.is_contiguous(), "rfq_matvec", "the rows of x and y must be contiguous")
+    _check(load_library().rfq_matvec(x.data_ptr(), x.stride(0), M, wq.c(), y.data_ptr(), dtype,
+                                     _raw_stream(stream, x)), "rfq_matvec")

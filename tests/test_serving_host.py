@@ -72,3 +72,38 @@ def test_cache_call_checks(lib):
     assert lib.rfq_kv_read(ref(bad), 16, 3, 16, 16, 1, None) == rfq.RFQ_ERR_INVALID_ARG
     bad = rfq._KV(0, 2, 64, 16, 3, 16, 16, 20, 16)
     assert lib.rfq_kv_read(ref(bad), 16, 3, 16, 16, 1, None) == rfq.RFQ_ERR_ALIGNMENT
+
+
+def test_attention_checks(lib):
+    from paper_2608_26581_gb300 import rfq
+    kv = rfq._KV(0, 2, 64, 16, 3, 16, 16, 16, 16)
+    good = [16, 256, 64, 3, 4, None, 16, 3, ctypes.byref(kv), 16, 4, 0.125, 0, 16, 16, 16, None]
+
+    def call(i, v):
+        a = list(good)
+        a[i] = v
+        return lib.rfq_kv_attention(*a)
+    for i in (0, 6, 8, 9, 13, 15):
+        assert call(i, None) == rfq.RFQ_ERR_INVALID_ARG
+    assert call(11, float("nan")) == rfq.RFQ_ERR_INVALID_ARG
+    for i, v in ((3, -1), (3, 2), (4, 0), (4, 3), (7, -1), (10, 0), (10, 2 ** 27), (12, -1), (1, -8)):
+        assert call(i, v) == rfq.RFQ_ERR_SHAPE
+    for i, v in ((0, 24), (13, 8), (15, 4), (1, 252), (6, 18), (14, 18)):
+        assert call(i, v) == rfq.RFQ_ERR_ALIGNMENT
+    assert lib.rfq_kv_attention_workspace_bytes(4, 96) == 0 and lib.rfq_kv_attention_workspace_bytes(0, 64) == 0
+
+
+def test_matvec_checks(lib):
+    from paper_2608_26581_gb300 import rfq
+    qt = lambda *a: ctypes.byref(rfq._QT(*a))  # noqa: E731
+    ok = (0, 1, 64, 128, 16, 16)
+    assert lib.rfq_matvec(16, 128, 1, None, 16, 0, None) == rfq.RFQ_ERR_INVALID_ARG
+    assert lib.rfq_matvec(16, 128, 1, qt(*ok), 16, 3, None) == rfq.RFQ_ERR_INVALID_ARG
+    assert lib.rfq_matvec(None, 128, 1, qt(*ok), 16, 0, None) == rfq.RFQ_ERR_INVALID_ARG
+    assert lib.rfq_matvec(16, 128, 33, qt(*ok), 16, 0, None) == rfq.RFQ_ERR_SHAPE
+    assert lib.rfq_matvec(16, 128, -1, qt(*ok), 16, 0, None) == rfq.RFQ_ERR_SHAPE
+    assert lib.rfq_matvec(16, 128, 1, qt(0, 1, 64, 96, 16, 16), 16, 0, None) == rfq.RFQ_ERR_SHAPE
+    assert lib.rfq_matvec(16, 128, 1, qt(0, 1, 2 ** 21 + 1, 128, 16, 16), 16, 0, None) == rfq.RFQ_ERR_SHAPE
+    assert lib.rfq_matvec(16, 128, 1, qt(3, 1, 64, 128, 16, 16), 16, 0, None) == rfq.RFQ_ERR_UNSUPPORTED
+    assert lib.rfq_matvec(16, 124, 1, qt(*ok), 16, 0, None) == rfq.RFQ_ERR_ALIGNMENT
+    assert lib.rfq_matvec(8, 128, 1, qt(*ok), 16, 0, None) == rfq.RFQ_ERR_ALIGNMENT
