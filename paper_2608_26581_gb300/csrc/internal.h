@@ -290,7 +290,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st);
 
 // ---- matrix-vector products with 4-bit weights (matvec.cu)
 constexpr int kMatvecRows = 32;                   // rows of x of one call
-constexpr int64_t kMatvecWeightRows = 1ll << 21;  // (64 of them a CTA; the grid's y holds 65535)
+constexpr int64_t kMatvecWeightRows = 1ll << 21;  // (at least 256 of them a CTA: the grid holds them)
 struct MatvecArgs {
     const void *x;
     int64_t x_row;

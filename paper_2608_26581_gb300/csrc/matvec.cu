@@ -8,42 +8,58 @@
 // one instruction and multiplied unscaled.  A block's scale multiplies the
 // fp32 sums of its 32 (MXFP4) or 64 (HiF4) products, so neither the scale nor
 // the codes are rounded.  x is made f16 by a power of two per row of x and
-// window of K (its maximum lands in [2^14, 2^15)): bf16 values down to 2^-28
+// 256 of K (its maximum lands in [2^14, 2^15)): bf16 values down to 2^-28
 // of the maximum are exact, the rest are off by less than 2^-39 of it.
 //
-// A CTA takes 64 rows of W~ and one share of K (a cluster of up to eight CTAs
-// splits K and adds its parts in shared memory, in the order of the ranks, so
-// a call gives the same bits every time).  W~ arrives in boxes of 64 rows x
-// 256 codes by TMA with the 128-byte swizzle; ldmatrix then hands every lane
-// its 8 codes of a 32-code block without a bank conflict.  Eight warps: four
-// row tiles of 16, two halves of the window's boxes.
+// Each of a CTA's 16 warps streams its own boxes, 16 rows of W~ x 256 codes,
+// through a ring that it alone fills (TMA, 128-byte swizzle) and empties
+// (ldmatrix hands every lane its 8 codes of a 32-code block without a bank
+// conflict), so nothing in the main loop waits for another warp.  A CTA has a
+// run of 16-row tiles and one share of K; its boxes, tile by tile, are dealt
+// to the warps in equal contiguous runs, and the parts of a tile that two
+// warps share are added in the order of the warps.  x lies in shared memory
+// in the order of the B operand.  K is split over a cluster only where that
+// pays (split_of): the CTAs' parts are then added over distributed shared
+// memory, in the order of the ranks.  All sums have a fixed order: a call
+// gives the same bits every time.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
 
 #include "internal.h"
 #include "kv_layout.cuh"
+#include "mxfp4_math.cuh"
 #include "ptx.cuh"
 
 namespace rfq {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kRows = 64;                    // rows of W~ per CTA
+constexpr int kWarps = 16, kThreads = 32 * kWarps;
+constexpr int kTile = 16;                    // rows of W~ per tile
 constexpr int kBoxK = 256;                   // codes per row of a box (128 bytes)
-constexpr int kBoxBytes = kRows * kBoxK / 2;
-
-// NT: tiles of 8 rows of x.  Boxes per window: the x of a window is
-// 8 NT boxes 512 bytes.
-template <int NT>
+constexpr int kBoxBytes = kTile * kBoxK / 2;
+constexpr int kMaxDepth = 6;                 // steps in a warp's ring
+constexpr int kSmemBytes = 225 * 1024;
+// MP: rows of x rounded up to a power of two.  The eight columns of an MMA
+// hold min(MP, 8) rows of x times kCb blocks of 32 codes: column n is row
+// n / kCb and block n % kCb of a group of kCb, and a block's MMAs see x in
+// its own columns and zeros in the others.  With one row the sums of all
+// eight blocks of a box thus stay apart in one accumulator, and the scales
+// multiply four numbers a lane and box instead of 32.
+template <int MP>
 struct Shape {
-    static constexpr int kBoxes = NT >= 4 ? 2 : 4;
-    static constexpr int kWinK = kBoxes * kBoxK;
-    static constexpr int kXBytes = 8 * NT * kWinK * 2;
-    static constexpr int kScaleWords = kRows * kWinK / 64;   // HiF4 (MXFP4: half)
-    static constexpr int kStage = kBoxes * kBoxBytes;
-    // two windows of W~, one of x and of scales
-    static constexpr int kSmem = 1024 + 2 * kStage + kXBytes + kScaleWords * 4;
+    static constexpr int kNt = MP > 8 ? MP / 8 : 1;                // column tiles
+    static constexpr int kCb = MP < 8 ? 8 / MP : 1;
+    static constexpr int kPart = kNt * 512;  // bytes of one tile's sums: [tile][lane][4] fp32
+    static constexpr int kTiles = 48 / kNt;  // most tiles of a CTA
+    // a step of the loop is two boxes along K, or one where x takes the room
+    static constexpr int kBx = kNt == 1 ? 2 : 1;
+    static constexpr int kStepK = kBx * kBoxK, kStepBytes = kBx * kBoxBytes;
+    static constexpr int kBlockX = MP * 64;  // bytes of a block of 32 codes' x: [row][4][16 bytes]
+    static constexpr int kStepX = kStepK / 32 * kBlockX;
+    static constexpr int kZero = MP < 8 ? kStepX : 0;              // zeros that the other blocks' columns read
+    // bytes of x in shared memory: rings of at least 6 KB a warp fit beside it
+    static constexpr int kMaxX = 80 * 1024;
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
@@ -57,52 +73,17 @@ struct Params {
     const __nv_bfloat16 *x;
     int64_t x_row;
     int M;
-    int64_t N, K;
+    int N, K;
     const uint8_t *scales;
     int mma_layout;
+    int words;             // four blocks' E8M0 bytes are an aligned word
     void *y;
     int bf16;
-    int win_per_cta;       // windows of K per cluster rank
+    int tiles;             // of W~
+    int steps;             // along K
+    int phase;             // steps of K at a time (what of x fits)
+    int depth;             // of the rings
 };
-
-// Scale word of row n and the 128 (MXFP4) or 64 (HiF4) codes at k.
-template <int FMT>
-__device__ __forceinline__ uint32_t scale_word(const Params &p, int64_t n, int64_t k)
-{
-    if (n >= p.N || k >= p.K)
-        return 0;
-    if (FMT == RFQ_FMT_HIF4) {
-        const int64_t at = p.mma_layout ? (k / 64) * ((p.N + 127) / 128 * 128) + n : n * (p.K / 64) + k / 64;
-        return __ldg(reinterpret_cast<const uint32_t *>(p.scales) + at);
-    }
-    if (p.mma_layout)
-        return __ldg(reinterpret_cast<const uint32_t *>(p.scales + sf_mma_offset(n, k / 32, p.K / 128)));
-    uint32_t w = 0;
-    const uint8_t *const s = p.scales + n * (p.K / 32) + k / 32;
-    if (p.K % 128 == 0)
-        return __ldg(reinterpret_cast<const uint32_t *>(s));
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (k + 32 * j < p.K)
-            w |= (uint32_t)__ldg(s + j) << (8 * j);
-    return w;
-}
-
-// Eight elements of an x row at k as fp32 (zero past its end).
-__device__ __forceinline__ void load_x8(const Params &p, int m, int64_t k, float (&f)[8])
-{
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (m < p.M && k < p.K) {
-        const __nv_bfloat16 *const s = p.x + m * p.x_row + k;
-        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(s));
-        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
@@ -110,274 +91,579 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <int FMT, int NT>
-__global__ void __launch_bounds__(kThreads) matvec_kernel(const __grid_constant__ CUtensorMap wmap, const Params p)
-{
-    using S = Shape<NT>;
-    constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
-    constexpr int WINK = S::kWinK;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) uint64_t s_full[2];
-    __shared__ float s_xscale[8 * NT];
-    uint8_t *const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-    uint8_t *const s_w = smem;                                 // [2][boxes][64 rows][128 bytes]
-    uint8_t *const s_x = s_w + 2 * S::kStage;                  // [block][tile][lane][16 bytes]
-    uint32_t *const s_sc = reinterpret_cast<uint32_t *>(s_x + S::kXBytes);
-
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int split = (int)gridDim.x, rank = blockIdx.x;       // the cluster spans x
-    const int64_t n0 = (int64_t)blockIdx.y * kRows;
-    const int windows = (int)((p.K + WINK - 1) / WINK);
-    const int w0 = min(windows, rank * p.win_per_cta), w1 = min(windows, w0 + p.win_per_cta);
-
-    if (tid == 0) {
-        mbar_init(&s_full[0], 1);
-        mbar_init(&s_full[1], 1);
-        fence_mbar_init();
-    }
-    __syncthreads();
-    auto fetch = [&](int w) {                                  // one thread
-        const int b = (w - w0) & 1;
-        mbar_arrive_expect_tx(&s_full[b], S::kStage);
+// A box's scale words that a lane needs, and where the next box's lie.
+//   MXFP4  the words (four blocks) of rows g and g + 8 that hold the blocks of
+//          its columns: one half of the box with kCb = 8, else both
+//   HiF4   block c of the box, rows g and g + 8 (the others by shuffles)
+template <int FMT, int CB, int BX>
+struct Scales {
+    static constexpr bool kHif4 = FMT == RFQ_FMT_HIF4;
+    static constexpr int kHalves = kHif4 || CB == 8 ? 1 : 2;
+    static constexpr int kN = 2 * kHalves;       // words a box
+    const uint8_t *at[2];      // rows g and g + 8
+    int64_t step, half;        // bytes to the next box, to the other half
+    int k;                     // code of at[]'s first word
+    bool in[2];                // rows of W~
+    __device__ __forceinline__ void tile(const Params &p, int n, int step0, int c)   // n: row g of the tile
+    {
+        k = step0 * BX * kBoxK + (kHif4 ? 64 * c : CB == 8 ? 128 * (c >> 1) : 0);
 #pragma unroll
-        for (int i = 0; i < S::kBoxes; ++i)
-            tma_load_2d(s_w + b * S::kStage + i * kBoxBytes, &wmap, &s_full[b], (w * WINK + i * kBoxK) / 2, (int)n0);
-    };
-    if (tid == 0) {
-        if (w0 < w1)
-            fetch(w0);
-        if (w0 + 1 < w1)
-            fetch(w0 + 1);
-    }
-
-    const int rt = warp & 3, half = warp >> 2;                 // rows 16 rt .., every second box
-    float acc[NT][4];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            acc[t][i] = 0.f;
-    bool ok = true;                                            // no wait has run out
-
-    for (int w = w0; w < w1; ++w) {
-        const int64_t k0 = (int64_t)w * WINK;
-        const int b = (w - w0) & 1;
-        // scales of the window: [k word][row]
-        constexpr int KW = WINK / (HIF4 ? 64 : 128);
-        for (int i = tid; i < KW * kRows; i += kThreads)
-            s_sc[i] = scale_word<FMT>(p, n0 + i % kRows, k0 + (int64_t)(i / kRows) * (HIF4 ? 64 : 128));
-        // x of the window as f16, each row scaled by a power of two: one warp a row
-        for (int m = warp; m < 8 * NT; m += kWarps) {
-            float f[WINK / 256][8];
-            float mx = 0.f;
-#pragma unroll
-            for (int i = 0; i < WINK / 256; ++i) {
-                load_x8(p, m, k0 + i * 256 + lane * 8, f[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    mx = fmaxf(mx, fabsf(f[i][j]));
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1)
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o));
-            const int e = (int)(__float_as_uint(mx) >> 23) - 127 - 14;   // x 2^-e: the maximum in [2^14, 2^15)
-            const int ec = max(min(e, 126), -126);
-            const float mul = __uint_as_float((uint32_t)(127 - ec) << 23);
-            if (lane == 0)
-                s_xscale[m] = __uint_as_float((uint32_t)(127 + ec) << 23);
-#pragma unroll
-            for (int i = 0; i < WINK / 256; ++i) {
-                uint32_t h[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    // HiF4 codes decode in the order 0 2 | 1 3 | 4 6 | 5 7
-                    const int lo = HIF4 ? (j >> 1) * 4 + (j & 1) : 2 * j, hi = HIF4 ? lo + 2 : lo + 1;
-                    h[j] = pack_f16(f[i][lo] * mul, f[i][hi] * mul);
-                }
-                const int blk = i * 8 + (lane >> 2), cc = lane & 3;
-                *reinterpret_cast<uint4 *>(s_x + (((blk * NT + (m >> 3)) * 32 + (m & 7) * 4 + cc) << 4)) =
-                    make_uint4(h[0], h[1], h[2], h[3]);
+        for (int r = 0; r < 2; ++r) {
+            const int m = n + 8 * r;
+            in[r] = m < p.N;
+            if (kHif4) {
+                const int64_t pad = (p.N + 127) / 128 * 128;
+                at[r] = p.scales + 4 * (p.mma_layout ? (int64_t)(k / 64) * pad + m : (int64_t)m * (p.K / 64) + k / 64);
+                step = p.mma_layout ? 16 * pad : 16;
+                half = 0;
+            } else {
+                at[r] = p.scales + (p.mma_layout ? sf_mma_offset(m, k / 32, p.K / 128) : (int64_t)m * (p.K / 32) + k / 32);
+                step = p.mma_layout ? 1024 : 8;
+                half = p.mma_layout ? 512 : 4;
             }
         }
+    }
+    // the words of a step: [box][half][row]
+    __device__ __forceinline__ void load(const Params &p, uint32_t (&w)[BX * kN])
+    {
+#pragma unroll
+        for (int b = 0; b < BX; ++b)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint8_t *const s = at[r] + b * step + h * half;
+                    const int kk = k + b * kBoxK + 128 * h;
+                    uint32_t v = 0;
+                    if (kHif4 || p.words) {
+                        if (in[r] && kk < p.K)
+                            v = __ldg(reinterpret_cast<const uint32_t *>(s));
+                    } else if (in[r]) {    // row-major E8M0 rows that are not whole words
+                        for (int j = 0; j < 4; ++j)
+                            if (kk + 32 * j < p.K)
+                                v |= (uint32_t)__ldg(s + j) << (8 * j);
+                    }
+                    w[b * kN + 2 * h + r] = v;
+                }
+        at[0] += BX * step;
+        at[1] += BX * step;
+        k += BX * kBoxK;
+    }
+};
+
+// Byte j of a word of E8M0 scales as fp32 (byte 0, a block of zeros or of
+// values below 2^-124, as 0)
+__device__ __forceinline__ float e8m0_byte(uint32_t w, int j)
+{
+    return __uint_as_float((j < 3 ? w << (23 - 8 * j) : w >> 1) & 0x7F800000u);
+}
+
+template <int FMT, int MP>
+__global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_constant__ CUtensorMap wmap, const Params p)
+{
+    using S = Shape<MP>;
+    constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
+    constexpr int NT = S::kNt, CB = S::kCb, BX = S::kBx, kStepK = S::kStepK, kStepBytes = S::kStepBytes;
+    constexpr uint32_t kAll = 0xFFFFFFFFu;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ alignas(8) uint64_t s_full[kWarps][kMaxDepth];
+    __shared__ int4 s_run[kWarps];           // [first box, end) of each warp, its first and last tile
+    uint8_t *const smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int M = MP == 1 ? 1 : p.M;
+    uint8_t *const s_ring = smem + warp * p.depth * kStepBytes;
+    // a warp's part of its first tile, in s_head; of its last, over its ring (all read by then)
+    uint8_t *const s_head = smem + kWarps * p.depth * kStepBytes;
+    uint8_t *const s_tot = s_head + kWarps * S::kPart;             // [tile] sums
+    uint8_t *const s_zero = s_tot + S::kTiles * S::kPart;
+    uint8_t *const s_x = s_zero + S::kZero;                        // [block][row][4][16 bytes]
+    float *const s_xs = reinterpret_cast<float *>(s_x + p.phase * S::kStepX);   // [step][row] undoes x's power of two
+
+    const int split = (int)gridDim.x, rank = blockIdx.x;           // a cluster spans x
+    const int t0 = (int)((uint32_t)p.tiles * blockIdx.y / gridDim.y);
+    const int nt = (int)((uint32_t)p.tiles * (blockIdx.y + 1) / gridDim.y) - t0;
+    const int b0 = (uint32_t)p.steps * rank / split, b1 = (uint32_t)p.steps * (rank + 1) / split;
+
+    if (lane == 0) {
+        for (int i = 0; i < p.depth; ++i)
+            mbar_init(&s_full[warp][i], 1);
+        fence_mbar_init();
+    }
+    for (int i = tid; i < S::kZero / 16; i += kThreads)
+        reinterpret_cast<uint4 *>(s_zero)[i] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
+    bool ok = true;                                                // no wait has run out
+    int slot = 0;                                                  // of the ring, and its phase
+    uint32_t parity = 0;
+
+    for (int pb = b0; pb < b1; pb += p.phase) {
+        const int nb = min(p.phase, b1 - pb);                      // steps of a tile in this phase
+        const uint32_t all = nt * nb;
+        const int f0 = (int)(all * warp / kWarps), f1 = (int)(all * (warp + 1) / kWarps);
+        const int first = f0 / nb, last = f1 > f0 ? (f1 - 1) / nb : first;   // this warp's tiles
+        // what comes next into the ring: step fstep of tile ftile, at slot fslot
+        int fstep = f0 - first * nb, ftile = first, fslot = slot, left = f1 - f0;
+        auto fetch = [&]() {
+            if (left <= 0)
+                return;
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&s_full[warp][fslot], kStepBytes);
+#pragma unroll
+                for (int i = 0; i < BX; ++i)
+                    tma_load_2d(s_ring + fslot * kStepBytes + i * kBoxBytes, &wmap, &s_full[warp][fslot],
+                                (pb + fstep) * (kStepK / 2) + i * (kBoxK / 2), (t0 + ftile) * kTile);
+            }
+            --left;
+            if (++fstep == nb) {
+                fstep = 0;
+                ++ftile;
+            }
+            if (++fslot == p.depth)
+                fslot = 0;
+        };
+        // x of the phase as f16, each (row, step) scaled by a power of two
+        auto load_x = [&](int i, uint4 (&u)[BX]) {
+            const int st = i / M, m = i - st * M, k = (pb + st) * kStepK + lane * 8;
+#pragma unroll
+            for (int j = 0; j < BX; ++j)
+                u[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < BX; ++j)
+                if (k + j * kBoxK < p.K)       // (volatile: where it stands)
+                    asm volatile("ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(u[j].x), "=r"(u[j].y), "=r"(u[j].z), "=r"(u[j].w)
+                                 : "l"(p.x + m * p.x_row + k + j * kBoxK));
+        };
+        auto store_x = [&](int i, const uint4 (&u)[BX]) {
+            const int st = i / M, m = i - st * M;
+            float f[BX][8], mx = 0.f;
+#pragma unroll
+            for (int j = 0; j < BX; ++j) {
+                bf16x8_to_f32(u[j], f[j]);
+                mx = fmaxf(mx, absmax8(f[j]));
+            }
+            // (non-negative floats compare as integers)
+            mx = __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(mx)));
+            const int e = (int)(__float_as_uint(mx) >> 23) - 127 - 14;   // x 2^-e: the maximum in [2^14, 2^15)
+            const int ec = max(min(e, 119), -126);
+            const float mul = __uint_as_float((uint32_t)(127 - ec) << 23);
+            if (lane == 0)                                         // (HiF4: a code's 2^-9 and the 1/4 of its step)
+                s_xs[st * MP + m] = __uint_as_float((uint32_t)(127 + ec + (HIF4 ? 7 : 0)) << 23);
+#pragma unroll
+            for (int j = 0; j < BX; ++j) {
+                uint32_t h[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    // HiF4 codes decode in the order 0 2 | 1 3 | 4 6 | 5 7
+                    const int lo = HIF4 ? (q >> 1) * 4 + (q & 1) : 2 * q, hi = HIF4 ? lo + 2 : lo + 1;
+                    h[q] = pack_f16(f[j][lo] * mul, f[j][hi] * mul);
+                }
+                *reinterpret_cast<uint4 *>(s_x + st * S::kStepX + (8 * j + g) * S::kBlockX + ((m * 4 + c) << 4)) =
+                    make_uint4(h[0], h[1], h[2], h[3]);
+            }
+        };
+        // (loops, not unrolled: a short kernel pays for every line of code it
+        // fetches)
+        constexpr int kAhead = MP < 4 ? 1 : 2;
+        const int tasks = nb * M;
+#pragma unroll 1
+        for (int i = warp; i < tasks; i += kAhead * kWarps) {
+            uint4 u[kAhead][BX];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                load_x(min(i + j * kWarps, tasks - 1), u[j]);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                store_x(min(i + j * kWarps, tasks - 1), u[j]);
+        }
+        // W~ only now: its boxes in front of x in the memory's queues would
+        // hold up every warp (15.0 us against 13.5 at 1 x 4096 x 24576)
+        if (pb > b0)                                               // (the rings held parts of tiles)
+            fence_proxy_async_smem();
+#pragma unroll 1
+        for (int i = 0; i < p.depth; ++i)
+            fetch();
+        Scales<FMT, CB, BX> sc;
+        uint32_t next[BX * sc.kN];
+        if (f0 < f1) {
+            sc.tile(p, (t0 + first) * kTile + g, pb + f0 - first * nb, c);
+            sc.load(p, next);
+        }
+        if (lane == 0)
+            s_run[warp] = make_int4(f0, f1, first, last);
         __syncthreads();
-        ok = ok && mbar_wait(&s_full[b], ((w - w0) >> 1) & 1, kWaitLimitNs);
-        if (!ok)                                               // (once more before its copies' memory may go)
-            mbar_wait(&s_full[b], ((w - w0) >> 1) & 1, kWaitLimitNs);
-        if (ok) {
+
+        float acc[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                acc[t][i] = 0.f;
+        // this lane's column of B: row of x (past the last one: the last, a
+        // column that nobody reads) and block of a group; for the other blocks
+        // it reads zeros
+        uint32_t xbase[NT][CB], xstep[CB];
+        int xcol[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+                xbase[t][j] = (CB == 1 || g % CB == j) ? smem_u32(s_x) + ((min(8 * t + g / CB, M - 1) * 4 + c) << 4)
+                                                       : smem_u32(s_zero);
+            xcol[t][0] = min(8 * t + 2 * c / CB, M - 1);
+            xcol[t][1] = min(8 * t + (2 * c + 1) / CB, M - 1);
+        }
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+            xstep[j] = CB == 1 || g % CB == j ? S::kStepX : 0;
+        auto flush = [&](int t) {
+            float4 *const d = reinterpret_cast<float4 *>(t == first  ? s_head + warp * S::kPart
+                                                         : t == last ? s_ring
+                                                                     : s_tot + t * S::kPart);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                float4 v = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+                if (!ok)
+                    v.x = v.y = v.z = v.w = __int_as_float(0x7FFFFFFF);
+                if (t != first && t != last && pb > b0) {
+                    const float4 u = d[j * 32 + lane];
+                    v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+                }
+                d[j * 32 + lane] = v;
+                acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+            }
+        };
+        // ldmatrix: matrix lane / 8 = (8 rows (lane / 8) % 2, block parity lane / 16)
+        const int row = ((lane >> 3) & 1) * 8 + (lane & 7);
+        uint32_t aoff[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            aoff[q] = smem_u32(s_ring) + row * 128 + (((q * 2 + (lane >> 4)) ^ (row & 7)) << 4);
+
+        int tile = first, step = f0 - first * nb;
+#pragma unroll 1
+        for (int f = f0; f < f1; ++f) {
+            uint32_t cur[BX * sc.kN];
+#pragma unroll
+            for (int i = 0; i < BX * sc.kN; ++i)
+                cur[i] = next[i];
+            if (f + 1 < f1) {
+                if (step + 1 == nb)
+                    sc.tile(p, (t0 + tile + 1) * kTile + g, pb, c);
+                sc.load(p, next);
+            }
+            uint32_t xat[NT][CB];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < CB; ++j)
+                    xat[t][j] = xbase[t][j] + step * xstep[j];
+            if (!mbar_wait(&s_full[warp][slot], parity, kWaitLimitNs))
+                ok = false;
             float win[NT][4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     win[t][i] = 0.f;
-#pragma unroll 1
-            for (int box = half; box < S::kBoxes; box += 2) {
-                const uint32_t base = smem_u32(s_w) + b * S::kStage + box * kBoxBytes;
-                // ldmatrix: matrix lane / 8 = (8 rows (lane / 8) % 2, block parity lane / 16)
-                const int row = rt * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
 #pragma unroll
-                for (int pair = 0; pair < 4; ++pair) {         // two 32-code blocks
-                    const int chunk = pair * 2 + (lane >> 4);  // 16 bytes
+            for (int b = 0; b < BX; ++b) {
+                float tmp[NT][4];
+                const uint32_t *const w = cur + b * sc.kN;         // [half][row]
+#pragma unroll
+                for (int pair = 0; pair < 4; ++pair) {             // two 32-code blocks
                     uint32_t a[4];
-                    ldmatrix_x4(base + row * 128 + ((chunk ^ (row & 7)) << 4), a);
-                    float tmp[NT][4];
+                    ldmatrix_x4(aoff[pair] + slot * kStepBytes + b * kBoxBytes, a);
+                    uint32_t m0 = 0, m1 = 0;                       // HiF4 metadata of rows g and g + 8
                     if (HIF4) {
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                tmp[t][i] = 0.f;
+                        m0 = __shfl_sync(kAll, w[0], 4 * g + pair);
+                        m1 = __shfl_sync(kAll, w[1], 4 * g + pair);
                     }
-                    const int kw = HIF4 ? box * 4 + pair : box * 2 + (pair >> 1);
-                    const uint32_t sw0 = s_sc[kw * kRows + rt * 16 + g], sw1 = s_sc[kw * kRows + rt * 16 + g + 8];
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        uint32_t h0[4], h1[4];                 // rows g and g + 8
+                        const int blk = pair * 2 + s;
+                        uint32_t h0[4], h1[4];                     // rows g and g + 8
                         if (HIF4) {
                             s1p2x8_f16(a[2 * s], h0);
                             s1p2x8_f16(a[2 * s + 1], h1);
-                            uint32_t t0, t1;
-                            hif4_pow2_pair(sw0, 4 * s + c, t0, t1);
-                            h0[0] = hmul2(h0[0], t0), h0[1] = hmul2(h0[1], t0);
-                            h0[2] = hmul2(h0[2], t1), h0[3] = hmul2(h0[3], t1);
-                            hif4_pow2_pair(sw1, 4 * s + c, t0, t1);
-                            h1[0] = hmul2(h1[0], t0), h1[1] = hmul2(h1[1], t0);
-                            h1[2] = hmul2(h1[2], t1), h1[3] = hmul2(h1[3], t1);
+                            uint32_t e0, e1;
+                            hif4_pow2_pair(m0, 4 * s + c, e0, e1);
+                            h0[0] = hmul2(h0[0], e0), h0[1] = hmul2(h0[1], e0);
+                            h0[2] = hmul2(h0[2], e1), h0[3] = hmul2(h0[3], e1);
+                            hif4_pow2_pair(m1, 4 * s + c, e0, e1);
+                            h1[0] = hmul2(h1[0], e0), h1[1] = hmul2(h1[1], e0);
+                            h1[2] = hmul2(h1[2], e1), h1[3] = hmul2(h1[3], e1);
                         } else {
                             e2m1x8_f16(a[2 * s], h0);
                             e2m1x8_f16(a[2 * s + 1], h1);
+                        }
+                        // (a HiF4 block of 64 is two of these: with one block a
+                        // column its sums stay in tmp until the second)
+                        constexpr int GROUP = CB > 1 ? CB : HIF4 ? 2 : 1;
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            uint4 x;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                                         : "r"(xat[t][blk % CB] + (8 * b + blk) * S::kBlockX));
+                            if (blk % GROUP == 0)
+                                mma_f16_first(tmp[t], h0[0], h1[0], h0[1], h1[1], x.x, x.y);
+                            else
+                                mma_f16(tmp[t], h0[0], h1[0], h0[1], h1[1], x.x, x.y);
+                            mma_f16(tmp[t], h0[2], h1[2], h0[3], h1[3], x.z, x.w);
+                        }
+                        if (blk % GROUP == GROUP - 1) {
+                            // scales of this lane's four sums: rows g, g + 8, columns 2c, 2c + 1
+                            float u[2][2];
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                if (HIF4) {             // CB 8: 64-code block c; 4: block c % 2 of the half box;
+                                                        // 2 and 1: the one at hand
+                                    u[r][0] = u[r][1] = hif4_macro_f32(
+                                        CB == 8   ? w[r]
+                                        : CB == 4 ? __shfl_sync(kAll, w[r], 4 * g + (blk >> 2) * 2 + (c & 1))
+                                        : r       ? m1
+                                                  : m0);
+                                } else if (CB >= 4) {   // 8: blocks 2c, 2c + 1; 4: (blk / 4) 4 + 2c % 4, + 1
+                                    const uint32_t v = w[(CB == 8 ? 0 : (blk >> 2) * 2) + r] >> (16 * (c & 1));
+                                    u[r][0] = e8m0_byte(v, 0), u[r][1] = e8m0_byte(v, 1);
+                                } else {
+                                    const uint32_t v = w[(blk >> 2) * 2 + r];
+                                    u[r][0] = e8m0_byte(v, CB == 2 ? (blk & 2) : blk & 3);
+                                    u[r][1] = CB == 2 ? e8m0_byte(v, (blk & 2) + 1) : u[r][0];
+                                }
+                            }
 #pragma unroll
                             for (int t = 0; t < NT; ++t)
 #pragma unroll
                                 for (int i = 0; i < 4; ++i)
-                                    tmp[t][i] = 0.f;
-                        }
-                        const int blk = box * 8 + pair * 2 + s;
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            const uint4 xb =
-                                *reinterpret_cast<const uint4 *>(s_x + (((blk * NT + t) * 32 + lane) << 4));
-                            mma_f16(tmp[t], h0[0], h1[0], h0[1], h1[1], xb.x, xb.y);
-                            mma_f16(tmp[t], h0[2], h1[2], h0[3], h1[3], xb.z, xb.w);
-                        }
-                        if (!HIF4) {
-                            const int sh = ((pair & 1) * 2 + s) * 8;
-                            const float f0 = e8m0_f32((sw0 >> sh) & 0xFFu), f1 = e8m0_f32((sw1 >> sh) & 0xFFu);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                win[t][0] = fmaf(tmp[t][0], f0, win[t][0]);
-                                win[t][1] = fmaf(tmp[t][1], f0, win[t][1]);
-                                win[t][2] = fmaf(tmp[t][2], f1, win[t][2]);
-                                win[t][3] = fmaf(tmp[t][3], f1, win[t][3]);
-                            }
-                        }
-                    }
-                    if (HIF4) {
-                        const float f0 = hif4_macro_f32(sw0), f1 = hif4_macro_f32(sw1);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            win[t][0] = fmaf(tmp[t][0], f0, win[t][0]);
-                            win[t][1] = fmaf(tmp[t][1], f0, win[t][1]);
-                            win[t][2] = fmaf(tmp[t][2], f1, win[t][2]);
-                            win[t][3] = fmaf(tmp[t][3], f1, win[t][3]);
+                                    win[t][i] = fmaf(tmp[t][i], u[i >> 1][i & 1], win[t][i]);
                         }
                     }
                 }
             }
-            // HiF4: a code's 2^-9 and the 1/4 of its step
-            constexpr float kUnit = HIF4 ? 128.f : 1.f;
+            __syncwarp();                                          // every lane has read the step
+            fetch();
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float u0 = s_xscale[8 * t + 2 * c] * kUnit, u1 = s_xscale[8 * t + 2 * c + 1] * kUnit;
-                acc[t][0] = fmaf(win[t][0], u0, acc[t][0]);
-                acc[t][1] = fmaf(win[t][1], u1, acc[t][1]);
-                acc[t][2] = fmaf(win[t][2], u0, acc[t][2]);
-                acc[t][3] = fmaf(win[t][3], u1, acc[t][3]);
+                const float x0 = s_xs[step * MP + xcol[t][0]], x1 = CB > 1 ? x0 : s_xs[step * MP + xcol[t][1]];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[t][i] = fmaf(win[t][i], i & 1 ? x1 : x0, acc[t][i]);
+            }
+            if (++slot == p.depth) {
+                slot = 0;
+                parity ^= 1;
+            }
+            if (++step == nb || f + 1 == f1) {
+                flush(tile);
+                if (step == nb) {
+                    step = 0;
+                    ++tile;
+                }
             }
         }
         __syncthreads();
-        if (tid == 0 && w + 2 < w1)
-            fetch(w + 2);
+        // tiles that a warp began or ended with: the warps' parts in order
+        for (int t = warp; t < nt; t += kWarps) {
+            float4 *const d = reinterpret_cast<float4 *>(s_tot + t * S::kPart);
+            float4 v[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+                v[j] = pb > b0 ? d[j * 32 + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+            bool inner = false;
+            for (int w = 0; w < kWarps; ++w) {
+                const int4 run = s_run[w];
+                if (run.x == run.y || t < run.z || t > run.w)
+                    continue;
+                if (t != run.z && t != run.w) {
+                    inner = true;
+                    break;
+                }
+                const float4 *const q =
+                    reinterpret_cast<const float4 *>(t == run.z ? s_head + w * S::kPart : smem + w * p.depth * kStepBytes);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const float4 u = q[j * 32 + lane];
+                    v[j].x += u.x, v[j].y += u.y, v[j].z += u.z, v[j].w += u.w;
+                }
+            }
+            if (!inner)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    d[j * 32 + lane] = v[j];
+        }
+        // a tile's y is written by the warp that summed it, unless other CTAs
+        // or another phase add to it
+        if (split > 1 || pb + p.phase < b1)
+            __syncthreads();
     }
 
-    if (!ok)
+    // ---- y: with a cluster, the ranks' sums in order, each rank a share of the tiles
+    if (split > 1)
+        cluster_sync();
+    for (int t = rank * kWarps + warp; t < nt; t += split * kWarps) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = __int_as_float(0x7FFFFFFF);
-    // the CTA's part: [half][x row][row of W~], over the codes' shared memory
-    float *const s_part = reinterpret_cast<float *>(smem);
+        for (int j = 0; j < NT; ++j) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint32_t at = smem_u32(s_tot) + t * S::kPart + (j * 32 + lane) * 16;
+            // (all ranks' loads in flight before the first sum)
+            float u[8][4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+            for (int q = 0; q < 8; ++q)
+                if (q < split)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(u[q][0]), "=f"(u[q][1]), "=f"(u[q][2]), "=f"(u[q][3])
+                                 : "r"(split > 1 ? mapa_shared(at, q) : at));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            s_part[(half * 8 * NT + 8 * t + 2 * c + (i & 1)) * kRows + rt * 16 + g + (i >> 1) * 8] = acc[t][i];
-    cluster_sync();
-    // each rank finishes its share of the elements, all ranks' parts added in order
-    const int elems = p.M * kRows;
-    const uint32_t part = smem_u32(s_part);
-    for (int i = rank * kThreads + tid; i < elems; i += split * kThreads) {
-        const int m = i / kRows, r = i % kRows;
-        float sum = 0.f;
-        for (int q = 0; q < split; ++q)
+            for (int q = 0; q < 8; ++q)
+                if (q < split)
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                float v;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                             : "=f"(v)
-                             : "r"(mapa_shared(part + ((hf * 8 * NT + m) * kRows + r) * 4, q)));
-                sum += v;
+                    for (int i = 0; i < 4; ++i)
+                        v[i] += u[q][i];
+            // the columns of a row of x
+            if (CB >= 2) {
+                v[0] += v[1];
+                v[2] += v[3];
             }
-        if (n0 + r < p.N) {
-            const int64_t o = (int64_t)m * p.N + n0 + r;
-            if (p.bf16)
-                static_cast<__nv_bfloat16 *>(p.y)[o] = __float2bfloat16_rn(sum);
-            else
-                static_cast<float *>(p.y)[o] = sum;
+            if (CB >= 4) {
+                v[0] += __shfl_xor_sync(kAll, v[0], 1);
+                v[2] += __shfl_xor_sync(kAll, v[2], 1);
+            }
+            if (CB >= 8) {
+                v[0] += __shfl_xor_sync(kAll, v[0], 2);
+                v[2] += __shfl_xor_sync(kAll, v[2], 2);
+            }
+            const bool owner = CB < 4 || 2 * c % CB == 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (CB >= 2 && (i & 1))
+                    continue;
+                const int m = 8 * j + (2 * c + (i & 1)) / CB, n = (t0 + t) * kTile + g + (i >> 1) * 8;
+                if (owner && m < M && n < p.N) {
+                    if (p.bf16)
+                        static_cast<__nv_bfloat16 *>(p.y)[(int64_t)m * p.N + n] = __float2bfloat16_rn(v[i]);
+                    else
+                        static_cast<float *>(p.y)[(int64_t)m * p.N + n] = v[i];
+                }
+            }
         }
     }
-    cluster_sync();
+    if (split > 1)
+        cluster_sync();
 }
 
-template <int FMT, int NT>
+// CTAs along K (a cluster): the choice with the least time by a count of
+// clocks of one SM: a box costs the decoding of its codes, and more with
+// HiF4's sub-group scales or several column tiles; a row of x and step costs
+// its conversion; a cluster its barriers and the sums over distributed shared
+// memory, more the wider it is; a phase after the first (x does not fit at
+// once) a pause.  Measured in us with 1, 2, 4 and 8 CTAs along K, MXFP4:
+// 4 x 12288 x 4096 15.8, 11.8, 11.3, 13.5; 16 x 4096 x 4096 14.1, 9.9, 9.0,
+// 12.3; 8 x 4096 x 4096 7.3, 7.4, 7.5, 9.8; 1 x 4096 x 24576 13.5, 17.0.
+constexpr int kRowClocks = 25, kClusterClocks = 1000, kPhaseClocks = 3000;
+
+// Clusters of `split` CTAs that the GPU holds at once (a GPC holds whole
+// clusters only: 152 SMs are not 19 clusters of eight).
+template <int FMT, int MP>
+int clusters_at_once(int split)
+{
+    static int known[4];           // by log2(split), 0: not asked yet
+    int &n = known[split == 1 ? 0 : split == 2 ? 1 : split == 4 ? 2 : 3];
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(split, num_sms());
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kSmemBytes;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {(unsigned)split, 1, 1};
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int got = 0;
+        if (split == 1 || cudaOccupancyMaxActiveClusters(&got, matvec_kernel<FMT, MP>, &cfg) != cudaSuccess || got < 1)
+            got = num_sms() / split;
+        n = got;
+    }
+    return n;
+}
+
+template <int FMT, int MP>
+int split_of(int64_t tiles, int steps, int phase, int M)
+{
+    using S = Shape<MP>;
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= 8 && s <= steps; s *= 2) {
+        const int64_t groups = clusters_at_once<FMT, MP>(s);
+        const int64_t waves = (tiles + groups * S::kTiles - 1) / (groups * S::kTiles);
+        const int64_t rounds = (tiles + groups - 1) / groups, nb = (steps + s - 1) / s;
+        const int64_t box = (FMT == RFQ_FMT_HIF4 ? 140 : 85) + 35 * (S::kNt - 1);
+        const int64_t t = rounds * nb * S::kBx * box + waves * (M * nb * kRowClocks + (s > 1 ? s * kClusterClocks : 0) +
+                                                                ((nb + phase - 1) / phase - 1) * kPhaseClocks);
+        if (t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
+}
+
+template <int FMT, int MP>
 cudaError_t launch(const MatvecArgs &a, cudaStream_t st)
 {
-    using S = Shape<NT>;
+    using S = Shape<MP>;
     const int64_t N = a.w.rows, K = a.w.k;
-    const int windows = (int)((K + S::kWinK - 1) / S::kWinK);
-    const int64_t tiles = (N + kRows - 1) / kRows;
-    // split K until every SM has a few CTAs
-    int split = 1;
-    while (split < 8 && split * 2 <= windows && tiles * split < 4 * (int64_t)num_sms())
-        split *= 2;
-    Params p = {static_cast<const __nv_bfloat16 *>(a.x), a.x_row, a.M, N, K, static_cast<const uint8_t *>(a.w.scales),
-                a.w.scale_layout == RFQ_SCALE_MMA, a.y, a.bf16, (windows + split - 1) / split};
-    CUtensorMap map;
-    if (!encode_tmap_2d_u8(&map, a.w.codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, kBoxK / 2, kRows, 128))
-        return cudaErrorInvalidValue;
+    const int64_t tiles = (N + kTile - 1) / kTile;
+    const int steps = (int)((K + S::kStepK - 1) / S::kStepK);
+    const int step_x = S::kStepX + MP * 4;                         // shared bytes of x a step
+    const int most = S::kMaxX / step_x;
     static bool ready = false;     // (per instantiation; setting it twice is harmless)
     if (!ready) {
-        if (cudaError_t e = cudaFuncSetAttribute(matvec_kernel<FMT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 S::kSmem))
+        if (cudaError_t e = cudaFuncSetAttribute(matvec_kernel<FMT, MP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 kSmemBytes))
             return e;
         ready = true;
     }
+    const int split = split_of<FMT, MP>(tiles, steps, most, a.M);
+    const int nb = (steps + split - 1) / split, phase = nb < most ? nb : most;
+    int64_t groups = clusters_at_once<FMT, MP>(split);
+    if (groups > tiles)
+        groups = tiles;
+    if ((tiles + groups - 1) / groups > S::kTiles)
+        groups = (tiles + S::kTiles - 1) / S::kTiles;
+    const int fixed = 1024 + (kWarps + S::kTiles) * S::kPart + S::kZero + phase * step_x;
+    int depth = (kSmemBytes - fixed) / (kWarps * S::kStepBytes);
+    depth = depth < kMaxDepth ? depth : kMaxDepth;
+    const bool mma = a.w.scale_layout == RFQ_SCALE_MMA;
+    const Params p = {static_cast<const __nv_bfloat16 *>(a.x), a.x_row, a.M, (int)N, (int)K,
+                      static_cast<const uint8_t *>(a.w.scales), mma, mma || K % 128 == 0, a.y, a.bf16,
+                      (int)tiles, steps, phase, depth};
+    CUtensorMap map;
+    if (!encode_tmap_2d_u8(&map, a.w.codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, kBoxK / 2, kTile, 128))
+        return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(split, (unsigned)tiles);
+    cfg.gridDim = dim3(split, (unsigned)groups);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = S::kSmem;
+    cfg.dynamicSmemBytes = fixed + depth * kWarps * S::kStepBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {(unsigned)split, 1, 1};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, matvec_kernel<FMT, NT>, map, p);
+    return cudaLaunchKernelEx(&cfg, matvec_kernel<FMT, MP>, map, p);
 }
 
 template <int FMT>
 cudaError_t launch_rows(const MatvecArgs &a, cudaStream_t st)
 {
-    return a.M <= 8 ? launch<FMT, 1>(a, st) : a.M <= 16 ? launch<FMT, 2>(a, st) : launch<FMT, 4>(a, st);
+    return a.M == 1   ? launch<FMT, 1>(a, st)
+           : a.M == 2 ? launch<FMT, 2>(a, st)
+           : a.M <= 4 ? launch<FMT, 4>(a, st)
+           : a.M <= 8 ? launch<FMT, 8>(a, st)
+           : a.M <= 16 ? launch<FMT, 16>(a, st)
+                       : launch<FMT, 32>(a, st);
 }
 
 } // namespace
