@@ -19,16 +19,19 @@
 //
 // Bound: HBM at long caches: 136 (MXFP4) or 144 (HiF4) bytes a key and head
 // of 128.  An SM's share of the measured copy rate is one of these every 5.8
-// clocks, so a key may cost at most 23 warp instructions.
+// clocks, so a key may cost at most 23 warp instructions, 11 of them on the
+// pipe that converts codes.
 //
 // Work: the (request, key head, row tile) segments of all requests laid end
-// to end, in units of 128 keys, are split evenly over the resident CTAs,
-// however ragged the lengths.  A segment that one CTA holds whole is written
-// by it; the parts of others go to the workspace, and the last CTA to finish
-// adds them in the order of the keys (the split depends on the lengths
-// alone: a call gives the same bits every time).  One producer warp copies the
-// pages' contiguous bytes into a ring of stages; eight consumer warps take 16
-// keys of a stage each and are joined once per segment.
+// to end, in chunks of 32 keys and one more unit a segment for its start, are
+// split evenly over the CTAs (one a SM) and there over the warps, however
+// ragged the lengths.  A warp copies the chunks of its run (contiguous pieces
+// of pages) into its own small ring and waits for no other warp.  It writes
+// the segments that it holds whole; the parts of others wait in shared memory
+// for the CTA's end, when all warps join them, and the parts of segments that
+// CTAs share go to the workspace, where the last CTA to finish joins them.
+// The split and the order of every sum depend on the lengths alone: a call
+// gives the same bits every time.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -40,8 +43,9 @@
 namespace rfq {
 namespace {
 
-constexpr int kConsumers = 8, kThreads = 32 * (kConsumers + 1);
-constexpr int kUnit = 16 * kConsumers;       // keys of a stage
+constexpr int kChunk = 32;                   // keys of a chunk
+constexpr int kLeast = 8;                    // units of a CTA, at least
+constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t a)
 {
@@ -63,345 +67,232 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-__device__ __forceinline__ void consumer_sync()
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kConsumers) : "memory");
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
 struct Params {
     KvAttentionArgs a;
     int group;                 // query heads per key head
-    int gran;                  // keys of one copy: the largest power of two dividing a page, at most 128
+    int gran;                  // keys of one copy: 32 where a page is whole chunks, else 16
     int32_t *status;
     int32_t *counter;          // [CTAs] parts of a split segment that have arrived
-    float *part_ml;            // [2 CTAs][rows][2]
-    float *part_o;             // [2 CTAs][rows][D]
+    float *part;               // [2 CTAs] parts: Shape::kPart bytes each
 };
 
 template <int FMT, int D, int NT>
 struct Shape {
-    static constexpr int kRows = 8 * NT;
+    // 12 warps leave a thread 168 registers: with 16 the loop over the keys
+    // spills at D = 128 (323 us against 230 at 8 x 131072 keys, MXFP4), and
+    // eight hide less latency (275 us)
+    static constexpr int kWarps = NT > 1 ? 8 : D == 64 ? 16 : 12, kThreads = 32 * kWarps;
+    static constexpr int kRows = 8 * NT, kMt = D / 16;
     static constexpr int kScale = FMT == RFQ_FMT_HIF4 ? D / 16 : D / 32;   // bytes a token
     static constexpr int kCode = D / 2;
-    static constexpr int kVOff = kUnit * kCode, kKsOff = 2 * kVOff, kVsOff = kKsOff + kUnit * kScale;
-    static constexpr int kStage = kVsOff + kUnit * kScale;
-    static constexpr int kBlocksPerSm = NT == 1 ? 2 : 1;
-    static constexpr int kMerge = kConsumers * 8 * D * 4;
-    static constexpr int kQ = NT > 1 ? NT * D * 16 : 0;
-    static constexpr int kStages = ((kBlocksPerSm == 2 ? 108 : 200) * 1024 - kMerge - kQ) / kStage;
-    static constexpr int kSmem = kStages * kStage + kMerge + kQ;
+    static constexpr int kVOff = kChunk * kCode, kKsOff = 2 * kVOff, kVsOff = kKsOff + kChunk * kScale;
+    static constexpr int kBytes = kVsOff + kChunk * kScale;                // of a chunk
+    static constexpr int kDepth = D == 64 ? 4 : 3;                              // chunks in a warp's ring
+    // a part: NT D/16 float4 a lane, and a float4 (m, m, l, l) a lane and column tile
+    static constexpr int kPart = NT * (kMt + 1) * 512;
+    static constexpr int kQ = NT > 1 ? NT * D * 16 : 0;                    // of a warp
+    static constexpr int kSmem = kWarps * (kDepth * kBytes + kPart + kQ);
+    static_assert(kDepth * kBytes >= kPart, "a warp's last part lies over its ring");
 };
 
 // One request: n new tokens (rows q0 .. of q) at the end of its L keys.
 struct Request {
     int n, L, q0;
-    __device__ void load(const KvAttentionArgs &a, int r, int32_t *status)
+    __device__ __forceinline__ void load(const KvAttentionArgs &a, int r, int32_t *status)
     {
-        const int64_t most = (int64_t)a.width * a.cache.page_size;
+        const int most = a.width * a.cache.page_size;      // (the host has seen that it fits an int)
         const int len = __ldg(a.lengths + r);
-        L = (int)min((int64_t)max(len, 0), most);
-        int q1 = r + 1;
+        L = min(max(len, 0), most);
         q0 = r;
+        n = 1;
+        bool ok = len == L;
         if (a.q_start) {
             q0 = __ldg(a.q_start + r);
-            q1 = __ldg(a.q_start + r + 1);
+            const int q1 = __ldg(a.q_start + r + 1);
+            n = q1 - q0;
+            if (q0 < 0 || q0 > q1 || q1 > a.tokens) {
+                ok = false;
+                n = 0;
+            }
         }
-        const bool rows_ok = q0 >= 0 && q0 <= q1 && q1 <= a.tokens;
-        n = rows_ok ? q1 - q0 : 0;
-        if ((len != L || !rows_ok) && status)
+        if (!ok && status)
             atomicCAS(status, kDevOk, kDevBadGroups);
     }
     // Tiles of `rows` (token, head) rows
-    __device__ int tiles(int group, int rows) const { return (int)(((int64_t)n * group + rows - 1) / rows); }
+    __device__ __forceinline__ int tiles(int group, int rows) const { return (n * group + rows - 1) / rows; }
     // Keys [kb, ke) that some row of the tile sees, kb rounded down to gran
-    __device__ void keys(int tile, int group, int rows, int window, int gran, int &kb, int &ke) const
+    __device__ __forceinline__ void keys(int tile, const Params &p, int rows, int &kb, int &ke) const
     {
-        const int first = (int)((int64_t)tile * rows / group);
-        const int last = (int)min((int64_t)n - 1, ((int64_t)(tile + 1) * rows - 1) / group);
+        int first = 0, last = 0;
+        if (n > 1) {
+            first = tile * rows / p.group;
+            last = min(n - 1, (tile * rows + rows - 1) / p.group);
+        }
         ke = max(0, L - n + last + 1);
-        kb = window > 0 ? max(0, L - n + first + 1 - window) / gran * gran : 0;
-        kb = min(kb, ke / gran * gran);
+        kb = p.a.window > 0 ? max(0, L - n + first + 1 - p.a.window) & -p.gran : 0;
+        kb = min(kb, ke & -p.gran);
     }
-    __device__ int units(int tile, int group, int rows, int window, int gran) const
+    // Units of a tile: its chunks (one at least) and one more
+    __device__ __forceinline__ uint32_t units(int tile, const Params &p, int rows) const
     {
         int kb, ke;
-        keys(tile, group, rows, window, gran, kb, ke);
-        return max(1, (ke - kb + kUnit - 1) / kUnit);
-    }
-    // Units of one key head
-    __device__ long long all_units(int group, int rows, int window, int gran) const
-    {
-        long long s = 0;
-        const int t = tiles(group, rows);
-        for (int i = 0; i < t; ++i)
-            s += units(i, group, rows, window, gran);
-        return s;
+        keys(tile, p, rows, kb, ke);
+        return max(1, (ke - kb + kChunk - 1) / kChunk) + 1;
     }
 };
 
-// The segments of a CTA's share of the units, one after the other.
+__device__ __forceinline__ uint32_t warp_scan(uint32_t v, int lane)    // inclusive
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t x = __shfl_up_sync(kAll, v, d);
+        if (lane >= d)
+            v += x;
+    }
+    return v;
+}
+
+// Units of one key head of a request (the whole warp together)
+template <int ROWS>
+__device__ __forceinline__ uint32_t head_units(const Request &q, const Params &p, int lane)
+{
+    const int n = q.tiles(p.group, ROWS);
+    uint32_t s = 0;
+#pragma unroll 1
+    for (int t = lane; t < n; t += 32)
+        s += q.units(t, p, ROWS);
+    return __reduce_add_sync(kAll, s);
+}
+
+// Walks requests [r, r1) with the whole warp until `rem` units lie behind:
+// returns the units of all of them, or stops at the request in which rem
+// runs out, with rem units of it.  Requests of one token are taken 32 at a
+// time, a lane each.
+template <int ROWS>
+__device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status)
+{
+    uint32_t all = 0;
+    const int H = p.a.cache.heads;
+    if (!p.a.q_start) {
+#pragma unroll 1
+        for (; r < r1; r += 32) {
+            uint32_t mine = 0;
+            if (r + lane < r1) {
+                Request q;
+                q.load(p.a, r + lane, status);
+                mine = H * (uint32_t)q.tiles(p.group, ROWS) * q.units(0, p, ROWS);
+            }
+            const uint32_t upto = warp_scan(mine, lane), sum = __shfl_sync(kAll, upto, 31);
+            if (rem < sum) {
+                const int at = __ffs(__ballot_sync(kAll, rem < upto)) - 1;
+                rem -= __shfl_sync(kAll, upto - mine, at);
+                r += at;
+                return all;
+            }
+            rem -= sum;
+            all += sum;
+        }
+    } else {
+#pragma unroll 1
+        for (; r < r1; ++r) {
+            Request q;
+            q.load(p.a, r, status);
+            const uint32_t sum = H * head_units<ROWS>(q, p, lane);
+            if (rem < sum)
+                return all;
+            rem -= sum;
+            all += sum;
+        }
+    }
+    return all;
+}
+
+// The segments of a warp's run of units, one after the other.
 template <int ROWS>
 struct Walk {
-    const Params &p;
     int r, head, tile, ntiles;
     Request q;
-    int kb, ke, units;         // of the segment
-    int i0, i1;                // this CTA's units of it
-    long long u, u1;           // the CTA's units left
-    __device__ Walk(const Params &pp, int r0, long long rem, long long first, long long last) : p(pp), r(r0), u(first), u1(last)
+    int kb, ke, chunks;        // of the segment
+    int i, i1;                 // the warp's chunks of it left
+    uint32_t u, end;           // the segment's first unit; the end of the warp's units
+    // from unit `first`, `rem` units into the segments of request r0
+    __device__ __forceinline__ void start(const Params &p, int r0, uint32_t rem, uint32_t first, uint32_t last, int lane)
     {
-        if (u >= u1)
+        r = r0;
+        end = last;
+        head = tile = i = i1 = 0;
+        u = last;
+        if (first >= last)
             return;
         q.load(p.a, r, nullptr);
         ntiles = q.tiles(p.group, ROWS);
-        const long long per = q.all_units(p.group, ROWS, p.a.window, p.gran);
+        const uint32_t per = head_units<ROWS>(q, p, lane);
         head = (int)(rem / per);
         rem -= head * per;
-        for (tile = 0;; ++tile) {
-            const int n = q.units(tile, p.group, ROWS, p.a.window, p.gran);
-            if (rem < n)
+#pragma unroll 1
+        for (;; tile += 32) {
+            const uint32_t mine = tile + lane < ntiles ? q.units(tile + lane, p, ROWS) : 0u;
+            const uint32_t upto = warp_scan(mine, lane);
+            const uint32_t hit = __ballot_sync(kAll, rem < upto);
+            if (hit) {
+                const int at = __ffs(hit) - 1;
+                rem -= __shfl_sync(kAll, upto - mine, at);
+                tile += at;
                 break;
-            rem -= n;
-        }
-        segment((int)rem);
-    }
-    __device__ void segment(int from)
-    {
-        q.keys(tile, p.group, ROWS, p.a.window, p.gran, kb, ke);
-        units = max(1, (ke - kb + kUnit - 1) / kUnit);
-        i0 = from;
-        i1 = (int)min((long long)units, from + (u1 - u));
-    }
-    __device__ bool more() const { return u < u1; }
-    __device__ void next()
-    {
-        u += i1 - i0;
-        if (u >= u1)
-            return;
-        if (++tile == ntiles) {
-            tile = 0;
-            if (++head == p.a.cache.heads) {
-                head = 0;
-                do {               // (requests without new tokens have no segment)
-                    ++r;
-                    q.load(p.a, r, nullptr);
-                    ntiles = q.tiles(p.group, ROWS);
-                } while (ntiles == 0);
             }
+            rem -= __shfl_sync(kAll, upto, 31);
         }
-        segment(0);
+        u = first - rem;
+        segment(p, first);
+    }
+    // the chunks of the segment at u that lie in [from, end): chunk k is unit u + 1 + k
+    __device__ __forceinline__ void segment(const Params &p, uint32_t from)
+    {
+        q.keys(tile, p, ROWS, kb, ke);
+        chunks = max(1, (ke - kb + kChunk - 1) / kChunk);
+        i = from > u + 1 ? (int)(from - u - 1) : 0;
+        i1 = end > u + 1 ? (int)min((uint32_t)chunks, end - u - 1) : 0;
+    }
+    __device__ __forceinline__ bool more() const { return i < i1; }
+    // on to the next segment that has a chunk here, if any, once more() is false
+    __device__ __forceinline__ void next(const Params &p)
+    {
+#pragma unroll 1
+        while (i >= i1 && u < end) {
+            u += chunks + 1;
+            if (u >= end)
+                return;
+            if (++tile == ntiles) {
+                tile = 0;
+                if (++head == p.a.cache.heads) {
+                    head = 0;
+#pragma unroll 1
+                    do {               // (requests without new tokens have no segment)
+                        ++r;
+                        q.load(p.a, r, nullptr);
+                        ntiles = q.tiles(p.group, ROWS);
+                    } while (ntiles == 0);
+                }
+            }
+            segment(p, u);
+        }
     }
 };
 
-template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::kBlocksPerSm) kv_attention_kernel(const Params p)
-{
-    using S = Shape<FMT, D, NT>;
-    constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
-    constexpr int NB = D / 32, ROWS = S::kRows, MT = D / 16, STAGES = S::kStages;
-    extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t *const s_ring = smem;
-    float *const s_merge = reinterpret_cast<float *>(smem + STAGES * S::kStage);   // [warp][8][D]
-    uint4 *const s_q = reinterpret_cast<uint4 *>(smem + STAGES * S::kStage + S::kMerge);
-    __shared__ alignas(8) uint64_t s_full[STAGES], s_empty[STAGES];
-    __shared__ float s_m[kConsumers][ROWS], s_l[kConsumers][ROWS], s_qs[ROWS];
-    __shared__ long long s_scan[kConsumers + 1], s_rem;
-    __shared__ int s_r0, s_flag;
-
-    const KvAttentionArgs &a = p.a;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int H = a.cache.heads, G = p.group;
-
-    if (tid == 0) {
-        for (int i = 0; i < STAGES; ++i) {
-            mbar_init(&s_full[i], 1);
-            mbar_init(&s_empty[i], kConsumers);
-        }
-        fence_mbar_init();
-    }
-    // ---- this CTA's share: units of all requests, in order
-    const int per = (a.requests + kThreads - 1) / kThreads;
-    const int r0 = min(a.requests, tid * per), r1 = min(a.requests, r0 + per);
-    long long mine = 0;
-    for (int r = r0; r < r1; ++r) {
-        Request q;
-        q.load(a, r, blockIdx.x == 0 ? p.status : nullptr);
-        mine += H * q.all_units(G, ROWS, a.window, p.gran);
-    }
-    long long inc = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, inc, d);
-        if (lane >= d)
-            inc += v;
-    }
-    if (lane == 31)
-        s_scan[warp] = inc;
-    __syncthreads();
-    long long before = inc - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w <= kConsumers; ++w) {
-        if (w < warp)
-            before += s_scan[w];
-        total += s_scan[w];
-    }
-    const int ctas = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
-    if (cta >= ctas)
-        return;
-    const long long u0 = total * cta / ctas, u1 = total * (cta + 1) / ctas;
-    if (before <= u0 && u0 < before + mine) {
-        long long at = u0 - before;
-        for (int r = r0;; ++r) {
-            Request q;
-            q.load(a, r, nullptr);
-            const long long n = H * q.all_units(G, ROWS, a.window, p.gran);
-            if (at < n) {
-                s_r0 = r;
-                s_rem = at;
-                break;
-            }
-            at -= n;
-        }
-    }
-    __syncthreads();
-    Walk<ROWS> walk(p, s_r0, s_rem, u0, u1);
-    const uint64_t limit = ws_wait_limit_ns(p.status);
-    bool ok = true;
-    uint32_t it = 0;                          // stages used so far
-
-    if (warp == kConsumers) {
-        // ---- producer: lane j copies granule j of a stage
-        const int64_t token_row = (int64_t)a.cache.page_size;
-        const uint32_t gbytes = p.gran * (2 * S::kCode + 2 * S::kScale);
-        for (; walk.more(); walk.next()) {
-            const int32_t *const row = a.table + (int64_t)walk.r * a.width;
-            for (int i = walk.i0; i < walk.i1; ++i, ++it) {
-                const int st = it % STAGES;
-                const int key = walk.kb + i * kUnit + lane * p.gran;
-                bool have = lane * p.gran < kUnit && key < walk.ke;
-                int64_t at = 0;
-                if (have) {
-                    const int pg = key / a.cache.page_size, page = __ldg(row + pg);
-                    if (page < 0 || page >= a.cache.pages) {
-                        atomicCAS(p.status, kDevOk, kDevBadGroups);
-                        have = false;
-                    }
-                    at = ((int64_t)page * H + walk.head) * token_row + (key - pg * a.cache.page_size);
-                }
-                const uint32_t granules = __popc(__ballot_sync(0xFFFFFFFFu, have));
-                if (it >= STAGES)
-                    ok = ok && mbar_wait(&s_empty[st], (it / STAGES - 1) & 1, limit);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok)
-                    have = false;
-                if (lane == 0)
-                    mbar_arrive_expect_tx(&s_full[st], ok ? granules * gbytes : 0);
-                __syncwarp();
-                if (have) {
-                    uint8_t *const d = s_ring + st * S::kStage;
-                    const int tok = lane * p.gran;
-                    bulk_load(d + tok * S::kCode, static_cast<const uint8_t *>(a.cache.k_codes) + at * S::kCode,
-                              p.gran * S::kCode, &s_full[st]);
-                    bulk_load(d + S::kKsOff + tok * S::kScale,
-                              static_cast<const uint8_t *>(a.cache.k_scales) + at * S::kScale, p.gran * S::kScale,
-                              &s_full[st]);
-                    bulk_load(d + S::kVOff + tok * S::kCode, static_cast<const uint8_t *>(a.cache.v_codes) + at * S::kCode,
-                              p.gran * S::kCode, &s_full[st]);
-                    bulk_load(d + S::kVsOff + tok * S::kScale,
-                              static_cast<const uint8_t *>(a.cache.v_scales) + at * S::kScale, p.gran * S::kScale,
-                              &s_full[st]);
-                }
-            }
-        }
-        // nothing leaves while a copy of its own is in flight
-        for (uint32_t k = it > STAGES ? it - STAGES : 0; k < it; ++k)
-            if (!mbar_wait(&s_full[k % STAGES], (k / STAGES) & 1, limit))
-                ok = false;
-        if (!ok && lane == 0)
-            atomicExch(p.status, kDevTimeout);
-        return;
-    }
-
-    // ---- consumers
-    const int g = lane >> 2, c = lane & 3;
-    for (; walk.more(); walk.next()) {
-        const Request &q = walk.q;
-        const int row0 = walk.tile * ROWS, rows = (int)min((int64_t)ROWS, (int64_t)q.n * G - row0);
-        // q as f16, scaled by a power of two per row
-        uint4 qf[NB];
-        float qs[NT][2];
-        int hi[NT][2];                        // keys that the thread's two rows see: [max(0, hi - window), hi)
-        {
-            const float base = a.scale * 1.4426950408889634f * (HIF4 ? 128.f : 1.f);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                if (NT == 1 || t == warp) {
-                    const int rr = 8 * t + g, ri = row0 + rr;
-                    uint4 raw[NB];
-                    float mx = 0.f;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        raw[b] = make_uint4(0, 0, 0, 0);
-                        if (rr < rows)
-                            raw[b] = __ldg(reinterpret_cast<const uint4 *>(
-                                static_cast<const __nv_bfloat16 *>(a.q) + (q.q0 + ri / G) * a.q_token +
-                                (int64_t)(walk.head * G + ri % G) * a.q_head + 32 * b + 8 * c));
-                        const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[j] << 16)),
-                                                 fabsf(__uint_as_float(w[j] & 0xFFFF0000u))));
-                    }
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
-                    const int e = max(min((int)(__float_as_uint(mx) >> 23) - 127 - 14, 126), -126);
-                    const float mul = __uint_as_float((uint32_t)(127 - e) << 23);
-                    const float undo = __uint_as_float((uint32_t)(127 + e) << 23) * base;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
-                        float f[8];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            f[2 * j] = __uint_as_float(w[j] << 16) * mul;
-                            f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u) * mul;
-                        }
-                        uint32_t h[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            // HiF4 codes decode in the order 0 2 | 1 3 | 4 6 | 5 7
-                            const int lo = HIF4 ? (j >> 1) * 4 + (j & 1) : 2 * j, up = HIF4 ? lo + 2 : lo + 1;
-                            h[j] = pack_f16(f[lo], f[up]);
-                        }
-                        qf[b] = make_uint4(h[0], h[1], h[2], h[3]);
-                        if (NT > 1)
-                            s_q[(t * NB + b) * 32 + lane] = qf[b];
-                    }
-                    if (NT == 1) {
-                        qs[0][0] = __shfl_sync(0xFFFFFFFFu, undo, 8 * c);
-                        qs[0][1] = __shfl_sync(0xFFFFFFFFu, undo, 8 * c + 4);
-                    } else if (c == 0) {
-                        s_qs[rr] = undo;
-                    }
-                }
-            }
-            if (NT > 1)
-                consumer_sync();
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (NT > 1)
-                        qs[t][j] = s_qs[8 * t + 2 * c + j];
-                    const int ri = row0 + min(8 * t + 2 * c + j, rows - 1);
-                    hi[t][j] = max(0, q.L - q.n + ri / G + 1);
-                }
-        }
-        const int all_hi = max(0, q.L - q.n + row0 / G + 1);   // every row sees [all_lo, all_hi)
-        const int all_lo = a.window > 0 ? max(0, q.L - q.n + (row0 + rows - 1) / G + 1 - a.window) : 0;
-
-        float o[NT][MT][4], m[NT][2], l[NT][2];
-        int vref = -1000;                     // V scale exponents are relative to it (the same in a row's quad)
+// One warp's share of a row tile: O^T (dimensions g D/8 + 2i and + 1 by rows
+// 2c, 2c + 1), the running maxima and the sums of weights.
+template <int D, int NT>
+struct Sums {
+    static constexpr int MT = D / 16;
+    float o[NT][MT][4], m[NT][2], l[NT][2];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             m[t][0] = m[t][1] = -INFINITY;
@@ -412,156 +303,545 @@ __global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::kBlocksPerSm) kv_
                 for (int j = 0; j < 4; ++j)
                     o[t][i][j] = 0.f;
         }
-
-        for (int i = walk.i0; i < walk.i1; ++i, ++it) {
-            const int st = it % STAGES;
-            ok = ok && mbar_wait(&s_full[st], (it / STAGES) & 1, limit);
-            const int key0 = walk.kb + i * kUnit + warp * 16;
-            if (ok && key0 < walk.ke) {
-                const uint8_t *const ring = s_ring + st * S::kStage;
-                // ---- scores of 16 keys: rows g and g + 8 of the tile
-                uint32_t k0[NB], k1[NB];
-                {
-                    const uint8_t *const kr = ring + (warp * 16 + g) * S::kCode + c * NB * 4;
-                    if (D == 128) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(kr);
-                        const uint4 y = *reinterpret_cast<const uint4 *>(kr + 8 * S::kCode);
-                        k0[0] = x.x, k0[1] = x.y, k0[NB - 2] = x.z, k0[NB - 1] = x.w;
-                        k1[0] = y.x, k1[1] = y.y, k1[NB - 2] = y.z, k1[NB - 1] = y.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(kr);
-                        const uint2 y = *reinterpret_cast<const uint2 *>(kr + 8 * S::kCode);
-                        k0[0] = x.x, k0[1] = x.y;
-                        k1[0] = y.x, k1[1] = y.y;
-                    }
-                }
-                const uint8_t *const ks = ring + S::kKsOff + (warp * 16 + g) * S::kScale;
-                float s[NT][4];
+    }
+    // as a part, in shared memory
+    __device__ __forceinline__ void store(uint8_t *dst, int lane) const
+    {
+        float4 *const d = reinterpret_cast<float4 *>(dst);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                d[(t * MT + i) * 32 + lane] = make_float4(o[t][i][0], o[t][i][1], o[t][i][2], o[t][i][3]);
+            d[(NT * MT + t) * 32 + lane] = make_float4(m[t][0], m[t][1], l[t][0], l[t][1]);
+        }
+    }
+    // adds a part
+    __device__ __forceinline__ void join(const uint8_t *src, int lane)
+    {
+        const float4 *const d = reinterpret_cast<const float4 *>(src);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float4 ml = d[(NT * MT + t) * 32 + lane];
+            const float mm[2] = {ml.x, ml.y}, ll[2] = {ml.z, ml.w};
+            float fa[2], fb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float top = fmaxf(m[t][j], mm[j]);
+                fa[j] = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - top);
+                fb[j] = mm[j] == -INFINITY ? 0.f : ex2(mm[j] - top);
+                l[t][j] = l[t][j] * fa[j] + ll[j] * fb[j];
+                m[t][j] = top;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const float4 v = d[(t * MT + i) * 32 + lane];
+                o[t][i][0] = o[t][i][0] * fa[0] + v.x * fb[0];
+                o[t][i][1] = o[t][i][1] * fa[1] + v.y * fb[1];
+                o[t][i][2] = o[t][i][2] * fa[0] + v.z * fb[0];
+                o[t][i][3] = o[t][i][3] * fa[1] + v.w * fb[1];
+            }
+        }
+    }
+};
+
+// What a warp left of a segment that it does not hold whole.
+struct PartInfo {
+    uint32_t seg;              // the segment's first unit
+    int chunks, head, row0, rows, q0;
+    int begins, ends;          // holds its first chunk, its last
+};
+constexpr uint32_t kNoPart = 0xFFFFFFFFu;
+
+// One lane's share of the joined parts of column tile t: four sums, of
+// dimensions g D/8 + 2i, + 1 and rows 2c, 2c + 1.
+struct Joined {
+    float o[4], m[2], l[2];
+    __device__ __forceinline__ void clear()
+    {
+        o[0] = o[1] = o[2] = o[3] = l[0] = l[1] = 0.f;
+        m[0] = m[1] = -INFINITY;
+    }
+    __device__ __forceinline__ void add(const float4 &v, const float4 &ml)
+    {
+        const float mm[2] = {ml.x, ml.y}, ll[2] = {ml.z, ml.w}, vv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float top = fmaxf(m[j], mm[j]);
+            const float fa = m[j] == -INFINITY ? 0.f : ex2(m[j] - top), fb = mm[j] == -INFINITY ? 0.f : ex2(mm[j] - top);
+            l[j] = l[j] * fa + ll[j] * fb;
+            o[j] = o[j] * fa + vv[j] * fb;
+            o[j + 2] = o[j + 2] * fa + vv[j + 2] * fb;
+            m[j] = top;
+        }
+    }
+};
+
+__device__ __forceinline__ float log_sum(float m, float l)
+{
+    return l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+// 1 / l, 0 for a row that saw no key (and NaN for one whose wait ran out)
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }
+
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
+    kv_attention_kernel(const __grid_constant__ Params p)
+{
+    using S = Shape<FMT, D, NT>;
+    constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
+    constexpr int NB = D / 32, ROWS = S::kRows, MT = S::kMt, W = S::kWarps, DEPTH = S::kDepth;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ alignas(8) uint64_t s_full[W][DEPTH];
+    __shared__ uint32_t s_scan[W];
+    __shared__ int s_flag[2];
+    __shared__ PartInfo s_info[W][2];        // of its first segment, of its last
+
+    const KvAttentionArgs &a = p.a;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int H = a.cache.heads, G = p.group;
+    uint8_t *const s_ring = smem + warp * DEPTH * S::kBytes;
+    uint8_t *const s_head = smem + W * DEPTH * S::kBytes;              // [warp] the part of its first segment
+    uint4 *const s_q = reinterpret_cast<uint4 *>(s_head + W * S::kPart + warp * S::kQ);
+
+    if (lane < 2)
+        s_info[warp][lane].seg = kNoPart;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i)
+            mbar_init(&s_full[warp][i], 1);
+        fence_mbar_init();
+    }
+    // ---- this warp's share: the units of all requests, in order; each warp
+    // counts a run of requests, then finds its own start in one of the runs
+    const int per = (a.requests + W - 1) / W;
+    {
+        int r = min(a.requests, warp * per);
+        uint32_t rem = 0xFFFFFFFFu;
+        const uint32_t sum =
+            seek<ROWS>(p, r, min(a.requests, r + per), rem, lane, blockIdx.x == 0 ? p.status : nullptr);
+        if (lane == 0)
+            s_scan[warp] = sum;
+    }
+    __syncthreads();
+    const uint32_t runs = warp_scan(lane < W ? s_scan[lane] : 0u, lane);
+    const uint32_t total = __shfl_sync(kAll, runs, 31);
+    // (a CTA with few units would only add parts to join)
+    const uint32_t ctas = min(gridDim.x, (total + kLeast - 1) / kLeast), cta = blockIdx.x;
+    if (cta >= ctas)
+        return;
+    // total cta / ctas without a wide product
+    auto bound = [&](uint32_t k) { return total / ctas * k + total % ctas * k / ctas; };
+    const uint32_t u0 = bound(cta), un = bound(cta + 1) - u0;
+    const uint32_t first = u0 + un / W * warp + un % W * warp / W;
+    const uint32_t last = u0 + un / W * (warp + 1) + un % W * (warp + 1) / W;
+    Walk<ROWS> walk, ahead;                  // what is computed, and what is copied
+    {
+        const int run = min(W - 1, __popc(__ballot_sync(kAll, lane < W && runs <= first)));
+        uint32_t rem = first - (run ? __shfl_sync(kAll, runs, run - 1) : 0u);
+        int r = min(a.requests, run * per);
+        if (first < last)
+            seek<ROWS>(p, r, min(a.requests, r + per), rem, lane, nullptr);
+        walk.start(p, r, rem, first, last, lane);
+        walk.next(p);
+        ahead = walk;
+    }
+    const uint64_t limit = ws_wait_limit_ns(p.status);
+    bool ok = true;                          // no wait has run out
+
+    // ---- copies: chunk ahead.i of segment `ahead` into slot fslot of this
+    // warp's ring.  Lane (h, array), h < 32 / gran, copies keys 16 h .. of one
+    // array; it keeps its place in the block table from chunk to chunk.
+    const int arr = lane & 3, page_size = a.cache.page_size;
+    const uint32_t unit = arr < 2 ? S::kCode : S::kScale;              // bytes a key
+    const uint8_t *const src = static_cast<const uint8_t *>(arr == 0   ? a.cache.k_codes
+                                                            : arr == 1 ? a.cache.v_codes
+                                                            : arr == 2 ? a.cache.k_scales
+                                                                       : a.cache.v_scales);
+    const uint32_t dst = smem_u32(s_ring) + (arr == 0 ? 0 : arr == 1 ? S::kVOff : arr == 2 ? S::kKsOff : S::kVsOff) +
+                         (lane >> 2) * 16 * unit;
+    const uint32_t bytes = p.gran * unit;
+    const uint64_t page_bytes = (uint64_t)H * page_size * unit;
+    const bool copies = (lane >> 2) < kChunk / p.gran;
+    const int32_t *entry = a.table;          // of the page of this lane's next key
+    uint32_t off = 0;                        // that key in its page
+    int key = 0;
+    const uint8_t *from = src;               // the key head's bytes in page 0
+    auto place = [&]() {
+        key = ahead.kb + ahead.i * kChunk + (lane >> 2) * 16;
+        const uint32_t pg = (uint32_t)key / (uint32_t)page_size;
+        off = key - pg * page_size;
+        entry = a.table + (int64_t)ahead.r * a.width + pg;
+        from = src + (uint64_t)ahead.head * page_size * unit;
+    };
+    int fslot = 0;
+    place();
+    auto fetch = [&]() {
+        if (!ahead.more())
+            return;
+        bool have = copies && key < ahead.ke;
+        int page = 0;
+        if (have) {
+            page = __ldg(entry);
+            if (page < 0 || page >= a.cache.pages) {
+                atomicCAS(p.status, kDevOk, kDevBadGroups);
+                have = false;
+            }
+        }
+        const uint32_t granules = __popc(__ballot_sync(kAll, have)) >> 2;
+        if (lane == 0)
+            mbar_arrive_expect_tx(&s_full[warp][fslot], granules * p.gran * (2 * S::kCode + 2 * S::kScale));
+        __syncwarp();
+        if (have)
+            bulk_load_at(dst + fslot * S::kBytes, from + page * page_bytes + off * unit, bytes, &s_full[warp][fslot]);
+        if (++fslot == DEPTH)
+            fslot = 0;
+        key += kChunk;
+        off += kChunk;
+        while (off >= (uint32_t)page_size) { // (a page may be shorter than a chunk)
+            off -= page_size;
+            ++entry;
+        }
+        if (++ahead.i == ahead.i1) {
+            ahead.next(p);
+            place();
+        }
+    };
+    // z, one lane's share of a segment's sums, to the output
+    Sums<D, NT> z;
+    auto write = [&](int row0, int rows, int q0, int head) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = 8 * t + 2 * c + j, ri = row0 + row;
+                if (row >= rows)
+                    continue;
+                const int64_t at = (int64_t)(q0 + ri / G) * a.heads + head * G + ri % G;
+                const float inv = inverse(z.l[t][j]);
+                uint32_t w[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    w[i] = pack_bf16(z.o[t][i][j] * inv, z.o[t][i][j + 2] * inv);
+                uint4 *const d = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at * D + g * (D / 8));
+#pragma unroll
+                for (int i = 0; i < MT / 4; ++i)
+                    d[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                if (a.lse && g == 0)
+                    a.lse[at] = log_sum(z.m[t][j], z.l[t][j]);
+            }
+    };
+    int slot = 0, warm = DEPTH - 1;          // chunks to copy before the first is computed
+    uint32_t parity = 0;
+    bool fresh = true;                       // a segment begins
+    bool begins = false;
+    Request q;
+    int row0 = 0, rows = 0;
+    uint4 qf[NB];
+    float qs[NT][2];
+    int hi[NT][2];                           // keys that the thread's two rows see: [max(0, hi - window), hi)
+    int all_hi = 0, all_lo = 0, least = 0;   // every row sees [all_lo, all_hi), none a key below least
+    int vref = -1000;                        // V scale exponents are relative to it (the same in a row's quad)
+#pragma unroll 1
+    while (walk.more()) {
+        fetch();
+        if (warm > 0) {
+            --warm;
+            continue;
+        }
+        if (fresh) {
+            fresh = false;
+            begins = walk.i == 0;
+            q = walk.q;
+            row0 = walk.tile * ROWS;
+            rows = min(ROWS, q.n * G - row0);
+            // ---- q as f16, scaled by a power of two per row
+            const float base = a.scale * 1.4426950408889634f * (HIF4 ? 128.f : 1.f);
+            __syncwarp();                     // (the rows of the segment before are done with)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int rr = 8 * t + g, ri = row0 + rr;
+                uint4 raw[NB];
+                float mx = 0.f;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    raw[b] = make_uint4(0, 0, 0, 0);
+                    if (rr < rows)
+                        raw[b] = __ldg(reinterpret_cast<const uint4 *>(
+                            static_cast<const __nv_bfloat16 *>(a.q) + (q.q0 + ri / G) * a.q_token +
+                            (int64_t)(walk.head * G + ri % G) * a.q_head + 32 * b + 8 * c));
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        s[t][j] = 0.f;
-                if (!HIF4) {
-                    uint32_t sw0, sw1;
+                        mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(w[j] << 16)),
+                                             fabsf(__uint_as_float(w[j] & 0xFFFF0000u))));
+                }
+                mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 2));
+                const int e = max(min((int)(__float_as_uint(mx) >> 23) - 127 - 14, 126), -126);
+                const float mul = __uint_as_float((uint32_t)(127 - e) << 23);
+                const float undo = __uint_as_float((uint32_t)(127 + e) << 23) * base;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        f[2 * j] = __uint_as_float(w[j] << 16) * mul;
+                        f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u) * mul;
+                    }
+                    uint32_t h[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        // HiF4 codes decode in the order 0 2 | 1 3 | 4 6 | 5 7
+                        const int lo = HIF4 ? (j >> 1) * 4 + (j & 1) : 2 * j, up = HIF4 ? lo + 2 : lo + 1;
+                        h[j] = pack_f16(f[lo], f[up]);
+                    }
+                    qf[b] = make_uint4(h[0], h[1], h[2], h[3]);
+                    if (NT > 1)
+                        s_q[(t * NB + b) * 32 + lane] = qf[b];
+                }
+                qs[t][0] = __shfl_sync(kAll, undo, 8 * c);
+                qs[t][1] = __shfl_sync(kAll, undo, 8 * c + 4);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int ri = row0 + min(8 * t + 2 * c + j, rows - 1);
+                    hi[t][j] = max(0, q.L - q.n + (q.n > 1 ? ri / G : 0) + 1);
+                }
+            all_hi = max(0, q.L - q.n + (q.n > 1 ? row0 / G : 0) + 1);
+            least = a.window > 0 ? max(0, all_hi - a.window) : 0;
+            all_lo = a.window > 0 ? max(0, q.L - q.n + (q.n > 1 ? (row0 + rows - 1) / G : 0) + 1 - a.window) : 0;
+            z.clear();
+            vref = -1000;
+        }
+
+        // ---- one chunk
+        {
+            const int i = walk.i;
+            if (!mbar_wait(&s_full[warp][slot], parity, limit))
+                ok = false;
+            const int key0 = walk.kb + i * kChunk;
+            const uint8_t *const ring = s_ring + slot * S::kBytes;
+            // ---- scores: s[h][t][j] is key 16 h + g + 8 (j / 2), row 8 t + 2 c + j % 2
+            float s[2][NT][4];
+            uint32_t kw[2][2][NB];            // [h][row g, g + 8][sub-block]
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const uint8_t *const kr = ring + (16 * h + 8 * r + g) * S::kCode + c * NB * 4;
                     if (D == 128) {
-                        sw0 = *reinterpret_cast<const uint32_t *>(ks);
-                        sw1 = *reinterpret_cast<const uint32_t *>(ks + 8 * S::kScale);
+                        const uint4 x = *reinterpret_cast<const uint4 *>(kr);
+                        kw[h][r][0] = x.x, kw[h][r][1] = x.y, kw[h][r][NB - 2] = x.z, kw[h][r][NB - 1] = x.w;
                     } else {
-                        sw0 = *reinterpret_cast<const uint16_t *>(ks);
-                        sw1 = *reinterpret_cast<const uint16_t *>(ks + 8 * S::kScale);
+                        const uint2 x = *reinterpret_cast<const uint2 *>(kr);
+                        kw[h][r][0] = x.x, kw[h][r][1] = x.y;
+                    }
+                }
+            const uint8_t *const ks = ring + S::kKsOff + g * S::kScale;
+            if (!HIF4) {
+                uint32_t sw[2][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint8_t *const q8 = ks + (16 * h + 8 * r) * S::kScale;
+                        sw[h][r] = D == 128 ? *reinterpret_cast<const uint32_t *>(q8)
+                                            : *reinterpret_cast<const uint16_t *>(q8);
                     }
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        uint32_t h0[4], h1[4];
-                        e2m1x8_f16(k0[b], h0);
-                        e2m1x8_f16(k1[b], h1);
-                        const float f0 = e8m0_f32((sw0 >> (8 * b)) & 0xFFu), f1 = e8m0_f32((sw1 >> (8 * b)) & 0xFFu);
+                for (int b = 0; b < NB; ++b) {
+                    uint32_t k0[2][4], k1[2][4];
+                    float f0[2], f1[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        e2m1x8_f16(kw[h][0][b], k0[h]);
+                        e2m1x8_f16(kw[h][1][b], k1[h]);
+                        f0[h] = e8m0_byte(sw[h][0], b);
+                        f1[h] = e8m0_byte(sw[h][1], b);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const uint4 qb = NT == 1 ? qf[b] : s_q[(t * NB + b) * 32 + lane];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float tmp[4];
+                            mma_f16_first(tmp, k0[h][0], k1[h][0], k0[h][1], k1[h][1], qb.x, qb.y);
+                            mma_f16(tmp, k0[h][2], k1[h][2], k0[h][3], k1[h][3], qb.z, qb.w);
+                            if (b == 0) {
+                                s[h][t][0] = tmp[0] * f0[h], s[h][t][1] = tmp[1] * f0[h];
+                                s[h][t][2] = tmp[2] * f1[h], s[h][t][3] = tmp[3] * f1[h];
+                            } else {
+                                s[h][t][0] = fmaf(tmp[0], f0[h], s[h][t][0]);
+                                s[h][t][1] = fmaf(tmp[1], f0[h], s[h][t][1]);
+                                s[h][t][2] = fmaf(tmp[2], f1[h], s[h][t][2]);
+                                s[h][t][3] = fmaf(tmp[3], f1[h], s[h][t][3]);
+                            }
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int bb = 0; bb < NB / 2; ++bb) {   // HiF4 blocks of 64
+                    float tmp[2][NT][4];
+                    uint32_t meta[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            meta[h][r] =
+                                *reinterpret_cast<const uint32_t *>(ks + (16 * h + 8 * r) * S::kScale + 4 * bb);
+#pragma unroll
+                    for (int hb = 0; hb < 2; ++hb) {
+                        const int b = 2 * bb + hb;
+                        uint32_t k0[2][4], k1[2][4];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t t0, t1;
+                            s1p2x8_f16(kw[h][0][b], k0[h]);
+                            hif4_pow2_pair(meta[h][0], 4 * hb + c, t0, t1);
+                            k0[h][0] = hmul2(k0[h][0], t0), k0[h][1] = hmul2(k0[h][1], t0);
+                            k0[h][2] = hmul2(k0[h][2], t1), k0[h][3] = hmul2(k0[h][3], t1);
+                            s1p2x8_f16(kw[h][1][b], k1[h]);
+                            hif4_pow2_pair(meta[h][1], 4 * hb + c, t0, t1);
+                            k1[h][0] = hmul2(k1[h][0], t0), k1[h][1] = hmul2(k1[h][1], t0);
+                            k1[h][2] = hmul2(k1[h][2], t1), k1[h][3] = hmul2(k1[h][3], t1);
+                        }
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
                             const uint4 qb = NT == 1 ? qf[b] : s_q[(t * NB + b) * 32 + lane];
-                            float tmp[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_f16(tmp, h0[0], h1[0], h0[1], h1[1], qb.x, qb.y);
-                            mma_f16(tmp, h0[2], h1[2], h0[3], h1[3], qb.z, qb.w);
-                            s[t][0] = fmaf(tmp[0], f0, s[t][0]);
-                            s[t][1] = fmaf(tmp[1], f0, s[t][1]);
-                            s[t][2] = fmaf(tmp[2], f1, s[t][2]);
-                            s[t][3] = fmaf(tmp[3], f1, s[t][3]);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                if (hb == 0)
+                                    mma_f16_first(tmp[h][t], k0[h][0], k1[h][0], k0[h][1], k1[h][1], qb.x, qb.y);
+                                else
+                                    mma_f16(tmp[h][t], k0[h][0], k1[h][0], k0[h][1], k1[h][1], qb.x, qb.y);
+                                mma_f16(tmp[h][t], k0[h][2], k1[h][2], k0[h][3], k1[h][3], qb.z, qb.w);
+                            }
                         }
                     }
-                } else {
 #pragma unroll
-                    for (int bb = 0; bb < NB / 2; ++bb) {   // HiF4 blocks of 64
-                        const uint32_t w0 = *reinterpret_cast<const uint32_t *>(ks + 4 * bb);
-                        const uint32_t w1 = *reinterpret_cast<const uint32_t *>(ks + 8 * S::kScale + 4 * bb);
-                        float tmp[NT][4];
+                    for (int h = 0; h < 2; ++h) {
+                        const float f0 = hif4_macro_f32(meta[h][0]), f1 = hif4_macro_f32(meta[h][1]);
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
-                                tmp[t][j] = 0.f;
-#pragma unroll
-                        for (int hb = 0; hb < 2; ++hb) {
-                            const int b = 2 * bb + hb;
-                            uint32_t h0[4], h1[4], t0, t1;
-                            s1p2x8_f16(k0[b], h0);
-                            s1p2x8_f16(k1[b], h1);
-                            hif4_pow2_pair(w0, 4 * hb + c, t0, t1);
-                            h0[0] = hmul2(h0[0], t0), h0[1] = hmul2(h0[1], t0);
-                            h0[2] = hmul2(h0[2], t1), h0[3] = hmul2(h0[3], t1);
-                            hif4_pow2_pair(w1, 4 * hb + c, t0, t1);
-                            h1[0] = hmul2(h1[0], t0), h1[1] = hmul2(h1[1], t0);
-                            h1[2] = hmul2(h1[2], t1), h1[3] = hmul2(h1[3], t1);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                const uint4 qb = NT == 1 ? qf[b] : s_q[(t * NB + b) * 32 + lane];
-                                mma_f16(tmp[t], h0[0], h1[0], h0[1], h1[1], qb.x, qb.y);
-                                mma_f16(tmp[t], h0[2], h1[2], h0[3], h1[3], qb.z, qb.w);
-                            }
-                        }
-                        const float f0 = hif4_macro_f32(w0), f1 = hif4_macro_f32(w1);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            s[t][0] = fmaf(tmp[t][0], f0, s[t][0]);
-                            s[t][1] = fmaf(tmp[t][1], f0, s[t][1]);
-                            s[t][2] = fmaf(tmp[t][2], f1, s[t][2]);
-                            s[t][3] = fmaf(tmp[t][3], f1, s[t][3]);
-                        }
+                                s[h][t][j] = bb == 0 ? tmp[h][t][j] * (j < 2 ? f0 : f1)
+                                                     : fmaf(tmp[h][t][j], j < 2 ? f0 : f1, s[h][t][j]);
                     }
                 }
-                // ---- softmax: s[t][j] is key g + 8 (j / 2), row 2 c + j % 2
-                const bool masked = key0 < all_lo || key0 + 16 > all_hi;
-                bool raise = false;
+            }
+            // ---- softmax
+            const bool whole = key0 >= all_lo && key0 + kChunk <= all_hi;   // every row sees every key
+            bool raise = false;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[t][j] *= qs[t][j & 1];
-                        if (masked) {
-                            const int key = key0 + g + 8 * (j >> 1), h = hi[t][j & 1];
-                            if (key >= h || (a.window > 0 && key < h - a.window))
-                                s[t][j] = -INFINITY;
+                        s[h][t][j] *= qs[t][j & 1];
+                        if (!whole) {
+                            const int key = key0 + 16 * h + g + 8 * (j >> 1), top = hi[t][j & 1];
+                            if (key >= top || (a.window > 0 && key < top - a.window))
+                                s[h][t][j] = -INFINITY;
                         }
                     }
-                    raise |= fmaxf(s[t][0], s[t][2]) > m[t][0] + 8.f || fmaxf(s[t][1], s[t][3]) > m[t][1] + 8.f;
-                }
-                if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                for (int j = 0; j < 2; ++j)
+                    raise |= fmaxf(fmaxf(s[0][t][j], s[0][t][j + 2]), fmaxf(s[1][t][j], s[1][t][j + 2])) >
+                             z.m[t][j] + 8.f;
+            }
+            if (__any_sync(kAll, raise)) {
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            float mx = fmaxf(s[t][j], s[t][j + 2]);
-                            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                            mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                            mx = fmaxf(mx, m[t][j]);
-                            const float f = m[t][j] == -INFINITY ? 0.f : ex2(m[t][j] - mx);
-                            m[t][j] = mx;
-                            l[t][j] *= f;
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                            for (int i2 = 0; i2 < MT; ++i2) {
-                                o[t][i2][j] *= f;
-                                o[t][i2][j + 2] *= f;
-                            }
+                    for (int j = 0; j < 2; ++j) {
+                        float mx = fmaxf(fmaxf(s[0][t][j], s[0][t][j + 2]), fmaxf(s[1][t][j], s[1][t][j + 2]));
+                        mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 16));
+                        mx = fmaxf(mx, z.m[t][j]);
+                        const float f = z.m[t][j] == -INFINITY ? 0.f : ex2(z.m[t][j] - mx);
+                        z.m[t][j] = mx;
+                        z.l[t][j] *= f;
+#pragma unroll
+                        for (int i2 = 0; i2 < MT; ++i2) {
+                            z.o[t][i2][j] *= f;
+                            z.o[t][i2][j + 2] *= f;
                         }
-                }
-                uint32_t pb[NT][2];
+                    }
+            }
+            uint32_t pb[2][NT][2];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    float e[4];
+            for (int t = 0; t < NT; ++t) {
+                // (a row that has seen no key yet: m is -inf and so is s)
+                const float m0 = z.m[t][0] == -INFINITY ? 0.f : z.m[t][0];
+                const float m1 = z.m[t][1] == -INFINITY ? 0.f : z.m[t][1];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)   // (a row that has seen no key yet: m is -inf and so is s)
-                        e[j] = ex2(s[t][j] - (m[t][j & 1] == -INFINITY ? 0.f : m[t][j & 1]));
-                    l[t][0] += e[0] + e[2];
-                    l[t][1] += e[1] + e[3];
-                    pb[t][0] = movmatrix(pack_f16(e[0], e[1]));
-                    pb[t][1] = movmatrix(pack_f16(e[2], e[3]));
+                for (int h = 0; h < 2; ++h) {
+                    const float e0 = ex2(s[h][t][0] - m0), e1 = ex2(s[h][t][1] - m1);
+                    const float e2 = ex2(s[h][t][2] - m0), e3 = ex2(s[h][t][3] - m1);
+                    z.l[t][0] += e0 + e2;
+                    z.l[t][1] += e1 + e3;
+                    pb[h][t][0] = movmatrix(pack_f16(e0, e1));
+                    pb[h][t][1] = movmatrix(pack_f16(e2, e3));
                 }
-                // ---- values: keys 2c, 2c + 1 (v0) and 2c + 8, 2c + 9 (v1), dimensions g D/8 ..
+            }
+            // ---- values: this lane's keys are 16 h + 2 c, + 1 and + 8, + 9, its dimensions g D/8 ..
+            const uint8_t *const vs = ring + S::kVsOff + 2 * c * S::kScale;
+            int ve[2][4];                     // exponents (MXFP4: byte; HiF4: E) of the keys
+            uint32_t vm[2][4];                // HiF4 metadata
+            int top = -2000;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int tok = 16 * h + (j & 1) + 8 * (j >> 1);
+                    if (HIF4) {
+                        vm[h][j] = *reinterpret_cast<const uint32_t *>(vs + tok * S::kScale + (g * (D / 8) / 64) * 4);
+                        ve[h][j] = (int)((vm[h][j] >> 2) & 63u);
+                    } else {
+                        ve[h][j] = (int)vs[tok * S::kScale + g * (D / 8) / 32];
+                    }
+                    if (!whole) {             // what no row sees is nothing, whatever its bytes
+                        const int key = key0 + 2 * c + tok;
+                        if (key >= walk.ke || key < least) {
+                            ve[h][j] = -2000;
+                            if (HIF4)
+                                vm[h][j] = 0;
+                        }
+                    }
+                    top = max(top, ve[h][j]);
+                }
+            if (__any_sync(kAll, top > vref + 3)) {
+                top = max(top, __shfl_xor_sync(kAll, top, 1));
+                top = max(top, __shfl_xor_sync(kAll, top, 2));
+                top = max(top, vref);
+                const float f = ex2((float)(vref - top));
+                vref = top;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i2 = 0; i2 < MT; ++i2)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            z.o[t][i2][j] *= f;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
                 constexpr int VW = D / 64;    // words a key
-                uint32_t v0[2 * VW], v1[2 * VW];
+                uint32_t v0[2 * VW], v1[2 * VW];   // keys 2c, 2c + 1; 2c + 8, 2c + 9
                 {
-                    const uint8_t *const vr = ring + S::kVOff + warp * 8 * D + lane * (D / 8);
+                    const uint8_t *const vr = ring + S::kVOff + h * 8 * D + lane * (D / 8);
                     if (D == 128) {
                         const uint4 x = *reinterpret_cast<const uint4 *>(vr);
                         const uint4 y = *reinterpret_cast<const uint4 *>(vr + 4 * D);
@@ -574,48 +854,15 @@ __global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::kBlocksPerSm) kv_
                         v1[0] = y.x, v1[1] = y.y;
                     }
                 }
-                const uint8_t *const vs = ring + S::kVsOff + (warp * 16 + 2 * c) * S::kScale;
-                int ve[4];                    // exponents (MXFP4: byte; HiF4: E) of the four keys
-                uint32_t vm[4];               // HiF4 metadata
-                int top = -2000;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int tok = (j & 1) + 8 * (j >> 1), key = key0 + 2 * c + tok;
-                    const bool seen = key < walk.ke && key >= walk.kb;
-                    if (HIF4) {
-                        vm[j] = *reinterpret_cast<const uint32_t *>(vs + tok * S::kScale + (g * (D / 8) / 64) * 4);
-                        vm[j] = seen ? vm[j] : 0u;
-                        ve[j] = seen ? (int)((vm[j] >> 2) & 63u) : -2000;
-                    } else {
-                        ve[j] = seen ? (int)vs[tok * S::kScale + g * (D / 8) / 32] : -2000;
-                    }
-                    top = max(top, ve[j]);
-                }
-                if (__any_sync(0xFFFFFFFFu, top > vref + 3)) {
-                    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                    top = max(top, vref);
-                    const float f = ex2((float)(vref - top));
-                    vref = top;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int i2 = 0; i2 < MT; ++i2)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                o[t][i2][j] *= f;
-                }
-                // f16 scale of each key: 2^(e - vref + 9)
+                // f16 scales of the key pairs: 2^(e - vref + 9)
                 uint32_t sc[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    uint32_t x[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const int f = ve[2 * j + k] - vref + 24;
-                        x[k] = f > 0 ? ((uint32_t)f << 10) | (HIF4 ? (vm[2 * j + k] & 3u) << 8 : 0u) : 0u;
-                    }
-                    sc[j] = x[0] | (x[1] << 16);
+                    const uint32_t x = (uint32_t)max(ve[h][2 * j] - vref + 24, 0);
+                    const uint32_t y = (uint32_t)max(ve[h][2 * j + 1] - vref + 24, 0);
+                    sc[j] = x * 0x400u + y * 0x04000000u;
+                    if (HIF4)                 // with the macro scale's two mantissa bits
+                        sc[j] += (x ? (vm[h][2 * j] & 3u) << 8 : 0u) + (y ? (vm[h][2 * j + 1] & 3u) << 24 : 0u);
                 }
 #pragma unroll
                 for (int w = 0; w < VW; ++w) {
@@ -647,12 +894,12 @@ __global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::kBlocksPerSm) kv_
                             od[2] = e4m3x2_f16(ob), od[3] = e4m3x2_f16(ob >> 16);
                             // sub-group exponents of both keys, added to the scale's exponent field
                             const int gi = (g * (D / 8) / 8) % 8 + w;     // group of 8 in the 64-element block
-                            const uint32_t m0 = vm[2 * kk], m1 = vm[2 * kk + 1];
-                            const uint32_t e8 = ((m0 >> (8 + gi)) & 1u) | (((m1 >> (8 + gi)) & 1u) << 16);
-                            const uint32_t q0 = m0 >> (16 + 2 * gi), q1 = m1 >> (16 + 2 * gi);
-                            const uint32_t ta = e8 + ((q0 & 1u) | ((q1 & 1u) << 16));
-                            const uint32_t tb = e8 + (((q0 >> 1) & 1u) | (((q1 >> 1) & 1u) << 16));
-                            const uint32_t sa = sc[kk] + (ta << 10), sb = sc[kk] + (tb << 10);
+                            const uint32_t m0 = vm[h][2 * kk], m1 = vm[h][2 * kk + 1];
+                            const uint32_t e8 = __byte_perm(m0, m1, 0x7531) >> gi;    // E1_8 bytes at 0 and 16
+                            const uint32_t e16 = __byte_perm(m0, m1, 0x7632) >> (2 * gi);
+                            const uint32_t t8 = e8 & 0x00010001u;
+                            const uint32_t sa = sc[kk] + (t8 + (e16 & 0x00010001u)) * 0x400u;
+                            const uint32_t sb = sc[kk] + (t8 + ((e16 >> 1) & 0x00010001u)) * 0x400u;
                             ev[0] = hmul2(ev[0], sa), od[0] = hmul2(od[0], sa);
                             ev[1] = hmul2(ev[1], sa), od[1] = hmul2(od[1], sa);
                             ev[2] = hmul2(ev[2], sb), od[2] = hmul2(od[2], sb);
@@ -663,133 +910,181 @@ __global__ void __launch_bounds__(kThreads, Shape<FMT, D, NT>::kBlocksPerSm) kv_
                     for (int j = 0; j < 4; ++j)
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
-                            mma_f16(o[t][4 * w + j], a0[j], a1[j], a2[j], a3[j], pb[t][0], pb[t][1]);
+                            mma_f16(z.o[t][4 * w + j], a0[j], a1[j], a2[j], a3[j], pb[h][t][0], pb[h][t][1]);
                 }
             }
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(&s_empty[st]);
+            __syncwarp();                     // every lane has read the chunk
+            if (++slot == DEPTH) {
+                slot = 0;
+                parity ^= 1;
+            }
         }
 
-        // ---- join the warps
+        if (++walk.i < walk.i1)
+            continue;
+        // ---- the segment ends here: the warp's sums in plain units
         const float vunit = scalbnf(1.f, vref - (HIF4 ? 50 : 136));
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float x = l[t][j];
-                x += __shfl_xor_sync(0xFFFFFFFFu, x, 4);
-                x += __shfl_xor_sync(0xFFFFFFFFu, x, 8);
-                x += __shfl_xor_sync(0xFFFFFFFFu, x, 16);
-                if (g == 0) {
-                    s_m[warp][8 * t + 2 * c + j] = m[t][j];
-                    s_l[warp][8 * t + 2 * c + j] = x;
-                }
-            }
-        const bool whole = walk.i0 == 0 && walk.i1 == walk.units;
-        const long long seg0 = walk.u - walk.i0;
-        const int c0 = (int)(((seg0 + 1) * ctas - 1) / total), c1 = (int)(((seg0 + walk.units) * ctas - 1) / total);
-        const int slot = 2 * cta + (walk.i0 == 0 ? 1 : 0);
-        constexpr int VPR = D / 4;            // float4 a row
-        const int mrow = tid / VPR, mcol = tid % VPR;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float x = z.l[t][j];
+                x += __shfl_xor_sync(kAll, x, 4);
+                x += __shfl_xor_sync(kAll, x, 8);
+                x += __shfl_xor_sync(kAll, x, 16);
+                z.l[t][j] = ok ? x : __int_as_float(0x7FFFFFFF);
+            }
+#pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    *reinterpret_cast<float2 *>(s_merge + (warp * 8 + 2 * c + j) * D + g * (D / 8) + 2 * i) =
-                        make_float2(o[t][i][j] * vunit, o[t][i][j + 2] * vunit);
-            consumer_sync();
-            if (mrow < 8) {
-                const int row = 8 * t + mrow;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int w = 0; w < kConsumers; ++w)
-                    mx = fmaxf(mx, s_m[w][row]);
-                float sum = 0.f;
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int w = 0; w < kConsumers; ++w) {
-                    const float f = s_m[w][row] == -INFINITY ? 0.f : ex2(s_m[w][row] - mx);
-                    const float4 y = *reinterpret_cast<const float4 *>(s_merge + (w * 8 + mrow) * D + 4 * mcol);
-                    sum = fmaf(f, s_l[w][row], sum);
-                    x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y);
-                    x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
-                }
-                if (!whole) {
-                    const int64_t at = (int64_t)slot * ROWS + row;
-                    __stcg(reinterpret_cast<float4 *>(p.part_o + at * D + 4 * mcol), x);
-                    if (mcol == 0)
-                        __stcg(reinterpret_cast<float2 *>(p.part_ml + at * 2), make_float2(mx, sum));
-                } else if (row < rows) {
-                    const int ri = row0 + row;
-                    const int64_t at = (int64_t)(q.q0 + ri / G) * a.heads + walk.head * G + ri % G;
-                    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-                    const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x * inv, x.y * inv);
-                    const __nv_bfloat162 up = __floats2bfloat162_rn(x.z * inv, x.w * inv);
-                    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at * D + 4 * mcol) = make_uint2(
-                        *reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&up));
-                    if (a.lse && mcol == 0)
-                        a.lse[at] = sum > 0.f ? (mx + log2f(sum)) * 0.69314718055994531f : -INFINITY;
-                }
-            }
-            consumer_sync();
+                for (int j = 0; j < 4; ++j)
+                    z.o[t][i][j] *= vunit;
         }
-        if (whole)
-            continue;
-        // ---- a split segment: the last of its CTAs adds the parts
-        __threadfence();
-        consumer_sync();
-        if (tid == 0)
-            s_flag = atomicAdd(p.counter + c0, 1) == c1 - c0;
-        consumer_sync();
-        if (s_flag) {
-            __threadfence();
-            for (int i = tid; i < rows * VPR; i += 32 * kConsumers) {
-                const int row = i / VPR, col = i % VPR;
-                float mx = -INFINITY;
-                for (int k = c0; k <= c1; ++k)
-                    mx = fmaxf(mx, __ldcg(p.part_ml + ((int64_t)(2 * k + (k == c0)) * ROWS + row) * 2));
-                float sum = 0.f;
-                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-                for (int k = c0; k <= c1; ++k) {
-                    const int64_t at = (int64_t)(2 * k + (k == c0)) * ROWS + row;
-                    const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + at * 2));
-                    const float4 y = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + 4 * col));
-                    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
-                    sum = fmaf(f, ml.y, sum);
-                    x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y);
-                    x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
-                }
-                const int ri = row0 + row;
-                const int64_t at = (int64_t)(q.q0 + ri / G) * a.heads + walk.head * G + ri % G;
-                const float inv = sum > 0.f ? 1.f / sum : 0.f;
-                const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x * inv, x.y * inv);
-                const __nv_bfloat162 up = __floats2bfloat162_rn(x.z * inv, x.w * inv);
-                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at * D + 4 * col) = make_uint2(
-                    *reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&up));
-                if (a.lse && col == 0)
-                    a.lse[at] = sum > 0.f ? (mx + log2f(sum)) * 0.69314718055994531f : -INFINITY;
+        const bool ends = walk.i1 == walk.chunks;
+        fresh = true;
+        if (!begins || !ends) {
+            // (over the ring only when nothing is left to copy: the run's last segment)
+            const int k = begins ? 1 : 0;
+            z.store(k ? s_ring : s_head + warp * S::kPart, lane);
+            if (lane == 0)
+                s_info[warp][k] = {walk.u, walk.chunks, walk.head, row0, rows, q.q0, begins, ends};
+        } else {
+            write(row0, rows, q.q0, walk.head);
+        }
+        walk.next(p);
+    }
+
+    // ---- join the parts: of one segment they follow each other in the order of the warps
+    __syncthreads();
+    constexpr int64_t kFloats = S::kPart / 4;
+    // lane e looks at entry e: entry 2w is warp w's first segment, 2w + 1 its last
+    const uint32_t seg = lane < 2 * W ? s_info[lane >> 1][lane & 1].seg : kNoPart;
+    const uint32_t have = __ballot_sync(kAll, seg != kNoPart);
+    const uint32_t below = have & ((1u << lane) - 1);
+    const uint32_t prev = __shfl_sync(kAll, seg, below ? 31 - __clz(below) : 0);
+    const uint32_t starts = __ballot_sync(kAll, seg != kNoPart && (!below || prev != seg));   // of a segment's entries
+    auto parts_of = [&](int e) {                                       // the entries of the segment that starts at e
+        const uint32_t after = starts & ~((2u << e) - 1);
+        return have & ~((1u << e) - 1) & (after ? (after & -after) - 1 : kAll);
+    };
+    auto part_at = [&](int k) -> const uint8_t * {
+        return k & 1 ? smem + (k >> 1) * DEPTH * S::kBytes : s_head + (k >> 1) * S::kPart;
+    };
+    // At most two segments reach into other CTAs: the first entries' one, if
+    // it began before this CTA, and the last entries' one.  All warps sum their
+    // parts; the CTA's sums go to the workspace.
+    int shared[2], nshared = 0;
+    if (have) {
+        const int e0 = __ffs(have) - 1, e1 = 31 - __clz(starts), le = 31 - __clz(have);
+        if (!s_info[e0 >> 1][e0 & 1].begins)
+            shared[nshared++] = e0;
+        if (!s_info[le >> 1][le & 1].ends && (nshared == 0 || e1 != e0))
+            shared[nshared++] = e1;
+    }
+#pragma unroll 1
+    for (int n = 0; n < nshared; ++n) {
+        const int e = n ? shared[1] : shared[0];
+        const bool first_cta = s_info[e >> 1][e & 1].begins != 0;
+        const uint32_t parts = parts_of(e);
+        float4 *const mine = reinterpret_cast<float4 *>(p.part + (2 * cta + (first_cta ? 1 : 0)) * kFloats);
+#pragma unroll 1
+        for (int u = warp; u < NT * MT; u += W) {
+            const int t = u / MT;
+            Joined x;
+            x.clear();
+#pragma unroll 2
+            for (uint32_t left = parts; left; left &= left - 1) {
+                const float4 *const d = reinterpret_cast<const float4 *>(part_at(__ffs(left) - 1));
+                x.add(d[u * 32 + lane], d[(NT * MT + t) * 32 + lane]);
             }
+            __stcg(mine + u * 32 + lane, make_float4(x.o[0], x.o[1], x.o[2], x.o[3]));
+            if (u % MT == 0)
+                __stcg(mine + (NT * MT + t) * 32 + lane, make_float4(x.m[0], x.m[1], x.l[0], x.l[1]));
+        }
+    }
+    auto first_owner = [&](const PartInfo &f) { return (int)(((uint64_t)(f.seg + 2) * ctas - 1) / total); };
+    auto last_owner = [&](const PartInfo &f) { return (int)(((uint64_t)(f.seg + 1 + f.chunks) * ctas - 1) / total); };
+    if (nshared > 0) {
+        __threadfence();
+        __syncthreads();
+        if (lane == 0 && warp < nshared) {
+            const int e = warp ? shared[1] : shared[0];
+            const PartInfo f = s_info[e >> 1][e & 1];
+            const int c0 = first_owner(f);
+            s_flag[warp] = atomicAdd(p.counter + c0, 1) == last_owner(f) - c0;
+        }
+    }
+    // A segment that warps of this CTA share among them starts in one warp's
+    // last entry: that warp joins it.
+    if (starts >> (2 * warp + 1) & 1) {
+        const int e = 2 * warp + 1;
+        const uint32_t parts = parts_of(e);
+        const int le = 31 - __clz(parts);
+        if (s_info[le >> 1][le & 1].ends) {
+            z.clear();
+#pragma unroll 1
+            for (uint32_t left = parts; left; left &= left - 1)
+                z.join(part_at(__ffs(left) - 1), lane);
+            const PartInfo f = s_info[warp][1];
+            write(f.row0, f.rows, f.q0, f.head);
+        }
+    }
+    // The last CTA of a shared segment joins all its parts.
+    if (nshared > 0) {
+        __syncthreads();
+#pragma unroll 1
+        for (int n = 0; n < nshared; ++n) {
+            if (!s_flag[n])
+                continue;
+            const int e = n ? shared[1] : shared[0];
+            const PartInfo f = s_info[e >> 1][e & 1];
+            const int c0 = first_owner(f), c1 = last_owner(f);
+            __threadfence();
             if (tid == 0)
                 atomicExch(p.counter + c0, 0);
+#pragma unroll 1
+            for (int u = warp; u < NT * MT; u += W) {
+                const int t = u / MT, i = u % MT;
+                Joined x;
+                x.clear();
+#pragma unroll 4
+                for (int k = c0; k <= c1; ++k) {
+                    const float4 *const d =
+                        reinterpret_cast<const float4 *>(p.part + (2 * k + (k == c0 ? 1 : 0)) * kFloats);
+                    x.add(__ldcg(d + u * 32 + lane), __ldcg(d + (NT * MT + t) * 32 + lane));
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int row = 8 * t + 2 * c + j, ri = f.row0 + row;
+                    if (row >= f.rows)
+                        continue;
+                    const int64_t at = (int64_t)(f.q0 + ri / G) * a.heads + f.head * G + ri % G;
+                    const float inv = inverse(x.l[j]);
+                    *reinterpret_cast<uint32_t *>(static_cast<__nv_bfloat16 *>(a.out) + at * D + g * (D / 8) + 2 * i) =
+                        pack_bf16(x.o[j] * inv, x.o[j + 2] * inv);
+                    if (a.lse && g == 0 && i == 0)
+                        a.lse[at] = log_sum(x.m[j], x.l[j]);
+                }
+            }
         }
-        consumer_sync();
+    }
+    if (!ok && lane == 0) {
+        // (what this warp still copies must land before the CTA's memory goes)
+        for (int i = 0; i < DEPTH; ++i)
+            mbar_wait(&s_full[warp][i], i < slot ? parity : parity ^ 1, limit);
+        atomicExch(p.status, kDevTimeout);
     }
 }
 
-constexpr int kMaxRows = 32, kMaxBlocksPerSm = 2;
 constexpr size_t kWsCounters = 256;
 
-size_t ws_parts_offset() { return kWsCounters + ((size_t)kMaxBlocksPerSm * num_sms() * 4 + 255) / 256 * 256; }
+size_t ws_parts_offset() { return kWsCounters + ((size_t)num_sms() * 4 + 255) / 256 * 256; }
 
 template <int FMT, int D, int NT>
 cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
 {
     using S = Shape<FMT, D, NT>;
-    static_assert(S::kStages >= 3, "the ring holds at least three stages");
+    static_assert(S::kSmem <= 226 * 1024, "fits an SM");
     static bool ready = false;     // (per instantiation; setting it twice is harmless)
     if (!ready) {
         if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT>,
@@ -797,18 +1092,14 @@ cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
             return e;
         ready = true;
     }
-    const int ctas = S::kBlocksPerSm * num_sms();
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
-    Params p;
-    p.a = a;
-    p.group = a.heads / a.cache.heads;
-    p.gran = a.cache.page_size & -a.cache.page_size;
-    p.gran = p.gran < kUnit ? p.gran : kUnit;
-    p.status = static_cast<int32_t *>(a.workspace);
-    p.counter = reinterpret_cast<int32_t *>(ws + kWsCounters);
-    p.part_o = reinterpret_cast<float *>(ws + ws_parts_offset());
-    p.part_ml = p.part_o + (int64_t)2 * ctas * S::kRows * D;
-    kv_attention_kernel<FMT, D, NT><<<ctas, kThreads, S::kSmem, st>>>(p);
+    const Params p = {a,
+                      a.heads / a.cache.heads,
+                      a.cache.page_size % kChunk == 0 ? kChunk : 16,
+                      static_cast<int32_t *>(a.workspace),
+                      reinterpret_cast<int32_t *>(ws + kWsCounters),
+                      reinterpret_cast<float *>(ws + ws_parts_offset())};
+    kv_attention_kernel<FMT, D, NT><<<num_sms(), S::kThreads, S::kSmem, st>>>(p);
     return cudaGetLastError();
 }
 
@@ -818,7 +1109,7 @@ cudaError_t launch_rows(const KvAttentionArgs &a, cudaStream_t st)
     // rows of a request and key head: the group's heads times its new tokens
     const int64_t per = a.q_start ? (a.tokens + a.requests - 1) / a.requests : 1;
     const int64_t rows = per * (a.heads / a.cache.heads);
-    return rows <= 8 ? launch<FMT, D, 1>(a, st) : rows <= 16 ? launch<FMT, D, 2>(a, st) : launch<FMT, D, 4>(a, st);
+    return rows <= 8 ? launch<FMT, D, 1>(a, st) : launch<FMT, D, 2>(a, st);
 }
 
 } // namespace
@@ -826,7 +1117,7 @@ cudaError_t launch_rows(const KvAttentionArgs &a, cudaStream_t st)
 size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
 {
     (void)heads;
-    return ws_parts_offset() + (size_t)2 * kMaxBlocksPerSm * num_sms() * kMaxRows * (head_dim + 2) * 4;
+    return ws_parts_offset() + (size_t)2 * num_sms() * 2 * (head_dim / 16 + 1) * 512;
 }
 
 cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)

@@ -86,6 +86,13 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
 // 2^(byte - 127), byte 0 the subnormal 2^-127
 __device__ __forceinline__ float e8m0_f32(uint32_t byte) { return __uint_as_float(max(byte << 23, 0x00400000u)); }
 
+// Byte j of a word of E8M0 scales as fp32 (byte 0, a block of zeros or of
+// values below 2^-124, as 0)
+__device__ __forceinline__ float e8m0_byte(uint32_t w, int j)
+{
+    return __uint_as_float((j < 3 ? w << (23 - 8 * j) : w >> 1) & 0x7F800000u);
+}
+
 // HiF4 macro scale of a metadata word: 2^(E - 48) (1 + M / 4)
 __device__ __forceinline__ float hif4_macro_f32(uint32_t meta)
 {

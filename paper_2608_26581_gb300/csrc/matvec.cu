@@ -151,13 +151,6 @@ struct Scales {
     }
 };
 
-// Byte j of a word of E8M0 scales as fp32 (byte 0, a block of zeros or of
-// values below 2^-124, as 0)
-__device__ __forceinline__ float e8m0_byte(uint32_t w, int j)
-{
-    return __uint_as_float((j < 3 ? w << (23 - 8 * j) : w >> 1) & 0x7F800000u);
-}
-
 template <int FMT, int MP>
 __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_constant__ CUtensorMap wmap, const Params p)
 {
