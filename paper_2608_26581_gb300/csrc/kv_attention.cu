@@ -38,14 +38,15 @@
 
 #include "internal.h"
 #include "kv_layout.cuh"
+#include "mxfp4_math.cuh"
 #include "ptx.cuh"
 
 namespace rfq {
 namespace {
 
-constexpr int kChunk = 32;                   // keys of a chunk
 constexpr int kLeast = 8;                    // units of a CTA, at least
 constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr int kHalves = 2, kChunk = 16 * kHalves;   // keys of a chunk: two MMA tiles
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t a)
 {
@@ -76,7 +77,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 struct Params {
     KvAttentionArgs a;
     int group;                 // query heads per key head
-    int gran;                  // keys of one copy: 32 where a page is whole chunks, else 16
+    int gran;                  // keys of one copy: a chunk where a page is whole chunks, else 16
     int32_t *status;
     int32_t *counter;          // [CTAs] parts of a split segment that have arrived
     float *part;               // [2 CTAs] parts: Shape::kPart bytes each
@@ -159,14 +160,14 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t v, int lane)    // inclus
 }
 
 // Units of one key head of a request (the whole warp together)
-template <int ROWS>
+template <typename S>
 __device__ __forceinline__ uint32_t head_units(const Request &q, const Params &p, int lane)
 {
-    const int n = q.tiles(p.group, ROWS);
+    const int n = q.tiles(p.group, S::kRows);
     uint32_t s = 0;
 #pragma unroll 1
     for (int t = lane; t < n; t += 32)
-        s += q.units(t, p, ROWS);
+        s += q.units(t, p, S::kRows);
     return __reduce_add_sync(kAll, s);
 }
 
@@ -174,7 +175,7 @@ __device__ __forceinline__ uint32_t head_units(const Request &q, const Params &p
 // returns the units of all of them, or stops at the request in which rem
 // runs out, with rem units of it.  Requests of one token are taken 32 at a
 // time, a lane each.
-template <int ROWS>
+template <typename S>
 __device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status)
 {
     uint32_t all = 0;
@@ -186,7 +187,7 @@ __device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32
             if (r + lane < r1) {
                 Request q;
                 q.load(p.a, r + lane, status);
-                mine = H * (uint32_t)q.tiles(p.group, ROWS) * q.units(0, p, ROWS);
+                mine = H * (uint32_t)q.tiles(p.group, S::kRows) * q.units(0, p, S::kRows);
             }
             const uint32_t upto = warp_scan(mine, lane), sum = __shfl_sync(kAll, upto, 31);
             if (rem < sum) {
@@ -203,7 +204,7 @@ __device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32
         for (; r < r1; ++r) {
             Request q;
             q.load(p.a, r, status);
-            const uint32_t sum = H * head_units<ROWS>(q, p, lane);
+            const uint32_t sum = H * head_units<S>(q, p, lane);
             if (rem < sum)
                 return all;
             rem -= sum;
@@ -214,8 +215,9 @@ __device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32
 }
 
 // The segments of a warp's run of units, one after the other.
-template <int ROWS>
+template <typename S>
 struct Walk {
+    static constexpr int ROWS = S::kRows;
     int r, head, tile, ntiles;
     Request q;
     int kb, ke, chunks;        // of the segment
@@ -232,7 +234,7 @@ struct Walk {
             return;
         q.load(p.a, r, nullptr);
         ntiles = q.tiles(p.group, ROWS);
-        const uint32_t per = head_units<ROWS>(q, p, lane);
+        const uint32_t per = head_units<S>(q, p, lane);
         head = (int)(rem / per);
         rem -= head * per;
 #pragma unroll 1
@@ -390,19 +392,23 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
 {
     using S = Shape<FMT, D, NT>;
     constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
-    constexpr int NB = D / 32, ROWS = S::kRows, MT = S::kMt, W = S::kWarps, DEPTH = S::kDepth;
+    constexpr int NB = D / 32, ROWS = S::kRows, MT = S::kMt, W = S::kWarps, DEPTH = S::kDepth, HV = kHalves;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ alignas(8) uint64_t s_full[W][DEPTH];
     __shared__ uint32_t s_scan[W];
     __shared__ int s_flag[2];
+    __shared__ int2 s_c[2];
     __shared__ PartInfo s_info[W][2];        // of its first segment, of its last
 
     const KvAttentionArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int H = a.cache.heads, G = p.group;
     uint8_t *const s_ring = smem + warp * DEPTH * S::kBytes;
-    uint8_t *const s_head = smem + W * DEPTH * S::kBytes;              // [warp] the part of its first segment
-    uint4 *const s_q = reinterpret_cast<uint4 *>(s_head + W * S::kPart + warp * S::kQ);
+    uint4 *const s_q = reinterpret_cast<uint4 *>(smem + W * DEPTH * S::kBytes + warp * S::kQ);
+    // the parts of a warp's first segment (k = 0) and of its last (k = 1)
+    auto part_of = [&](int w, int k) -> uint8_t * {
+        return k ? smem + w * DEPTH * S::kBytes : smem + W * (DEPTH * S::kBytes + S::kQ) + w * S::kPart;
+    };
 
     if (lane < 2)
         s_info[warp][lane].seg = kNoPart;
@@ -412,40 +418,43 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             mbar_init(&s_full[warp][i], 1);
         fence_mbar_init();
     }
-    // ---- this warp's share: the units of all requests, in order; each warp
-    // counts a run of requests, then finds its own start in one of the runs
+    // ---- this warp's share of the units of all requests, in order: each warp
+    // counts a run of requests, then finds its own start in one of the runs.
+    // (One loop for both: the second pass finds its code at hand.)
     const int per = (a.requests + W - 1) / W;
-    {
-        int r = min(a.requests, warp * per);
-        uint32_t rem = 0xFFFFFFFFu;
-        const uint32_t sum =
-            seek<ROWS>(p, r, min(a.requests, r + per), rem, lane, blockIdx.x == 0 ? p.status : nullptr);
+    int run = warp, r_at = 0;
+    uint32_t rem = 0xFFFFFFFFu, total = 0, ctas = 0, first = 0, last = 0;
+    const uint32_t cta = blockIdx.x;
+#pragma unroll 1
+    for (int pass = 0;; ++pass) {
+        r_at = min(a.requests, run * per);
+        const uint32_t sum = seek<S>(p, r_at, min(a.requests, r_at + per), rem, lane,
+                                        pass == 0 && cta == 0 ? p.status : nullptr);
+        if (pass == 1)
+            break;
         if (lane == 0)
             s_scan[warp] = sum;
+        __syncthreads();
+        const uint32_t runs = warp_scan(lane < W ? s_scan[lane] : 0u, lane);
+        total = __shfl_sync(kAll, runs, 31);
+        // (a CTA with few units would only add parts to join)
+        ctas = min(gridDim.x, (total + kLeast - 1) / kLeast);
+        if (cta >= ctas)
+            return;
+        // total cta / ctas without a wide product
+        const uint32_t each = total / ctas, more = total % ctas;
+        const uint32_t u0 = each * cta + more * cta / ctas, un = each * (cta + 1) + more * (cta + 1) / ctas - u0;
+        first = u0 + un / W * warp + un % W * warp / W;
+        last = u0 + un / W * (warp + 1) + un % W * (warp + 1) / W;
+        run = min(W - 1, __popc(__ballot_sync(kAll, lane < W && runs <= first)));
+        rem = first - (run ? __shfl_sync(kAll, runs, run - 1) : 0u);
+        if (first >= last)
+            rem = 0;
     }
-    __syncthreads();
-    const uint32_t runs = warp_scan(lane < W ? s_scan[lane] : 0u, lane);
-    const uint32_t total = __shfl_sync(kAll, runs, 31);
-    // (a CTA with few units would only add parts to join)
-    const uint32_t ctas = min(gridDim.x, (total + kLeast - 1) / kLeast), cta = blockIdx.x;
-    if (cta >= ctas)
-        return;
-    // total cta / ctas without a wide product
-    auto bound = [&](uint32_t k) { return total / ctas * k + total % ctas * k / ctas; };
-    const uint32_t u0 = bound(cta), un = bound(cta + 1) - u0;
-    const uint32_t first = u0 + un / W * warp + un % W * warp / W;
-    const uint32_t last = u0 + un / W * (warp + 1) + un % W * (warp + 1) / W;
-    Walk<ROWS> walk, ahead;                  // what is computed, and what is copied
-    {
-        const int run = min(W - 1, __popc(__ballot_sync(kAll, lane < W && runs <= first)));
-        uint32_t rem = first - (run ? __shfl_sync(kAll, runs, run - 1) : 0u);
-        int r = min(a.requests, run * per);
-        if (first < last)
-            seek<ROWS>(p, r, min(a.requests, r + per), rem, lane, nullptr);
-        walk.start(p, r, rem, first, last, lane);
-        walk.next(p);
-        ahead = walk;
-    }
+    Walk<S> walk, ahead;                  // what is computed, and what is copied
+    walk.start(p, r_at, rem, first, last, lane);
+    walk.next(p);
+    ahead = walk;
     const uint64_t limit = ws_wait_limit_ns(p.status);
     bool ok = true;                          // no wait has run out
 
@@ -467,26 +476,29 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     uint32_t off = 0;                        // that key in its page
     int key = 0;
     const uint8_t *from = src;               // the key head's bytes in page 0
+    int page = -1;                           // *entry, read a chunk before it is used
+    auto read_page = [&]() {
+        if (copies && ahead.more() && key < ahead.ke)
+            page = __ldg(entry);
+    };
     auto place = [&]() {
         key = ahead.kb + ahead.i * kChunk + (lane >> 2) * 16;
         const uint32_t pg = (uint32_t)key / (uint32_t)page_size;
         off = key - pg * page_size;
         entry = a.table + (int64_t)ahead.r * a.width + pg;
         from = src + (uint64_t)ahead.head * page_size * unit;
+        read_page();
     };
     int fslot = 0;
-    place();
+    if (walk.more())
+        place();
     auto fetch = [&]() {
         if (!ahead.more())
             return;
         bool have = copies && key < ahead.ke;
-        int page = 0;
-        if (have) {
-            page = __ldg(entry);
-            if (page < 0 || page >= a.cache.pages) {
-                atomicCAS(p.status, kDevOk, kDevBadGroups);
-                have = false;
-            }
+        if (have && (page < 0 || page >= a.cache.pages)) {
+            atomicCAS(p.status, kDevOk, kDevBadGroups);
+            have = false;
         }
         const uint32_t granules = __popc(__ballot_sync(kAll, have)) >> 2;
         if (lane == 0)
@@ -496,15 +508,22 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             bulk_load_at(dst + fslot * S::kBytes, from + page * page_bytes + off * unit, bytes, &s_full[warp][fslot]);
         if (++fslot == DEPTH)
             fslot = 0;
-        key += kChunk;
-        off += kChunk;
-        while (off >= (uint32_t)page_size) { // (a page may be shorter than a chunk)
-            off -= page_size;
-            ++entry;
-        }
         if (++ahead.i == ahead.i1) {
             ahead.next(p);
-            place();
+            if (ahead.more())
+                place();
+            return;
+        }
+        key += kChunk;
+        off += kChunk;
+        if (off >= (uint32_t)page_size) {
+            off -= page_size;
+            ++entry;
+            if (off >= (uint32_t)page_size) {    // (a page of 16 is shorter than a chunk)
+                off -= page_size;
+                ++entry;
+            }
+            read_page();
         }
     };
     // z, one lane's share of a segment's sums, to the output
@@ -533,44 +552,51 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     };
     int slot = 0, warm = DEPTH - 1;          // chunks to copy before the first is computed
     uint32_t parity = 0;
-    bool fresh = true;                       // a segment begins
+    bool fresh = true, loaded = false;       // a segment begins; its rows of q are on their way
     bool begins = false;
-    Request q;
+    Request q = {0, 0, 0};
     int row0 = 0, rows = 0;
-    uint4 qf[NB];
+    uint4 raw[NB];                           // eight of them, as they come and then as f16
+    auto read_q = [&](int t) {
+        const int rr = 8 * t + g, ri = row0 + rr, tok = ri / G;
+        const __nv_bfloat16 *const at = static_cast<const __nv_bfloat16 *>(a.q) + (q.q0 + tok) * a.q_token +
+                                        (int64_t)(walk.head * G + ri - tok * G) * a.q_head + 8 * c;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            raw[b] = rr < rows ? __ldg(reinterpret_cast<const uint4 *>(at + 32 * b)) : make_uint4(0, 0, 0, 0);
+    };
     float qs[NT][2];
     int hi[NT][2];                           // keys that the thread's two rows see: [max(0, hi - window), hi)
     int all_hi = 0, all_lo = 0, least = 0;   // every row sees [all_lo, all_hi), none a key below least
     int vref = -1000;                        // V scale exponents are relative to it (the same in a row's quad)
 #pragma unroll 1
     while (walk.more()) {
+        // the segment's rows of q, on their way while chunks are copied (of one
+        // row tile: more would take the registers)
+        if (fresh && !loaded) {
+            loaded = true;
+            begins = walk.i == 0;
+            q = walk.q;
+            row0 = walk.tile * ROWS;
+            rows = min(ROWS, q.n * G - row0);
+            if (NT == 1)
+                read_q(0);
+        }
         fetch();
         if (warm > 0) {
             --warm;
             continue;
         }
         if (fresh) {
-            fresh = false;
-            begins = walk.i == 0;
-            q = walk.q;
-            row0 = walk.tile * ROWS;
-            rows = min(ROWS, q.n * G - row0);
+            fresh = loaded = false;
             // ---- q as f16, scaled by a power of two per row
             const float base = a.scale * 1.4426950408889634f * (HIF4 ? 128.f : 1.f);
             __syncwarp();                     // (the rows of the segment before are done with)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const int rr = 8 * t + g, ri = row0 + rr;
-                uint4 raw[NB];
+                if (NT > 1)
+                    read_q(t);
                 float mx = 0.f;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    raw[b] = make_uint4(0, 0, 0, 0);
-                    if (rr < rows)
-                        raw[b] = __ldg(reinterpret_cast<const uint4 *>(
-                            static_cast<const __nv_bfloat16 *>(a.q) + (q.q0 + ri / G) * a.q_token +
-                            (int64_t)(walk.head * G + ri % G) * a.q_head + 32 * b + 8 * c));
-                }
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     const uint32_t w[4] = {raw[b].x, raw[b].y, raw[b].z, raw[b].w};
@@ -600,9 +626,9 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                         const int lo = HIF4 ? (j >> 1) * 4 + (j & 1) : 2 * j, up = HIF4 ? lo + 2 : lo + 1;
                         h[j] = pack_f16(f[lo], f[up]);
                     }
-                    qf[b] = make_uint4(h[0], h[1], h[2], h[3]);
+                    raw[b] = make_uint4(h[0], h[1], h[2], h[3]);
                     if (NT > 1)
-                        s_q[(t * NB + b) * 32 + lane] = qf[b];
+                        s_q[(t * NB + b) * 32 + lane] = raw[b];
                 }
                 qs[t][0] = __shfl_sync(kAll, undo, 8 * c);
                 qs[t][1] = __shfl_sync(kAll, undo, 8 * c + 4);
@@ -630,10 +656,10 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             const int key0 = walk.kb + i * kChunk;
             const uint8_t *const ring = s_ring + slot * S::kBytes;
             // ---- scores: s[h][t][j] is key 16 h + g + 8 (j / 2), row 8 t + 2 c + j % 2
-            float s[2][NT][4];
-            uint32_t kw[2][2][NB];            // [h][row g, g + 8][sub-block]
+            float s[HV][NT][4];
+            uint32_t kw[HV][2][NB];            // [h][row g, g + 8][sub-block]
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < HV; ++h)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const uint8_t *const kr = ring + (16 * h + 8 * r + g) * S::kCode + c * NB * 4;
@@ -647,9 +673,9 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 }
             const uint8_t *const ks = ring + S::kKsOff + g * S::kScale;
             if (!HIF4) {
-                uint32_t sw[2][2];
+                uint32_t sw[HV][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < HV; ++h)
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
                         const uint8_t *const q8 = ks + (16 * h + 8 * r) * S::kScale;
@@ -658,10 +684,10 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                     }
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    uint32_t k0[2][4], k1[2][4];
-                    float f0[2], f1[2];
+                    uint32_t k0[HV][4], k1[HV][4];
+                    float f0[HV], f1[HV];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < HV; ++h) {
                         e2m1x8_f16(kw[h][0][b], k0[h]);
                         e2m1x8_f16(kw[h][1][b], k1[h]);
                         f0[h] = e8m0_byte(sw[h][0], b);
@@ -669,9 +695,9 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                     }
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const uint4 qb = NT == 1 ? qf[b] : s_q[(t * NB + b) * 32 + lane];
+                        const uint4 qb = NT == 1 ? raw[b] : s_q[(t * NB + b) * 32 + lane];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                        for (int h = 0; h < HV; ++h) {
                             float tmp[4];
                             mma_f16_first(tmp, k0[h][0], k1[h][0], k0[h][1], k1[h][1], qb.x, qb.y);
                             mma_f16(tmp, k0[h][2], k1[h][2], k0[h][3], k1[h][3], qb.z, qb.w);
@@ -690,10 +716,10 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             } else {
 #pragma unroll
                 for (int bb = 0; bb < NB / 2; ++bb) {   // HiF4 blocks of 64
-                    float tmp[2][NT][4];
-                    uint32_t meta[2][2];
+                    float tmp[HV][NT][4];
+                    uint32_t meta[HV][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < HV; ++h)
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
                             meta[h][r] =
@@ -701,9 +727,9 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
 #pragma unroll
                     for (int hb = 0; hb < 2; ++hb) {
                         const int b = 2 * bb + hb;
-                        uint32_t k0[2][4], k1[2][4];
+                        uint32_t k0[HV][4], k1[HV][4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                        for (int h = 0; h < HV; ++h) {
                             uint32_t t0, t1;
                             s1p2x8_f16(kw[h][0][b], k0[h]);
                             hif4_pow2_pair(meta[h][0], 4 * hb + c, t0, t1);
@@ -716,9 +742,9 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                         }
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            const uint4 qb = NT == 1 ? qf[b] : s_q[(t * NB + b) * 32 + lane];
+                            const uint4 qb = NT == 1 ? raw[b] : s_q[(t * NB + b) * 32 + lane];
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
+                            for (int h = 0; h < HV; ++h) {
                                 if (hb == 0)
                                     mma_f16_first(tmp[h][t], k0[h][0], k1[h][0], k0[h][1], k1[h][1], qb.x, qb.y);
                                 else
@@ -728,7 +754,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                         }
                     }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < HV; ++h) {
                         const float f0 = hif4_macro_f32(meta[h][0]), f1 = hif4_macro_f32(meta[h][1]);
 #pragma unroll
                         for (int t = 0; t < NT; ++t)
@@ -741,31 +767,37 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             }
             // ---- softmax
             const bool whole = key0 >= all_lo && key0 + kChunk <= all_hi;   // every row sees every key
-            bool raise = false;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < HV; ++h)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < 4; ++j)
                         s[h][t][j] *= qs[t][j & 1];
-                        if (!whole) {
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int h = 0; h < HV; ++h)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
                             const int key = key0 + 16 * h + g + 8 * (j >> 1), top = hi[t][j & 1];
                             if (key >= top || (a.window > 0 && key < top - a.window))
                                 s[h][t][j] = -INFINITY;
                         }
-                    }
+            }
+            bool raise = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    raise |= fmaxf(fmaxf(s[0][t][j], s[0][t][j + 2]), fmaxf(s[1][t][j], s[1][t][j + 2])) >
-                             z.m[t][j] + 8.f;
-            }
+                    raise |= fmaxf(fmax3(s[0][t][j], s[0][t][j + 2], s[HV - 1][t][j]), s[HV - 1][t][j + 2]) > z.m[t][j] + 8.f;
             if (__any_sync(kAll, raise)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float mx = fmaxf(fmaxf(s[0][t][j], s[0][t][j + 2]), fmaxf(s[1][t][j], s[1][t][j + 2]));
+                        float mx = fmaxf(fmax3(s[0][t][j], s[0][t][j + 2], s[HV - 1][t][j]), s[HV - 1][t][j + 2]);
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 16));
@@ -780,14 +812,14 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                         }
                     }
             }
-            uint32_t pb[2][NT][2];
+            uint32_t pb[HV][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 // (a row that has seen no key yet: m is -inf and so is s)
                 const float m0 = z.m[t][0] == -INFINITY ? 0.f : z.m[t][0];
                 const float m1 = z.m[t][1] == -INFINITY ? 0.f : z.m[t][1];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < HV; ++h) {
                     const float e0 = ex2(s[h][t][0] - m0), e1 = ex2(s[h][t][1] - m1);
                     const float e2 = ex2(s[h][t][2] - m0), e3 = ex2(s[h][t][3] - m1);
                     z.l[t][0] += e0 + e2;
@@ -798,11 +830,11 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             }
             // ---- values: this lane's keys are 16 h + 2 c, + 1 and + 8, + 9, its dimensions g D/8 ..
             const uint8_t *const vs = ring + S::kVsOff + 2 * c * S::kScale;
-            int ve[2][4];                     // exponents (MXFP4: byte; HiF4: E) of the keys
-            uint32_t vm[2][4];                // HiF4 metadata
+            int ve[HV][4];                    // exponents (MXFP4: byte; HiF4: E) of the keys
+            uint32_t vm[HV][4];               // HiF4 metadata
             int top = -2000;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < HV; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int tok = 16 * h + (j & 1) + 8 * (j >> 1);
@@ -812,16 +844,23 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                     } else {
                         ve[h][j] = (int)vs[tok * S::kScale + g * (D / 8) / 32];
                     }
-                    if (!whole) {             // what no row sees is nothing, whatever its bytes
-                        const int key = key0 + 2 * c + tok;
+                }
+            if (!whole) {                     // what no row sees is nothing, whatever its bytes
+#pragma unroll
+                for (int h = 0; h < HV; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int key = key0 + 16 * h + 2 * c + (j & 1) + 8 * (j >> 1);
                         if (key >= walk.ke || key < least) {
                             ve[h][j] = -2000;
                             if (HIF4)
                                 vm[h][j] = 0;
                         }
                     }
-                    top = max(top, ve[h][j]);
-                }
+            }
+#pragma unroll
+            for (int h = 0; h < HV; ++h)
+                top = __vimax3_s32(__vimax3_s32(top, ve[h][0], ve[h][1]), ve[h][2], ve[h][3]);
             if (__any_sync(kAll, top > vref + 3)) {
                 top = max(top, __shfl_xor_sync(kAll, top, 1));
                 top = max(top, __shfl_xor_sync(kAll, top, 2));
@@ -837,7 +876,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                             z.o[t][i2][j] *= f;
             }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < HV; ++h) {
                 constexpr int VW = D / 64;    // words a key
                 uint32_t v0[2 * VW], v1[2 * VW];   // keys 2c, 2c + 1; 2c + 8, 2c + 9
                 {
@@ -858,8 +897,8 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 uint32_t sc[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t x = (uint32_t)max(ve[h][2 * j] - vref + 24, 0);
-                    const uint32_t y = (uint32_t)max(ve[h][2 * j + 1] - vref + 24, 0);
+                    const uint32_t x = (uint32_t)__viaddmax_s32(ve[h][2 * j], 24 - vref, 0);
+                    const uint32_t y = (uint32_t)__viaddmax_s32(ve[h][2 * j + 1], 24 - vref, 0);
                     sc[j] = x * 0x400u + y * 0x04000000u;
                     if (HIF4)                 // with the macro scale's two mantissa bits
                         sc[j] += (x ? (vm[h][2 * j] & 3u) << 8 : 0u) + (y ? (vm[h][2 * j + 1] & 3u) << 24 : 0u);
@@ -945,7 +984,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
         if (!begins || !ends) {
             // (over the ring only when nothing is left to copy: the run's last segment)
             const int k = begins ? 1 : 0;
-            z.store(k ? s_ring : s_head + warp * S::kPart, lane);
+            z.store(part_of(warp, k), lane);
             if (lane == 0)
                 s_info[warp][k] = {walk.u, walk.chunks, walk.head, row0, rows, q.q0, begins, ends};
         } else {
@@ -967,9 +1006,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
         const uint32_t after = starts & ~((2u << e) - 1);
         return have & ~((1u << e) - 1) & (after ? (after & -after) - 1 : kAll);
     };
-    auto part_at = [&](int k) -> const uint8_t * {
-        return k & 1 ? smem + (k >> 1) * DEPTH * S::kBytes : s_head + (k >> 1) * S::kPart;
-    };
+    auto part_at = [&](int k) -> const uint8_t * { return part_of(k >> 1, k & 1); };
     // At most two segments reach into other CTAs: the first entries' one, if
     // it began before this CTA, and the last entries' one.  All warps sum their
     // parts; the CTA's sums go to the workspace.
@@ -1002,16 +1039,25 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 __stcg(mine + (NT * MT + t) * 32 + lane, make_float4(x.m[0], x.m[1], x.l[0], x.l[1]));
         }
     }
-    auto first_owner = [&](const PartInfo &f) { return (int)(((uint64_t)(f.seg + 2) * ctas - 1) / total); };
-    auto last_owner = [&](const PartInfo &f) { return (int)(((uint64_t)(f.seg + 1 + f.chunks) * ctas - 1) / total); };
+    // the CTA whose run holds unit u
+    auto owner = [&](uint32_t u) {
+        const uint32_t each = total / ctas, more = total % ctas;
+        uint32_t k = min(ctas - 1, (uint32_t)((float)u * (float)ctas / (float)total));
+        while (each * k + more * k / ctas > u)
+            --k;
+        while (each * (k + 1) + more * (k + 1) / ctas <= u)
+            ++k;
+        return (int)k;
+    };
     if (nshared > 0) {
         __threadfence();
         __syncthreads();
         if (lane == 0 && warp < nshared) {
             const int e = warp ? shared[1] : shared[0];
             const PartInfo f = s_info[e >> 1][e & 1];
-            const int c0 = first_owner(f);
-            s_flag[warp] = atomicAdd(p.counter + c0, 1) == last_owner(f) - c0;
+            const int c0 = owner(f.seg + 1), c1 = owner(f.seg + f.chunks);
+            s_c[warp] = make_int2(c0, c1);
+            s_flag[warp] = atomicAdd(p.counter + c0, 1) == c1 - c0;
         }
     }
     // A segment that warps of this CTA share among them starts in one warp's
@@ -1038,7 +1084,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 continue;
             const int e = n ? shared[1] : shared[0];
             const PartInfo f = s_info[e >> 1][e & 1];
-            const int c0 = first_owner(f), c1 = last_owner(f);
+            const int c0 = s_c[n].x, c1 = s_c[n].y;
             __threadfence();
             if (tid == 0)
                 atomicExch(p.counter + c0, 0);
@@ -1106,7 +1152,9 @@ cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
 template <int FMT, int D>
 cudaError_t launch_rows(const KvAttentionArgs &a, cudaStream_t st)
 {
-    // rows of a request and key head: the group's heads times its new tokens
+    // rows of a request and key head: the group's heads times its new tokens.
+    // (Four row tiles a warp and 16 keys a chunk: 283 us against 239 with two,
+    // 256 new tokens over up to 8192, D = 128: the sums leave no registers.)
     const int64_t per = a.q_start ? (a.tokens + a.requests - 1) / a.requests : 1;
     const int64_t rows = per * (a.heads / a.cache.heads);
     return rows <= 8 ? launch<FMT, D, 1>(a, st) : launch<FMT, D, 2>(a, st);
