@@ -505,9 +505,9 @@ RFQ_API rfq_status rfq_dequant(const rfq_qtensor *q, void *out, int32_t out_dtyp
  * free_pages holds free_capacity entries; pages given back past it are
  * dropped (device status RFQ_ERR_SHAPE).  free_out may be free_in and lengths
  * may be cached; no other arrays overlap.  0 <= requests <= 8192,
- * page_size >= 1, table_width >= 1, tokens >= 0.  workspace: device, 256
- * bytes zeroed by the caller once, for the device status
- * (rfq_workspace_status).
+ * page_size >= 1, table_width >= 1, requests * table_width < 2^31,
+ * tokens >= 0.  workspace: device, 256 bytes zeroed by
+ * the caller once, for the device status (rfq_workspace_status).
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
  * RFQ_ERR_DEVICE. */
 RFQ_API rfq_status rfq_slot_map(const int32_t *cached, const int32_t *added, int32_t requests, int32_t page_size,

@@ -51,7 +51,7 @@ rfq_status rfq_slot_map(const int32_t *cached, const int32_t *added, int32_t req
                         int64_t *slots, int32_t *positions, int64_t tokens, void *workspace, void *stream)
 {
     if (requests < 0 || requests > kSlotMapRequests || page_size < 1 || table_width < 1 || free_capacity < 0 ||
-        tokens < 0)
+        tokens < 0 || (int64_t)requests * table_width > INT32_MAX)
         return RFQ_ERR_SHAPE;
     if (!free_in || !free_out || !token_start || !workspace || (free_capacity > 0 && !free_pages) ||
         (requests > 0 && (!cached || !added || !block_table || !lengths)) || (tokens > 0 && (!slots || !positions)))

@@ -27,8 +27,10 @@ constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kCluster = 8;
 constexpr int64_t kSoloTokens = 2048;
 
+// (pages of one table: 32 bits, as the host has seen; tokens may be more)
 struct Sums {
-    long long back, need, tok;
+    uint32_t back, need;
+    unsigned long long tok;
 };
 
 __device__ __forceinline__ Sums operator+(const Sums &x, const Sums &y)
@@ -36,18 +38,13 @@ __device__ __forceinline__ Sums operator+(const Sums &x, const Sums &y)
     return {x.back + y.back, x.need + y.need, x.tok + y.tok};
 }
 
-__device__ __forceinline__ Sums shfl_up(const Sums &x, int d)
-{
-    return {__shfl_up_sync(0xFFFFFFFFu, x.back, d), __shfl_up_sync(0xFFFFFFFFu, x.need, d),
-            __shfl_up_sync(0xFFFFFFFFu, x.tok, d)};
-}
-
 // Inclusive sums over the warp's lanes.
 __device__ __forceinline__ Sums warp_scan(Sums v, int lane)
 {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const Sums u = shfl_up(v, d);
+        const Sums u = {__shfl_up_sync(0xFFFFFFFFu, v.back, d), __shfl_up_sync(0xFFFFFFFFu, v.need, d),
+                        __shfl_up_sync(0xFFFFFFFFu, v.tok, d)};
         if (lane >= d)
             v = v + u;
     }
@@ -57,20 +54,22 @@ __device__ __forceinline__ Sums warp_scan(Sums v, int lane)
 // What request r holds and wants.  fits: its lengths are sane and its pages
 // fit the table's row; a request that does not fit takes and gives nothing.
 struct Request {
-    long long cached, after, p0, p1;
+    int cached, added;
+    uint32_t p0, p1, after;
     bool fits;
-    __device__ Request(const SlotMapArgs &a, int r)
+    __device__ __forceinline__ Request(const SlotMapArgs &a, int r)
     {
-        cached = a.cached[r];
-        const long long n = cached + (long long)a.added[r];
-        after = n > 0 ? n : 0;
-        p0 = cached > 0 ? (cached + a.page_size - 1) / a.page_size : 0;
-        p1 = (after + a.page_size - 1) / a.page_size;
-        fits = cached >= 0 && p0 <= a.width && p1 <= a.width;
+        cached = __ldcg(a.cached + r);
+        added = __ldcg(a.added + r);
+        const uint32_t page = a.page_size, c = max(cached, 0);
+        after = added >= 0 ? c + (uint32_t)added : c > (uint32_t)-(int64_t)added ? c - (uint32_t)-(int64_t)added : 0u;
+        p0 = c / page + (c % page != 0);
+        p1 = after / page + (after % page != 0);
+        fits = cached >= 0 && p0 <= (uint32_t)a.width && p1 <= (uint32_t)a.width;
     }
-    __device__ Sums sums(int added) const
+    __device__ __forceinline__ Sums sums() const
     {
-        return {fits && p0 > p1 ? p0 - p1 : 0, fits && p1 > p0 ? p1 - p0 : 0, added > 0 ? added : 0};
+        return {fits && p0 > p1 ? p0 - p1 : 0u, fits && p1 > p0 ? p1 - p0 : 0u, (unsigned long long)max(added, 0)};
     }
 };
 
@@ -78,16 +77,20 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
 {
     extern __shared__ int32_t smem[];
     __shared__ Sums s_warp[kWarps];
-    __shared__ int s_taken;
+    __shared__ uint32_t s_taken;
     const int R = a.requests, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t *const s_start = smem;            // [R + 1] first token of each request
     int32_t *const s_cached = s_start + R + 1;
-    int32_t *const s_nth = s_cached + R;      // its first page's place among the pages taken; -1: not served
-    int32_t *const s_back = s_nth + R;        // its first page's place among the pages given back
+    uint32_t *const s_p0 = reinterpret_cast<uint32_t *>(s_cached + R);   // pages before
+    uint32_t *const s_p1 = s_p0 + R;          // and after; before if it does not fit
+    int32_t *const s_nth = reinterpret_cast<int32_t *>(s_p1 + R);   // its first page's place among the pages
+                                              // taken; -1: not served
+    uint32_t *const s_back = reinterpret_cast<uint32_t *>(s_nth + R);   // and among the pages given back
     const int rank = (int)cluster_ctarank(), ctas = gridDim.x;
 
     if (tid == 0)
         s_taken = 0;
+    const int given = __ldcg(a.free_in);
     // this thread's requests, then the block's sums before them
     const int per = (R + kThreads - 1) / kThreads;
     const int r0 = min(R, tid * per), r1 = min(R, r0 + per);
@@ -96,41 +99,44 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
     for (int r = r0; r < r1; ++r) {
         const Request q(a, r);
         bad |= !q.fits;
-        own = own + q.sums(a.added[r]);
+        own = own + q.sums();
+        s_cached[r] = q.cached;
+        s_p0[r] = q.p0;
+        s_p1[r] = q.fits ? q.p1 : q.p0;
+        s_nth[r] = q.fits ? q.added : INT32_MIN;     // (until the sums are known)
     }
     const Sums inc = warp_scan(own, lane);
     if (lane == 31)
         s_warp[warp] = inc;
     __syncthreads();
     const Sums w = warp_scan(s_warp[lane], lane);      // kWarps == 32
-    Sums before = {__shfl_sync(0xFFFFFFFFu, w.back, (warp + 31) & 31), __shfl_sync(0xFFFFFFFFu, w.need, (warp + 31) & 31),
-                   __shfl_sync(0xFFFFFFFFu, w.tok, (warp + 31) & 31)};
+    Sums at = {__shfl_sync(0xFFFFFFFFu, w.back, (warp + 31) & 31), __shfl_sync(0xFFFFFFFFu, w.need, (warp + 31) & 31),
+               __shfl_sync(0xFFFFFFFFu, w.tok, (warp + 31) & 31)};
     if (warp == 0)
-        before = {0, 0, 0};
+        at = {0, 0, 0};
     const Sums all = {__shfl_sync(0xFFFFFFFFu, w.back, 31), __shfl_sync(0xFFFFFFFFu, w.need, 31),
                       __shfl_sync(0xFFFFFFFFu, w.tok, 31)};
-    Sums at = before + inc;
+    at = at + inc;
     at = {at.back - own.back, at.need - own.need, at.tok - own.tok};
-    const long long given = *a.free_in;
-    const long long count = given < 0 ? 0 : given > a.free_capacity ? a.free_capacity : given;
+    const uint32_t count = min(max(given, 0), a.free_capacity);
     // (pages given back beyond the list's end are dropped)
-    const long long top = min(count + all.back, (long long)a.free_capacity);
-    bad |= count != given || count + all.back > a.free_capacity || all.tok > a.tokens;
-    int taken = 0;
+    const uint32_t top = min(count + all.back, (uint32_t)a.free_capacity);
+    bad |= (int)count != given || count + all.back > (uint32_t)a.free_capacity || all.tok > (unsigned long long)a.tokens;
+    uint32_t taken = 0;
     for (int r = r0; r < r1; ++r) {
-        const Request q(a, r);
-        const Sums s = q.sums(a.added[r]);
-        const bool served = q.fits && (s.need == 0 || at.need + s.need <= top);
-        s_start[r] = (int32_t)min(at.tok, (long long)INT32_MAX);
-        s_cached[r] = (int32_t)q.cached;
-        s_nth[r] = served ? (int32_t)min(at.need, (long long)INT32_MAX) : -1;
-        s_back[r] = (int32_t)min(at.back, (long long)INT32_MAX);
-        if (served && s.need > 0)
-            taken = max(taken, (int)(at.need + s.need));
-        at = at + s;
+        const bool fits = s_nth[r] != INT32_MIN;
+        const int added = fits ? s_nth[r] : __ldcg(a.added + r);
+        const uint32_t p0 = s_p0[r], p1 = s_p1[r], need = p1 > p0 ? p1 - p0 : 0u;
+        const bool served = fits && (need == 0 || at.need + need <= top);
+        s_start[r] = (int32_t)min(at.tok, (unsigned long long)INT32_MAX);
+        s_nth[r] = served ? (int32_t)min(at.need, (uint32_t)INT32_MAX) : -1;
+        s_back[r] = at.back;
+        if (served && need > 0)
+            taken = max(taken, at.need + need);
+        at = at + Sums{p0 > p1 ? p0 - p1 : 0u, need, (unsigned long long)max(added, 0)};
     }
     if (tid == 0)
-        s_start[R] = (int32_t)min(all.tok, (long long)INT32_MAX);
+        s_start[R] = (int32_t)min(all.tok, (unsigned long long)INT32_MAX);
     if (taken > 0)
         atomicMax(&s_taken, taken);
     if (bad && rank == 0)
@@ -139,42 +145,42 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
 
     // pages given back: onto the stack, in the order of the requests
     if (all.back > 0)
-        for (int r = rank * kWarps + warp; r < R; r += ctas * kWarps) {
-            const Request q(a, r);
-            if (!q.fits)
-                continue;
-            for (long long j = q.p1 + lane; j < q.p0; j += 32) {
-                const long long to = count + s_back[r] + (j - q.p1);
-                if (to < a.free_capacity)
-                    a.free_pages[to] = a.table[(int64_t)r * a.width + j];
+        for (int r = rank * kWarps + warp; r < R; r += ctas * kWarps)
+            for (uint32_t j = s_p1[r] + lane; j < s_p0[r]; j += 32) {
+                const uint32_t to = count + s_back[r] + (j - s_p1[r]);
+                if (to < (uint32_t)a.free_capacity)
+                    a.free_pages[to] = __ldcg(a.table + (int64_t)r * a.width + j);
             }
-        }
-    // lengths that the outputs below may overwrite are in shared memory now;
-    // `added` is read again, and is nobody's output
-    cluster_sync();
+    // what the outputs below may overwrite has been read now (`added` is
+    // nobody's output)
+    if (ctas > 1)
+        cluster_sync();
+    else
+        __syncthreads();
 
     // pages taken: from the top, request by request
-    if (s_taken > 0)
+    const uint32_t top_taken = s_taken;
+    if (top_taken > 0)
         for (int r = rank * kWarps + warp; r < R; r += ctas * kWarps) {
-            if (s_nth[r] < 0)
-                continue;
-            const long long cached = s_cached[r], after = max(cached + (long long)a.added[r], 0ll);
-            const long long p0 = (cached + a.page_size - 1) / a.page_size, p1 = (after + a.page_size - 1) / a.page_size;
-            for (long long j = p0 + lane; j < p1; j += 32)
-                a.table[(int64_t)r * a.width + j] = __ldcg(a.free_pages + (top - 1 - s_nth[r] - (j - p0)));
+            const int nth = s_nth[r];
+            const uint32_t p0 = s_p0[r], p1 = s_p1[r];
+            if (nth >= 0)
+                for (uint32_t j = p0 + lane; j < p1; j += 32)
+                    a.table[(int64_t)r * a.width + j] = __ldcg(a.free_pages + (top - 1 - nth - (j - p0)));
         }
     if (rank == 0) {
         for (int r = tid; r < R; r += kThreads) {
-            const long long after = max((long long)s_cached[r] + a.added[r], 0ll);
-            a.lengths[r] = s_nth[r] >= 0 ? (int32_t)after : s_cached[r];
+            const int64_t after = (int64_t)s_cached[r] + __ldcg(a.added + r);
+            a.lengths[r] = s_nth[r] >= 0 ? (int32_t)max(after, (int64_t)0) : s_cached[r];
         }
         for (int r = tid; r <= R; r += kThreads)
             a.token_start[r] = s_start[r];
         if (tid == 0)
-            *a.free_out = (int32_t)(top - s_taken);
+            *a.free_out = (int32_t)(top - top_taken);
     }
     // tokens: the last request that starts at or before t and has tokens
-    const long long total = min(all.tok, (long long)INT32_MAX);
+    const int total = s_start[R];
+    const uint32_t page_size = a.page_size;
     for (int64_t t = (int64_t)rank * kThreads + tid; t < a.tokens; t += (int64_t)ctas * kThreads) {
         int64_t slot = -1;
         int32_t pos = 0;
@@ -182,19 +188,19 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
             int lo = 0, hi = R;              // s_start[lo] <= t < s_start[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (s_start[mid] <= t)
+                if (s_start[mid] <= (int)t)
                     lo = mid;
                 else
                     hi = mid;
             }
-            const long long cached = s_cached[lo], p = cached + (t - s_start[lo]);
-            pos = (int32_t)p;
-            if (s_nth[lo] >= 0) {
-                const long long p0 = (cached + a.page_size - 1) / a.page_size, j = p / a.page_size;
-                const int32_t page = j < p0 ? a.table[(int64_t)lo * a.width + j]
-                                            : __ldcg(a.free_pages + (top - 1 - s_nth[lo] - (j - p0)));
+            const int nth = s_nth[lo];
+            pos = s_cached[lo] + ((int)t - s_start[lo]);
+            if (nth >= 0) {
+                const uint32_t p0 = s_p0[lo], j = (uint32_t)pos / page_size;
+                const int32_t page = j < p0 ? __ldcg(a.table + (int64_t)lo * a.width + j)
+                                            : __ldcg(a.free_pages + (top - 1 - nth - (j - p0)));
                 if (page >= 0)
-                    slot = (int64_t)page * a.page_size + (p - j * a.page_size);
+                    slot = (int64_t)page * page_size + ((uint32_t)pos - j * page_size);
             }
         }
         a.slots[t] = slot;
@@ -206,10 +212,10 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
 
 cudaError_t launch_slot_map(const SlotMapArgs &a, cudaStream_t st)
 {
-    const size_t smem = (4 * (size_t)a.requests + 1) * sizeof(int32_t);
+    const size_t smem = (6 * (size_t)a.requests + 1) * sizeof(int32_t);
     if (smem > 48 * 1024)
         if (cudaError_t e = cudaFuncSetAttribute(slot_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (4 * kSlotMapRequests + 1) * (int)sizeof(int32_t)))
+                                                 (6 * kSlotMapRequests + 1) * (int)sizeof(int32_t)))
             return e;
     const int ctas = a.tokens > kSoloTokens ? kCluster : 1;
     cudaLaunchConfig_t cfg = {};
