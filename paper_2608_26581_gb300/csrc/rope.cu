@@ -19,8 +19,7 @@
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 256;
-
+constexpr int kThreads = 256;                // of a block, at most (more where a head has more chunks)
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Vec {
     T v[VEC];
@@ -31,18 +30,44 @@ __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162flo
 __device__ __forceinline__ void from_f32(float &d, float x) { d = x; }
 __device__ __forceinline__ void from_f32(__nv_bfloat16 &d, float x) { d = __float2bfloat16_rn(x); }
 
-// Block: tokens [blockIdx.x tb, + tb), heads in blockIdx.y's share.  An item is
-// one chunk of VEC consecutive elements of the output, or with !INTER for
-// rotated elements the chunk and its partner `pairs` elements further on.
+// Block: tokens [blockIdx.x tb, + tb), heads in blockIdx.y's share; a row is
+// one (token, head).  A thread takes the same chunk of every row it visits:
+// VEC consecutive elements (a whole pair at least with INTER), or with !INTER
+// for rotated elements the chunk and its partner `pairs` elements further on.
 template <typename T, int VEC, bool INTER>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int tb, int heads_per)
+__global__ void rope_kernel(const RopeArgs a, int tb, int heads_per, int chunks, int rot)
 {
     extern __shared__ float2 s_cs[];         // [tb][pairs]
     const int64_t t0 = (int64_t)blockIdx.x * tb;
     const int nt = (int)min((int64_t)tb, a.tokens - t0);
     const int h0 = blockIdx.y * heads_per, nh = min(heads_per, a.heads - h0);
     const int P = a.pairs;
-    for (int i = threadIdx.x; i < nt * P; i += kThreads) {
+    const T *const x = static_cast<const T *>(a.x) + t0 * a.x_token + h0 * a.x_head;
+    T *const out = static_cast<T *>(a.out) + t0 * a.out_token + h0 * a.out_head;
+    using V = Vec<T, VEC>;
+    constexpr int PV = INTER && VEC < 2 ? 2 : VEC;      // elements of a chunk
+    constexpr int NV = INTER ? PV / VEC : 2;            // vectors of a chunk: of a pair, or a chunk and its partner
+    const int c = threadIdx.x % chunks, step = blockDim.x / chunks, rows = nt * nh;
+    const bool turn = c < rot;
+    // first element; distance of the second vector (a chunk that passes through has one)
+    const int d = turn ? c * PV : 2 * P + (c - rot) * VEC;
+    const int dist = INTER ? VEC : P, nv = turn ? NV : 1;
+    const float inv_nh = 1.f / (float)nh;
+    auto token_of = [&](int r) { return (int)(((float)r + 0.5f) * inv_nh); };   // r / nh: both are far below 2^22
+    auto load = [&](int r, V (&v)[NV]) {
+        const int t = token_of(r), h = r - t * nh;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < nv)
+                v[i] = *reinterpret_cast<const V *>(x + t * a.x_token + h * a.x_head + d + i * dist);
+    };
+    // the first row is on its way while the angles are formed, every other
+    // while the one before it is turned
+    int r = threadIdx.x / chunks;
+    V v[NV];
+    if (r < rows)
+        load(r, v);
+    for (int i = threadIdx.x; i < nt * P; i += blockDim.x) {
         const int t = i / P, p = i - t * P;
         const int axis = a.axis_of[p];
         float2 cs = make_float2(1.f, 0.f);
@@ -56,49 +81,29 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int tb
     }
     __syncthreads();
 
-    const T *const x = static_cast<const T *>(a.x);
-    T *const out = static_cast<T *>(a.out);
-    using V = Vec<T, VEC>;
-    const int D = a.head_dim;
-    // chunks of a head: rotated ones first, then the elements that pass through
-    constexpr int PV = VEC < 2 ? 2 : VEC;    // elements of an INTER chunk: whole pairs
-    const int rot = INTER ? 2 * P / PV : P / VEC, chunks = rot + (D - 2 * P) / VEC;
-    const int per_token = nh * chunks, items = nt * per_token;
-    for (int i = threadIdx.x; i < items; i += kThreads) {
-        const int t = i / per_token, r = i - t * per_token, h = r / chunks, c = r - h * chunks;
-        const int64_t xo = (t0 + t) * a.x_token + (int64_t)(h0 + h) * a.x_head;
-        const int64_t oo = (t0 + t) * a.out_token + (int64_t)(h0 + h) * a.out_head;
-        if (c >= rot) {
-            const int d = 2 * P + (c - rot) * VEC;
-            *reinterpret_cast<V *>(out + oo + d) = *reinterpret_cast<const V *>(x + xo + d);
-        } else if (INTER) {
-            const int d = c * PV;
-            alignas(sizeof(T) * PV) T v[PV];
+#pragma unroll 1
+    for (; r < rows; r += step) {
+        V next[NV];
+        if (r + step < rows)
+            load(r + step, next);
+        const int t = token_of(r), h = r - t * nh;
+        if (turn) {
+            const float2 *const cs = s_cs + t * P + (INTER ? d / 2 : d);
 #pragma unroll
-            for (int j = 0; j < PV; j += VEC)
-                *reinterpret_cast<V *>(v + j) = *reinterpret_cast<const V *>(x + xo + d + j);
-#pragma unroll
-            for (int j = 0; j < PV; j += 2) {
-                const float2 cs = s_cs[t * P + (d + j) / 2];
-                const float p = to_f32(v[j]), q = to_f32(v[j + 1]);
-                from_f32(v[j], p * cs.x - q * cs.y);
-                from_f32(v[j + 1], q * cs.x + p * cs.y);
+            for (int j = 0; j < (INTER ? PV / 2 : VEC); ++j) {
+                T &e0 = INTER ? v[2 * j / VEC].v[2 * j % VEC] : v[0].v[j];
+                T &e1 = INTER ? v[(2 * j + 1) / VEC].v[(2 * j + 1) % VEC] : v[NV - 1].v[j];
+                const float2 w = cs[j];
+                const float p = to_f32(e0), q = to_f32(e1);
+                from_f32(e0, p * w.x - q * w.y);
+                from_f32(e1, q * w.x + p * w.y);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < PV; j += VEC)
-                *reinterpret_cast<V *>(out + oo + d + j) = *reinterpret_cast<const V *>(v + j);
-        } else {
-            const int d = c * VEC;
-            V v = *reinterpret_cast<const V *>(x + xo + d), w = *reinterpret_cast<const V *>(x + xo + d + P);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                const float2 cs = s_cs[t * P + d + j];
-                const float p = to_f32(v.v[j]), q = to_f32(w.v[j]);
-                from_f32(v.v[j], p * cs.x - q * cs.y);
-                from_f32(w.v[j], q * cs.x + p * cs.y);
-            }
-            *reinterpret_cast<V *>(out + oo + d) = v;
-            *reinterpret_cast<V *>(out + oo + d + P) = w;
+        for (int i = 0; i < NV; ++i) {
+            if (i < nv)
+                *reinterpret_cast<V *>(out + t * a.out_token + h * a.out_head + d + i * dist) = v[i];
+            v[i] = next[i];
         }
     }
 }
@@ -115,10 +120,15 @@ cudaError_t launch(const RopeArgs &a, cudaStream_t st)
     const int hp = (a.heads + by - 1) / by;
     const dim3 grid((unsigned)bx, (unsigned)((a.heads + hp - 1) / hp));
     const size_t smem = (size_t)tb * a.pairs * sizeof(float2);
+    // chunks of a head: rotated ones first, then the elements that pass through
+    const int pv = a.interleaved && VEC < 2 ? 2 : VEC;
+    const int rot = a.interleaved ? 2 * a.pairs / pv : a.pairs / VEC;
+    const int chunks = rot + (a.head_dim - 2 * a.pairs) / VEC;
+    const int threads = chunks >= kThreads ? chunks : kThreads / chunks * chunks;
     if (a.interleaved)
-        rope_kernel<T, VEC, true><<<grid, kThreads, smem, st>>>(a, tb, hp);
+        rope_kernel<T, VEC, true><<<grid, threads, smem, st>>>(a, tb, hp, chunks, rot);
     else
-        rope_kernel<T, VEC, false><<<grid, kThreads, smem, st>>>(a, tb, hp);
+        rope_kernel<T, VEC, false><<<grid, threads, smem, st>>>(a, tb, hp, chunks, rot);
     return cudaGetLastError();
 }
 
