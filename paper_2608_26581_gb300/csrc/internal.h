@@ -309,4 +309,26 @@ int resident_blocks_per_sm(const void *kern, int threads, size_t smem);
 // Number of SMs of the current device (cached).
 int num_sms();
 
+// Launches a kernel that calls wait_for_previous() (ptx.cuh) before it touches
+// global memory: its blocks may start while the last ones of the kernel before
+// it in the stream still run, so short kernels of one step follow each other
+// without a gap.  cluster: blocks of a cluster along x.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, static_cast<A &&>(args)...);
+}
+
 } // namespace rfq

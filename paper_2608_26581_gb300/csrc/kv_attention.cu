@@ -108,14 +108,14 @@ struct Request {
     __device__ __forceinline__ void load(const KvAttentionArgs &a, int r, int32_t *status)
     {
         const int most = a.width * a.cache.page_size;      // (the host has seen that it fits an int)
-        const int len = __ldg(a.lengths + r);
+        const int len = a.lengths[r];
         L = min(max(len, 0), most);
         q0 = r;
         n = 1;
         bool ok = len == L;
         if (a.q_start) {
-            q0 = __ldg(a.q_start + r);
-            const int q1 = __ldg(a.q_start + r + 1);
+            q0 = a.q_start[r];
+            const int q1 = a.q_start[r + 1];
             n = q1 - q0;
             if (q0 < 0 || q0 > q1 || q1 > a.tokens) {
                 ok = false;
@@ -418,6 +418,8 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             mbar_init(&s_full[warp][i], 1);
         fence_mbar_init();
     }
+    wait_for_previous();
+    let_next_start();
     // ---- this warp's share of the units of all requests, in order: each warp
     // counts a run of requests, then finds its own start in one of the runs.
     // (One loop for both: the second pass finds its code at hand.)
@@ -479,7 +481,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     int page = -1;                           // *entry, read a chunk before it is used
     auto read_page = [&]() {
         if (copies && ahead.more() && key < ahead.ke)
-            page = __ldg(entry);
+            page = *entry;
     };
     auto place = [&]() {
         key = ahead.kb + ahead.i * kChunk + (lane >> 2) * 16;
@@ -563,7 +565,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                                         (int64_t)(walk.head * G + ri - tok * G) * a.q_head + 8 * c;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-            raw[b] = rr < rows ? __ldg(reinterpret_cast<const uint4 *>(at + 32 * b)) : make_uint4(0, 0, 0, 0);
+            raw[b] = rr < rows ? *reinterpret_cast<const uint4 *>(at + 32 * b) : make_uint4(0, 0, 0, 0);
     };
     float qs[NT][2];
     int hi[NT][2];                           // keys that the thread's two rows see: [max(0, hi - window), hi)
@@ -1145,8 +1147,7 @@ cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
                       static_cast<int32_t *>(a.workspace),
                       reinterpret_cast<int32_t *>(ws + kWsCounters),
                       reinterpret_cast<float *>(ws + ws_parts_offset())};
-    kv_attention_kernel<FMT, D, NT><<<num_sms(), S::kThreads, S::kSmem, st>>>(p);
-    return cudaGetLastError();
+    return launch_early(kv_attention_kernel<FMT, D, NT>, dim3(num_sms()), S::kThreads, S::kSmem, st, 1, p);
 }
 
 template <int FMT, int D>

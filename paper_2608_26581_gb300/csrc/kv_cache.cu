@@ -17,6 +17,7 @@
 
 #include "hif4_math.cuh"
 #include "kv_layout.cuh"
+#include "ptx.cuh"
 
 namespace rfq {
 namespace {
@@ -77,15 +78,17 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const KvAppendAr
                                      (int64_t)head * (value ? a.v_head : a.k_head) + b * 32;
     uint8_t *const codes0 = static_cast<uint8_t *>(value ? c.v_codes : c.k_codes);
     uint8_t *const scales0 = static_cast<uint8_t *>(value ? c.v_scales : c.k_scales);
+    wait_for_previous();
+    let_next_start();
     // every lane of a warp stays to the end (its lanes shuffle)
     for (int64_t t0 = ((int64_t)blockIdx.y * kWarps + (threadIdx.x >> 5)) * TOK; t0 < a.tokens;
          t0 += (int64_t)gridDim.y * kWarps * TOK) {
         const int64_t t = min(t0 + lane / NB, a.tokens - 1);
-        const int64_t slot = __ldg(a.slots + t);
+        const int64_t slot = a.slots[t];
         uint32_t w[16];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(src + t * token) + j);
+            const uint4 u = reinterpret_cast<const uint4 *>(src + t * token)[j];
             w[4 * j] = u.x, w[4 * j + 1] = u.y, w[4 * j + 2] = u.z, w[4 * j + 3] = u.w;
         }
         const bool ok = t0 + lane / NB < a.tokens && slot_ok(slot, c);
@@ -209,9 +212,11 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const rfq_kv_cache c,
     void *const dst = value ? v : k;
     const uint8_t *const codes0 = static_cast<const uint8_t *>(value ? c.v_codes : c.k_codes);
     const uint8_t *const scales0 = static_cast<const uint8_t *>(value ? c.v_scales : c.k_scales);
+    wait_for_previous();
+    let_next_start();
     for (int64_t t = ((int64_t)blockIdx.y * kWarps + (threadIdx.x >> 5)) * TOK + lane / NB; t < tokens;
          t += (int64_t)gridDim.y * kWarps * TOK) {
-        const int64_t slot = __ldg(slots + t), o = (t * c.heads + head) * D;
+        const int64_t slot = slots[t], o = (t * c.heads + head) * D;
         float x[8];
         if (!slot_ok(slot, c)) {
 #pragma unroll
@@ -277,8 +282,7 @@ cudaError_t launch_kv_append(const KvAppendArgs &a, cudaStream_t st)
     const bool hif4 = a.cache.fmt == RFQ_FMT_HIF4;
     auto *const kern = hif4 ? (D == 128 ? kv_append_kernel<RFQ_FMT_HIF4, 128> : kv_append_kernel<RFQ_FMT_HIF4, 64>)
                             : (D == 128 ? kv_append_kernel<RFQ_FMT_MXFP4, 128> : kv_append_kernel<RFQ_FMT_MXFP4, 64>);
-    kern<<<grid_for(a.tokens, a.cache.heads, D), kThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch_early(kern, grid_for(a.tokens, a.cache.heads, D), kThreads, 0, st, 1, a);
 }
 
 cudaError_t launch_kv_read(const rfq_kv_cache &c, const int64_t *slots, int64_t tokens, void *k, void *v, bool bf16,
@@ -293,8 +297,7 @@ cudaError_t launch_kv_read(const rfq_kv_cache &c, const int64_t *slots, int64_t 
     else
         kern = wide ? (bf16 ? kv_read_kernel<RFQ_FMT_MXFP4, 128, true> : kv_read_kernel<RFQ_FMT_MXFP4, 128, false>)
                     : (bf16 ? kv_read_kernel<RFQ_FMT_MXFP4, 64, true> : kv_read_kernel<RFQ_FMT_MXFP4, 64, false>);
-    kern<<<grid_for(tokens, c.heads, c.head_dim), kThreads, 0, st>>>(c, slots, tokens, k, v);
-    return cudaGetLastError();
+    return launch_early(kern, grid_for(tokens, c.heads, c.head_dim), kThreads, 0, st, 1, c, slots, tokens, k, v);
 }
 
 } // namespace rfq

@@ -137,11 +137,11 @@ struct Scales {
                     uint32_t v = 0;
                     if (kHif4 || p.words) {
                         if (in[r] && kk < p.K)
-                            v = __ldg(reinterpret_cast<const uint32_t *>(s));
+                            v = *reinterpret_cast<const uint32_t *>(s);
                     } else if (in[r]) {    // row-major E8M0 rows that are not whole words
                         for (int j = 0; j < 4; ++j)
                             if (kk + 32 * j < p.K)
-                                v |= (uint32_t)__ldg(s + j) << (8 * j);
+                                v |= (uint32_t)s[j] << (8 * j);
                     }
                     w[b * kN + 2 * h + r] = v;
                 }
@@ -185,6 +185,10 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
     for (int i = tid; i < S::kZero / 16; i += kThreads)
         reinterpret_cast<uint4 *>(s_zero)[i] = make_uint4(0, 0, 0, 0);
     __syncwarp();
+    if (tid == 0)
+        prefetch_tmap(&wmap);
+    wait_for_previous();
+    let_next_start();
     bool ok = true;                                                // no wait has run out
     int slot = 0;                                                  // of the ring, and its phase
     uint32_t parity = 0;
@@ -223,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
 #pragma unroll
             for (int j = 0; j < BX; ++j)
                 if (k + j * kBoxK < p.K)       // (volatile: where it stands)
-                    asm volatile("ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];"
+                    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(u[j].x), "=r"(u[j].y), "=r"(u[j].z), "=r"(u[j].w)
                                  : "l"(p.x + m * p.x_row + k + j * kBoxK));
         };
@@ -635,17 +639,8 @@ cudaError_t launch(const MatvecArgs &a, cudaStream_t st)
     CUtensorMap map;
     if (!encode_tmap_2d_u8(&map, a.w.codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, kBoxK / 2, kTile, 128))
         return cudaErrorInvalidValue;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(split, (unsigned)groups);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = fixed + depth * kWarps * S::kStepBytes;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {(unsigned)split, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, matvec_kernel<FMT, MP>, map, p);
+    return launch_early(matvec_kernel<FMT, MP>, dim3(split, (unsigned)groups), kThreads,
+                        (size_t)fixed + depth * kWarps * S::kStepBytes, st, split, map, p);
 }
 
 template <int FMT>

@@ -20,6 +20,17 @@ __device__ __forceinline__ uint64_t globaltimer_ns()
     return t;
 }
 
+// ------------------------------------------------- programmatic launches
+// A kernel launched with launch_early (internal.h) may start while the kernel
+// before it in the stream still runs: it touches no global memory before
+// wait_for_previous(), which returns once that kernel is complete and its
+// writes are visible; what it reads after that goes through plain loads
+// (a non-coherent one, __ldg, may be moved before the wait).
+// let_next_start() lets the next such kernel start as soon as every block of
+// this one has come here and resources allow.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---------------------------------------------------------------- mbarrier
 
 __device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)

@@ -15,6 +15,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace rfq {
 namespace {
@@ -65,6 +66,8 @@ __global__ void rope_kernel(const RopeArgs a, int tb, int heads_per, int chunks,
     // while the one before it is turned
     int r = threadIdx.x / chunks;
     V v[NV];
+    wait_for_previous();
+    let_next_start();
     if (r < rows)
         load(r, v);
     for (int i = threadIdx.x; i < nt * P; i += blockDim.x) {
@@ -126,10 +129,8 @@ cudaError_t launch(const RopeArgs &a, cudaStream_t st)
     const int chunks = rot + (a.head_dim - 2 * a.pairs) / VEC;
     const int threads = chunks >= kThreads ? chunks : kThreads / chunks * chunks;
     if (a.interleaved)
-        rope_kernel<T, VEC, true><<<grid, threads, smem, st>>>(a, tb, hp, chunks, rot);
-    else
-        rope_kernel<T, VEC, false><<<grid, threads, smem, st>>>(a, tb, hp, chunks, rot);
-    return cudaGetLastError();
+        return launch_early(rope_kernel<T, VEC, true>, grid, threads, smem, st, 1, a, tb, hp, chunks, rot);
+    return launch_early(rope_kernel<T, VEC, false>, grid, threads, smem, st, 1, a, tb, hp, chunks, rot);
 }
 
 } // namespace

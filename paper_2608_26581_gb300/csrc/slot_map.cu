@@ -90,6 +90,8 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
 
     if (tid == 0)
         s_taken = 0;
+    wait_for_previous();
+    let_next_start();
     const int given = __ldcg(a.free_in);
     // this thread's requests, then the block's sums before them
     const int per = (R + kThreads - 1) / kThreads;
@@ -218,17 +220,7 @@ cudaError_t launch_slot_map(const SlotMapArgs &a, cudaStream_t st)
                                                  (6 * kSlotMapRequests + 1) * (int)sizeof(int32_t)))
             return e;
     const int ctas = a.tokens > kSoloTokens ? kCluster : 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {(unsigned)ctas, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, slot_map_kernel, a);
+    return launch_early(slot_map_kernel, dim3(ctas), kThreads, smem, st, ctas, a);
 }
 
 } // namespace rfq
