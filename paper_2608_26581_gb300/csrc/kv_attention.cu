@@ -36,29 +36,20 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
-#include "internal.h"
+#include "kv_attention.cuh"
 #include "kv_layout.cuh"
 #include "mxfp4_math.cuh"
-#include "ptx.cuh"
 
 namespace rfq {
 namespace {
 
 constexpr int kLeast = 8;                    // units of a CTA, at least
-constexpr uint32_t kAll = 0xFFFFFFFFu;
-constexpr int kHalves = 2, kChunk = 16 * kHalves;   // keys of a chunk: two MMA tiles
+constexpr int kHalves = 2;                   // MMA tiles of 16 keys in a chunk
 
 __device__ __forceinline__ uint32_t movmatrix(uint32_t a)
 {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
-    return r;
-}
-
-__device__ __forceinline__ float ex2(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 
@@ -68,28 +59,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
-struct Params {
-    KvAttentionArgs a;
-    int group;                 // query heads per key head
-    int gran;                  // keys of one copy: a chunk where a page is whole chunks, else 16
-    int32_t *status;
-    int32_t *counter;          // [CTAs] parts of a split segment that have arrived
-    float *part;               // [2 CTAs] parts: Shape::kPart bytes each
-};
-
 template <int FMT, int D, int NT>
 struct Shape {
     // 12 warps leave a thread 168 registers: with 16 the loop over the keys
     // spills at D = 128 (323 us against 230 at 8 x 131072 keys, MXFP4), and
     // eight hide less latency (275 us)
     static constexpr int kWarps = NT > 1 ? 8 : D == 64 ? 16 : 12, kThreads = 32 * kWarps;
-    static constexpr int kRows = 8 * NT, kMt = D / 16;
+    static constexpr int kRows = 8 * NT, kMt = D / 16, kChunk = 16 * kHalves, kStart = 1;
     static constexpr int kScale = FMT == RFQ_FMT_HIF4 ? D / 16 : D / 32;   // bytes a token
     static constexpr int kCode = D / 2;
     static constexpr int kVOff = kChunk * kCode, kKsOff = 2 * kVOff, kVsOff = kKsOff + kChunk * kScale;
@@ -100,191 +76,6 @@ struct Shape {
     static constexpr int kQ = NT > 1 ? NT * D * 16 : 0;                    // of a warp
     static constexpr int kSmem = kWarps * (kDepth * kBytes + kPart + kQ);
     static_assert(kDepth * kBytes >= kPart, "a warp's last part lies over its ring");
-};
-
-// One request: n new tokens (rows q0 .. of q) at the end of its L keys.
-struct Request {
-    int n, L, q0;
-    __device__ __forceinline__ void load(const KvAttentionArgs &a, int r, int32_t *status)
-    {
-        const int most = a.width * a.cache.page_size;      // (the host has seen that it fits an int)
-        const int len = a.lengths[r];
-        L = min(max(len, 0), most);
-        q0 = r;
-        n = 1;
-        bool ok = len == L;
-        if (a.q_start) {
-            q0 = a.q_start[r];
-            const int q1 = a.q_start[r + 1];
-            n = q1 - q0;
-            if (q0 < 0 || q0 > q1 || q1 > a.tokens) {
-                ok = false;
-                n = 0;
-            }
-        }
-        if (!ok && status)
-            atomicCAS(status, kDevOk, kDevBadGroups);
-    }
-    // Tiles of `rows` (token, head) rows
-    __device__ __forceinline__ int tiles(int group, int rows) const { return (n * group + rows - 1) / rows; }
-    // Keys [kb, ke) that some row of the tile sees, kb rounded down to gran
-    __device__ __forceinline__ void keys(int tile, const Params &p, int rows, int &kb, int &ke) const
-    {
-        int first = 0, last = 0;
-        if (n > 1) {
-            first = tile * rows / p.group;
-            last = min(n - 1, (tile * rows + rows - 1) / p.group);
-        }
-        ke = max(0, L - n + last + 1);
-        kb = p.a.window > 0 ? max(0, L - n + first + 1 - p.a.window) & -p.gran : 0;
-        kb = min(kb, ke & -p.gran);
-    }
-    // Units of a tile: its chunks (one at least) and one more
-    __device__ __forceinline__ uint32_t units(int tile, const Params &p, int rows) const
-    {
-        int kb, ke;
-        keys(tile, p, rows, kb, ke);
-        return max(1, (ke - kb + kChunk - 1) / kChunk) + 1;
-    }
-};
-
-__device__ __forceinline__ uint32_t warp_scan(uint32_t v, int lane)    // inclusive
-{
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t x = __shfl_up_sync(kAll, v, d);
-        if (lane >= d)
-            v += x;
-    }
-    return v;
-}
-
-// Units of one key head of a request (the whole warp together)
-template <typename S>
-__device__ __forceinline__ uint32_t head_units(const Request &q, const Params &p, int lane)
-{
-    const int n = q.tiles(p.group, S::kRows);
-    uint32_t s = 0;
-#pragma unroll 1
-    for (int t = lane; t < n; t += 32)
-        s += q.units(t, p, S::kRows);
-    return __reduce_add_sync(kAll, s);
-}
-
-// Walks requests [r, r1) with the whole warp until `rem` units lie behind:
-// returns the units of all of them, or stops at the request in which rem
-// runs out, with rem units of it.  Requests of one token are taken 32 at a
-// time, a lane each.
-template <typename S>
-__device__ __forceinline__ uint32_t seek(const Params &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status)
-{
-    uint32_t all = 0;
-    const int H = p.a.cache.heads;
-    if (!p.a.q_start) {
-#pragma unroll 1
-        for (; r < r1; r += 32) {
-            uint32_t mine = 0;
-            if (r + lane < r1) {
-                Request q;
-                q.load(p.a, r + lane, status);
-                mine = H * (uint32_t)q.tiles(p.group, S::kRows) * q.units(0, p, S::kRows);
-            }
-            const uint32_t upto = warp_scan(mine, lane), sum = __shfl_sync(kAll, upto, 31);
-            if (rem < sum) {
-                const int at = __ffs(__ballot_sync(kAll, rem < upto)) - 1;
-                rem -= __shfl_sync(kAll, upto - mine, at);
-                r += at;
-                return all;
-            }
-            rem -= sum;
-            all += sum;
-        }
-    } else {
-#pragma unroll 1
-        for (; r < r1; ++r) {
-            Request q;
-            q.load(p.a, r, status);
-            const uint32_t sum = H * head_units<S>(q, p, lane);
-            if (rem < sum)
-                return all;
-            rem -= sum;
-            all += sum;
-        }
-    }
-    return all;
-}
-
-// The segments of a warp's run of units, one after the other.
-template <typename S>
-struct Walk {
-    static constexpr int ROWS = S::kRows;
-    int r, head, tile, ntiles;
-    Request q;
-    int kb, ke, chunks;        // of the segment
-    int i, i1;                 // the warp's chunks of it left
-    uint32_t u, end;           // the segment's first unit; the end of the warp's units
-    // from unit `first`, `rem` units into the segments of request r0
-    __device__ __forceinline__ void start(const Params &p, int r0, uint32_t rem, uint32_t first, uint32_t last, int lane)
-    {
-        r = r0;
-        end = last;
-        head = tile = i = i1 = 0;
-        u = last;
-        if (first >= last)
-            return;
-        q.load(p.a, r, nullptr);
-        ntiles = q.tiles(p.group, ROWS);
-        const uint32_t per = head_units<S>(q, p, lane);
-        head = (int)(rem / per);
-        rem -= head * per;
-#pragma unroll 1
-        for (;; tile += 32) {
-            const uint32_t mine = tile + lane < ntiles ? q.units(tile + lane, p, ROWS) : 0u;
-            const uint32_t upto = warp_scan(mine, lane);
-            const uint32_t hit = __ballot_sync(kAll, rem < upto);
-            if (hit) {
-                const int at = __ffs(hit) - 1;
-                rem -= __shfl_sync(kAll, upto - mine, at);
-                tile += at;
-                break;
-            }
-            rem -= __shfl_sync(kAll, upto, 31);
-        }
-        u = first - rem;
-        segment(p, first);
-    }
-    // the chunks of the segment at u that lie in [from, end): chunk k is unit u + 1 + k
-    __device__ __forceinline__ void segment(const Params &p, uint32_t from)
-    {
-        q.keys(tile, p, ROWS, kb, ke);
-        chunks = max(1, (ke - kb + kChunk - 1) / kChunk);
-        i = from > u + 1 ? (int)(from - u - 1) : 0;
-        i1 = end > u + 1 ? (int)min((uint32_t)chunks, end - u - 1) : 0;
-    }
-    __device__ __forceinline__ bool more() const { return i < i1; }
-    // on to the next segment that has a chunk here, if any, once more() is false
-    __device__ __forceinline__ void next(const Params &p)
-    {
-#pragma unroll 1
-        while (i >= i1 && u < end) {
-            u += chunks + 1;
-            if (u >= end)
-                return;
-            if (++tile == ntiles) {
-                tile = 0;
-                if (++head == p.a.cache.heads) {
-                    head = 0;
-#pragma unroll 1
-                    do {               // (requests without new tokens have no segment)
-                        ++r;
-                        q.load(p.a, r, nullptr);
-                        ntiles = q.tiles(p.group, ROWS);
-                    } while (ntiles == 0);
-                }
-            }
-            segment(p, u);
-        }
-    }
 };
 
 // One warp's share of a row tile: O^T (dimensions g D/8 + 2i and + 1 by rows
@@ -379,20 +170,13 @@ struct Joined {
     }
 };
 
-__device__ __forceinline__ float log_sum(float m, float l)
-{
-    return l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-}
-// 1 / l, 0 for a row that saw no key (and NaN for one whose wait ran out)
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }
-
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
-    kv_attention_kernel(const __grid_constant__ Params p)
+    kv_attention_kernel(const __grid_constant__ AttnParams p)
 {
     using S = Shape<FMT, D, NT>;
     constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
-    constexpr int NB = D / 32, ROWS = S::kRows, MT = S::kMt, W = S::kWarps, DEPTH = S::kDepth, HV = kHalves;
+    constexpr int NB = D / 32, ROWS = S::kRows, MT = S::kMt, W = S::kWarps, DEPTH = S::kDepth, HV = kHalves, kChunk = S::kChunk;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ alignas(8) uint64_t s_full[W][DEPTH];
     __shared__ uint32_t s_scan[W];
@@ -420,41 +204,13 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     }
     wait_for_previous();
     let_next_start();
-    // ---- this warp's share of the units of all requests, in order: each warp
-    // counts a run of requests, then finds its own start in one of the runs.
-    // (One loop for both: the second pass finds its code at hand.)
-    const int per = (a.requests + W - 1) / W;
-    int run = warp, r_at = 0;
-    uint32_t rem = 0xFFFFFFFFu, total = 0, ctas = 0, first = 0, last = 0;
-    const uint32_t cta = blockIdx.x;
-#pragma unroll 1
-    for (int pass = 0;; ++pass) {
-        r_at = min(a.requests, run * per);
-        const uint32_t sum = seek<S>(p, r_at, min(a.requests, r_at + per), rem, lane,
-                                        pass == 0 && cta == 0 ? p.status : nullptr);
-        if (pass == 1)
-            break;
-        if (lane == 0)
-            s_scan[warp] = sum;
-        __syncthreads();
-        const uint32_t runs = warp_scan(lane < W ? s_scan[lane] : 0u, lane);
-        total = __shfl_sync(kAll, runs, 31);
-        // (a CTA with few units would only add parts to join)
-        ctas = min(gridDim.x, (total + kLeast - 1) / kLeast);
-        if (cta >= ctas)
-            return;
-        // total cta / ctas without a wide product
-        const uint32_t each = total / ctas, more = total % ctas;
-        const uint32_t u0 = each * cta + more * cta / ctas, un = each * (cta + 1) + more * (cta + 1) / ctas - u0;
-        first = u0 + un / W * warp + un % W * warp / W;
-        last = u0 + un / W * (warp + 1) + un % W * (warp + 1) / W;
-        run = min(W - 1, __popc(__ballot_sync(kAll, lane < W && runs <= first)));
-        rem = first - (run ? __shfl_sync(kAll, runs, run - 1) : 0u);
-        if (first >= last)
-            rem = 0;
-    }
+    // ---- this warp's share of the units of all requests, in order
+    Share sh;
+    if (!find_share<S>(p, s_scan, W, kLeast, sh))
+        return;
+    const uint32_t total = sh.total, ctas = sh.ctas, cta = blockIdx.x;
     Walk<S> walk, ahead;                  // what is computed, and what is copied
-    walk.start(p, r_at, rem, first, last, lane);
+    walk.start(p, sh.r, sh.rem, sh.first, sh.last, lane);
     walk.next(p);
     ahead = walk;
     const uint64_t limit = ws_wait_limit_ns(p.status);
@@ -1041,23 +797,13 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 __stcg(mine + (NT * MT + t) * 32 + lane, make_float4(x.m[0], x.m[1], x.l[0], x.l[1]));
         }
     }
-    // the CTA whose run holds unit u
-    auto owner = [&](uint32_t u) {
-        const uint32_t each = total / ctas, more = total % ctas;
-        uint32_t k = min(ctas - 1, (uint32_t)((float)u * (float)ctas / (float)total));
-        while (each * k + more * k / ctas > u)
-            --k;
-        while (each * (k + 1) + more * (k + 1) / ctas <= u)
-            ++k;
-        return (int)k;
-    };
     if (nshared > 0) {
         __threadfence();
         __syncthreads();
         if (lane == 0 && warp < nshared) {
             const int e = warp ? shared[1] : shared[0];
             const PartInfo f = s_info[e >> 1][e & 1];
-            const int c0 = owner(f.seg + 1), c1 = owner(f.seg + f.chunks);
+            const int c0 = owner(sh, f.seg + S::kStart), c1 = owner(sh, f.seg + S::kStart + f.chunks - 1);
             s_c[warp] = make_int2(c0, c1);
             s_flag[warp] = atomicAdd(p.counter + c0, 1) == c1 - c0;
         }
@@ -1129,7 +875,7 @@ constexpr size_t kWsCounters = 256;
 size_t ws_parts_offset() { return kWsCounters + ((size_t)num_sms() * 4 + 255) / 256 * 256; }
 
 template <int FMT, int D, int NT>
-cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
+cudaError_t launch(AttnParams p, cudaStream_t st)
 {
     using S = Shape<FMT, D, NT>;
     static_assert(S::kSmem <= 226 * 1024, "fits an SM");
@@ -1140,41 +886,59 @@ cudaError_t launch(const KvAttentionArgs &a, cudaStream_t st)
             return e;
         ready = true;
     }
-    uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
-    const Params p = {a,
-                      a.heads / a.cache.heads,
-                      a.cache.page_size % kChunk == 0 ? kChunk : 16,
-                      static_cast<int32_t *>(a.workspace),
-                      reinterpret_cast<int32_t *>(ws + kWsCounters),
-                      reinterpret_cast<float *>(ws + ws_parts_offset())};
+    p.gran = p.a.cache.page_size % S::kChunk == 0 ? S::kChunk : 16;
     return launch_early(kv_attention_kernel<FMT, D, NT>, dim3(num_sms()), S::kThreads, S::kSmem, st, 1, p);
 }
 
 template <int FMT, int D>
-cudaError_t launch_rows(const KvAttentionArgs &a, cudaStream_t st)
+cudaError_t launch_rows(const AttnParams &p, int64_t rows, cudaStream_t st)
 {
-    // rows of a request and key head: the group's heads times its new tokens.
     // (Four row tiles a warp and 16 keys a chunk: 283 us against 239 with two,
     // 256 new tokens over up to 8192, D = 128: the sums leave no registers.)
-    const int64_t per = a.q_start ? (a.tokens + a.requests - 1) / a.requests : 1;
-    const int64_t rows = per * (a.heads / a.cache.heads);
-    return rows <= 8 ? launch<FMT, D, 1>(a, st) : launch<FMT, D, 2>(a, st);
+    return rows <= 8 ? launch<FMT, D, 1>(p, st) : launch<FMT, D, 2>(p, st);
 }
+
+// Rows of a request and key head (the group's heads times its new tokens) from
+// which on kv_attention_tile.cu takes it.
+constexpr int kTileRows = 33;
 
 } // namespace
 
 size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
 {
     (void)heads;
-    return ws_parts_offset() + (size_t)2 * num_sms() * 2 * (head_dim / 16 + 1) * 512;
+    const size_t part = (size_t)2 * (head_dim / 16 + 1) * 512, tile = kv_attention_tile_part_bytes(head_dim);
+    return ws_parts_offset() + (size_t)2 * num_sms() * (part > tile ? part : tile);
 }
 
 cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)
 {
+    uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
+    AttnParams p = {a,
+                    a.heads / a.cache.heads,
+                    0,
+                    static_cast<int32_t *>(a.workspace),
+                    reinterpret_cast<int32_t *>(ws + kWsCounters),
+                    reinterpret_cast<float *>(ws + ws_parts_offset()),
+                    0,
+                    INT32_MAX};
+    int64_t rows = a.q_start ? (a.tokens + a.requests - 1) / a.requests * p.group : p.group;
+    // Only the device knows who has how many new tokens.  Where each request
+    // has one at least and none can have kTileRows rows, the tiles have nothing to do.
+    const int64_t most = a.q_start ? (a.tokens - a.requests + 1) * p.group : p.group;
+    if (most >= kTileRows) {
+        p.least_rows = kTileRows;
+        if (cudaError_t e = launch_kv_attention_tile(p, st))
+            return e;
+        p.least_rows = 0;
+        p.most_rows = kTileRows - 1;
+        if (!a.q_start)
+            return cudaSuccess;              // (every request has the same rows)
+    }
     const bool wide = a.cache.head_dim == 128;
     if (a.cache.fmt == RFQ_FMT_HIF4)
-        return wide ? launch_rows<RFQ_FMT_HIF4, 128>(a, st) : launch_rows<RFQ_FMT_HIF4, 64>(a, st);
-    return wide ? launch_rows<RFQ_FMT_MXFP4, 128>(a, st) : launch_rows<RFQ_FMT_MXFP4, 64>(a, st);
+        return wide ? launch_rows<RFQ_FMT_HIF4, 128>(p, rows, st) : launch_rows<RFQ_FMT_HIF4, 64>(p, rows, st);
+    return wide ? launch_rows<RFQ_FMT_MXFP4, 128>(p, rows, st) : launch_rows<RFQ_FMT_MXFP4, 64>(p, rows, st);
 }
 
 } // namespace rfq

@@ -152,34 +152,6 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append_kernel(const KvAppendAr
     }
 }
 
-// Values of eight codes with elements in order.  MXFP4: scale word or half
-// word, sub-block b.  HiF4: meta, group gi of its block.
-__device__ __forceinline__ void mxfp4_values(uint32_t code, uint32_t scale, float (&x)[8])
-{
-    e2m1x8_decode(code, x);
-    const float s = e8m0_f32(scale);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        x[e] *= s;
-}
-__device__ __forceinline__ void hif4_values(uint32_t code, uint32_t meta, int gi, float (&x)[8])
-{
-    // S 2^t / 4, and 2^9 that the codes' conversion leaves out
-    const float unit = 128.f * hif4_macro_f32(meta);
-    const uint32_t e8 = (meta >> (8 + gi)) & 1u, e16 = meta >> (16 + 2 * gi);
-    const float s0 = unit * (float)(1 << (e8 + (e16 & 1u)));
-    const float s1 = unit * (float)(1 << (e8 + ((e16 >> 1) & 1u)));
-    uint32_t h[4];
-    s1p2x8_f16(code, h);                     // elements (0, 2), (1, 3), (4, 6), (5, 7)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[j]));
-        const int e = (j >> 1) * 4 + (j & 1);
-        x[e] = f.x * (j < 2 ? s0 : s1);
-        x[e + 2] = f.y * (j < 2 ? s0 : s1);
-    }
-}
-
 template <bool BF16>
 __device__ __forceinline__ void store8(void *dst, int64_t at, const float (&x)[8])
 {
