@@ -54,7 +54,7 @@ struct Tile {
     static constexpr int kBytes = kVsOff + kChunk * kScale;
     static constexpr int kOperand = 128 * D * 2;                           // bytes of Q, of a K and of a V
     static constexpr int kQ = 0, kK = kOperand, kV = 3 * kOperand, kRing = 5 * kOperand;
-    static constexpr int kSmem = kRing + kDepth * kBytes + 1024;           // (the operands lie on 1024 bytes)
+    static constexpr int kSmem = 1024 + kRing + kDepth * kBytes + 1024;    // (the operands lie on 1024 bytes)
     static constexpr int64_t kPart = 128 * (D + 2);                        // floats
 };
 
@@ -63,7 +63,10 @@ struct Bars {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t s_full[2], s_empty[2], p_full[2];
     uint64_t drain;
+    uint64_t limit;                          // of a wait, in ns
+    int32_t abort;                           // a wait has run out
 };
+extern __shared__ __align__(16) uint8_t smem_raw[];   // Bars, then the operands and the ring
 
 // A segment that the CTA does not hold whole.
 struct Shared {
@@ -241,9 +244,27 @@ __device__ __forceinline__ float row_weights(uint32_t s_at, uint32_t p_at, float
 }
 
 // The rest of a wait that did not end at once: out of the way of the loops.
-__device__ __noinline__ bool wait_on(uint64_t *b, uint32_t parity, uint64_t limit, const volatile int32_t *abort)
+__device__ __noinline__ bool wait_on(uint32_t b, uint32_t parity)
 {
-    return mbar_wait(b, parity, limit, abort);
+    const Bars &bar = *reinterpret_cast<const Bars *>(smem_raw);
+    const uint64_t t0 = globaltimer_ns();
+    for (uint32_t i = 1;; ++i) {
+        if (mbar_try_wait(b, parity))
+            return true;
+        if ((i & 63) == 0 && (globaltimer_ns() - t0 > bar.limit || *reinterpret_cast<const volatile int32_t *>(&bar.abort)))
+            return false;
+    }
+}
+// A warp waits as one, and every wait of the CTA gives up once one has run out.
+__device__ __forceinline__ bool wait(uint64_t *b, uint32_t parity)
+{
+    const uint32_t at = smem_u32(b);
+    if (__all_sync(kAll, mbar_try_wait(at, parity)))
+        return true;
+    if (__all_sync(kAll, wait_on(at, parity)))
+        return true;
+    *reinterpret_cast<volatile int32_t *>(&reinterpret_cast<Bars *>(smem_raw)->abort) = 1;
+    return false;
 }
 
 template <int FMT, int D>
@@ -253,16 +274,15 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
     constexpr bool HIF4 = FMT == RFQ_FMT_HIF4;
     constexpr int NB = D / 32, DEPTH = S::kDepth;
     constexpr int kBias = HIF4 ? 50 : 136;   // operand = value 2^(kBias - exponent)
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ alignas(8) Bars bar;
+    Bars &bar = *reinterpret_cast<Bars *>(smem_raw);
     __shared__ uint32_t s_scan[kWarps], s_tmem;
-    __shared__ int32_t s_abort;
     __shared__ int s_unit[DEPTH][NB + 1];    // the exponents that V (32 dimensions each) and K are relative to
     __shared__ int s_vref[2][NB], s_kref[4]; // the same by chunk, for the softmax
     __shared__ float s_qs[4][128];           // by segment: what a row of Q was divided by
     __shared__ Shared s_shared[2];
     __shared__ int s_nshared;
-    uint8_t *const smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
+    static_assert(sizeof(Bars) <= 1024, "in front of the operands");
+    uint8_t *const smem = smem_raw + 1024 + (-smem_u32(smem_raw) & 1023u);
 
     const KvAttentionArgs &a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -285,7 +305,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         }
         mbar_init(&bar.drain, 1);
         fence_mbar_init();
-        s_abort = 0;
+        bar.abort = 0;
         s_nshared = 0;
     }
     wait_for_previous();
@@ -293,6 +313,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
     Share sh;
     if (!find_share<S, false>(p, s_scan, kWarps, kLeast, sh))
         return;
+    if (tid == 0)
+        bar.limit = ws_wait_limit_ns(p.status);
     // (TMEM only now: a kernel in front that is still to take its own has finished)
     if (warp == kMma) {
         tmem_alloc(&s_tmem, kTmemCols);
@@ -302,18 +324,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    const uint64_t limit = ws_wait_limit_ns(p.status);
     Walk<S> walk;
     walk.start(p, sh.r, sh.rem, sh.first, sh.last, lane);
     walk.next(p);
-    // A warp waits as one, and every wait of the CTA gives up once one has run out.
-    auto wait = [&](uint64_t *b, uint32_t parity) {
-        if (__all_sync(kAll, mbar_try_wait(smem_u32(b), parity) || wait_on(b, parity, limit, &s_abort)))
-            return true;
-        *reinterpret_cast<volatile int32_t *>(&s_abort) = 1;
-        return false;
-    };
-
     if (warp < kKeys) {
         // ------------------------------------------------ softmax and output
         const uint32_t lane_at = tmem + ((uint32_t)(warp * 32) << 16);
@@ -458,23 +471,36 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         for (; walk.more(); ++segs) {
             // ---- the rows as f16, once all MMAs that read those before are done
             const int row0 = walk.tile * 128, rows = min(128, walk.q.n * G - row0);
-            constexpr int C = D / 8;         // pieces of 8 dimensions, a lane each
+            constexpr int C = D / 8, kStep = 128 / C;    // pieces of 8 dimensions, a lane each; rows at a time
+            const int row = t / C, ch = t % C;
             uint4 x[C];
+            {
+                int tok = (row0 + row) / G, head = row0 + row - tok * G;
+                const int more = kStep / G, rest = kStep - more * G;
+                const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(a.q) + walk.q.q0 * a.q_token +
+                                               (int64_t)walk.head * G * a.q_head + 8 * ch;
 #pragma unroll
-            for (int u = 0; u < C; ++u) {
-                const int row = (128 * u + t) / C, ch = t % C, ri = row0 + row, tok = ri / G;
-                x[u] = make_uint4(0, 0, 0, 0);
-                if (row < rows)
-                    x[u] = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) +
-                                                            (walk.q.q0 + tok) * a.q_token +
-                                                            (int64_t)(walk.head * G + ri - tok * G) * a.q_head + 8 * ch);
+                for (int u = 0; u < C; ++u) {
+                    x[u] = make_uint4(0, 0, 0, 0);
+                    if (kStep * u + row < rows)
+                        x[u] = *reinterpret_cast<const uint4 *>(q + tok * a.q_token + head * a.q_head);
+                    tok += more, head += rest;
+                    if (head >= G)
+                        head -= G, ++tok;
+                }
             }
             if (j > 0 && !wait(&bar.k_empty[(j - 1) & 1], ((j - 1) >> 1) & 1))
                 break;
+            uint8_t *at = smem + S::kQ + (ch >> 3) * 16384 + row * 128;
+            const int b = ch >> 2, even = (2 * (ch & 3) + (b & 1)) << 4;
 #pragma unroll
-            for (int u = 0; u < C; ++u) {
-                const int row = (128 * u + t) / C, ch = t % C;
-                const uint32_t w[4] = {x[u].x ^ sign, x[u].y ^ sign, x[u].z ^ sign, x[u].w ^ sign};
+            for (int u = 0; u < C; ++u)
+                *reinterpret_cast<uint4 *>(at + u * (kStep * 128) + (even ^ ((kStep * u + row & 7) << 4))) = x[u];
+#pragma unroll 1
+            for (int u = row; u < 128; u += kStep, at += kStep * 128) {
+                uint4 *const mine = reinterpret_cast<uint4 *>(at + (even ^ ((u & 7) << 4)));
+                const uint4 y = *mine;
+                const uint32_t w[4] = {y.x ^ sign, y.y ^ sign, y.z ^ sign, y.w ^ sign};
                 float f[8], mx = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -492,14 +518,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 for (int i = 0; i < 4; ++i) {
                     // HiF4 codes decode in the order 0 2 | 1 3 | 4 6 | 5 7
                     const int lo = HIF4 ? (i >> 1) * 4 + (i & 1) : 2 * i, up = HIF4 ? lo + 2 : lo + 1;
-                    const __half2 y = __floats2half2_rn(f[lo] * mul, f[up] * mul);
-                    h[i] = *reinterpret_cast<const uint32_t *>(&y);
+                    const __half2 z = __floats2half2_rn(f[lo] * mul, f[up] * mul);
+                    h[i] = *reinterpret_cast<const uint32_t *>(&z);
                 }
-                const int b = ch >> 2, at = (2 * (ch & 3) + (b & 1)) ^ (row & 7);
-                *reinterpret_cast<uint4 *>(smem + S::kQ + (b >> 1) * 16384 + row * 128 + at * 16) =
-                    make_uint4(h[0], h[1], h[2], h[3]);
+                *mine = make_uint4(h[0], h[1], h[2], h[3]);
                 if (ch == 0)
-                    s_qs[segs & 3][row] = __uint_as_float((uint32_t)(127 + e) << 23);
+                    s_qs[segs & 3][u] = __uint_as_float((uint32_t)(127 + e) << 23);
             }
             const int least = a.window > 0 ? max(0, walk.q.L - walk.q.n + row0 / G + 1 - a.window) : 0;
 #pragma unroll 1
@@ -706,19 +730,22 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         bool ok = true;
 #pragma unroll 1
         while (ok && walk.more()) {
-            ok = scores(j);
+            const int n = walk.i1 - walk.i;
 #pragma unroll 1
-            for (bool first = true; ok && walk.i < walk.i1; ++walk.i, ++j, first = false) {
-                if (walk.i + 1 < walk.i1)
-                    ok = scores(j + 1);
-                ok = ok && sums(j, first);
+            for (int k = 0; ok && k <= n; ++k) {
+                if (k < n)
+                    ok = scores(j + k);
+                if (ok && k > 0)
+                    ok = sums(j + k - 1, k == 1);
             }
+            j += n;
+            walk.i = walk.i1;
             if (ok)
                 walk.next(p);
         }
         if (lane == 0) {
             tc_commit(&bar.drain);           // (all of them, before TMEM goes back)
-            mbar_wait(&bar.drain, 0, limit);
+            mbar_wait(&bar.drain, 0, bar.limit);
         }
     } else {
         // ------------------------------------------------ copies
@@ -766,7 +793,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         }
         // (copies in flight land before the CTA's memory goes: fill f is phase f / DEPTH of its slot)
         for (uint32_t f = filled > DEPTH ? filled - DEPTH : 0; f < filled; ++f)
-            mbar_wait(&bar.full[f % DEPTH], (f / DEPTH) & 1, limit);
+            mbar_wait(&bar.full[f % DEPTH], (f / DEPTH) & 1, bar.limit);
     }
     tc_fence_before();
     __syncthreads();
