@@ -899,7 +899,11 @@ cudaError_t launch_rows(const AttnParams &p, int64_t rows, cudaStream_t st)
 }
 
 // Rows of a request and key head (the group's heads times its new tokens) from
-// which on kv_attention_tile.cu takes it.
+// which on kv_attention_tile.cu takes it: more than two of this kernel's tiles.
+// 8 requests of 4096 keys, 32 heads on 8, D = 128, MXFP4, tiles against this
+// kernel: 32 rows 43 against 33 us, 48 rows 44 against 47, 64 rows 42 against
+// 40, 96 rows 44 against 73, 256 rows 54 against 96 (HiF4: 48 against 39, 49
+// against 58, 46 against 49; D = 64: 37 against 25, 38 against 36).
 constexpr int kTileRows = 33;
 
 } // namespace

@@ -17,19 +17,23 @@
 // Work: the (request, key head, 128 rows) segments laid end to end in chunks
 // of 128 keys, split evenly over the CTAs, one a SM.  In a CTA, warp by warp:
 //   0-3    softmax: a thread has one row; S from TMEM twice (for its maximum,
-//          then its weights), P to TMEM
-//   4-11   K codes to f16 (and Q, when a segment begins), dimensions contiguous
-//   12-19  V codes to f16, dimensions contiguous
-//   20     one thread issues the MMAs: S of the next chunk before P V of this
-//   21     copies the chunks' codes and scales, three ahead
-//   22     the running powers of two
+//          then for its weights), P to TMEM
+//   4-7    K codes to f16 (and Q, when a segment begins), dimensions contiguous
+//   8-11   V codes to f16, dimensions contiguous
+//   12     one thread issues the MMAs: S of the next chunk before P V of this
+//   13     the running powers of two
+//   14     copies the chunks' codes and scales, three ahead
 // K, V, S and P have two buffers each.  A segment that CTAs share leaves its
 // parts in the workspace, where the last CTA to finish joins them: the split
 // and the order of every sum depend on the lengths alone.
 //
-// Bound: instruction issue, and the fetch of the instructions: 16384 scores
-// and 32768 codes a chunk.  The loops stay rolled because the roles' code has
-// to fit the instruction caches together (all unrolled: 186 us for 135).
+// Bound: the instructions of 16384 scores and 32768 codes a chunk (6000 clocks,
+// of which the tensor cores take 1600), and their fetch: the roles' loops have
+// to fit the instruction caches together, so they stay rolled (unrolled: 186
+// us where this takes 85).  Eight warps for K and V each or for the softmax
+// are slower (95 and 92 us).
+// 256 new tokens of 5 requests over 300 to 8192 keys, 32 heads on 8, D = 128,
+// MXFP4: 85 us, 420 TFLOP/s.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -42,7 +46,7 @@ namespace rfq {
 namespace {
 
 constexpr int kLeast = 4;                    // units of a CTA, at least
-constexpr int kKeys = 4, kValues = 8, kMma = 12, kCopy = 13, kUnits = 14, kWarps = 15;   // a role's first warp
+constexpr int kKeys = 4, kValues = 8, kMma = 12, kUnits = 13, kWarps = 15;   // a role's first warp
 constexpr uint32_t kTmemCols = 512;          // S: 0, 128; O: 256; P: 384, 448
 
 template <int FMT, int D>
@@ -249,7 +253,14 @@ __device__ __noinline__ bool wait_on(uint32_t b, uint32_t parity)
     const Bars &bar = *reinterpret_cast<const Bars *>(smem_raw);
     const uint64_t t0 = globaltimer_ns();
     for (uint32_t i = 1;; ++i) {
-        if (mbar_try_wait(b, parity))
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\t"
+                     "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+                     "selp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(b), "r"(parity), "r"(2000u)             // (asleep for at most this many ns)
+                     : "memory");
+        if (done)
             return true;
         if ((i & 63) == 0 && (globaltimer_ns() - t0 > bar.limit || *reinterpret_cast<const volatile int32_t *>(&bar.abort)))
             return false;
@@ -429,10 +440,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 tmem_ld_32x32b_x32(lane_at + 256 + 32 * b, x);
                 tmem_ld_ready(x);
                 const float f = scalbnf(inv, pick(vref, b) - kBias);
-                if (tid >= rows)
-                    continue;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 4 && tid < rows; ++k) {
                     float y[8];              // (HiF4 columns stand in the order 0 2 | 1 3 | 4 6 | 5 7)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
@@ -445,6 +454,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                                                     pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
                     }
                 }
+                __syncwarp();
             }
             if (part) {
                 if (tid < rows)
