@@ -32,7 +32,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 struct AttnParams {
     KvAttentionArgs a;
     int group;                 // query heads per key head
-    int gran;                  // keys of one copy: a chunk where a page is whole chunks, else 16
+    int gran;                  // keys of one copy: they lie in one page
     int32_t *status;
     int32_t *counter;          // [CTAs] parts of a split segment that have arrived
     float *part;               // [2 CTAs] parts of split segments

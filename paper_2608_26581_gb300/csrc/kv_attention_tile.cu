@@ -710,7 +710,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
             tc_fence_after();
             if (lane == 0) {
                 const uint64_t k_desc = sdesc_k_sw128(k_at + buf * S::kOperand);
-#pragma unroll 1
+#pragma unroll
                 for (int k = 0; k < D / 16; ++k) {           // (offsets in 16 bytes)
                     const int at = (k >> 2) * 1024 + (k & 3) * 2;
                     tc_mma_f16(tmem + buf * 128, q_desc + at, k_desc + at, id_s, k > 0);
@@ -728,7 +728,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
             tc_fence_after();
             if (lane == 0) {
                 const uint64_t v_desc = sdesc_n_sw128(v_at + buf * S::kOperand);
-#pragma unroll 1
+#pragma unroll
                 for (int k = 0; k < 8; ++k)
                     tc_mma_f16_ts(tmem + 256, tmem + 384 + buf * 64 + 8 * k, v_desc + 128 * k, id_o, !first || k > 0);
                 tc_commit(&bar.v_empty[buf]);
@@ -768,21 +768,38 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                                                                            : a.cache.v_scales);
         const uint32_t dst = smem_u32(smem + S::kRing) +
                              (arr == 0 ? 0 : arr == 1 ? S::kVOff : arr == 2 ? S::kKsOff : S::kVsOff) +
-                             (lane >> 2) * 16 * unit;
+                             (lane >> 2) * p.gran * unit;
         const bool copies = (lane >> 2) < 128 / p.gran;
         const uint64_t head_bytes = (uint64_t)page_size * unit;
         uint32_t slot = 0, ring = 0, filled = 0;
-#pragma unroll 1
-        while (walk.more()) {
-            const int key = walk.kb + walk.i * 128 + (lane >> 2) * 16;
-            const bool in = copies && key < walk.ke;
+        // a chunk's page, head and place in the page: read a chunk before they are used
+        int page = -1, head = 0;
+        uint32_t off = 0;
+        bool in = false;
+        auto next = [&]() {
+            const int key = walk.kb + walk.i * 128 + (lane >> 2) * p.gran;
+            in = copies && key < walk.ke;
             const uint32_t pg = (uint32_t)key / (uint32_t)page_size;
-            int page = -1;
+            head = walk.head;
+            off = (key - pg * page_size) * unit;
+            page = -1;
             if (in)
                 page = a.table[(int64_t)walk.r * a.width + pg];
+            if (++walk.i == walk.i1)
+                walk.next(p);
+        };
+        bool left = walk.more();
+        if (left)
+            next();
+#pragma unroll 1
+        while (left) {
             const bool have = in && page >= 0 && page < a.cache.pages;
             if (in && !have)
                 atomicCAS(p.status, kDevOk, kDevBadGroups);
+            const uint8_t *const from = src + ((uint64_t)(have ? page : 0) * H + head) * head_bytes + off;
+            left = walk.more();
+            if (left)
+                next();
             if (!wait(&bar.empty[slot], ring ^ 1))
                 break;
             const uint32_t pieces = __popc(__ballot_sync(kAll, have)) >> 2;
@@ -790,16 +807,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 mbar_arrive_expect_tx(&bar.full[slot], pieces * p.gran * (2 * S::kCode + 2 * S::kScale));
             __syncwarp();
             if (have)
-                bulk_load_at(dst + slot * S::kBytes,
-                             src + ((uint64_t)page * H + walk.head) * head_bytes + (uint64_t)(key - pg * page_size) * unit,
-                             p.gran * unit, &bar.full[slot]);
+                bulk_load_at(dst + slot * S::kBytes, from, p.gran * unit, &bar.full[slot]);
             ++filled;
             if (++slot == DEPTH) {
                 slot = 0;
                 ring ^= 1;
             }
-            if (++walk.i == walk.i1)
-                walk.next(p);
         }
         // (copies in flight land before the CTA's memory goes: fill f is phase f / DEPTH of its slot)
         for (uint32_t f = filled > DEPTH ? filled - DEPTH : 0; f < filled; ++f)
@@ -833,35 +846,49 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         __threadfence();
         if (tid == 0)
             atomicExch(p.counter + f.c0, 0);
-        // a thread takes 8 dimensions of a row
-#pragma unroll 1
-        for (int u = tid; u < 128 * (D / 8); u += S::kThreads) {
-            const int row = u & 127, ch = u >> 7, ri = f.row0 + row;
-            if (row >= f.rows)
-                continue;
-            float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-#pragma unroll 2
-            for (int k = f.c0; k <= f.c1; ++k) {
-                const float4 *const d = reinterpret_cast<const float4 *>(p.part + (2 * k + (k == f.c0 ? 1 : 0)) * S::kPart);
-                const float2 ml = __ldcg(reinterpret_cast<const float2 *>(d + (D / 4) * 128) + row);
-                const float4 x0 = __ldcg(d + 2 * ch * 128 + row), x1 = __ldcg(d + (2 * ch + 1) * 128 + row);
-                const float top = fmaxf(m, ml.x);
-                const float fa = m == -INFINITY ? 0.f : ex2(m - top), fb = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
-                const float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-                l = l * fa + ml.y * fb;
-                m = top;
+        // a thread takes every third 8 dimensions of a row
+        constexpr int kThird = 3, kPieces = (D / 8 + kThird - 1) / kThird;
+        const int row = tid & 127, ch0 = tid >> 7, ri = f.row0 + row;
+        if (ch0 >= kThird || row >= f.rows)
+            continue;
+        float y[kPieces][8], m = -INFINITY, l = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    y[i] = y[i] * fa + x[i] * fb;
+        for (int i = 0; i < 8 * kPieces; ++i)
+            y[i / 8][i % 8] = 0.f;
+#pragma unroll 1
+        for (int k = f.c0; k <= f.c1; ++k) {
+            const float4 *const d = reinterpret_cast<const float4 *>(p.part + (2 * k + (k == f.c0 ? 1 : 0)) * S::kPart);
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(d + (D / 4) * 128) + row);
+            float4 x[kPieces][2];
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int ch = min(ch0 + kThird * i, D / 8 - 1);
+                x[i][0] = __ldcg(d + 2 * ch * 128 + row), x[i][1] = __ldcg(d + (2 * ch + 1) * 128 + row);
             }
-            const int64_t at = (int64_t)(f.q0 + ri / G) * a.heads + f.head * G + ri % G;
-            const float inv = inverse(l);
-            reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at * D)[ch] =
-                make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                           pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
-            if (a.lse && ch == 0)
-                a.lse[at] = log_sum(m, l);
+            const float top = fmaxf(m, ml.x);
+            const float fa = m == -INFINITY ? 0.f : ex2(m - top), fb = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+            l = l * fa + ml.y * fb;
+            m = top;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const float z[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[i][e] = y[i][e] * fa + z[e] * fb;
+            }
         }
+        const int64_t at = (int64_t)(f.q0 + ri / G) * a.heads + f.head * G + ri % G;
+        const float inv = inverse(l);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int ch = ch0 + kThird * i;
+            if (ch < D / 8)
+                reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + at * D)[ch] =
+                    make_uint4(pack_bf16(y[i][0] * inv, y[i][1] * inv), pack_bf16(y[i][2] * inv, y[i][3] * inv),
+                               pack_bf16(y[i][4] * inv, y[i][5] * inv), pack_bf16(y[i][6] * inv, y[i][7] * inv));
+        }
+        if (a.lse && ch0 == 0)
+            a.lse[at] = log_sum(m, l);
     }
 }
 
@@ -887,7 +914,10 @@ size_t kv_attention_tile_part_bytes(int32_t head_dim) { return (size_t)128 * (he
 cudaError_t launch_kv_attention_tile(const AttnParams &p, cudaStream_t st)
 {
     AttnParams t = p;
-    t.gran = p.a.cache.page_size % 128 == 0 ? 128 : 16;
+    // the longest piece that never crosses a page: a power of two that divides it
+    // (a copy costs its thread some 100 clocks, whatever its size)
+    const int page = p.a.cache.page_size, pow2 = page & -page;
+    t.gran = pow2 < 128 ? pow2 : 128;
     const bool wide = p.a.cache.head_dim == 128;
     if (p.a.cache.fmt == RFQ_FMT_HIF4)
         return wide ? launch<RFQ_FMT_HIF4, 128>(t, st) : launch<RFQ_FMT_HIF4, 64>(t, st);
