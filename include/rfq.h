@@ -604,9 +604,11 @@ RFQ_API rfq_status rfq_kv_read(const rfq_kv_cache *cache, const int64_t *slots, 
  * `heads` query heads of head_dim (whatever the lengths and requests). */
 RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim);
 
-/* Attention over the paged 4-bit cache, in one launch:
+/* Attention over the paged 4-bit cache:
  *     o = softmax(scale q k^T) v
- * for the last tokens of every request over its cached keys (causal).
+ * for the last tokens of every request over its cached keys (causal).  One
+ * launch, or two where q_start lets a request have more than 32 rows (new
+ * tokens times heads / cache->heads): those go through a kernel of their own.
  *   q: device bf16 [tokens][heads][head_dim], strides in elements (multiples
  *     of 8).  heads is a multiple of cache->heads: query head i reads key head
  *     i / (heads / cache->heads).
@@ -627,7 +629,10 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * the tensor cores exactly, q as f16 scaled by a power of two per row, and the
  * softmax weights rounded to f16.  Values whose block scale lies more than
  * 2^24 below the largest of the same head and dimensions in that request are
- * taken as zero.  q must be finite.  The same inputs give the same bits.
+ * taken as zero, and so are keys with the smallest E8M0 scale (byte 0,
+ * 2^-127); a request with more than 32 rows may lose of a key what lies 2^-33
+ * below the largest key scale of its head.  q must be finite.  The same inputs
+ * give the same bits.
  * Lengths past table_width pages, rows outside q and pages outside the cache
  * set the device status RFQ_ERR_SHAPE (rfq_workspace_status); such requests'
  * rows are unspecified.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT.
@@ -649,7 +654,8 @@ RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64
  *   y: device [rows][wq->rows], fp32 or bf16 by out_dtype.
  * Products and sums are fp32; W~ enters the tensor cores exactly and x as f16
  * scaled by a power of two per row and stretch of k, which keeps every bf16
- * bit down to 2^-28 of the stretch's maximum.  The same inputs give the same
+ * bit down to 2^-28 of the stretch's maximum; blocks of W~ with the smallest
+ * E8M0 scale (byte 0, 2^-127) count as zero.  The same inputs give the same
  * bits.  Should a bounded wait run out, y is NaN.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
  * RFQ_ERR_UNSUPPORTED (other formats), RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
