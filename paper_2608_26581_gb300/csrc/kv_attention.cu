@@ -870,7 +870,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     if (!ok && lane == 0) {
         // (what this warp still copies must land before the CTA's memory goes)
         for (int i = 0; i < DEPTH; ++i)
-            mbar_wait(&s_full[warp][i], i < slot ? parity : parity ^ 1, limit);
+            mbar_wait(&s_full[warp][i], i < slot ? parity : parity ^ 1, kWaitLimitNs);
         atomicExch(p.status, kDevTimeout);
     }
 }

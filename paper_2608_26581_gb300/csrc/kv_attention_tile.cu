@@ -254,17 +254,17 @@ __device__ __noinline__ bool wait_on(uint32_t b, uint32_t parity)
 {
     const Bars &bar = *reinterpret_cast<const Bars *>(smem_raw);
     const uint64_t t0 = globaltimer_ns();
-    for (uint32_t i = 1;; ++i) {
+    for (;;) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\t"
                      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
                      "selp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done)
-                     : "r"(b), "r"(parity), "r"(2000u)             // (asleep for at most this many ns)
+                     : "r"(b), "r"(parity), "r"(1000u)             // (asleep for at most this many ns)
                      : "memory");
         if (done)
             return true;
-        if ((i & 63) == 0 && (globaltimer_ns() - t0 > bar.limit || *reinterpret_cast<const volatile int32_t *>(&bar.abort)))
+        if (globaltimer_ns() - t0 > bar.limit || *reinterpret_cast<const volatile int32_t *>(&bar.abort))
             return false;
     }
 }
@@ -757,7 +757,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         }
         if (lane == 0) {
             tc_commit(&bar.drain);           // (all of them, before TMEM goes back)
-            mbar_wait(&bar.drain, 0, bar.limit);
+            mbar_wait(&bar.drain, 0, kWaitLimitNs);
         }
     } else {
         // ------------------------------------------------ copies
@@ -791,6 +791,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 walk.next(p);
         };
         bool left = walk.more();
+        if (left && !__all_sync(kAll, held_start_wait(p.status, bar.limit))) {
+            *reinterpret_cast<volatile int32_t *>(&bar.abort) = 1;
+            left = false;
+        }
         if (left)
             next();
 #pragma unroll 1
@@ -818,7 +822,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         }
         // (copies in flight land before the CTA's memory goes: fill f is phase f / DEPTH of its slot)
         for (uint32_t f = filled > DEPTH ? filled - DEPTH : 0; f < filled; ++f)
-            mbar_wait(&bar.full[f % DEPTH], (f / DEPTH) & 1, bar.limit);
+            mbar_wait(&bar.full[f % DEPTH], (f / DEPTH) & 1, kWaitLimitNs);
     }
     tc_fence_before();
     __syncthreads();

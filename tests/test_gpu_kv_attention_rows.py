@@ -108,6 +108,29 @@ def test_same_bits_twice_and_workspace_reuse():
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@FMTS
+def test_a_wait_that_runs_out(fmt):
+    """The held start (word 2 set, word 3 zero) keeps the copies from starting:
+    every wait of the kernel ends at its limit, none of its copies or MMAs in
+    flight.  The status tells, the rows are NaN, and once the words are cleared
+    the workspace serves the next call."""
+    c = Case(fmt, 128, 2, 4, 16, [3000, 100], new=[100, 30], seed=13)
+    ws = rfq.kv_attention_workspace(8, 128)
+    words = ws[:4]
+    words[1] = 20000
+    words[2] = 1
+    q, out = bits_to_dev(c.qb), torch.zeros(c.qb.shape, dtype=torch.bfloat16, device=DEV)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    rfq.rfq_kv_attention(q, c.cache, c.table, i32(c.lens), out, ws, q_start=i32(c.start))
+    assert rfq.rfq_workspace_status(ws) == rfq.RFQ_ERR_TIMEOUT
+    assert torch.isnan(out.float()).all()
+    words.zero_()
+    c.check(ws=ws)
+    words[2] = 1                      # an open gate
+    words[3] = 1
+    c.check(ws=ws)
+
+
 def test_bad_device_sizes_set_the_status():
     c = Case(ref.FMT_MXFP4, 64, 1, 2, 16, [150, 30], new=[60, 40], seed=12, poison=False)
     q = bits_to_dev(c.qb)
