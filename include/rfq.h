@@ -630,9 +630,9 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * softmax weights rounded to f16.  Values whose block scale lies more than
  * 2^24 below the largest of the same head and dimensions in that request are
  * taken as zero, and so are keys with the smallest E8M0 scale (byte 0,
- * 2^-127); a request with more than 32 rows may lose of a key what lies 2^-33
- * below the largest key scale of its head.  q must be finite.  The same inputs
- * give the same bits.
+ * 2^-127) or, for a request with more than 32 rows, with a scale more than 2^24
+ * below the largest key scale of the same head and request.  q must be finite.
+ * The same inputs give the same bits.
  * Lengths past table_width pages, rows outside q and pages outside the cache
  * set the device status RFQ_ERR_SHAPE (rfq_workspace_status); such requests'
  * rows are unspecified.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT and

@@ -8,8 +8,9 @@
 //   Q: scaled by a power of two per row (maximum in [2^14, 2^15)): exact down
 //      to 2^-28 of the maximum, off by less than 2^-39 of it below.
 //   K: codes times scale relative to a running power of two, exact while the
-//      scales span less than 2^24 over the keys seen so far; smaller ones lose
-//      less than 2^-33 of the largest scale.
+//      scales span less than 2^24 over the keys seen so far; what lies below
+//      counts as zero (a score is then off by what its fp32 sum is off by
+//      beside a key of the largest scale).
 //   P: exp2(s - m) rounded to f16 (relative 2^-11; its sum l stays fp32); m is
 //      raised only when a score passes it by 8, which f16 has room for.
 //   V: as K, the power of two per 32 dimensions.

@@ -74,9 +74,8 @@ def test_scales_span_many_octaves(fmt):
 
 @FMTS
 def test_keys_span_many_octaves(fmt):
-    """Keys 2^12 apart in one tile and between tiles: a score is off by less
-    than 2^-33 of the largest key scale times the query, far inside the bound
-    on fp32 scores.  (Queries that make the largest score some tens.)"""
+    """Keys 2^12 apart in one tile and between tiles, which f16 holds exactly
+    beside the largest scale."""
     rng = np.random.default_rng(8)
     c = Case(fmt, 64, 1, 2, 16, [500], new=[60], seed=8)
     k = rng.standard_normal((500, 1, 64)) * 2.0 ** rng.integers(-12, 1, (500, 1, 1))
