@@ -25,7 +25,7 @@
 // gives the same bits every time.
 //
 // Measured, MXFP4: 1 x 4096 x 24576 12.6 us, 4.2 TB/s, 62% of the copy rate;
-// 8 x 5120 x 13824 14.5 us; 32 rows 37 us; 13 x 12288 x 4096 in HiF4 23 us.
+// 8 x 5120 x 13824 14.5 us; 32 rows 30 us; 13 x 12288 x 4096 in HiF4 18.4 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -62,8 +62,11 @@ struct Shape {
     static constexpr int kBlockX = MP * 64;  // bytes of a block of 32 codes' x: [row][4][16 bytes]
     static constexpr int kStepX = kStepK / 32 * kBlockX;
     static constexpr int kZero = MP < 8 ? kStepX : 0;              // zeros that the other blocks' columns read
-    // bytes of x in shared memory: rings of at least 6 KB a warp fit beside it
-    static constexpr int kMaxX = 80 * 1024;
+    // bytes of x in shared memory: with several column tiles all that leaves
+    // rings of two steps (a second phase costs more than the deeper rings give:
+    // 13 x 12288 x 4096, HiF4, 18.9 us with 12 steps of x, 22.7 with 9)
+    static constexpr int kMaxX = kNt > 1 ? kSmemBytes - 1024 - (kWarps + kTiles) * kPart - 2 * kWarps * kStepBytes
+                                         : 80 * 1024;
 };
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4])
@@ -264,8 +267,9 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
             }
         };
         // (loops, not unrolled: a short kernel pays for every line of code it
-        // fetches)
-        constexpr int kAhead = MP < 4 ? 1 : 2;
+        // fetches; four rows in flight where there are many, 32 x 5120 x 13824
+        // 30.3 us against 31.9 with two)
+        constexpr int kAhead = MP < 4 ? 1 : MP < 16 ? 2 : 4;
         const int tasks = nb * M;
 #pragma unroll 1
         for (int i = warp; i < tasks; i += kAhead * kWarps) {
