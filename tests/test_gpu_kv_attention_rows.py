@@ -61,6 +61,13 @@ def test_many_requests():
     Case(ref.FMT_MXFP4, 64, 1, 1, 16, rng.integers(0, 300, 60).tolist(), new=new, seed=6).check()
 
 
+def test_many_requests_some_of_many_tiles():
+    """More requests than a CTA's warps take one by one, among them some with
+    more tiles than one lane counts."""
+    new = [1, 0, 300, 2, 9] * 10
+    Case(ref.FMT_HIF4, 64, 2, 4, 32, [(17 * i) % 420 for i in range(50)], new=new, seed=14).check()
+
+
 @FMTS
 def test_scales_span_many_octaves(fmt):
     """Values, and with them the running powers of two, grow and fall by 2^20
