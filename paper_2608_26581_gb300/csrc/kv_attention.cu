@@ -11,8 +11,10 @@
 //      (HiF4) dimensions: nothing is rounded.
 //   q: made f16 by a power of two per row (maximum in [2^14, 2^15)): exact
 //      down to 2^-28 of the maximum, off by less than 2^-39 of it below.
-//   P: exp2(s - m) rounded to f16 (relative 2^-11; its sum l stays fp32); m
-//      is raised only when a score passes it by 8, which f16 has room for.
+//   P: exp2(s - m) rounded to f16 (its sum l stays fp32), m 7 below the
+//      maximum when it is set and raised only when a score passes it by 15:
+//      weights down to 2^-21 of the largest are off by 2^-11 of themselves,
+//      smaller ones by 2^-32 of the largest.
 //   V: codes times scale relative to a running power of two, exact in f16
 //      while the scales of one 32-dimension block span less than 2^24 over
 //      the keys seen so far; smaller ones fade out.
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    raise |= fmaxf(fmax3(s[0][t][j], s[0][t][j + 2], s[HV - 1][t][j]), s[HV - 1][t][j + 2]) > z.m[t][j] + 8.f;
+                    raise |= fmaxf(fmax3(s[0][t][j], s[0][t][j + 2], s[HV - 1][t][j]), s[HV - 1][t][j + 2]) > z.m[t][j] + kRoom;
             if (__any_sync(kAll, raise)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -564,7 +566,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(kAll, mx, 16));
-                        mx = fmaxf(mx, z.m[t][j]);
+                        mx = fmaxf(mx - kBelow, z.m[t][j]);
                         const float f = z.m[t][j] == -INFINITY ? 0.f : ex2(z.m[t][j] - mx);
                         z.m[t][j] = mx;
                         z.l[t][j] *= f;

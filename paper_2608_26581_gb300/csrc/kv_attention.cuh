@@ -16,6 +16,12 @@ namespace rfq {
 
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
+// The reference m of a row's weights exp2(s - m), which are held in f16 (up to
+// 2^16, all 11 bits down to 2^-14, multiples of 2^-24 below): kBelow octaves
+// below the maximum when it is set, so that f16's range serves the small weights,
+// and raised when a score passes it by more than kRoom.
+constexpr float kBelow = 7.f, kRoom = 15.f;
+
 __device__ __forceinline__ float ex2(float x)
 {
     float r;

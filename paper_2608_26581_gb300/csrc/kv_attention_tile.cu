@@ -11,8 +11,10 @@
 //      scales span less than 2^24 over the keys seen so far; what lies below
 //      counts as zero (a score is then off by what its fp32 sum is off by
 //      beside a key of the largest scale).
-//   P: exp2(s - m) rounded to f16 (relative 2^-11; its sum l stays fp32); m is
-//      raised only when a score passes it by 8, which f16 has room for.
+//   P: exp2(s - m) rounded to f16 (its sum l stays fp32), m 7 below the maximum
+//      when it is set and raised only when a score passes it by 15: weights down
+//      to 2^-21 of the largest are off by 2^-11 of themselves, smaller ones by
+//      2^-32 of the largest.
 //   V: as K, the power of two per 32 dimensions.
 //
 // Work: the (request, key head, 128 rows) segments laid end to end in chunks
@@ -233,7 +235,7 @@ __device__ __forceinline__ float row_weights(uint32_t s_at, uint32_t p_at, float
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             float e0, e1;
-            // (the product is rounded, as the maximum is: none passes it)
+            // (the product is rounded, as the maximum is)
             mul2(e0, e1, __uint_as_float(x[i]), __uint_as_float(x[i + 1]), c);
             add2(e0, e1, -m, -m);
             e0 = ex2(e0), e1 = ex2(e1);
@@ -372,10 +374,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 const float mx = whole ? row_max<true>(s_at, 0, 0) : row_max<false>(s_at, lo - key0, hi - key0);
                 const float top = mx == -INFINITY ? mx : mx * c;
                 float f = 1.f;
-                const bool raise = top > m + 8.f;
+                const bool raise = top > m + kRoom;
                 if (raise) {
-                    f = m == -INFINITY ? 0.f : ex2(m - top);
-                    m = top;
+                    f = m == -INFINITY ? 0.f : ex2(m - (top - kBelow));
+                    m = top - kBelow;
                     l *= f;
                 }
                 const float m0 = m == -INFINITY ? 0.f : m;
