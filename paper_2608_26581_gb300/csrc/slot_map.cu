@@ -99,14 +99,17 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
     const int r0 = min(R, tid * per), r1 = min(R, r0 + per);
     Sums own = {0, 0, 0};
     bool bad = false;
+    uint32_t fit = 0;                         // which of them fit
+    static_assert(kSlotMapRequests <= 32 * kThreads, "a bit for each of a thread's requests");
     for (int r = r0; r < r1; ++r) {
         const Request q(a, r);
         bad |= !q.fits;
+        fit |= (uint32_t)q.fits << (r - r0);
         own = own + q.sums();
         s_cached[r] = q.cached;
         s_p0[r] = q.p0;
         s_p1[r] = q.fits ? q.p1 : q.p0;
-        s_nth[r] = q.fits ? q.added : INT32_MIN;     // (until the sums are known)
+        s_nth[r] = q.added;                  // (until the sums are known)
     }
     const Sums inc = warp_scan(own, lane);
     if (lane == 31)
@@ -127,8 +130,8 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
     bad |= (int)count != given || count + all.back > (uint32_t)a.free_capacity || all.tok > (unsigned long long)a.tokens;
     uint32_t taken = 0;
     for (int r = r0; r < r1; ++r) {
-        const bool fits = s_nth[r] != INT32_MIN;
-        const int added = fits ? s_nth[r] : __ldcg(a.added + r);
+        const bool fits = fit >> (r - r0) & 1u;
+        const int added = s_nth[r];
         const uint32_t p0 = s_p0[r], p1 = s_p1[r], need = p1 > p0 ? p1 - p0 : 0u;
         const bool served = fits && (need == 0 || at.need + need <= top);
         s_start[r] = (int32_t)min(at.tok, (unsigned long long)INT32_MAX);
