@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
     extern __shared__ int32_t smem[];
     __shared__ Sums s_warp[kWarps];
     __shared__ uint32_t s_taken;
+    static_assert(sizeof(s_warp) + sizeof(s_taken) <= 1024, "beside 47 KB of dynamic shared memory");
     const int R = a.requests, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t *const s_start = smem;            // [R + 1] first token of each request
     int32_t *const s_cached = s_start + R + 1;
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) slot_map_kernel(const SlotMapArgs a)
 cudaError_t launch_slot_map(const SlotMapArgs &a, cudaStream_t st)
 {
     const size_t smem = (6 * (size_t)a.requests + 1) * sizeof(int32_t);
-    if (smem > 48 * 1024)
+    if (smem > 47 * 1024)                    // (of 48 KB; the kernel's own arrays take some of it)
         if (cudaError_t e = cudaFuncSetAttribute(slot_map_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  (6 * kSlotMapRequests + 1) * (int)sizeof(int32_t)))
             return e;
