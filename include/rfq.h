@@ -490,8 +490,8 @@ RFQ_API rfq_status rfq_dequant(const rfq_qtensor *q, void *out, int32_t out_dtyp
  *      request whose pages are not all there, and every later one that wants
  *      any, gets none: it is not served.  Requests that want none are served.
  *      A request whose pages exceed table_width (or whose cached is negative
- *      or exceeds it) is not served either, takes and gives nothing, and the
- *      device status becomes RFQ_ERR_SHAPE.
+ *      or exceeds it, or whose after passes int32) is not served either, takes
+ *      and gives nothing, and the device status becomes RFQ_ERR_SHAPE.
  *   3. block_table (device int32 [requests][table_width], in place) gets the
  *      pages taken; free_out the stack's new height; lengths [requests] after,
  *      or cached where a request was not served.

@@ -66,7 +66,7 @@ struct Request {
         after = added >= 0 ? c + (uint32_t)added : c > (uint32_t)-(int64_t)added ? c - (uint32_t)-(int64_t)added : 0u;
         p0 = c / page + (c % page != 0);
         p1 = after / page + (after % page != 0);
-        fits = cached >= 0 && p0 <= (uint32_t)a.width && p1 <= (uint32_t)a.width;
+        fits = cached >= 0 && after <= (uint32_t)INT32_MAX && p0 <= (uint32_t)a.width && p1 <= (uint32_t)a.width;
     }
     __device__ __forceinline__ Sums sums() const
     {
