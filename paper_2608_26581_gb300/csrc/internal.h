@@ -309,6 +309,31 @@ int resident_blocks_per_sm(const void *kern, int threads, size_t smem);
 // Number of SMs of the current device (cached).
 int num_sms();
 
+// A value kept for each device: here() is the current one's (check_device has
+// seen that there are no more than these).
+template <typename T>
+struct PerDevice {
+    T of[64];
+    T &here()
+    {
+        int dev = 0;
+        cudaGetDevice(&dev);
+        return of[dev & 63];
+    }
+};
+
+// Allows a kernel `bytes` of dynamic shared memory on the current device, once
+// (`allowed`: the caller's, zero at first; two threads may both set it).
+inline cudaError_t allow_smem(const void *kern, int bytes, PerDevice<bool> &allowed)
+{
+    bool &done = allowed.here();
+    if (done)
+        return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    done = e == cudaSuccess;
+    return e;
+}
+
 // Launches a kernel that calls wait_for_previous() (ptx.cuh) before it touches
 // global memory: its blocks may start while the last ones of the kernel before
 // it in the stream still run, so short kernels of one step follow each other

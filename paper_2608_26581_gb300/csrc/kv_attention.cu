@@ -886,13 +886,9 @@ cudaError_t launch(AttnParams p, cudaStream_t st)
 {
     using S = Shape<FMT, D, NT>;
     static_assert(S::kSmem <= 226 * 1024, "fits an SM");
-    static bool ready = false;     // (per instantiation; setting it twice is harmless)
-    if (!ready) {
-        if (cudaError_t e = cudaFuncSetAttribute(kv_attention_kernel<FMT, D, NT>,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem))
-            return e;
-        ready = true;
-    }
+    static PerDevice<bool> allowed;
+    if (cudaError_t e = allow_smem(reinterpret_cast<const void *>(kv_attention_kernel<FMT, D, NT>), S::kSmem, allowed))
+        return e;
     p.gran = p.a.cache.page_size % S::kChunk == 0 ? S::kChunk : 16;
     return launch_early(kv_attention_kernel<FMT, D, NT>, dim3(num_sms()), S::kThreads, S::kSmem, st, 1, p);
 }

@@ -906,13 +906,9 @@ cudaError_t launch(const AttnParams &p, cudaStream_t st)
 {
     using S = Tile<FMT, D>;
     static_assert(S::kSmem <= 226 * 1024, "fits an SM");
-    static bool ready = false;     // (per instantiation; setting it twice is harmless)
-    if (!ready) {
-        if (cudaError_t e = cudaFuncSetAttribute(kv_attention_tile_kernel<FMT, D>,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem))
-            return e;
-        ready = true;
-    }
+    static PerDevice<bool> allowed;
+    if (cudaError_t e = allow_smem(reinterpret_cast<const void *>(kv_attention_tile_kernel<FMT, D>), S::kSmem, allowed))
+        return e;
     return launch_early(kv_attention_tile_kernel<FMT, D>, dim3(num_sms()), S::kThreads, S::kSmem, st, 1, p);
 }
 

@@ -573,8 +573,11 @@ constexpr int kRowClocks = 25, kClusterClocks = 1000, kPhaseClocks = 3000;
 template <int FMT, int MP>
 int clusters_at_once(int split)
 {
-    static int known[4];           // by log2(split), 0: not asked yet
-    int &n = known[split == 1 ? 0 : split == 2 ? 1 : split == 4 ? 2 : 3];
+    struct Counts {
+        int n[4];                  // by log2(split), 0: not asked yet
+    };
+    static PerDevice<Counts> known;
+    int &n = known.here().n[split == 1 ? 0 : split == 2 ? 1 : split == 4 ? 2 : 3];
     if (n == 0) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(split, num_sms());
@@ -623,13 +626,9 @@ cudaError_t launch(const MatvecArgs &a, cudaStream_t st)
     const int steps = (int)((K + S::kStepK - 1) / S::kStepK);
     const int step_x = S::kStepX + MP * 4;                         // shared bytes of x a step
     const int most = S::kMaxX / step_x;
-    static bool ready = false;     // (per instantiation; setting it twice is harmless)
-    if (!ready) {
-        if (cudaError_t e = cudaFuncSetAttribute(matvec_kernel<FMT, MP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 kSmemBytes))
-            return e;
-        ready = true;
-    }
+    static PerDevice<bool> allowed;
+    if (cudaError_t e = allow_smem(reinterpret_cast<const void *>(matvec_kernel<FMT, MP>), kSmemBytes, allowed))
+        return e;
     const int split = split_of<FMT, MP>(tiles, steps, most, a.M);
     const int nb = (steps + split - 1) / split, phase = nb < most ? nb : most;
     int64_t groups = clusters_at_once<FMT, MP>(split);
