@@ -332,7 +332,7 @@ __device__ __forceinline__ int owner(const Share &s, uint32_t u)
 // (m + log2 l) in nats: -inf for a row that saw no key, NaN for one whose wait ran out
 __device__ __forceinline__ float log_sum(float m, float l)
 {
-    return l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : l == 0.f ? -INFINITY : l;
+    return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 // 1 / l, 0 for a row that saw no key (and NaN for one whose wait ran out)
 __device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }
