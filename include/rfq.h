@@ -639,7 +639,7 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * rows are unspecified.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT and
  * leaves NaN in the rows of out and lse that it concerns; int32 word 1 of the workspace is its
  * limit as for rfq_linear, and words 2 and 3 hold the start of the kernel for
- * more than 32 rows.
+ * more than 32 rows (of both in the debug build).
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
  * RFQ_ERR_UNSUPPORTED, RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
 RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t tokens,

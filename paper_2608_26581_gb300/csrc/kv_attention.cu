@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     walk.next(p);
     ahead = walk;
     const uint64_t limit = ws_wait_limit_ns(p.status);
-    bool ok = true;                          // no wait has run out
+    bool ok = true;                          // no wait of this warp has run out
 
     // ---- copies: chunk ahead.i of segment `ahead` into slot fslot of this
     // warp's ring.  Lane (h, array), h < 32 / gran, copies keys 16 h .. of one
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     int slot = 0, warm = DEPTH - 1;          // chunks to copy before the first is computed
     uint32_t parity = 0;
     bool fresh = true, loaded = false;       // a segment begins; its rows of q are on their way
-    bool begins = false;
+    bool begins = walk.i == 0;
     Request q = {0, 0, 0};
     int row0 = 0, rows = 0;
     uint4 raw[NB];                           // eight of them, as they come and then as f16
@@ -334,8 +334,13 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     int hi[NT][2];                           // keys that the thread's two rows see: [max(0, hi - window), hi)
     int all_hi = 0, all_lo = 0, least = 0;   // every row sees [all_lo, all_hi), none a key below least
     int vref = -1000;                        // V scale exponents are relative to it (the same in a row's quad)
+#ifdef RFQ_DEBUG_BOUNDS
+    // (the held start, by which a test makes a wait run out with nothing in flight,
+    // costs 0.3 us of a short request: the debug build alone has it)
+    ok = __all_sync(kAll, held_start_wait(p.status, limit));
+#endif
 #pragma unroll 1
-    while (walk.more()) {
+    while (ok && walk.more()) {
         // the segment's rows of q, on their way while chunks are copied (of one
         // row tile: more would take the registers)
         if (fresh && !loaded) {
@@ -416,8 +421,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
         // ---- one chunk
         {
             const int i = walk.i;
-            if (!mbar_wait(&s_full[warp][slot], parity, limit))
-                ok = false;
+            const bool here = mbar_wait(&s_full[warp][slot], parity, limit);
             const int key0 = walk.kb + i * kChunk;
             const uint8_t *const ring = s_ring + slot * S::kBytes;
             // ---- scores: s[h][t][j] is key 16 h + g + 8 (j / 2), row 8 t + 2 c + j % 2
@@ -551,13 +555,17 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                                 s[h][t][j] = -INFINITY;
                         }
             }
-            bool raise = false;
+            bool raise = !here;              // (one vote for both)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
                     raise |= fmaxf(fmax3(s[0][t][j], s[0][t][j + 2], s[HV - 1][t][j]), s[HV - 1][t][j + 2]) > z.m[t][j] + kRoom;
             if (__any_sync(kAll, raise)) {
+                if (!__all_sync(kAll, here)) {
+                    ok = false;
+                    break;
+                }
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -736,7 +744,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 x += __shfl_xor_sync(kAll, x, 4);
                 x += __shfl_xor_sync(kAll, x, 8);
                 x += __shfl_xor_sync(kAll, x, 16);
-                z.l[t][j] = ok ? x : __int_as_float(0x7FFFFFFF);
+                z.l[t][j] = x;
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -756,6 +764,46 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
             write(row0, rows, q.q0, walk.head);
         }
         walk.next(p);
+    }
+
+    // ---- a wait has run out: the warp copies nothing more and waits for nothing
+    // more, and its segments from this one on are NaN
+    if (!ok) {
+        if (warm == 0) {                     // (its copies in flight, of slots slot .. fslot, land before a part lies over them)
+            int i = slot;
+            do {
+                mbar_wait(&s_full[warp][i], parity, kWaitLimitNs);
+                if (++i == DEPTH) {
+                    i = 0;
+                    parity ^= 1;
+                }
+            } while (i != fslot);
+        }
+        if (lane == 0)
+            atomicExch(p.status, kDevTimeout);
+#pragma unroll 1
+        for (; walk.more(); walk.next(p), begins = true) {
+            const bool ends = walk.i1 == walk.chunks;
+            const float nan = __int_as_float(0x7FFFFFFF);
+            row0 = walk.tile * ROWS;
+            rows = min(ROWS, walk.q.n * G - row0);
+            if (!begins || !ends) {
+                const int k = begins ? 1 : 0;
+                for (int i = lane; i < S::kPart / 16; i += 32)
+                    reinterpret_cast<float4 *>(part_of(warp, k))[i] = make_float4(nan, nan, nan, nan);
+                if (lane == 0)
+                    s_info[warp][k] = {walk.u, walk.chunks, walk.head, row0, rows, walk.q.q0, begins, ends};
+            } else {
+                for (int i = lane; i < rows * D; i += 32) {
+                    const int ri = row0 + i / D;
+                    const int64_t at = (int64_t)(walk.q.q0 + ri / G) * a.heads + walk.head * G + ri % G;
+                    static_cast<__nv_bfloat16 *>(a.out)[at * D + i % D] = __float2bfloat16_rn(nan);
+                    if (a.lse && i % D == 0)
+                        a.lse[at] = nan;
+                }
+            }
+            walk.i = walk.i1;
+        }
     }
 
     // ---- join the parts: of one segment they follow each other in the order of the warps
@@ -868,12 +916,6 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                 }
             }
         }
-    }
-    if (!ok && lane == 0) {
-        // (what this warp still copies must land before the CTA's memory goes)
-        for (int i = 0; i < DEPTH; ++i)
-            mbar_wait(&s_full[warp][i], i < slot ? parity : parity ^ 1, kWaitLimitNs);
-        atomicExch(p.status, kDevTimeout);
     }
 }
 

@@ -1,11 +1,17 @@
 """Bounded waits of the serving kernels, made to run out on purpose: a held start
 keeps a kernel from issuing its first copy, so that its waits end at their limit
 with nothing in flight."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
+import serving_ref as ref
+from conftest import ROOT
 from gpu_util import DEV
-from paper_2608_26581_gb300 import rfq
+from paper_2608_26581_gb300 import _build, rfq
 from test_gpu_kv_attention import FMTS, Case, bits_to_dev
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +39,35 @@ def test_attention_tiles_leave_nan_in_both_outputs(fmt):
     assert status == rfq.RFQ_ERR_TIMEOUT
     assert torch.isnan(out.float()).all() and torch.isnan(lse).all()
     c.check(ws=ws)
+
+
+def _in_debug_build(code):
+    """Runs code against the debug build, whose kernels of few rows have a held start too."""
+    code = f"import sys\nsys.path[:0] = [{ROOT!r}, {os.path.join(ROOT, 'tests')!r}]\n" + code
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=900,
+                       env=dict(os.environ, RFQ_LIBRARY=_build.build(debug=True)))
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-3000:]
+
+
+def few_rows():
+    """Requests inside a warp's share, over many warps and CTAs, and without
+    keys.  The parts of those that are shared are joined all the same, so the
+    workspace serves the next call."""
+    lens = [3000, 100, 0, 20000, 17]
+    for fmt in (ref.FMT_MXFP4, ref.FMT_HIF4):
+        for D in (64, 128):
+            for new in (1, 4):
+                c = Case(fmt, D, 2, 4, 16, lens, new=[new] * len(lens), seed=14)
+                ws = rfq.kv_attention_workspace(8, D)
+                for _ in range(2):
+                    out, lse, status = _held(c, ws)
+                    assert status == rfq.RFQ_ERR_TIMEOUT
+                    assert torch.isnan(out.float()).all() and torch.isnan(lse).all()
+                    c.check(ws=ws, decode=False)
+                ws[2] = 1                 # an open gate
+                ws[3] = 1
+                c.check(ws=ws, decode=False)
+
+
+def test_attention_of_few_rows():
+    _in_debug_build("import test_gpu_serving_timeouts as t\nt.few_rows()\n")
