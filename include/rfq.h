@@ -660,7 +660,8 @@ RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64
  * scaled by a power of two per row and stretch of k, which keeps every bf16
  * bit down to 2^-28 of the stretch's maximum; blocks of W~ with the smallest
  * E8M0 scale (byte 0, 2^-127) count as zero.  The same inputs give the same
- * bits.  Should a bounded wait run out, y is NaN.
+ * bits.  Should a bounded wait run out, the sums that it concerns are NaN (the
+ * call has no workspace, and so no device status).
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
  * RFQ_ERR_UNSUPPORTED (other formats), RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
 RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows, const rfq_qtensor *wq, void *y,

@@ -29,6 +29,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
+#include <cstdlib>
 
 #include "internal.h"
 #include "kv_layout.cuh"
@@ -90,6 +91,9 @@ struct Params {
     int steps;             // along K
     int phase;             // steps of K at a time (what of x fits)
     int depth;             // of the rings
+#ifdef RFQ_DEBUG_BOUNDS
+    int hold_us;           // not 0: no box is copied, and a wait lasts this long
+#endif
 };
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
@@ -158,6 +162,19 @@ struct Scales {
     }
 };
 
+// Waits for a ring's boxes in flight, of slots `slot` to `end`: they land before
+// sums are laid over them and before the CTA's memory goes.
+__device__ __forceinline__ void let_land(uint64_t *full, int depth, int slot, uint32_t parity, int end, uint64_t limit)
+{
+    do {
+        mbar_wait(full + slot, parity, limit);
+        if (++slot == depth) {
+            slot = 0;
+            parity ^= 1;
+        }
+    } while (slot != end);
+}
+
 template <int FMT, int MP>
 __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_constant__ CUtensorMap wmap, const Params p)
 {
@@ -196,7 +213,16 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
         prefetch_tmap(&wmap);
     wait_for_previous();
     let_next_start();
-    bool ok = true;                                                // no wait has run out
+#ifdef RFQ_DEBUG_BOUNDS
+    const bool held = p.hold_us > 0;
+    const uint64_t limit = held ? p.hold_us * 1000ull : kWaitLimitNs;
+#else
+    constexpr bool held = false;
+    constexpr uint64_t limit = kWaitLimitNs;
+#endif
+    // No wait of this lane has run out.  One that has waits for nothing more, its
+    // sums are NaN from then on, and if it is lane 0 the warp copies nothing more.
+    bool ok = true;
     int slot = 0;                                                  // of the ring, and its phase
     uint32_t parity = 0;
 
@@ -210,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
         auto fetch = [&]() {
             if (left <= 0)
                 return;
-            if (lane == 0) {
+            if (lane == 0 && ok && !held) {
                 mbar_arrive_expect_tx(&s_full[warp][fslot], kStepBytes);
 #pragma unroll
                 for (int i = 0; i < BX; ++i)
@@ -363,8 +389,10 @@ __global__ void __launch_bounds__(kThreads, 1) matvec_kernel(const __grid_consta
 #pragma unroll
                 for (int j = 0; j < CB; ++j)
                     xat[t][j] = xbase[t][j] + step * xstep[j];
-            if (!mbar_wait(&s_full[warp][slot], parity, kWaitLimitNs))
+            if (ok && !mbar_wait(&s_full[warp][slot], parity, limit)) {
                 ok = false;
+                let_land(s_full[warp], p.depth, slot, parity, fslot, limit);
+            }
             float win[NT][4];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -642,7 +670,11 @@ cudaError_t launch(const MatvecArgs &a, cudaStream_t st)
     const bool mma = a.w.scale_layout == RFQ_SCALE_MMA;
     const Params p = {static_cast<const __nv_bfloat16 *>(a.x), a.x_row, a.M, (int)N, (int)K,
                       static_cast<const uint8_t *>(a.w.scales), mma, mma || K % 128 == 0, a.y, a.bf16,
-                      (int)tiles, steps, phase, depth};
+                      (int)tiles, steps, phase, depth,
+#ifdef RFQ_DEBUG_BOUNDS
+                      getenv("RFQ_DEBUG_HOLD_US") ? atoi(getenv("RFQ_DEBUG_HOLD_US")) : 0
+#endif
+    };
     CUtensorMap map;
     if (!encode_tmap_2d_u8(&map, a.w.codes, (uint64_t)K / 2, (uint64_t)N, (uint64_t)K / 2, kBoxK / 2, kTile, 128))
         return cudaErrorInvalidValue;

@@ -71,3 +71,28 @@ def few_rows():
 
 def test_attention_of_few_rows():
     _in_debug_build("import test_gpu_serving_timeouts as t\nt.few_rows()\n")
+
+
+def matvec():
+    """Of every number of rows, with K in one share, over a cluster, and in
+    phases of what of x fits; the next call is right."""
+    rng = torch.Generator(device=DEV)
+    rng.manual_seed(0)
+    for fmt in (rfq.RFQ_FMT_MXFP4, rfq.RFQ_FMT_HIF4):
+        for M, K, N in ((1, 512, 40), (2, 4096, 5000), (4, 12288, 300), (8, 2048, 700), (13, 12288, 300), (32, 12288, 130)):
+            w = rfq.empty_qtensor(fmt, rfq.RFQ_SCALE_MMA, N, K)
+            rfq.rfq_quantize_weight(torch.randn(K, N, generator=rng, device=DEV).bfloat16(), w)
+            x = torch.randn(M, K, generator=rng, device=DEV).bfloat16()
+            want, y = torch.empty(M, N, device=DEV), torch.zeros(M, N, device=DEV)
+            rfq.rfq_matvec(x, w, want)
+            os.environ["RFQ_DEBUG_HOLD_US"] = "2000"
+            rfq.rfq_matvec(x, w, y)
+            torch.cuda.synchronize()
+            del os.environ["RFQ_DEBUG_HOLD_US"]
+            assert torch.isnan(y).all()
+            rfq.rfq_matvec(x, w, y)
+            assert torch.isfinite(want).all() and torch.equal(y, want)
+
+
+def test_matvec():
+    _in_debug_build("import test_gpu_serving_timeouts as t\nt.matvec()\n")
