@@ -177,11 +177,10 @@ rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_hea
         table_width < 1 || window < 0 || q_token_stride < 0 || q_head_stride < 0 ||
         (!q_start && tokens != requests) || (int64_t)table_width * cache->page_size > INT32_MAX - 4096)
         return RFQ_ERR_SHAPE;
-    // (the kernel counts its units of work, 32 keys each, in 32 bits)
-    const double group = (double)heads / cache->heads;
+    // (the kernels count rows and units of work in 32 bits)
     if ((double)tokens * heads >= 2147483648.0 ||
-        ((double)requests + tokens * group / 8) * cache->heads * ((double)table_width * cache->page_size / 32 + 2) >=
-            4294967296.0)
+        kv_attention_most_units(tokens, heads / cache->heads, q_start != nullptr, requests, cache->heads,
+                                (int64_t)table_width * cache->page_size) >= 4294967296.0)
         return RFQ_ERR_SHAPE;
     if (!workspace || !(scale == scale) ||
         (tokens > 0 && requests > 0 && (!q || !out || !lengths || !block_table)))

@@ -286,6 +286,9 @@ struct KvAttentionArgs {
     void *workspace;
 };
 size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim);
+// Units of work that a kernel of the call may have to count, at most (`keys`: of a request).
+double kv_attention_most_units(int64_t tokens, int32_t group, bool q_start, int32_t requests, int32_t kv_heads,
+                               int64_t keys);
 cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st);
 
 // ---- matrix-vector products with 4-bit weights (matvec.cu)

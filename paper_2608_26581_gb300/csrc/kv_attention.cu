@@ -41,6 +41,7 @@
 // the latency of its dependent steps.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <algorithm>
 #include <cstdint>
 
 #include "kv_attention.cuh"
@@ -952,7 +953,30 @@ cudaError_t launch_rows(const AttnParams &p, int64_t rows, cudaStream_t st)
 // 55, 41 against 74).
 constexpr int kTileRows = 33;
 
+// The rows that a request of the call may have at most, as far as the host
+// knows: each request has one token at least, or the tiles may be left out all the same.
+int64_t most_rows(int64_t tokens, int32_t group, bool q_start, int32_t requests)
+{
+    return q_start ? (tokens - requests + 1) * group : group;
+}
+
 } // namespace
+
+double kv_attention_most_units(int64_t tokens, int32_t group, bool q_start, int32_t requests, int32_t kv_heads, int64_t keys)
+{
+    // A request of r rows has ceil(r / 8) tiles here (of 16 rows, fewer), or
+    // ceil(r / 128) there; a tile has a unit for each chunk of keys that is begun
+    // (the first key may lie inside one) and those of its start.
+    const double rows = (double)tokens * group, R = requests;
+    const double here = kv_heads * (keys / 32.0 + 2), there = kv_heads * (keys / (double)kTileChunk + 1 + kTileStart);
+    const bool tiles = most_rows(tokens, group, q_start, requests) >= kTileRows;
+    if (!q_start)
+        return tiles ? (R + rows / kTileRowsEach) * there : (R + rows / 8) * here;
+    if (!tiles)
+        return (R + rows / 8) * here;
+    const double few = std::min(R + rows / 8, R * ((kTileRows - 1 + 7) / 8));   // of requests below kTileRows rows
+    return std::max(few * here, (std::min(R, rows / kTileRows) + rows / kTileRowsEach) * there);
+}
 
 size_t kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
 {
@@ -975,8 +999,7 @@ cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)
     int64_t rows = a.q_start ? (a.tokens + a.requests - 1) / a.requests * p.group : p.group;
     // Only the device knows who has how many new tokens.  Where each request
     // has one at least and none can have kTileRows rows, the tiles have nothing to do.
-    const int64_t most = a.q_start ? (a.tokens - a.requests + 1) * p.group : p.group;
-    if (most >= kTileRows) {
+    if (most_rows(a.tokens, p.group, a.q_start != nullptr, a.requests) >= kTileRows) {
         p.least_rows = kTileRows;
         if (cudaError_t e = launch_kv_attention_tile(p, st))
             return e;

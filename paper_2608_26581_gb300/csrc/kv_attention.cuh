@@ -337,7 +337,9 @@ __device__ __forceinline__ float log_sum(float m, float l)
 // 1 / l, 0 for a row that saw no key (and NaN for one whose wait ran out)
 __device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }
 
-// kv_attention_tile.cu: the requests of p's row range, in tiles of 128 rows
+// kv_attention_tile.cu: the requests of p's row range, in tiles of 128 rows by
+// 128 keys; a segment's start counts as 3 units
+constexpr int kTileRowsEach = 128, kTileChunk = 128, kTileStart = 3;
 size_t kv_attention_tile_part_bytes(int32_t head_dim);
 cudaError_t launch_kv_attention_tile(const AttnParams &p, cudaStream_t st);
 

@@ -56,7 +56,7 @@ constexpr uint32_t kTmemCols = 512;          // S: 0, 128; O: 256; P: 384, 448
 
 template <int FMT, int D>
 struct Tile {
-    static constexpr int kRows = 128, kChunk = 128, kStart = 3, kThreads = 32 * kWarps, kDepth = 3;
+    static constexpr int kRows = kTileRowsEach, kChunk = kTileChunk, kStart = kTileStart, kThreads = 32 * kWarps, kDepth = 3;
     static constexpr int kScale = FMT == RFQ_FMT_HIF4 ? D / 16 : D / 32;   // bytes a token
     static constexpr int kCode = D / 2;
     static constexpr int kVOff = kChunk * kCode, kKsOff = 2 * kVOff, kVsOff = kKsOff + kChunk * kScale;

@@ -47,3 +47,21 @@ def test_matvec_on_each_device(fake, fmt, rows):
             (x, y, _, _, cluster, _), = fake.launches()[before:]
             # one wave of this device's clusters, where that many hold the tiles
             assert x == cluster and x * y <= sms
+
+
+def test_the_work_that_is_taken(fake):
+    """What the kernels can count is taken: prompts by tiles of 128 rows, tokens
+    by tiles of 8; more is refused."""
+    fake.device(0)
+    kv = rfq._KV(rfq.RFQ_FMT_MXFP4, 8, 128, 64, 2 ** 20, 256, 256, 256, 256)
+
+    def call(tokens, requests, q_start, keys, heads=64):
+        return fake.lib.rfq_kv_attention(256, heads * 128, 128, tokens, heads, q_start, 256, requests, ctypes.byref(kv), 256, keys // 64,
+                                         0.125, 0, 256, 256, 256, None)
+    assert call(131072, 1, 256, 131072) == rfq.RFQ_OK                 # a prompt of as many tokens
+    assert call(262144, 64, 256, 131072) == rfq.RFQ_OK                # many of 4096
+    assert call(1024, 1024, None, 2 ** 20) == rfq.RFQ_OK              # one token each of long requests
+    assert call(1024, 1024, None, 2 ** 20, heads=8 * 128) == rfq.RFQ_OK
+    assert call(131072, 1, 256, 2 ** 28) == rfq.RFQ_ERR_SHAPE
+    assert call(2 ** 15, 2 ** 15, None, 2 ** 20) == rfq.RFQ_ERR_SHAPE
+    assert call(2 ** 25, 1, 256, 64) == rfq.RFQ_ERR_SHAPE             # rows past 32 bits
