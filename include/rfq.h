@@ -607,14 +607,17 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
 /* Attention over the paged 4-bit cache:
  *     o = softmax(scale q k^T) v
  * for the last tokens of every request over its cached keys (causal).  One
- * launch, or two where q_start lets a request have more than 32 rows (new
- * tokens times heads / cache->heads): those go through a kernel of their own.
+ * launch, or two with q_start: requests with more than 32 rows (new tokens times
+ * heads / cache->heads) go through a kernel of their own, or if none can have as
+ * many, rows of no request do.
  *   q: device bf16 [tokens][heads][head_dim], strides in elements (multiples
  *     of 8).  heads is a multiple of cache->heads: query head i reads key head
  *     i / (heads / cache->heads).
  *   q_start: device int32 [requests + 1]: rows q_start[r] .. q_start[r + 1] of
  *     q are the last tokens of request r (their keys are in the cache), or
- *     NULL: one token a request (tokens == requests).
+ *     NULL: one token a request (tokens == requests).  Rows before q_start[0]
+ *     and from q_start[requests] on belong to no request (the spare rows of a
+ *     step of fixed size): they get o = 0 and lse = -inf.
  *   lengths: device int32 [requests]: keys of each request, its new tokens
  *     included.  Token i of n sees keys j <= length - n + i, and with
  *     window > 0 only j > length - n + i - window (window 0: all).  A row

@@ -183,7 +183,7 @@ rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_hea
                                 (int64_t)table_width * cache->page_size) >= 4294967296.0)
         return RFQ_ERR_SHAPE;
     if (!workspace || !(scale == scale) ||
-        (tokens > 0 && requests > 0 && (!q || !out || !lengths || !block_table)))
+        (tokens > 0 && (!out || (requests > 0 && (!q || !lengths || !block_table)))))
         return RFQ_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(q_start, 4) ||
         !aligned(lengths, 4) || !aligned(block_table, 4) || !aligned(lse, 4) ||
@@ -191,7 +191,7 @@ rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64_t q_hea
         return RFQ_ERR_ALIGNMENT;
     if ((s = check_device()) != RFQ_OK)
         return s;
-    if (tokens == 0 || requests == 0)
+    if (tokens == 0)
         return RFQ_OK;
     return from_cuda(launch_kv_attention({q, q_token_stride, q_head_stride, tokens, heads, q_start, lengths, requests,
                                           *cache, block_table, table_width, scale, window, out, lse, workspace},

@@ -920,6 +920,17 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
     }
 }
 
+// The rows of no request where no tile kernel runs to see to them: in the kernel
+// above, whatever is added costs 2 to 3% of a long request.
+constexpr int kRestThreads = 256;
+
+__global__ void __launch_bounds__(kRestThreads) kv_attention_rest_kernel(const KvAttentionArgs a)
+{
+    wait_for_previous();
+    let_next_start();
+    clear_rest(a, threadIdx.x, kRestThreads);
+}
+
 constexpr size_t kWsCounters = 256;
 
 size_t ws_parts_offset() { return kWsCounters + ((size_t)num_sms() * 4 + 255) / 256 * 256; }
@@ -996,10 +1007,9 @@ cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)
                     reinterpret_cast<float *>(ws + ws_parts_offset()),
                     0,
                     INT32_MAX};
-    int64_t rows = a.q_start ? (a.tokens + a.requests - 1) / a.requests * p.group : p.group;
     // Only the device knows who has how many new tokens.  Where each request
     // has one at least and none can have kTileRows rows, the tiles have nothing to do.
-    if (most_rows(a.tokens, p.group, a.q_start != nullptr, a.requests) >= kTileRows) {
+    if (a.requests > 0 && most_rows(a.tokens, p.group, a.q_start != nullptr, a.requests) >= kTileRows) {
         p.least_rows = kTileRows;
         if (cudaError_t e = launch_kv_attention_tile(p, st))
             return e;
@@ -1007,7 +1017,13 @@ cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)
         p.most_rows = kTileRows - 1;
         if (!a.q_start)
             return cudaSuccess;              // (every request has the same rows)
+    } else if (a.q_start) {
+        if (cudaError_t e = launch_early(kv_attention_rest_kernel, dim3(num_sms()), kRestThreads, 0, st, 1, a))
+            return e;
+        if (a.requests == 0)
+            return cudaSuccess;
     }
+    const int64_t rows = a.q_start ? (a.tokens + a.requests - 1) / a.requests * p.group : p.group;
     const bool wide = a.cache.head_dim == 128;
     if (a.cache.fmt == RFQ_FMT_HIF4)
         return wide ? launch_rows<RFQ_FMT_HIF4, 128>(p, rows, st) : launch_rows<RFQ_FMT_HIF4, 64>(p, rows, st);

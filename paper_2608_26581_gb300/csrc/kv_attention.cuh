@@ -334,6 +334,30 @@ __device__ __forceinline__ float log_sum(float m, float l)
 {
     return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
+// Rows of no request, before q_start[0] and from q_start[requests] on (a step of
+// fixed size has such): o = 0, lse = -inf, as for a row that sees no key.  A CTA's
+// share, by `threads` of its threads.
+__device__ __forceinline__ void clear_rest(const KvAttentionArgs &a, int thread, int threads)
+{
+    const int first = a.q_start[0], end = a.q_start[a.requests];
+    if (first < 0 || end < first || end > a.tokens)
+        return;                              // (the status says so)
+    const int64_t rest = first + (a.tokens - end);
+    const int row = a.heads * a.cache.head_dim / 8;
+#pragma unroll 1
+    for (int64_t i = blockIdx.x; i < rest; i += gridDim.x) {
+        const int64_t t = i < first ? i : end + (i - first);
+        uint4 *const out = static_cast<uint4 *>(a.out) + t * row;
+#pragma unroll 1
+        for (int j = thread; j < row; j += threads)
+            out[j] = make_uint4(0, 0, 0, 0);
+        if (a.lse)
+#pragma unroll 1
+            for (int j = thread; j < a.heads; j += threads)
+                a.lse[t * a.heads + j] = -INFINITY;
+    }
+}
+
 // 1 / l, 0 for a row that saw no key (and NaN for one whose wait ran out)
 __device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l; }
 

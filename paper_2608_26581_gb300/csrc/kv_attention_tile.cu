@@ -327,8 +327,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
     wait_for_previous();
     let_next_start();
     Share sh;
-    if (!find_share<S, false>(p, s_scan, kWarps, kLeast, sh))
+    if (!find_share<S, false>(p, s_scan, kWarps, kLeast, sh)) {
+        if (a.q_start)
+            clear_rest(a, tid, S::kThreads);
         return;
+    }
     if (tid == 0)
         bar.limit = ws_wait_limit_ns(p.status);
     // (TMEM only now: a kernel in front that is still to take its own has finished)
@@ -834,6 +837,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         tmem_dealloc(tmem, kTmemCols);
 
     // ---- the parts of segments that CTAs share (the first and the last of this one)
+    if (a.q_start && warp == kUnits)
+        clear_rest(a, lane, 32);
     const int nshared = s_nshared;
     if (nshared == 0)
         return;

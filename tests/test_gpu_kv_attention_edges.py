@@ -20,3 +20,40 @@ def test_a_table_for_many_keys(fmt, new):
     wide[:, :c.table.shape[1]] = c.table
     c.table = wide
     c.check()
+
+
+@FMTS
+@pytest.mark.parametrize("new", [[3, 0, 2], [40, 1, 30]])
+@pytest.mark.parametrize("before,after", [(0, 5), (2, 0), (700, 900)])
+def test_rows_of_no_request(fmt, new, before, after):
+    """Before the first request's and past the last one's: zeros, as for a row
+    that sees no key, and the requests' rows are what they are without them."""
+    c = Case(fmt, 64, 2, 2, 16, [100, 7, 60], new=new, seed=4)
+    T = before + sum(new) + after
+    q = torch.full((T, 4, 64), float("nan"), dtype=torch.bfloat16, device=DEV)
+    q[before:T - after] = bits_to_dev(c.qb)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    want, want_lse = c.run(decode=False)
+    for with_lse in (True, False):
+        out, lse = torch.full((T, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((T, 4), 7.0, device=DEV)
+        ws = rfq.kv_attention_workspace(4, 64)
+        rfq.rfq_kv_attention(q, c.cache, c.table, i32(c.lens), out, ws, lse=lse if with_lse else None, q_start=i32(c.start + before))
+        assert rfq.rfq_workspace_status(ws) == rfq.RFQ_OK
+        assert torch.equal(out[before:T - after], want)
+        for rest in (slice(0, before), slice(T - after, T)):
+            assert (out[rest] == 0).all()
+            assert (lse[rest] == (-float("inf") if with_lse else 7.0)).all()
+        if with_lse:
+            assert torch.equal(lse[before:T - after], want_lse)
+
+
+def test_no_request_at_all():
+    c = Case(ref.FMT_MXFP4, 64, 2, 2, 16, [20], seed=5)
+    q, out, lse = (torch.full(s, 7.0, dtype=d, device=DEV) for s, d in (((9, 4, 64), torch.bfloat16), ((9, 4, 64), torch.bfloat16), ((9, 4), torch.float32)))
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    for start in (0, 9):
+        out.fill_(7.0)
+        ws = rfq.kv_attention_workspace(4, 64)
+        rfq.rfq_kv_attention(q, c.cache, none.view(0, 3), none, out, ws, lse=lse, q_start=torch.full((1,), start, dtype=torch.int32, device=DEV))
+        assert rfq.rfq_workspace_status(ws) == rfq.RFQ_OK
+        assert (out == 0).all() and torch.isneginf(lse).all()
