@@ -631,11 +631,13 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * Scores, their maximum and sum and the accumulators are fp32; the codes enter
  * the tensor cores exactly, q as f16 scaled by a power of two per row, and the
  * softmax weights rounded to f16: by 2^-11 of themselves down to 2^-21 of the
- * row's largest, by 2^-32 of that one below.  Values whose block scale lies more than
- * 2^24 below the largest of the same head and dimensions in that request are
- * taken as zero, and so are keys with the smallest E8M0 scale (byte 0,
- * 2^-127) or, for a request with more than 32 rows, with a scale more than 2^24
- * below the largest key scale of the same head and request.  q must be finite.
+ * row's largest, by 2^-32 of that one below.  Values whose block scale lies
+ * 2^24 or more below the largest of the same head and dimensions in that request
+ * may count as zero (HiF4, for a request with up to 32 rows: as anything up to
+ * 2^-21 of the largest scale).  Keys with the smallest E8M0 scale (byte 0, 2^-127)
+ * count as zero and, for a request with more than 32 rows, so may those with a
+ * scale 2^24 or more below the largest key scale of the same head and request.
+ * q must be finite.
  * The same inputs give the same bits.
  * Lengths past table_width pages, rows outside q and pages outside the cache
  * set the device status RFQ_ERR_SHAPE (rfq_workspace_status); such requests'

@@ -17,7 +17,9 @@
 //      smaller ones by 2^-32 of the largest.
 //   V: codes times scale relative to a running power of two, exact in f16
 //      while the scales of one 32-dimension block span less than 2^24 over
-//      the keys seen so far; smaller ones fade out.
+//      the keys seen so far; smaller ones fade out (HiF4: but for their
+//      sub-group exponents, which make 2^-21 of the largest scale at most;
+//      taking those out as well costs 2% of a long request).
 //
 // Bound: HBM at long caches: 136 (MXFP4) or 144 (HiF4) bytes a key and head
 // of 128.  An SM's share of the measured copy rate is one of these every 5.8

@@ -57,3 +57,39 @@ def test_no_request_at_all():
         rfq.rfq_kv_attention(q, c.cache, none.view(0, 3), none, out, ws, lse=lse, q_start=torch.full((1,), start, dtype=torch.int32, device=DEV))
         assert rfq.rfq_workspace_status(ws) == rfq.RFQ_OK
         assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+@FMTS
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new", [1, 4, 40])
+def test_values_far_below_the_largest(fmt, D, new):
+    """Values 2^24 and more below the largest of their block's dimensions may
+    count as zero (HiF4 up to 32 rows: as up to 2^-21 of the largest scale);
+    those of other dimensions are what they are."""
+    c = Case(fmt, D, 1, 2, 16, [200], new=[new], seed=6)
+    rng = np.random.default_rng(6)
+    v = (rng.standard_normal((200, 1, D)) * 2.0 ** -30).astype(np.float32)
+    v[7] = 0
+    v[7, 0, 0] = 1000
+    if D == 128:
+        v[:, :, 64:] *= 2.0 ** 30
+    k = torch.zeros(200, 1, D, dtype=torch.bfloat16, device=DEV)       # every key weighs the same
+    slots = torch.tensor([int(c.table[0, j // 16]) * 16 + j % 16 for j in range(200)], device=DEV)
+    rfq.rfq_kv_append(k, torch.from_numpy(v).to(DEV).bfloat16(), slots, c.cache)
+    ko, vo = torch.empty(200, 1, D, device=DEV), torch.empty(200, 1, D, device=DEV)
+    rfq.rfq_kv_read(c.cache, slots, ko, vo)
+    vo = vo.double()[:, 0]
+    largest = 160 if fmt == ref.FMT_HIF4 else 2.0 ** 7                 # scale of 1000: 7 x 160, 2^(9 - 2)
+    block = 64 if fmt == ref.FMT_HIF4 else 32
+    off = vo.abs().clone()
+    off[:, block:] = 0                                                 # (blocks without a large value are exact)
+    if fmt == ref.FMT_HIF4 and new * 2 <= 32:
+        off[:, :block] += 2.0 ** -21 * largest
+    off[7] = 0
+    o, lse = c.run()
+    for i in range(new):
+        n = 200 - new + i + 1
+        mean = vo[:n].mean(0)
+        # beside it bf16's rounding and the fp32 sums; the weights are all alike, a power of two
+        bound = off[:n].mean(0) + 2.0 ** -8 * mean.abs() + 2.0 ** -16 * vo[:n].abs().mean(0)
+        assert ((o[i].double() - mean).abs() <= bound).all()
