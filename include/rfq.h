@@ -641,7 +641,7 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * The same inputs give the same bits.
  * Lengths past table_width pages, rows outside q and pages outside the cache
  * set the device status RFQ_ERR_SHAPE (rfq_workspace_status); such requests'
- * rows are unspecified.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT and
+ * rows are unspecified, and all rows are where q_start descends.  A bounded wait that runs out sets RFQ_ERR_TIMEOUT and
  * leaves NaN in the rows of out and lse that it concerns; int32 word 1 of the workspace is its
  * limit as for rfq_linear, and words 2 and 3 hold the start of the kernel for
  * more than 32 rows (of both in the debug build).

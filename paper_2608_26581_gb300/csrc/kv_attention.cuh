@@ -48,7 +48,8 @@ struct AttnParams {
 // One request: n new tokens (rows q0 .. of q) at the end of its L keys.
 struct Request {
     int n, L, q0;
-    __device__ __forceinline__ void load(const AttnParams &p, int r, int32_t *status)
+    // (true if q_start descends here)
+    __device__ __forceinline__ bool load(const AttnParams &p, int r, int32_t *status)
     {
         const KvAttentionArgs &a = p.a;
         const int most = a.width * a.cache.page_size;      // (the host has seen that it fits an int)
@@ -56,11 +57,12 @@ struct Request {
         L = min(max(len, 0), most);
         q0 = r;
         n = 1;
-        bool ok = len == L;
+        bool ok = len == L, descends = false;
         if (a.q_start) {
             q0 = a.q_start[r];
             const int q1 = a.q_start[r + 1];
             n = q1 - q0;
+            descends = q0 > q1;
             if (q0 < 0 || q0 > q1 || q1 > a.tokens) {
                 ok = false;
                 n = 0;
@@ -71,6 +73,7 @@ struct Request {
         const int64_t rows = (int64_t)n * p.group;
         if (rows < p.least_rows || rows > p.most_rows)
             n = 0;
+        return descends;
     }
     // Tiles of `rows` (token, head) rows
     __device__ __forceinline__ int tiles(int group, int rows) const { return (n * group + rows - 1) / rows; }
@@ -127,7 +130,8 @@ __device__ __forceinline__ uint32_t head_units(const Request &q, const AttnParam
 // of 512 keys, 32 heads on 8: with one token each 44.5 us where one by one gives
 // 55, with 1 to 4 72 where it gives 89).
 template <typename S>
-__device__ __forceinline__ uint32_t seek(const AttnParams &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status)
+__device__ __forceinline__ uint32_t seek(const AttnParams &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status,
+                                         bool &descends)
 {
     constexpr int kFew = 4;
     uint32_t all = 0;
@@ -163,7 +167,7 @@ __device__ __forceinline__ uint32_t seek(const AttnParams &p, int &r, int r1, ui
             uint32_t mine = 0;
             Request q = {0, 0, 0};
             if (r + lane < r1)
-                q.load(p, r + lane, status);
+                descends |= q.load(p, r + lane, status);
             const int tiles = q.tiles(p.group, S::kRows);
             if (tiles <= kFew)
 #pragma unroll 1
@@ -184,7 +188,7 @@ __device__ __forceinline__ uint32_t seek(const AttnParams &p, int &r, int r1, ui
 #pragma unroll 1
         for (; r < r1; ++r) {
             Request q;
-            q.load(p, r, status);
+            descends |= q.load(p, r, status);
             const uint32_t sum = H * head_units<S>(q, p, lane);
             if (rem < sum)
                 return all;
@@ -276,7 +280,9 @@ struct Share {
 };
 
 // The share of this warp (ALL_WARPS) or of the CTA, found by the whole CTA of W
-// warps; false if the CTA has none.  Each warp counts a run of requests, then
+// warps; false if the CTA has none, and in every CTA if q_start descends
+// somewhere (its requests' rows would overlap, and their units pass 32 bits:
+// where it ascends the host has seen that they do not).  Each warp counts a run of requests, then
 // finds its start in one of the runs.  (One loop for both: the second pass
 // finds its code at hand.)  least: units of a CTA, at least: one with fewer
 // would only add parts to join.
@@ -288,17 +294,21 @@ __device__ __forceinline__ bool find_share(const AttnParams &p, uint32_t *s_scan
     const uint32_t cta = blockIdx.x;
     const int per = (a.requests + W - 1) / W;
     int run = warp;
+    bool descends = false;
     o.rem = 0xFFFFFFFFu;
 #pragma unroll 1
     for (int pass = 0;; ++pass) {
         o.r = min(a.requests, run * per);
         const uint32_t sum = seek<S>(p, o.r, min(a.requests, o.r + per), o.rem, lane,
-                                     pass == 0 && cta == 0 ? p.status : nullptr);
+                                     pass == 0 && cta == 0 ? p.status : nullptr, descends);
         if (pass == 1)
             return true;
         if (lane == 0)
             s_scan[warp] = sum;
-        __syncthreads();
+        if (!a.q_start)
+            __syncthreads();
+        else if (__syncthreads_or(descends))
+            return false;
         const uint32_t runs = warp_scan(lane < W ? s_scan[lane] : 0u, lane);
         o.total = __shfl_sync(kAll, runs, 31);
         o.ctas = min(gridDim.x, (o.total + least - 1) / least);

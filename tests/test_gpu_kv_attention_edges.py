@@ -93,3 +93,25 @@ def test_values_far_below_the_largest(fmt, D, new):
         # beside it bf16's rounding and the fp32 sums; the weights are all alike, a power of two
         bound = off[:n].mean(0) + 2.0 ** -8 * mean.abs() + 2.0 ** -16 * vo[:n].abs().mean(0)
         assert ((o[i].double() - mean).abs() <= bound).all()
+
+
+@FMTS
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("requests", [3, 900])
+def test_a_q_start_that_descends(fmt, new, requests):
+    """The requests' rows overlap, so their work is not bounded by the tokens:
+    the status says so, nothing is computed, and the workspace stays usable."""
+    c = Case(fmt, 64, 1, 4, 16, [600], new=[new], seed=7)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    T = 2000
+    q, out = torch.zeros(T, 4, 64, dtype=torch.bfloat16, device=DEV), torch.full((T, 4, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    ws = rfq.kv_attention_workspace(4, 64)
+    table = torch.zeros(requests, 4096, dtype=torch.int32, device=DEV)
+    for start in ([T, 0] * requests, [0, T] * requests, [0] * (requests // 2) + [T] * (requests // 2) + [5] * requests):
+        start = start[:requests + 1]
+        rfq.rfq_kv_attention(q, c.cache, table, i32([65536] * requests), out, ws, q_start=i32(start))
+        assert rfq.rfq_workspace_status(ws, clear=True) == rfq.RFQ_ERR_SHAPE
+        lo, hi = start[0], start[-1]                # (what is clear of all requests may be zeros)
+        assert (out[min(lo, hi):max(lo, hi)] == 7).all()
+        out.fill_(7.0)
+    c.check(ws=ws, decode=False)
