@@ -23,6 +23,7 @@ namespace rfq {
 namespace {
 
 constexpr int kThreads = 256;                // of a block, at most (more where a head has more chunks)
+constexpr int kMostHeads = 65536;            // of a block: its rows, of four tokens, are told apart in fp32
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Vec {
     T v[VEC];
@@ -56,7 +57,7 @@ __global__ void rope_kernel(const RopeArgs a, int tb, int heads_per, int chunks,
     const int d = turn ? c * PV : 2 * P + (c - rot) * VEC;
     const int dist = INTER ? VEC : P, nv = turn ? NV : 1;
     const float inv_nh = 1.f / (float)nh;
-    auto token_of = [&](int r) { return (int)(((float)r + 0.5f) * inv_nh); };   // r / nh: both are far below 2^22
+    auto token_of = [&](int r) { return (int)(((float)r + 0.5f) * inv_nh); };   // r / nh (nh <= kMostHeads, r < 4 nh)
     auto load = [&](int r, V (&v)[NV]) {
         const int t = token_of(r), h = r - t * nh;
 #pragma unroll
@@ -121,9 +122,9 @@ cudaError_t launch(const RopeArgs &a, cudaStream_t st)
     const int64_t target = 2ll * num_sms();
     int tb = (int)min((int64_t)4, max((int64_t)1, a.tokens / target));
     const int64_t bx = (a.tokens + tb - 1) / tb;
-    const int by = (int)min((int64_t)a.heads, max((int64_t)1, target / bx));
-    const int hp = (a.heads + by - 1) / by;
-    const dim3 grid((unsigned)bx, (unsigned)((a.heads + hp - 1) / hp));
+    const int by = (int)min((int64_t)a.heads, max(((int64_t)a.heads + kMostHeads - 1) / kMostHeads, target / bx));
+    const int hp = (int)(((int64_t)a.heads + by - 1) / by);
+    const dim3 grid((unsigned)bx, (unsigned)(((int64_t)a.heads + hp - 1) / hp));
     const size_t smem = (size_t)tb * a.pairs * sizeof(float2);
     // chunks of a head: rotated ones first, then the elements that pass through
     const int pv = a.interleaved && VEC < 2 ? 2 : VEC;

@@ -2,6 +2,7 @@
 kernel has to be allowed, and what a launch is sized by, belongs to a device."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from fake_cuda import FakeCuda
@@ -65,3 +66,22 @@ def test_the_work_that_is_taken(fake):
     assert call(131072, 1, 256, 2 ** 28) == rfq.RFQ_ERR_SHAPE
     assert call(2 ** 15, 2 ** 15, None, 2 ** 20) == rfq.RFQ_ERR_SHAPE
     assert call(2 ** 25, 1, 256, 64) == rfq.RFQ_ERR_SHAPE             # rows past 32 bits
+
+
+@pytest.mark.parametrize("tokens,heads", [(1, 1), (7, 40), (32760, 40), (2000, 2 ** 22 + 1), (5, 2 ** 31 - 1)])
+def test_rope_blocks(fake, tokens, heads):
+    """A block's rows are four tokens of at most 65536 heads: their quotient by
+    the heads, (r + 1/2) / heads in fp32, then rounds down to r / heads."""
+    fake.device(0)
+    before = len(fake.launches())
+    assert fake.lib.rfq_rope(256, heads * 2, 2, 256, heads * 2, 2, 1, tokens, heads, 2, 256, 1, 256, 256, 1, 0, 0, None) == rfq.RFQ_OK
+    (x, y, _, _, _, _), = fake.launches()[before:]
+    each = -(-heads // y)
+    assert x * 4 >= tokens and y <= 65535 and each <= 65536
+
+
+def test_the_quotient_of_a_block_s_rows():
+    f = np.float32
+    for heads in (1, 2, 3, 5, 7, 40, 48, 1000, 4097, 65521, 65535, 65536):
+        r = np.arange(4 * heads)
+        assert (((r.astype(f) + f(0.5)) * (f(1) / f(heads))).astype(np.int64) == r // heads).all()
