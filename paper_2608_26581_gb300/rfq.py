@@ -394,6 +394,12 @@ def _want(ok: bool, call: str, what: str):
         raise ValueError(f"{call}: {what}")
 
 
+def _strides(t: torch.Tensor):
+    """Strides of [tokens, heads, head_dim].  That of an axis with one element is any number in torch and says nothing."""
+    (T, H, _), (st, sh, sd) = t.shape, t.stride()
+    return st if T > 1 else 0, sh if H > 1 else 0, sd
+
+
 _DTYPES = {torch.float32: RFQ_OUT_F32, torch.bfloat16: RFQ_OUT_BF16}
 
 
@@ -437,7 +443,7 @@ def rfq_rope(x: torch.Tensor, out: torch.Tensor, positions: torch.Tensor, inv_fr
           "x and out are fp32 or bf16 alike, positions and axis_of int32, inv_freq fp32")
     _want(out.shape == x.shape and positions.dim() == 2 and positions.shape[1] == T and
           axis_of.numel() == inv_freq.numel(), "rfq_rope", "sizes do not match")
-    (xt, xh, xd), (ot, oh, od) = x.stride(), out.stride()
+    (xt, xh, xd), (ot, oh, od) = _strides(x), _strides(out)
     _want((xd == 1 and od == 1) or D == 1, "rfq_rope", "the elements of a head must be contiguous")
     _want(positions.is_contiguous() and inv_freq.is_contiguous() and axis_of.is_contiguous(), "rfq_rope",
           "positions, inv_freq and axis_of must be contiguous")
@@ -502,7 +508,7 @@ def rfq_kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: 
           "k and v are bf16, slots int64")
     _want(v.shape == k.shape and H == cache.heads and D == cache.head_dim and slots.numel() == T, "rfq_kv_append",
           "sizes do not match the cache")
-    (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
+    (kt, kh, kd), (vt, vh, vd) = _strides(k), _strides(v)
     _want(kd == 1 and vd == 1 and slots.is_contiguous(), "rfq_kv_append",
           "the elements of a head and the slots must be contiguous")
     _check(load_library().rfq_kv_append(k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, T, slots.data_ptr(), cache._c,
@@ -553,7 +559,7 @@ def rfq_kv_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
     _want(D == cache.head_dim and out.shape == q.shape and lengths.numel() == R and
           (lse is None or lse.numel() == T * Hq) and (T == R if q_start is None else q_start.numel() == R + 1),
           "rfq_kv_attention", "sizes do not match")
-    qt, qh, qd = q.stride()
+    qt, qh, qd = _strides(q)
     _want(qd == 1 and out.is_contiguous() and block_table.is_contiguous() and lengths.is_contiguous() and
           (lse is None or lse.is_contiguous()) and (q_start is None or q_start.is_contiguous()), "rfq_kv_attention",
           "the elements of a head and every other tensor must be contiguous")
@@ -573,5 +579,5 @@ def rfq_matvec(x: torch.Tensor, wq: QTensor, y: torch.Tensor, stream=None):
     _want(x.dtype is torch.bfloat16 and dtype is not None, "rfq_matvec", "x is bf16, y fp32 or bf16")
     _want(K == wq.k and y.shape == (M, wq.rows), "rfq_matvec", "sizes do not match")
     _want(x.stride(1) == 1 and y.is_contiguous(), "rfq_matvec", "the rows of x and y must be contiguous")
-    _check(load_library().rfq_matvec(x.data_ptr(), x.stride(0), M, wq.c(), y.data_ptr(), dtype,
+    _check(load_library().rfq_matvec(x.data_ptr(), x.stride(0) if M > 1 else 0, M, wq.c(), y.data_ptr(), dtype,
                                      _raw_stream(stream, x)), "rfq_matvec")
