@@ -473,17 +473,17 @@ class KVCache:
                   "codes and scales are contiguous uint8 tensors of rfq_kv_cache_bytes bytes")
         self._c = _KV(self.fmt, self.heads, self.head_dim, self.page_size, self.pages, self.k_codes.data_ptr(),
                       self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr())
-        self._ws = None
+        self._ws = {}
 
     def c(self) -> _KV:
         return self._c
 
     def attention_workspace_bytes(self, heads: int) -> int:
-        """rfq_kv_attention_workspace_bytes, asked once for a cache's device."""
-        if self._ws is None:
+        """rfq_kv_attention_workspace_bytes, asked once for each number of heads on a cache's device."""
+        if heads not in self._ws:
             with torch.cuda.device(self.k_codes.device):
-                self._ws = rfq_kv_attention_workspace_bytes(heads, self.head_dim)
-        return self._ws
+                self._ws[heads] = rfq_kv_attention_workspace_bytes(heads, self.head_dim)
+        return self._ws[heads]
 
 
 def rfq_kv_cache_bytes(fmt: int, heads: int, head_dim: int, page_size: int, pages: int):

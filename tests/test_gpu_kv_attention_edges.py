@@ -115,3 +115,18 @@ def test_a_q_start_that_descends(fmt, new, requests):
         assert (out[min(lo, hi):max(lo, hi)] == 7).all()
         out.fill_(7.0)
     c.check(ws=ws, decode=False)
+
+
+def test_the_workspace_of_each_number_of_heads():
+    """A call without heads is refused, and a short workspace still is after it."""
+    c = Case(ref.FMT_MXFP4, 64, 2, 2, 16, [20], seed=8)
+    q, lens = bits_to_dev(c.qb), torch.tensor(c.lens, dtype=torch.int32, device=DEV)
+    none = torch.zeros(1, 0, 64, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(rfq.RFQError) as e:
+        rfq.rfq_kv_attention(none, c.cache, c.table, lens, torch.empty_like(none), rfq.kv_attention_workspace(4, 64))
+    assert e.value.status == rfq.RFQ_ERR_SHAPE
+    with pytest.raises(ValueError):
+        rfq.rfq_kv_attention(q, c.cache, c.table, lens, torch.empty_like(q), torch.zeros(64, dtype=torch.int32, device=DEV))
+    for heads in (1, 4, 64):
+        assert c.cache.attention_workspace_bytes(heads) == rfq.rfq_kv_attention_workspace_bytes(heads, 64) > 0
+    c.check()
