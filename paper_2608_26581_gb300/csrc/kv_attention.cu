@@ -415,8 +415,8 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
                     hi[t][j] = max(0, q.L - q.n + (q.n > 1 ? ri / G : 0) + 1);
                 }
             all_hi = max(0, q.L - q.n + (q.n > 1 ? row0 / G : 0) + 1);
-            least = a.window > 0 ? max(0, all_hi - a.window) : 0;
-            all_lo = a.window > 0 ? max(0, q.L - q.n + (q.n > 1 ? (row0 + rows - 1) / G : 0) + 1 - a.window) : 0;
+            least = first_seen(all_hi, a.window);
+            all_lo = first_seen(q.L - q.n + (q.n > 1 ? (row0 + rows - 1) / G : 0) + 1, a.window);
             z.clear();
             vref = -1000;
         }

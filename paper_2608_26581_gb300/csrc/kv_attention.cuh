@@ -45,6 +45,10 @@ struct AttnParams {
     int least_rows, most_rows; // the requests taken: those with this many rows a key head
 };
 
+// The first key that a row sees of those before `end` (below zero: it sees none);
+// the difference of the two may not fit 32 bits where end is negative.
+__device__ __forceinline__ int first_seen(int end, int window) { return window > 0 ? max(0, max(0, end) - window) : 0; }
+
 // One request: n new tokens (rows q0 .. of q) at the end of its L keys.
 struct Request {
     int n, L, q0;
@@ -86,7 +90,7 @@ struct Request {
             last = min(n - 1, (tile * rows + rows - 1) / p.group);
         }
         ke = max(0, L - n + last + 1);
-        kb = p.a.window > 0 ? max(0, L - n + first + 1 - p.a.window) & -p.gran : 0;
+        kb = first_seen(L - n + first + 1, p.a.window) & -p.gran;
         kb = min(kb, ke & -p.gran);
     }
     // Units of a tile: its chunks (one at least) and S::kStart more

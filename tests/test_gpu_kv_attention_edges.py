@@ -130,3 +130,12 @@ def test_the_workspace_of_each_number_of_heads():
     for heads in (1, 4, 64):
         assert c.cache.attention_workspace_bytes(heads) == rfq.rfq_kv_attention_workspace_bytes(heads, 64) > 0
     c.check()
+
+
+@FMTS
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 130, 2 ** 30, 400])
+def test_windows_beyond_all_keys(fmt, window):
+    """They hide nothing, also from requests with more new tokens than keys."""
+    Case(fmt, 64, 2, 2, 16, [300, 5, 40], new=[10, 16, 12], seed=9).check(window=window)
+    Case(fmt, 128, 1, 1, 16, [300, 5, 140], new=[450, 200, 33], seed=9).check(window=window)
+    Case(fmt, 64, 1, 2, 32, [300, 140], seed=9).check(window=window)
