@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(Shape<FMT, D, NT>::kThreads, 1)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int key = key0 + 16 * h + g + 8 * (j >> 1), top = hi[t][j & 1];
-                            if (key >= top || (a.window > 0 && key < top - a.window))
+                            if (key >= top || key < top - a.window)
                                 s[h][t][j] = -INFINITY;
                         }
             }
@@ -1009,6 +1009,8 @@ cudaError_t launch_kv_attention(const KvAttentionArgs &a, cudaStream_t st)
                     reinterpret_cast<float *>(ws + ws_parts_offset()),
                     0,
                     INT32_MAX};
+    if (a.window == 0)                       // (none: the kernels know windows alone)
+        p.a.window = INT32_MAX;
     // Only the device knows who has how many new tokens.  Where each request
     // has one at least and none can have kTileRows rows, the tiles have nothing to do.
     if (a.requests > 0 && most_rows(a.tokens, p.group, a.q_start != nullptr, a.requests) >= kTileRows) {

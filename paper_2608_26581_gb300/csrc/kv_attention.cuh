@@ -45,9 +45,9 @@ struct AttnParams {
     int least_rows, most_rows; // the requests taken: those with this many rows a key head
 };
 
-// The first key that a row sees of those before `end` (below zero: it sees none);
-// the difference of the two may not fit 32 bits where end is negative.
-__device__ __forceinline__ int first_seen(int end, int window) { return window > 0 ? max(0, max(0, end) - window) : 0; }
+// The first key that a row sees of those before `end` (below zero: it sees none, and
+// end - window may not fit 32 bits).
+__device__ __forceinline__ int first_seen(int end, int window) { return max(0, max(0, end) - window); }
 
 // One request: n new tokens (rows q0 .. of q) at the end of its L keys.
 struct Request {
@@ -81,8 +81,8 @@ struct Request {
     }
     // Tiles of `rows` (token, head) rows
     __device__ __forceinline__ int tiles(int group, int rows) const { return (n * group + rows - 1) / rows; }
-    // Keys [kb, ke) that some row of the tile sees, kb rounded down to gran
-    __device__ __forceinline__ void keys(int tile, const AttnParams &p, int rows, int &kb, int &ke) const
+    // Keys [least, ke) that some row of the tile sees; kb is least rounded down to gran
+    __device__ __forceinline__ void keys(int tile, const AttnParams &p, int rows, int &kb, int &ke, int &least) const
     {
         int first = 0, last = 0;
         if (n > 1) {
@@ -90,15 +90,15 @@ struct Request {
             last = min(n - 1, (tile * rows + rows - 1) / p.group);
         }
         ke = max(0, L - n + last + 1);
-        kb = first_seen(L - n + first + 1, p.a.window) & -p.gran;
-        kb = min(kb, ke & -p.gran);
+        least = first_seen(L - n + first + 1, p.a.window);
+        kb = min(least & -p.gran, ke & -p.gran);
     }
     // Units of a tile: its chunks (one at least) and S::kStart more
     template <typename S>
     __device__ __forceinline__ uint32_t units(int tile, const AttnParams &p) const
     {
-        int kb, ke;
-        keys(tile, p, S::kRows, kb, ke);
+        int kb, ke, least;
+        keys(tile, p, S::kRows, kb, ke, least);
         return max(1, (ke - kb + S::kChunk - 1) / S::kChunk) + S::kStart;
     }
 };
@@ -210,6 +210,7 @@ struct Walk {
     int r, head, tile, ntiles;
     Request q;
     int kb, ke, chunks;        // of the segment
+    int least;                 // no row of it sees a key below
     int i, i1;                 // the warp's chunks of it left
     uint32_t u, end;           // the segment's first unit; the end of the warp's units
     // from unit `first`, `rem` units into the segments of request r0
@@ -245,7 +246,7 @@ struct Walk {
     // the chunks of the segment at u that lie in [from, end): chunk k is unit u + kStart + k
     __device__ __forceinline__ void segment(const AttnParams &p, uint32_t from)
     {
-        q.keys(tile, p, ROWS, kb, ke);
+        q.keys(tile, p, ROWS, kb, ke, least);
         chunks = max(1, (ke - kb + S::kChunk - 1) / S::kChunk);
         i = from > u + S::kStart ? (int)(from - u - S::kStart) : 0;
         i1 = end > u + S::kStart ? (int)min((uint32_t)chunks, end - u - S::kStart) : 0;

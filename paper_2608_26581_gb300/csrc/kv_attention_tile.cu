@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
             const bool begins = walk.i == 0, ends = walk.i1 == walk.chunks;
             const int row0 = walk.tile * 128, rows = min(128, walk.q.n * G - row0), n = walk.q.n, L = walk.q.L;
             const int ri = row0 + min(tid, rows - 1);
-            const int hi = max(0, L - n + ri / G + 1), lo = a.window > 0 ? hi - a.window : 0;
+            const int hi = max(0, L - n + ri / G + 1), lo = first_seen(hi, a.window);
             const int all_hi = max(0, L - n + row0 / G + 1);
             const int all_lo = first_seen(L - n + (row0 + rows - 1) / G + 1, a.window);
             float m = -INFINITY, l = 0.f, qs = 0.f;
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
                 if (ch == 0)
                     s_qs[segs & 3][u] = __uint_as_float((uint32_t)(127 + e) << 23);
             }
-            const int least = first_seen(walk.q.L - walk.q.n + row0 / G + 1, a.window);
+            const int least = walk.least;
 #pragma unroll 1
             for (; walk.i < walk.i1; ++walk.i, ++j) {
                 const uint32_t buf = j & 1;
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         bool ok = true;
 #pragma unroll 1
         while (walk.more()) {
-            const int least = first_seen(walk.q.L - walk.q.n + walk.tile * 128 / G + 1, a.window);
+            const int least = walk.least;
 #pragma unroll 1
             for (; walk.i < walk.i1; ++walk.i, ++j) {
                 const uint32_t buf = j & 1;
@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) kv_attention_tile_kernel(const
         bool ok = true;
 #pragma unroll 1
         while (walk.more()) {
-            const int least = first_seen(walk.q.L - walk.q.n + walk.tile * 128 / G + 1, a.window);
+            const int least = walk.least;
             int ref[NB + 1];
 #pragma unroll
             for (int b = 0; b <= NB; ++b)
