@@ -637,6 +637,7 @@ RFQ_API size_t rfq_kv_attention_workspace_bytes(int32_t heads, int32_t head_dim)
  * 2^-21 of the largest scale).  Keys with the smallest E8M0 scale (byte 0, 2^-127)
  * count as zero and, for a request with more than 32 rows, so may those with a
  * scale 2^24 or more below the largest key scale of the same head and request.
+ * Block scales of 2^100 and more (keys) or 2^80 and more (values) may overflow.
  * q must be finite.
  * The same inputs give the same bits.
  * Lengths past table_width pages, rows outside q and pages outside the cache
@@ -664,7 +665,8 @@ RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64
  * Products and sums are fp32; W~ enters the tensor cores exactly and x as f16
  * scaled by a power of two per row and stretch of k, which keeps every bf16
  * bit down to 2^-28 of the stretch's maximum; blocks of W~ with the smallest
- * E8M0 scale (byte 0, 2^-127) count as zero.  The same inputs give the same
+ * E8M0 scale (byte 0, 2^-127) count as zero, and scales of 2^100 and more may
+ * overflow.  The same inputs give the same
  * bits.  Should a bounded wait run out, the sums that it concerns are NaN (the
  * call has no workspace, and so no device status).
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,

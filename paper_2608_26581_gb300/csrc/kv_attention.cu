@@ -38,8 +38,8 @@
 // gives the same bits every time.
 //
 // Measured, 32 heads on 8, D = 128: 8 requests of 98304 to 131072 keys, MXFP4
-// 226 us, 4.4 TB/s, 65% of the copy rate; HiF4, whose codes take more
-// instructions to decode, 352 us at 44%.  One request of 777 keys: 10.4 us,
+// 218 us, 4.5 TB/s, 67% of the copy rate; HiF4, whose codes take more
+// instructions to decode, 351 us at 44%.  One request of 777 keys: 10.4 us,
 // the latency of its dependent steps.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

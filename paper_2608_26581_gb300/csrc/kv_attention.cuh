@@ -131,8 +131,8 @@ __device__ __forceinline__ uint32_t head_units(const Request &q, const AttnParam
 // runs out, with rem units of it.  Requests are taken 32 at a time, a lane
 // each (of several tokens: those of many tiles are counted by the whole warp);
 // one or two of several tokens one by one, which is less to do (256 requests
-// of 512 keys, 32 heads on 8: with one token each 44.5 us where one by one gives
-// 55, with 1 to 4 72 where it gives 89).
+// of 512 keys, 32 heads on 8: with one token each 46 us, 11 more one by one, with
+// 1 to 4 74 us, 17 more).
 template <typename S>
 __device__ __forceinline__ uint32_t seek(const AttnParams &p, int &r, int r1, uint32_t &rem, int lane, int32_t *status,
                                          bool &descends)

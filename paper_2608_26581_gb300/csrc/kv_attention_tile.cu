@@ -35,7 +35,8 @@
 // loops have to fit the instruction caches together, so they stay rolled (all
 // unrolled: 186 us before what else follows, against 135).
 // 256 new tokens of 5 requests over 300 to 8192 keys, 32 heads on 8, D = 128,
-// MXFP4, pages of 32: 77 us, 460 TFLOP/s.  Tried there: eight warps for the
+// MXFP4, pages of 32: 78 us, 457 TFLOP/s; HiF4 87; one request of 4096 new
+// tokens, MXFP4: 159 us, 658 TFLOP/s.  Tried there: eight warps for the
 // softmax 83 us, for K and for V 95 against 92; one pass over the scores with
 // the maximum so far, repeated where it was passed, 79; the units of a
 // segment's start 1, 3, 5, 7: 107, 95, 96, 101.

@@ -11,8 +11,8 @@
 // transposition over the token's lanes, done with shuffles, so that codes go
 // out 16 bytes at a time.  Blocks run over the heads first: a token's row of
 // all heads is read by blocks that run at the same time.
-// 16384 tokens, 8 heads of 128, K and V, appended and read back: MXFP4 32.5 us,
-// 77% of the copy rate; HiF4 44 us, 58%, 28 of them the append, which its
+// 16384 tokens, 8 heads of 128, K and V, appended and read back: MXFP4 32 us,
+// 78% of the copy rate; HiF4 44 us, 58%, 28 of them the append, which its
 // encoder keeps on the ALUs.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -24,8 +24,8 @@
 // memory, in the order of the ranks.  All sums have a fixed order: a call
 // gives the same bits every time.
 //
-// Measured, MXFP4: 1 x 4096 x 24576 12.6 us, 4.2 TB/s, 62% of the copy rate;
-// 8 x 5120 x 13824 14.5 us; 32 rows 30 us; 13 x 12288 x 4096 in HiF4 18.4 us.
+// Measured, MXFP4: 1 x 4096 x 24576 12.8 us, 4.2 TB/s, 62% of the copy rate;
+// 8 x 5120 x 13824 13.0 us; 32 rows 30.7 us; 13 x 12288 x 4096 in HiF4 18.6 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
