@@ -674,6 +674,183 @@ RFQ_API rfq_status rfq_kv_attention(const void *q, int64_t q_token_stride, int64
 RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows, const rfq_qtensor *wq, void *y,
                               int32_t out_dtype, void *stream);
 
+/* ---- Around a mixture-of-experts block ------------------------------------
+ * The entry points below bring tokens to rfq_linear_grouped and back: norms in
+ * front of a block (rfq_norm), the router (rfq_route), the pairs of tokens and
+ * experts sorted into the groups of rows that the grouped product reads
+ * (rfq_moe_sort), the tokens' rows brought there (rfq_moe_gather, or quantized
+ * on the way: rfq_moe_quantize) and back (rfq_moe_combine), and the gradients
+ * of all of them but the quantizer.  The paper's linear layer has no
+ * counterpart for them; the format is its own (Sec. 3.2.2, Sec. 4.3).  Arrays
+ * of int32 and fp32 results need their natural alignment only; every other
+ * device pointer must be 16-byte aligned.  Rows whose strides and sizes are
+ * multiples of 16 bytes are read and written 16 bytes at a time, others element
+ * by element.  The same inputs give the same bits. */
+
+/* RFQ_NORM_LAYER  y = (x - mean) rstd w + b,  rstd = 1 / sqrt(variance + eps)
+ * RFQ_NORM_RMS    y = x rstd w + b,           rstd = 1 / sqrt(mean x^2 + eps) */
+typedef enum { RFQ_NORM_LAYER = 0, RFQ_NORM_RMS = 1 } rfq_norm_kind;
+
+/* Layer norm or RMS norm over the last axis.
+ *   x, y: device [tokens][heads][dim] of dtype (RFQ_OUT_F32 or RFQ_OUT_BF16)
+ *     with the given strides in elements between tokens and heads (so the heads
+ *     of a packed projection need no copy; heads = 1 for plain rows); y may be x
+ *     with the same strides, and does not overlap it otherwise.
+ *   weight, bias: device [dim] of w_dtype, or NULL (1 and 0).
+ *   mean, rstd: device fp32 [tokens][heads], what rfq_norm_grad needs, or NULL
+ *     (with RFQ_NORM_RMS mean gets 0).
+ * Mean, variance (from the differences to the mean) and everything between are
+ * fp32; y is rounded once.  Squares that pass fp32 (elements beyond 1e18) give
+ * rstd = 0; a row with an Inf or NaN gives NaN in that row alone.
+ * 1 <= dim <= 16384, tokens * heads < 2^31, eps >= 0.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_norm(const void *x, int64_t x_token_stride, int64_t x_head_stride, void *y,
+                            int64_t y_token_stride, int64_t y_head_stride, int32_t dtype, int64_t tokens,
+                            int32_t heads, int32_t dim, int32_t kind, float eps, const void *weight, const void *bias,
+                            int32_t w_dtype, float *mean, float *rstd, void *stream);
+
+/* Bytes of device workspace rfq_norm_grad needs on the current device for rows
+ * of dim elements (whatever their number); 0 for a dim it rejects. */
+RFQ_API size_t rfq_norm_grad_workspace_bytes(int32_t dim);
+
+/* Gradient of rfq_norm.  With h = (x - mean) rstd (RFQ_NORM_RMS: x rstd) and
+ * g = dy w:
+ *     dx = rstd (g - mean(g) - h mean(g h))      (RFQ_NORM_RMS: without mean(g))
+ *     dweight = sum over rows of dy h,  dbias = sum over rows of dy
+ *   dy, x, dx: device [tokens][heads][dim] of dtype, strided like rfq_norm's x;
+ *     dx may be dy or x with the same strides.
+ *   mean, rstd: device fp32 [tokens][heads] as rfq_norm wrote them (mean may be
+ *     NULL with RFQ_NORM_RMS).
+ *   weight: as rfq_norm got it, or NULL.
+ *   dweight, dbias: device fp32 [dim], or NULL; written also when there are no
+ *     rows (zeros).  The sums are fp32 in an order that the sizes and the device
+ *     alone decide.
+ *   workspace: rfq_norm_grad_workspace_bytes bytes, needed for dweight or dbias;
+ *     calls that overlap on the GPU must not share it.  Its contents do not
+ *     matter.
+ * Errors: as rfq_norm. */
+RFQ_API rfq_status rfq_norm_grad(const void *dy, int64_t dy_token_stride, int64_t dy_head_stride, const void *x,
+                                 int64_t x_token_stride, int64_t x_head_stride, void *dx, int64_t dx_token_stride,
+                                 int64_t dx_head_stride, int32_t dtype, int64_t tokens, int32_t heads, int32_t dim,
+                                 int32_t kind, const float *mean, const float *rstd, const void *weight,
+                                 int32_t w_dtype, float *dweight, float *dbias, void *workspace, void *stream);
+
+/* The router: each token's top_k experts and their weights.  With
+ * p = softmax(logits) over a token's experts,
+ *     ids[t][j] = the expert of the j-th largest logit (of equal ones the lowest)
+ *     weights[t][j] = p[ids[t][j]], or with normalize != 0 divided by their sum
+ * (the softmax over the chosen logits alone).  A logit of -inf is never chosen:
+ * a token with fewer than top_k others gets id -1 and weight 0 for the rest, and
+ * one with none of them for all.  A row with a NaN or +inf gives NaN weights (its
+ * ids are experts all the same, NaN counting as the largest).
+ *   logits: device [tokens][experts] of dtype, row_stride in elements.
+ *   ids: device int32 [tokens][top_k]; weights: device fp32 [tokens][top_k].
+ * 1 <= experts <= 256, 1 <= top_k <= min(32, experts), tokens * top_k < 2^31.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_route(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens, int32_t experts,
+                             int32_t top_k, int32_t normalize, int32_t *ids, float *weights, void *stream);
+
+/* Gradient of rfq_route's weights in the logits: with d[i] = dweights[t][j]
+ * where ids[t][j] = i, 0 for experts that were not chosen, and p the softmax over
+ * all experts, or with normalize != 0 over the chosen ones (0 elsewhere),
+ *     dlogits[t][i] = p[i] (d[i] - sum of p d).
+ * ids outside [0, experts) and their dweights are not looked at.  dlogits: device
+ * [tokens][experts] of dtype, every element written; it may be logits with the
+ * same stride.  The rest as for rfq_route.
+ * Errors: as rfq_route. */
+RFQ_API rfq_status rfq_route_grad(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens,
+                                  int32_t experts, int32_t top_k, int32_t normalize, const int32_t *ids,
+                                  const float *dweights, void *dlogits, int64_t dlogits_row_stride, void *stream);
+
+/* Rows that hold the groups of tokens * top_k pairs over the experts whatever
+ * the ids, each group's rows rounded up to a multiple of align (host only);
+ * -1 for sizes that rfq_moe_sort rejects. */
+RFQ_API int64_t rfq_moe_rows(int64_t tokens, int32_t top_k, int32_t experts, int32_t align);
+
+/* Pairs (token, choice) sorted by expert, in one launch.  Pair p = t top_k + j is
+ * of expert ids[t][j]; the rows of expert e's pairs, in the order of the pairs,
+ * are group_off[e], group_off[e] + 1, ...
+ *   ids: device int32 [tokens][top_k]; a pair whose id is outside [0, experts) (of
+ *     a place of the batch that holds no token) is of no group.
+ *   group_off: device int32 [experts + 1], group_off[0] = 0; every group's rows are
+ *     rounded up to a multiple of align (128 for rfq_linear_grouped).
+ *   row_of: device int32 [tokens][top_k], the row of each pair, or -1.
+ *   pair_of: device int32 [rows], the pair of each row, or -1 (rows that round a
+ *     group up, and all from group_off[experts] on).
+ *   rows: of the stacked matrix; rfq_moe_rows are always enough.  Pairs whose row
+ *     is not among the first align * floor(rows / align) get none (row_of = -1),
+ *     group_off is cut there, and the device status becomes RFQ_ERR_SHAPE.
+ *   workspace: device, 256 bytes zeroed by the caller once, for the device status
+ *     (rfq_workspace_status).
+ * 1 <= experts <= 256, 1 <= top_k <= 32, 1 <= align <= 4096,
+ * tokens * top_k + experts * align < 2^31, rows < 2^31.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_moe_sort(const int32_t *ids, int64_t tokens, int32_t top_k, int32_t experts, int32_t align,
+                                int32_t *group_off, int32_t *row_of, int32_t *pair_of, int64_t rows, void *workspace,
+                                void *stream);
+
+/* The tokens' rows brought to their groups: out[row_of[t][j]] = x[t] for every
+ * pair whose row is in [0, rows).
+ *   x: device [tokens][dim] of dtype, x_row_stride in elements.
+ *   row_of, pair_of: as rfq_moe_sort wrote them.  With pair_of, rows whose
+ *     pair_of is negative are cleared, so that every row of out is written;
+ *     without (NULL), rows of no pair are left as they were.
+ *   out: device [rows][dim] of dtype, contiguous; not x.
+ * A row that two pairs name gets either token.  Its gradient in x is
+ * rfq_moe_combine without weights.
+ * 1 <= dim <= 65536, 1 <= top_k <= 32, tokens * top_k < 2^31, rows < 2^31 and
+ * (tokens * top_k + rows) ceil(dim / 32) < 2^34.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
+ * RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_moe_gather(const void *x, int64_t x_row_stride, int32_t dtype, int64_t tokens, int32_t dim,
+                                  const int32_t *row_of, int32_t top_k, const int32_t *pair_of, void *out,
+                                  int64_t rows, void *stream);
+
+/* The groups' rows brought back: out[t] = sum over j of
+ * weights[t][j] y[row_of[t][j]], in the order of j, in fp32, rounded once; pairs
+ * whose row is not in [0, rows) add nothing (out[t] = 0 where all are so).
+ *   y: device [rows][dim] of dtype, contiguous.
+ *   weights: device fp32 [tokens][top_k], or NULL (1).
+ *   out: device [tokens][dim] of dtype, out_row_stride in elements; not y.
+ * Sizes and errors: as rfq_moe_gather. */
+RFQ_API rfq_status rfq_moe_combine(const void *y, int32_t dtype, int64_t rows, int32_t dim, const int32_t *row_of,
+                                   const float *weights, int64_t tokens, int32_t top_k, void *out,
+                                   int64_t out_row_stride, void *stream);
+
+/* Gradients of rfq_moe_combine in y and in the weights: for every pair whose row
+ * r is in [0, rows)
+ *     dy[r] = weights[t][j] dout[t],  dweights[t][j] = <dout[t], y[r]>
+ * and dweights[t][j] = 0 for the others.  With pair_of, rows of dy whose pair_of is
+ * negative are cleared; without (NULL), rows of no pair are left as they were.
+ *   dout: device [tokens][dim] of dtype, dout_row_stride in elements.
+ *   y, dy: device [rows][dim] of dtype, contiguous; dy may be y.
+ *   dweights: device fp32 [tokens][top_k].
+ * A row that two pairs name gets either one's gradient.
+ * Sizes and errors: as rfq_moe_gather. */
+RFQ_API rfq_status rfq_moe_combine_grad(const void *dout, int64_t dout_row_stride, const void *y, int32_t dtype,
+                                        int64_t rows, int32_t dim, const int32_t *row_of, const int32_t *pair_of,
+                                        const float *weights, int64_t tokens, int32_t top_k, void *dy,
+                                        float *dweights, void *stream);
+
+/* rfq_moe_gather that quantizes: the rows of xq and xr are what rfq_quantize_act
+ * (RFQ_FALLBACK_ALL, or RFQ_FALLBACK_NONE without xr) would write for the gathered
+ * rows, but each token is read and quantized once for all its pairs.
+ *   x: device bf16 [tokens][xq->k], x_row_stride in elements (a multiple of 8).
+ *   xq, xr: MXFP4 of the same rows and k with RFQ_SCALE_MMA, the operands of
+ *     rfq_linear_grouped; xr may be NULL.  Scale bytes of the layout's padding
+ *     rows (from xq->rows on) are zero.
+ *   row_of, pair_of: as for rfq_moe_gather; a cleared row has zero codes and
+ *     scales.
+ * k <= 65536; the other sizes as for rfq_moe_gather.
+ * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
+ * RFQ_ERR_UNSUPPORTED (other formats or layouts), RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */
+RFQ_API rfq_status rfq_moe_quantize(const void *x, int64_t x_row_stride, int64_t tokens, const int32_t *row_of,
+                                    int32_t top_k, const int32_t *pair_of, rfq_qtensor *xq, rfq_qtensor *xr,
+                                    void *stream);
+
 #ifdef __cplusplus
 }
 #endif

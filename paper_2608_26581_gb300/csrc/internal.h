@@ -304,6 +304,139 @@ struct MatvecArgs {
 };
 cudaError_t launch_matvec(const MatvecArgs &a, cudaStream_t st);
 
+// ---- norms of rows (norm.cu); strides in elements
+constexpr int kNormDim = 16384;                   // elements of a row
+struct NormArgs {
+    const void *x;
+    int64_t x_token, x_head;
+    void *y;
+    int64_t y_token, y_head;
+    bool bf16;
+    int64_t rows;                                 // tokens times heads
+    int32_t heads, dim;
+    bool rms;
+    float eps;
+    const void *weight, *bias;
+    bool w_bf16;
+    float *mean, *rstd;
+};
+struct NormGradArgs {
+    const void *dy;
+    int64_t dy_token, dy_head;
+    const void *x;
+    int64_t x_token, x_head;
+    void *dx;
+    int64_t dx_token, dx_head;
+    bool bf16;
+    int64_t rows;
+    int32_t heads, dim;
+    bool rms;
+    const float *mean, *rstd;
+    const void *weight;
+    bool w_bf16;
+    float *dweight, *dbias;
+    void *workspace;
+    float *partial;                               // (the launcher's: the workspace, or null without dweight and dbias)
+};
+size_t norm_grad_workspace_bytes(int32_t dim);
+cudaError_t launch_norm(const NormArgs &a, cudaStream_t st);
+cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st);
+
+// ---- the router of a mixture of experts (route.cu); strides in elements
+constexpr int kRouteExperts = 256, kRouteTopK = 32;
+struct RouteArgs {
+    const void *logits;
+    int64_t row;
+    bool bf16;
+    int64_t tokens;
+    int32_t experts, top_k;
+    bool normalize;
+    int32_t *ids;
+    float *weights;
+};
+struct RouteGradArgs {
+    const void *logits;
+    int64_t row;
+    bool bf16;
+    int64_t tokens;
+    int32_t experts, top_k;
+    bool normalize;
+    const int32_t *ids;
+    const float *dweights;
+    void *dlogits;
+    int64_t out_row;
+};
+cudaError_t launch_route(const RouteArgs &a, cudaStream_t st);
+cudaError_t launch_route_grad(const RouteGradArgs &a, cudaStream_t st);
+
+// ---- pairs (token, choice) sorted by expert (moe_sort.cu)
+constexpr int kMoeExperts = kRouteExperts, kMoeAlign = 4096;
+struct MoeSortArgs {
+    const int32_t *ids;
+    int64_t pairs;
+    int32_t experts, align;
+    int32_t *group_off, *row_of, *pair_of;
+    int64_t rows;
+    int32_t *status;
+};
+cudaError_t launch_moe_sort(const MoeSortArgs &a, cudaStream_t st);
+
+// ---- rows brought to experts and back (moe_rows.cu); strides in elements
+constexpr int kMoeDim = 65536;
+struct MoeGatherArgs {
+    const void *x;
+    int64_t x_row;
+    bool bf16;
+    int64_t tokens;
+    int32_t dim;
+    const int32_t *row_of;
+    int32_t top_k;
+    const int32_t *pair_of;                       // or null
+    void *out;
+    int64_t rows;
+};
+struct MoeCombineArgs {
+    const void *y;
+    bool bf16;
+    int64_t rows;
+    int32_t dim;
+    const int32_t *row_of;
+    const float *weights;                         // or null
+    int64_t tokens;
+    int32_t top_k;
+    void *out;
+    int64_t out_row;
+};
+struct MoeCombineGradArgs {
+    const void *dout;
+    int64_t dout_row;
+    const void *y;
+    bool bf16;
+    int64_t rows;
+    int32_t dim;
+    const int32_t *row_of, *pair_of;              // pair_of or null
+    const float *weights;
+    int64_t tokens;
+    int32_t top_k;
+    void *dy;
+    float *dweights;
+};
+struct MoeQuantizeArgs {
+    const void *x;
+    int64_t x_row, tokens;
+    int32_t dim;
+    const int32_t *row_of;
+    int32_t top_k;
+    const int32_t *pair_of;                       // or null
+    void *m_codes, *m_scales, *r_codes, *r_scales;    // r_*: null without a residual
+    int64_t rows;
+    int64_t padded, pad_from;                     // (the launcher's: rows of the scale layout, first one to clear)
+};
+cudaError_t launch_moe_gather(const MoeGatherArgs &a, cudaStream_t st);
+cudaError_t launch_moe_combine(const MoeCombineArgs &a, cudaStream_t st);
+cudaError_t launch_moe_combine_grad(const MoeCombineGradArgs &a, cudaStream_t st);
+cudaError_t launch_moe_quantize(const MoeQuantizeArgs &a, cudaStream_t st);
+
 // Blocks of `threads` threads (and `smem` dynamic shared bytes) of `kern`
 // resident on one SM at once (cached per kernel): grid-stride kernels launch
 // at most that many per SM, so no partial second wave trails the first.

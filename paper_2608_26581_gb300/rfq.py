@@ -22,6 +22,7 @@ RFQ_SCALE_ROWMAJOR, RFQ_SCALE_MMA = 0, 1
 RFQ_FALLBACK_NONE, RFQ_FALLBACK_ALL, RFQ_FALLBACK_AMAX = 0, 1, 2
 RFQ_OUT_F32, RFQ_OUT_BF16 = 0, 1
 RFQ_ROPE_HALF, RFQ_ROPE_INTERLEAVED = 0, 1
+RFQ_NORM_LAYER, RFQ_NORM_RMS = 0, 1
 (RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_UNSUPPORTED, RFQ_ERR_CUDA, RFQ_ERR_TIMEOUT,
  RFQ_ERR_DEVICE, RFQ_ERR_NONFINITE) = range(1, 9)
 STATUS_NAMES = {0: "RFQ_OK", 1: "RFQ_ERR_INVALID_ARG", 2: "RFQ_ERR_SHAPE", 3: "RFQ_ERR_ALIGNMENT",
@@ -34,7 +35,10 @@ EXPORTED = ("rfq_status_string", "rfq_qtensor_bytes", "rfq_quantize_weight", "rf
             "rfq_quantize_act_expand", "rfq_fp4_mma_peak", "rfq_linear_fused_workspace_bytes",
             "rfq_linear_profile", "rfq_debug_bounds", "rfq_linear_mixed", "rfq_linear_host",
             "rfq_slot_map", "rfq_rope", "rfq_kv_cache_bytes", "rfq_kv_append", "rfq_kv_read",
-            "rfq_kv_attention_workspace_bytes", "rfq_kv_attention", "rfq_matvec")
+            "rfq_kv_attention_workspace_bytes", "rfq_kv_attention", "rfq_matvec",
+            "rfq_norm", "rfq_norm_grad_workspace_bytes", "rfq_norm_grad", "rfq_route", "rfq_route_grad",
+            "rfq_moe_rows", "rfq_moe_sort", "rfq_moe_gather", "rfq_moe_combine", "rfq_moe_combine_grad",
+            "rfq_moe_quantize")
 
 
 class RFQError(RuntimeError):
@@ -128,6 +132,29 @@ def load_library(path: str = LIB_PATH):
         lib.rfq_kv_attention.argtypes = [P, I64, I64, I64, I32, P, P, I32, KVP, P, I32, F32, I32, P, P, P, P]
         lib.rfq_matvec.restype = I32
         lib.rfq_matvec.argtypes = [P, I64, I64, QTP, P, I32, P]
+        lib.rfq_norm.restype = I32
+        lib.rfq_norm.argtypes = [P, I64, I64, P, I64, I64, I32, I64, I32, I32, I32, F32, P, P, I32, P, P, P]
+        lib.rfq_norm_grad_workspace_bytes.restype = SZ
+        lib.rfq_norm_grad_workspace_bytes.argtypes = [I32]
+        lib.rfq_norm_grad.restype = I32
+        lib.rfq_norm_grad.argtypes = [P, I64, I64, P, I64, I64, P, I64, I64, I32, I64, I32, I32, I32, P, P, P, I32,
+                                      P, P, P, P]
+        lib.rfq_route.restype = I32
+        lib.rfq_route.argtypes = [P, I64, I32, I64, I32, I32, I32, P, P, P]
+        lib.rfq_route_grad.restype = I32
+        lib.rfq_route_grad.argtypes = [P, I64, I32, I64, I32, I32, I32, P, P, P, I64, P]
+        lib.rfq_moe_rows.restype = I64
+        lib.rfq_moe_rows.argtypes = [I64, I32, I32, I32]
+        lib.rfq_moe_sort.restype = I32
+        lib.rfq_moe_sort.argtypes = [P, I64, I32, I32, I32, P, P, P, I64, P, P]
+        lib.rfq_moe_gather.restype = I32
+        lib.rfq_moe_gather.argtypes = [P, I64, I32, I64, I32, P, I32, P, P, I64, P]
+        lib.rfq_moe_combine.restype = I32
+        lib.rfq_moe_combine.argtypes = [P, I32, I64, I32, P, P, I64, I32, P, I64, P]
+        lib.rfq_moe_combine_grad.restype = I32
+        lib.rfq_moe_combine_grad.argtypes = [P, I64, P, I32, I64, I32, P, P, P, I64, I32, P, P, P]
+        lib.rfq_moe_quantize.restype = I32
+        lib.rfq_moe_quantize.argtypes = [P, I64, I64, P, I32, P, QTP, QTP, P]
         _lib = lib
     return _lib
 
@@ -581,3 +608,251 @@ def rfq_matvec(x: torch.Tensor, wq: QTensor, y: torch.Tensor, stream=None):
     _want(x.stride(1) == 1 and y.is_contiguous(), "rfq_matvec", "the rows of x and y must be contiguous")
     _check(load_library().rfq_matvec(x.data_ptr(), x.stride(0) if M > 1 else 0, M, wq.c(), y.data_ptr(), dtype,
                                      _raw_stream(stream, x)), "rfq_matvec")
+
+
+# ---- around a mixture-of-experts block: norms, the router, rows to experts and back
+
+def _device_call(call: str, f, args, stream, *tensors):
+    """Runs f(*args, stream) on the device that every tensor (None: left out) lies on."""
+    dev = tensors[0].device
+    _want(dev.type == "cuda", call, "tensors must be on a CUDA device")
+    for t in tensors:
+        _want(t is None or t.device == dev, call, "tensors must be on one device")
+    if dev.index == torch.cuda.current_device():
+        _check(f(*args, _raw_stream(stream, tensors[0])), call)
+    else:
+        with torch.cuda.device(dev):
+            _check(f(*args, _raw_stream(stream, tensors[0])), call)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _dense(dtype, n: int, *tensors) -> bool:
+    """Every tensor (None: left out) is contiguous, of that type and of n elements."""
+    return all(t is None or (t.dtype is dtype and t.numel() == n and t.is_contiguous()) for t in tensors)
+
+
+def _rows3(t: torch.Tensor):
+    """[tokens, heads, dim] of a norm's rows: a 2-d tensor has one head."""
+    return t if t.dim() == 3 else t.unsqueeze(1)
+
+
+def _rows2(t: torch.Tensor, call: str) -> int:
+    """Stride between the rows of a [rows, n] tensor, whose elements lie together."""
+    _want(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), call, "the elements of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _norm_params(call: str, dim: int, weight, bias) -> int:
+    """The type of weight and bias."""
+    w = weight if weight is not None else bias
+    if w is None:
+        return RFQ_OUT_F32
+    dtype = _DTYPES.get(w.dtype)
+    _want(dtype is not None and _dense(w.dtype, dim, weight, bias), call,
+          "weight and bias are contiguous [dim] tensors, fp32 or bf16 alike")
+    return dtype
+
+
+def rfq_norm(x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+             kind: int = RFQ_NORM_LAYER, eps: float = 1e-6, mean: torch.Tensor | None = None,
+             rstd: torch.Tensor | None = None, stream=None):
+    """Layer norm or RMS norm over the last axis: x, y [rows, dim] or [tokens,
+    heads, dim] (fp32 or bf16 alike, any strides with unit stride in dim; y may
+    be x); weight, bias [dim]; mean, rstd fp32 of one element a row, kept for
+    rfq_norm_grad (see include/rfq.h)."""
+    dtype = _DTYPES.get(x.dtype)
+    _want(dtype is not None and y.dtype is x.dtype, "rfq_norm", "x and y are fp32 or bf16 alike")
+    _want(x.dim() in (2, 3) and y.shape == x.shape, "rfq_norm", "x and y are [rows, dim] or [tokens, heads, dim]")
+    x3, y3 = _rows3(x), _rows3(y)
+    T, H, D = x3.shape
+    (xt, xh, xd), (yt, yh, yd) = _strides(x3), _strides(y3)
+    _want((xd == 1 and yd == 1) or D == 1, "rfq_norm", "the elements of a row must be contiguous")
+    w_dtype = _norm_params("rfq_norm", D, weight, bias)
+    _want(_dense(torch.float32, T * H, mean, rstd), "rfq_norm", "mean and rstd are contiguous fp32, one element a row")
+    _device_call("rfq_norm", load_library().rfq_norm,
+                 (x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, dtype, T, H, D, kind, eps, _at(weight), _at(bias), w_dtype,
+                  _at(mean), _at(rstd)), stream, x, y, weight, bias, mean, rstd)
+
+
+_norm_ws: dict[tuple[int, int], int] = {}     # workspace bytes by device and dim
+
+
+def rfq_norm_grad_workspace_bytes(dim: int) -> int:
+    return load_library().rfq_norm_grad_workspace_bytes(dim)
+
+
+def norm_workspace(dim: int, device="cuda") -> torch.Tensor:
+    """A workspace for rfq_norm_grad (fp32 words)."""
+    with torch.cuda.device(device):
+        n = rfq_norm_grad_workspace_bytes(dim)
+    _want(n > 0, "norm_workspace", "dim is 1 to 16384")
+    return torch.empty(n // 4, dtype=torch.float32, device=device)
+
+
+def rfq_norm_grad(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
+                  mean: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+                  dweight: torch.Tensor | None = None, dbias: torch.Tensor | None = None,
+                  workspace: torch.Tensor | None = None, kind: int = RFQ_NORM_LAYER, stream=None):
+    """Gradient of rfq_norm: dy, x, dx like rfq_norm's x (dx may be dy or x);
+    mean, rstd as rfq_norm wrote them (mean None with RFQ_NORM_RMS); dweight,
+    dbias fp32 [dim] or None, for which workspace is norm_workspace(dim) (see
+    include/rfq.h)."""
+    dtype = _DTYPES.get(x.dtype)
+    _want(dtype is not None and dy.dtype is x.dtype and dx.dtype is x.dtype, "rfq_norm_grad",
+          "dy, x and dx are fp32 or bf16 alike")
+    _want(x.dim() in (2, 3) and dy.shape == x.shape and dx.shape == x.shape, "rfq_norm_grad",
+          "dy, x and dx are [rows, dim] or [tokens, heads, dim]")
+    x3 = _rows3(x)
+    T, H, D = x3.shape
+    (dt, dh, dd), (xt, xh, xd), (ot, oh, od) = _strides(_rows3(dy)), _strides(x3), _strides(_rows3(dx))
+    _want((dd == 1 and xd == 1 and od == 1) or D == 1, "rfq_norm_grad", "the elements of a row must be contiguous")
+    w_dtype = _norm_params("rfq_norm_grad", D, weight, None)
+    _want(_dense(torch.float32, T * H, mean, rstd), "rfq_norm_grad", "mean and rstd are contiguous fp32, one element a row")
+    _want(_dense(torch.float32, D, dweight, dbias), "rfq_norm_grad", "dweight and dbias are contiguous fp32 [dim] tensors")
+    if dweight is not None or dbias is not None:
+        key = (x.device.index, D)
+        if key not in _norm_ws and x.device.type == "cuda":
+            with torch.cuda.device(x.device):
+                _norm_ws[key] = rfq_norm_grad_workspace_bytes(D)
+        _want(workspace is not None and workspace.is_contiguous() and
+              workspace.numel() * workspace.element_size() >= _norm_ws.get(key, 0), "rfq_norm_grad",
+              "the workspace is smaller than rfq_norm_grad_workspace_bytes")
+    _device_call("rfq_norm_grad", load_library().rfq_norm_grad,
+                 (dy.data_ptr(), dt, dh, x.data_ptr(), xt, xh, dx.data_ptr(), ot, oh, dtype, T, H, D, kind, _at(mean),
+                  _at(rstd), _at(weight), w_dtype, _at(dweight), _at(dbias), _at(workspace)), stream, x, dy, dx, rstd,
+                 mean, weight, dweight, dbias, workspace)
+
+
+def rfq_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, normalize: bool = True, stream=None):
+    """The router: the top_k experts of each token and their weights from
+    logits [tokens, experts] (fp32 or bf16, rows strided) into ids int32 and
+    weights fp32 [tokens, top_k] (see include/rfq.h)."""
+    dtype = _DTYPES.get(logits.dtype)
+    _want(dtype is not None, "rfq_route", "logits are fp32 or bf16")
+    row = _rows2(logits, "rfq_route")
+    T, E = logits.shape
+    _want(ids.dim() == 2 and ids.shape[0] == T and weights.shape == ids.shape and _dense(torch.int32, ids.numel(), ids) and
+          _dense(torch.float32, ids.numel(), weights), "rfq_route",
+          "ids (int32) and weights (fp32) are contiguous [tokens, top_k]")
+    _device_call("rfq_route", load_library().rfq_route,
+                 (logits.data_ptr(), row, dtype, T, E, ids.shape[1], 1 if normalize else 0, ids.data_ptr(),
+                  weights.data_ptr()), stream, logits, ids, weights)
+
+
+def rfq_route_grad(logits: torch.Tensor, ids: torch.Tensor, dweights: torch.Tensor, dlogits: torch.Tensor,
+                   normalize: bool = True, stream=None):
+    """Gradient of rfq_route's weights: dweights fp32 [tokens, top_k] into
+    dlogits like logits (see include/rfq.h)."""
+    dtype = _DTYPES.get(logits.dtype)
+    _want(dtype is not None and dlogits.dtype is logits.dtype and dlogits.shape == logits.shape, "rfq_route_grad",
+          "logits and dlogits are fp32 or bf16 and of one shape")
+    row, out_row = _rows2(logits, "rfq_route_grad"), _rows2(dlogits, "rfq_route_grad")
+    T, E = logits.shape
+    _want(ids.dim() == 2 and ids.shape[0] == T and dweights.shape == ids.shape and _dense(torch.int32, ids.numel(), ids) and
+          _dense(torch.float32, ids.numel(), dweights), "rfq_route_grad",
+          "ids (int32) and dweights (fp32) are contiguous [tokens, top_k]")
+    _device_call("rfq_route_grad", load_library().rfq_route_grad,
+                 (logits.data_ptr(), row, dtype, T, E, ids.shape[1], 1 if normalize else 0, ids.data_ptr(),
+                  dweights.data_ptr(), dlogits.data_ptr(), out_row), stream, logits, ids, dweights, dlogits)
+
+
+def rfq_moe_rows(tokens: int, top_k: int, experts: int, align: int = 128) -> int:
+    """Rows that hold the groups of tokens * top_k pairs whatever the ids."""
+    n = load_library().rfq_moe_rows(tokens, top_k, experts, align)
+    _want(n >= 0, "rfq_moe_rows", "sizes out of range")
+    return n
+
+
+def rfq_moe_sort(ids: torch.Tensor, group_off: torch.Tensor, row_of: torch.Tensor, pair_of: torch.Tensor,
+                 workspace: torch.Tensor, align: int = 128, stream=None):
+    """Pairs of ids [tokens, top_k] sorted by expert: group_off [experts + 1],
+    row_of [tokens, top_k], pair_of [rows], all int32 and contiguous; workspace:
+    256 bytes, zeroed once, for the device status (see include/rfq.h)."""
+    i32 = torch.int32
+    _want(ids.dim() == 2 and row_of.shape == ids.shape and group_off.numel() >= 1 and
+          _dense(i32, ids.numel(), ids, row_of) and _dense(i32, group_off.numel(), group_off) and
+          _dense(i32, pair_of.numel(), pair_of), "rfq_moe_sort",
+          "ids and row_of are [tokens, top_k], group_off [experts + 1], pair_of [rows], contiguous int32")
+    _want(workspace.numel() * workspace.element_size() >= 256, "rfq_moe_sort", "the workspace is 256 bytes")
+    _device_call("rfq_moe_sort", load_library().rfq_moe_sort,
+                 (ids.data_ptr(), ids.shape[0], ids.shape[1], group_off.numel() - 1, align, group_off.data_ptr(),
+                  row_of.data_ptr(), pair_of.data_ptr(), pair_of.numel(), workspace.data_ptr()), stream, ids, group_off,
+                 row_of, pair_of, workspace)
+
+
+def _moe_maps(call: str, tokens: int, rows: int, row_of: torch.Tensor, pair_of: torch.Tensor | None):
+    _want(row_of.dim() == 2 and row_of.shape[0] == tokens and _dense(torch.int32, row_of.numel(), row_of), call,
+          "row_of is a contiguous int32 [tokens, top_k]")
+    _want(_dense(torch.int32, rows, pair_of), call, "pair_of is a contiguous int32 [rows]")
+
+
+def rfq_moe_gather(x: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, pair_of: torch.Tensor | None = None,
+                   stream=None):
+    """out[row_of[t, j]] = x[t]: x [tokens, dim] (fp32 or bf16, rows strided),
+    out [rows, dim] contiguous; rows of no pair are cleared with pair_of, left
+    alone without (see include/rfq.h)."""
+    dtype = _DTYPES.get(x.dtype)
+    _want(dtype is not None and out.dtype is x.dtype, "rfq_moe_gather", "x and out are fp32 or bf16 alike")
+    row = _rows2(x, "rfq_moe_gather")
+    _want(out.dim() == 2 and out.shape[1] == x.shape[1] and out.is_contiguous(), "rfq_moe_gather",
+          "out is a contiguous [rows, dim]")
+    _moe_maps("rfq_moe_gather", x.shape[0], out.shape[0], row_of, pair_of)
+    _device_call("rfq_moe_gather", load_library().rfq_moe_gather,
+                 (x.data_ptr(), row, dtype, x.shape[0], x.shape[1], row_of.data_ptr(), row_of.shape[1], _at(pair_of),
+                  out.data_ptr(), out.shape[0]), stream, x, row_of, pair_of, out)
+
+
+def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, weights: torch.Tensor | None = None,
+                    stream=None):
+    """out[t] = sum_j weights[t, j] y[row_of[t, j]]: y [rows, dim] contiguous,
+    out [tokens, dim] (fp32 or bf16 alike, rows strided), weights fp32 [tokens,
+    top_k] or None (1; see include/rfq.h)."""
+    dtype = _DTYPES.get(y.dtype)
+    _want(dtype is not None and out.dtype is y.dtype, "rfq_moe_combine", "y and out are fp32 or bf16 alike")
+    row = _rows2(out, "rfq_moe_combine")
+    _want(y.dim() == 2 and y.shape[1] == out.shape[1] and y.is_contiguous(), "rfq_moe_combine",
+          "y is a contiguous [rows, dim]")
+    _moe_maps("rfq_moe_combine", out.shape[0], y.shape[0], row_of, None)
+    _want(_dense(torch.float32, row_of.numel(), weights), "rfq_moe_combine", "weights are contiguous fp32 [tokens, top_k]")
+    _device_call("rfq_moe_combine", load_library().rfq_moe_combine,
+                 (y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(weights), out.shape[0],
+                  row_of.shape[1], out.data_ptr(), row), stream, y, row_of, weights, out)
+
+
+def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tensor, weights: torch.Tensor,
+                         dy: torch.Tensor, dweights: torch.Tensor, pair_of: torch.Tensor | None = None, stream=None):
+    """Gradients of rfq_moe_combine: dout [tokens, dim] (rows strided) into dy
+    like y (may be y) and dweights fp32 [tokens, top_k]; rows of no pair are
+    cleared with pair_of, left alone without (see include/rfq.h)."""
+    dtype = _DTYPES.get(y.dtype)
+    _want(dtype is not None and dout.dtype is y.dtype and dy.dtype is y.dtype, "rfq_moe_combine_grad",
+          "dout, y and dy are fp32 or bf16 alike")
+    row = _rows2(dout, "rfq_moe_combine_grad")
+    _want(y.dim() == 2 and y.shape[1] == dout.shape[1] and dy.shape == y.shape and y.is_contiguous() and
+          dy.is_contiguous(), "rfq_moe_combine_grad", "y and dy are contiguous [rows, dim]")
+    _moe_maps("rfq_moe_combine_grad", dout.shape[0], y.shape[0], row_of, pair_of)
+    _want(_dense(torch.float32, row_of.numel(), weights, dweights), "rfq_moe_combine_grad",
+          "weights and dweights are contiguous fp32 [tokens, top_k]")
+    _device_call("rfq_moe_combine_grad", load_library().rfq_moe_combine_grad,
+                 (dout.data_ptr(), row, y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(pair_of),
+                  weights.data_ptr(), dout.shape[0], row_of.shape[1], dy.data_ptr(), dweights.data_ptr()), stream, y,
+                 dout, row_of, pair_of, weights, dy, dweights)
+
+
+def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTensor | None = None,
+                     pair_of: torch.Tensor | None = None, stream=None):
+    """rfq_moe_gather that quantizes x (bf16 [tokens, k], rows strided) into
+    the MXFP4 operands of rfq_linear_grouped, X~ into xq and X^ into xr (see
+    include/rfq.h)."""
+    _want(x.dtype is torch.bfloat16, "rfq_moe_quantize", "x is bf16")
+    row = _rows2(x, "rfq_moe_quantize")
+    _want(xq.k == x.shape[1] and (xr is None or (xr.rows == xq.rows and xr.k == xq.k)), "rfq_moe_quantize",
+          "sizes do not match")
+    _moe_maps("rfq_moe_quantize", x.shape[0], xq.rows, row_of, pair_of)
+    _device_call("rfq_moe_quantize", load_library().rfq_moe_quantize,
+                 (x.data_ptr(), row, x.shape[0], row_of.data_ptr(), row_of.shape[1], _at(pair_of), xq.c(),
+                  None if xr is None else xr.c()), stream, x, row_of, pair_of, xq.codes, xq.scales,
+                 None if xr is None else xr.codes, None if xr is None else xr.scales)
