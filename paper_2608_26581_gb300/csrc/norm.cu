@@ -8,11 +8,16 @@
 //            dw = sum over rows of dy h,  db = sum over rows of dy.
 //
 // Bound: HBM (x read and y written once; dy and x read and dx written once).
-// A row is held in registers by the threads that share it, so the mean and
-// the squared distances from it are two passes over registers.  The weight's
-// gradient is summed in fp32 in the registers of persistent blocks, whose
-// threads keep their columns over all their rows; the blocks' sums go through
-// the workspace and a second kernel adds them, both in a fixed order.
+// Persistent blocks take rows in turn.  The threads that share a row hold it
+// in registers, so the mean and the squared distances from it are two passes
+// over registers.  Rows that come next are on their way to shared memory: a
+// thread copies (cp.async) and reads its own 16-byte chunks alone, so the ring
+// needs no barrier.  (Rows that are not whole 16-byte chunks are loaded when
+// their turn comes.)  A thread's chunks lie a fixed distance apart, which
+// leaves one address a row; arithmetic is on pairs of fp32 values.  The
+// weight's gradient is summed in fp32 in registers by threads that keep their
+// columns over all their rows; the blocks' sums go through the workspace and a
+// second kernel adds them, both in a fixed order.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -24,187 +29,385 @@
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 256;                // of a block, at least where a row takes more
+constexpr int kThreads = 256;                // of a block whose rows take a warp or less
+constexpr size_t kMostSmem = 200 * 1024;     // of an SM's blocks together
+constexpr size_t kPlainSmem = 47 * 1024;     // dynamic, beside the kernels' own (512 bytes at most), without asking
+
+struct Pair {
+    float x, y;
+};
+__device__ __forceinline__ Pair operator+(const Pair &a, const Pair &b) { return {a.x + b.x, a.y + b.y}; }
+__device__ __forceinline__ float shfl_xor(float v, int d) { return __shfl_xor_sync(0xFFFFFFFFu, v, d); }
+__device__ __forceinline__ Pair shfl_xor(const Pair &v, int d) { return {shfl_xor(v.x, d), shfl_xor(v.y, d)}; }
+
+// How a row lies over threads: TPR of them share it, NV chunks of VEC elements
+// each, TPR chunks apart; with TPR = 64 it takes all warps of the block, each
+// of them 32 NV chunks that lie together.
+template <typename T_, int VEC_, int NV_, int TPR_>
+struct Split {
+    using T = T_;
+    static constexpr int VEC = VEC_, NV = NV_, TPR = TPR_;
+    static constexpr bool kBlock = TPR > 32;
+    static constexpr int kStep = kBlock ? 32 : TPR;                   // chunks between a thread's
+    static constexpr int kLanesOf = kLanes<VEC>;
+    using F = Lane<VEC>;
+    int group, first;                                                 // row of the block's; this thread's first chunk
+    __device__ __forceinline__ Split()
+        : group(kBlock ? 0 : threadIdx.x / TPR),
+          first(kBlock ? (threadIdx.x >> 5) * 32 * NV + (threadIdx.x & 31) : threadIdx.x % TPR)
+    {
+    }
+    static __device__ __forceinline__ int groups() { return kBlock ? 1 : blockDim.x / TPR; }
+    __device__ __forceinline__ bool leads() const { return first == 0; }
+    // chunk i of this thread is one of the row's
+    __device__ __forceinline__ bool has(int i, int chunks) const { return first + i * kStep < chunks; }
+
+    // Sum over the row's threads.  A block's go through `part` (32 values, zero
+    // where it has no warp); two sums in a row take different ones, which makes
+    // one barrier a sum enough: who writes has passed the barrier behind the
+    // last use.
+    template <typename V>
+    __device__ __forceinline__ V sum(V v, V *part) const
+    {
+#pragma unroll
+        for (int d = kStep / 2; d > 0; d >>= 1)
+            v = v + shfl_xor(v, d);
+        if constexpr (kBlock) {
+            if ((threadIdx.x & 31) == 0)
+                part[threadIdx.x >> 5] = v;
+            __syncthreads();
+            v = part[0];
+            const int n = blockDim.x >> 5;
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                v = v + part[i];
+#pragma unroll 1
+            for (int i = 4; i < n; i += 4)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    v = v + part[i + j];
+        }
+        return v;
+    }
+};
 
 // Where rows lie: [tokens][heads] with two strides in elements.
-struct Place {
-    int64_t token, head;
-};
-__device__ __forceinline__ int64_t row_at(const Place &p, int64_t row, int heads)
+template <typename T>
+__device__ __forceinline__ T *row_at(T *p, int64_t token, int64_t head, uint32_t row, uint32_t heads)
 {
     if (heads == 1)
-        return row * p.token;
-    const int64_t t = (uint64_t)row / (uint32_t)heads;
-    return t * p.token + (row - t * heads) * p.head;
+        return p + row * token;
+    const uint32_t t = row / heads;
+    return p + t * token + (row - t * heads) * head;
 }
 
-// Sum over the `tpr` threads of a row: a power of two up to a warp, or whole
-// warps, whose sums go through s_part (one float a warp of the block).
-__device__ __forceinline__ float row_sum(float v, int tpr, float *s_part)
+// VEC parameters from column c on, in fp32.
+template <int VEC>
+__device__ __forceinline__ void load_params(const void *p, bool bf16, int c, Lane<VEC> *v)
 {
-    if (tpr <= 32)
-        return lane_sum(v, tpr);
-    v = lane_sum(v);
-    const int warp = threadIdx.x >> 5, n = tpr >> 5, first = warp / n * n;
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0)
-        s_part[warp] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < n; ++i)
-        v += s_part[first + i];
-    return v;
+    if (bf16)
+        unpack<__nv_bfloat16, VEC>(load_vec<__nv_bfloat16, VEC>(static_cast<const __nv_bfloat16 *>(p) + c), v);
+    else {
+        constexpr int F = VEC < 4 ? VEC : 4;
+#pragma unroll
+        for (int g = 0; g < VEC / F; ++g)
+            unpack<float, F>(load_vec<float, F>(static_cast<const float *>(p) + c + g * F), v + g * kLanes<F>);
+    }
 }
 
-__device__ __forceinline__ float param(const void *p, bool bf16, int i)
-{
-    return bf16 ? to_f32(static_cast<const __nv_bfloat16 *>(p)[i]) : static_cast<const float *>(p)[i];
-}
-
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(1024) norm_kernel(const NormArgs a, int tpr)
-{
-    __shared__ float s_part[32];
-    const int group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / tpr) + group;
-    const bool there = row < a.rows;
-    const int chunks = a.dim / VEC;
-    wait_for_previous();
-    let_next_start();
-    const T *const x = static_cast<const T *>(a.x) + row_at({a.x_token, a.x_head}, row, a.heads);
-    Vec<T, VEC> v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = lane + i * tpr;
-        v[i] = there && c < chunks ? load_vec<T, VEC>(x + (int64_t)c * VEC) : zero_vec<T, VEC>();
+// Rows on their way, S deep, N arrays: chunks of 16 bytes copied ahead into
+// shared memory (with S = 0 a row is loaded when its turn comes).
+template <typename P, int N, int S>
+struct Ring {
+    using T = typename P::T;
+    uint32_t base, row;                      // shared address of this thread's chunks; bytes of a row of all threads
+    __device__ __forceinline__ Ring(const void *smem)
+        : base(smem_u32(smem) + ((threadIdx.x >> 5) * 32 * P::NV + (threadIdx.x & 31)) * 16), row(blockDim.x * P::NV * 16)
+    {
     }
-    const float inv = 1.f / (float)a.dim;
-    float mean = 0.f;
-    if (!a.rms) {
-        float s = 0.f;
+    static constexpr size_t bytes(int threads) { return (size_t)S * N * P::NV * 16 * threads; }
+    __device__ __forceinline__ void copy(const P &p, int slot, int n, const T *x, bool there, int chunks) const
+    {
+        const uint32_t to = base + (slot * N + n) * row;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                s += to_f32(v[i].v[e]);
-        mean = row_sum(s, tpr, s_part) * inv;
+        for (int i = 0; i < P::NV; ++i)
+            if (there && p.has(i, chunks))
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(x + (p.first + i * P::kStep) * P::VEC) : "memory");
     }
-    float q = 0.f;
+    __device__ __forceinline__ void read(const P &p, int slot, int n, bool there, int chunks, typename P::F (&x)[P::NV][P::kLanesOf]) const
+    {
+        const uint32_t at = base + (slot * N + n) * row;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (lane + i * tpr < chunks)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = to_f32(v[i].v[e]) - mean;
-                q += d * d;
-            }
-    const float rstd = 1.f / sqrtf(row_sum(q, tpr, s_part) * inv + a.eps);
-    if (!there)
-        return;
-    if (lane == 0) {
-        if (a.mean)
-            a.mean[row] = mean;
-        if (a.rstd)
-            a.rstd[row] = rstd;
-    }
-    T *const y = static_cast<T *>(a.y) + row_at({a.y_token, a.y_head}, row, a.heads);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = lane + i * tpr;
-        if (c < chunks) {
-            Vec<T, VEC> o;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                float t = (to_f32(v[i].v[e]) - mean) * rstd;
-                if (a.weight)
-                    t *= param(a.weight, a.w_bf16, c * VEC + e);
-                if (a.bias)
-                    t += param(a.bias, a.w_bf16, c * VEC + e);
-                from_f32(o.v[e], t);
-            }
-            store_vec<T, VEC>(y + (int64_t)c * VEC, o);
+        for (int i = 0; i < P::NV; ++i) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (there && p.has(i, chunks))
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at + i * 512) : "memory");
+            unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), x[i]);
         }
     }
+};
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int S>
+__device__ __forceinline__ void ring_wait() // until the oldest of S - 1 rows has landed
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
 }
+
+template <typename P>
+__device__ __forceinline__ void load_row(const P &p, const typename P::T *row, bool there, int chunks, typename P::F (&x)[P::NV][P::kLanesOf])
+{
+#pragma unroll
+    for (int i = 0; i < P::NV; ++i) {
+        auto v = zero_vec<typename P::T, P::VEC>();
+        if (there && p.has(i, chunks))
+            v = load_vec<typename P::T, P::VEC>(row + (p.first + i * P::kStep) * P::VEC);
+        unpack<typename P::T, P::VEC>(v, x[i]);
+    }
+}
+
+// The most threads of a block.
+template <typename P>
+constexpr int kMostThreads = P::kBlock ? kNormDim / (32 * P::NV * P::VEC) * 32 : kThreads;
+
+// Rows of the forward ring: some 100 KB of an SM's copies in flight.
+template <typename P>
+constexpr int kForwardRows = P::VEC == 1 ? 0 : P::NV == 2 ? 4 : 3;
+
+template <typename P>
+__global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : kMostThreads<P> <= 512 ? 2 : 1) norm_kernel(const NormArgs a)
+{
+    using T = typename P::T;
+    using F = typename P::F;
+    constexpr int S = kForwardRows<P>, NV = P::NV, L = P::kLanesOf;
+    extern __shared__ __align__(16) uint8_t s_ring[];
+    __shared__ float s_part[2][32];
+    const P p;
+    const Ring<P, 1, S> ring(s_ring);
+    const int chunks = a.dim / P::VEC;
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * p.groups();
+    const float inv = 1.f / (float)a.dim;
+    auto row_x = [&](uint32_t r) { return row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads); };
+    auto ahead = [&](int slot, uint32_t r) {
+        ring.copy(p, slot, 0, row_x(r), r < rows, chunks);
+        ring_commit();
+    };
+    if (P::kBlock && threadIdx.x < 32)
+        s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = 0.f;
+    wait_for_previous();
+    let_next_start();
+    uint32_t first = blockIdx.x * p.groups();
+    if constexpr (S > 0)
+#pragma unroll 1
+        for (int s = 0; s < S - 1; ++s)
+            ahead(s, first + p.group + s * step);
+    if (P::kBlock)
+        __syncthreads();
+    int slot = 0, turn = 0;
+    // (every thread of the block takes part in the sums of every turn)
+#pragma unroll 1
+    for (; first < rows; first += step, turn ^= 1) {
+        const uint32_t row = first + p.group;
+        const bool there = P::kBlock || row < rows;
+        F d[NV][L];
+        if constexpr (S > 0) {
+            ring_wait<S>();
+            ring.read(p, slot, 0, there, chunks, d);
+            ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
+            slot = slot == S - 1 ? 0 : slot + 1;
+        } else
+            load_row(p, row_x(row), there, chunks, d);
+        float mean = 0.f;
+        if (!a.rms) {
+            F s = all_of<P::VEC>(0.f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < L; ++e)
+                    s = s + d[i][e];
+            mean = p.sum(both(s), s_part[0]) * inv;
+        }
+        const F less = all_of<P::VEC>(-mean);
+        F q = all_of<P::VEC>(0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (p.has(i, chunks))
+#pragma unroll
+                for (int e = 0; e < L; ++e) {
+                    d[i][e] = d[i][e] + less;
+                    q = fused(d[i][e], d[i][e], q);
+                }
+        // (two sums a turn, or with RMS one; rsqrtf is off by two steps of fp32 at most)
+        const float rstd = rsqrtf(p.sum(both(q), s_part[a.rms ? turn : 1]) * inv + a.eps);
+        if (!there)
+            continue;
+        if (p.leads()) {
+            if (a.mean)
+                a.mean[row] = mean;
+            if (a.rstd)
+                a.rstd[row] = rstd;
+        }
+        const F scale = all_of<P::VEC>(rstd);
+        T *const y = row_at(static_cast<T *>(a.y), a.y_token, a.y_head, row, a.heads);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (p.has(i, chunks)) {
+                const int c = (p.first + i * P::kStep) * P::VEC;
+                F f[L];
+#pragma unroll
+                for (int e = 0; e < L; ++e)
+                    d[i][e] = d[i][e] * scale;
+                if (a.weight) {
+                    load_params<P::VEC>(a.weight, a.w_bf16, c, f);
+#pragma unroll
+                    for (int e = 0; e < L; ++e)
+                        d[i][e] = d[i][e] * f[e];
+                }
+                if (a.bias) {
+                    load_params<P::VEC>(a.bias, a.w_bf16, c, f);
+#pragma unroll
+                    for (int e = 0; e < L; ++e)
+                        d[i][e] = d[i][e] + f[e];
+                }
+                store_vec<T, P::VEC>(y + c, pack<T, P::VEC>(d[i]));
+            }
+    }
+}
+
+constexpr int rows_that_fit(size_t smem, size_t row) { return smem / row < 6 ? (int)(smem / row) : 6; }
+
+// Blocks of the backward kernel on an SM, and rows of its ring (of two arrays;
+// none where fewer than two fit), for blocks of up to THREADS threads.
+template <int THREADS>
+constexpr int kBackwardBlocks = THREADS <= 320 ? 2 : 1;
+template <typename P, int THREADS>
+constexpr int kBackwardRows = P::VEC == 1 || THREADS > 512 ? 0
+                              : rows_that_fit(kMostSmem / kBackwardBlocks<THREADS>, P::NV * 2 * 16 * THREADS);
 
 // Blocks take rows in turn; a thread keeps its columns.  Partial sums of the
 // weight's gradient: a.partial [blocks][2][dim].
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(1024) norm_grad_kernel(const NormGradArgs a, int tpr)
+template <typename P, int THREADS>
+__global__ void __launch_bounds__(THREADS, kBackwardBlocks<THREADS>) norm_grad_kernel(const NormGradArgs a)
 {
-    extern __shared__ float s_sums[];        // [groups][2][dim] where a block has several groups
-    __shared__ float s_part[32];
-    const int groups = blockDim.x / tpr, group = threadIdx.x / tpr, lane = threadIdx.x - group * tpr;
-    const int chunks = a.dim / VEC;
+    using T = typename P::T;
+    using F = typename P::F;
+    constexpr int S = kBackwardRows<P, THREADS>, NV = P::NV, L = P::kLanesOf;
+    extern __shared__ __align__(16) uint8_t s_ring[];    // after the last row: [groups][2][dim] sums where a block has several groups
+    __shared__ Pair s_part[2][32];
+    const P p;
+    const Ring<P, 2, S> ring(s_ring);
+    const int chunks = a.dim / P::VEC, groups = p.groups();
+    const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * groups;
     const float inv = 1.f / (float)a.dim;
+    auto row_x = [&](uint32_t r) { return row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads); };
+    auto row_dy = [&](uint32_t r) { return row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, r, a.heads); };
+    auto ahead = [&](int slot, uint32_t r) {
+        ring.copy(p, slot, 0, row_x(r), r < rows, chunks);
+        ring.copy(p, slot, 1, row_dy(r), r < rows, chunks);
+        ring_commit();
+    };
+    if (P::kBlock && threadIdx.x < 32)
+        s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = {0.f, 0.f};
     wait_for_previous();
     let_next_start();
-    float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+    uint32_t first = blockIdx.x * groups;
+    if constexpr (S > 0)
+#pragma unroll 1
+        for (int s = 0; s < S - 1; ++s)
+            ahead(s, first + p.group + s * step);
+    F dw[NV][L], db[NV][L];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const int c = lane + i * tpr;
-            w[i][e] = a.weight && c < chunks ? param(a.weight, a.w_bf16, c * VEC + e) : 1.f;
-            dw[i][e] = db[i][e] = 0.f;
+        for (int e = 0; e < L; ++e)
+            dw[i][e] = db[i][e] = all_of<P::VEC>(0.f);
+    // (a row's statistics are loaded one row ahead)
+    float next_rstd = 0.f, next_mean = 0.f;
+    auto stats = [&](uint32_t r) {
+        if (r < rows) {
+            next_rstd = a.rstd[r];
+            next_mean = a.rms ? 0.f : a.mean[r];
         }
+    };
+    stats(first + p.group);
+    if (P::kBlock)
+        __syncthreads();
+    int slot = 0, turn = 0;
     // (every thread of the block takes part in the sums of every turn)
-    for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += (int64_t)gridDim.x * groups) {
-        const int64_t row = first + group;
-        const bool there = row < a.rows;
-        const int64_t r = there ? row : 0;
-        const T *const x = static_cast<const T *>(a.x) + row_at({a.x_token, a.x_head}, r, a.heads);
-        const T *const dy = static_cast<const T *>(a.dy) + row_at({a.dy_token, a.dy_head}, r, a.heads);
-        const float rstd = a.rstd[r], mean = a.rms ? 0.f : a.mean[r];
-        Vec<T, VEC> vx[NV], vd[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = lane + i * tpr;
-            const bool in = there && c < chunks;
-            vx[i] = in ? load_vec<T, VEC>(x + (int64_t)c * VEC) : zero_vec<T, VEC>();
-            vd[i] = in ? load_vec<T, VEC>(dy + (int64_t)c * VEC) : zero_vec<T, VEC>();
+#pragma unroll 1
+    for (; first < rows; first += step, turn ^= 1) {
+        const uint32_t row = first + p.group;
+        const bool there = P::kBlock || row < rows;
+        const F less = all_of<P::VEC>(-next_mean);
+        const float rstd = next_rstd;
+        const F scale = all_of<P::VEC>(rstd);
+        stats(row + step);
+        F h[NV][L], g[NV][L];
+        if constexpr (S > 0) {
+            ring_wait<S>();
+            ring.read(p, slot, 0, there, chunks, h);
+            ring.read(p, slot, 1, there, chunks, g);
+            ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
+            slot = slot == S - 1 ? 0 : slot + 1;
+        } else {
+            load_row(p, row_x(row), there, chunks, h);
+            load_row(p, row_dy(row), there, chunks, g);
         }
-        float sg = 0.f, sh = 0.f;
+        F sg = all_of<P::VEC>(0.f), sh = sg;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (there && lane + i * tpr < chunks)
+            if (there && p.has(i, chunks)) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = to_f32(vd[i].v[e]), h = (to_f32(vx[i].v[e]) - mean) * rstd, g = d * w[i][e];
-                    dw[i][e] += d * h;
-                    db[i][e] += d;
-                    sg += g;
-                    sh += g * h;
+                for (int e = 0; e < L; ++e) {
+                    h[i][e] = (h[i][e] + less) * scale;
+                    dw[i][e] = fused(g[i][e], h[i][e], dw[i][e]);
+                    db[i][e] = db[i][e] + g[i][e];
                 }
-        const float mh = row_sum(sh, tpr, s_part) * inv;
-        const float mg = a.rms ? 0.f : row_sum(sg, tpr, s_part) * inv;
-        T *const dx = static_cast<T *>(a.dx) + row_at({a.dx_token, a.dx_head}, r, a.heads);
+                if (a.weight) {
+                    F w[L];
+                    load_params<P::VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * P::VEC, w);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = lane + i * tpr;
-            if (there && c < chunks) {
-                Vec<T, VEC> o;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float h = (to_f32(vx[i].v[e]) - mean) * rstd, g = to_f32(vd[i].v[e]) * w[i][e];
-                    from_f32(o.v[e], (g - mg - h * mh) * rstd);
+                    for (int e = 0; e < L; ++e)
+                        g[i][e] = g[i][e] * w[e];
                 }
-                store_vec<T, VEC>(dx + (int64_t)c * VEC, o);
+#pragma unroll
+                for (int e = 0; e < L; ++e) {
+                    sg = sg + g[i][e];
+                    sh = fused(g[i][e], h[i][e], sh);
+                }
             }
-        }
+        const Pair s = p.sum(Pair{both(sg), both(sh)}, s_part[turn]);
+        if (!there)
+            continue;
+        // (g - mean g - h mean(g h)) rstd
+        const F to_g = all_of<P::VEC>(a.rms ? 0.f : -(s.x * inv) * rstd), to_h = all_of<P::VEC>(-(s.y * inv) * rstd);
+        T *const dx = row_at(static_cast<T *>(a.dx), a.dx_token, a.dx_head, row, a.heads);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (p.has(i, chunks)) {
+#pragma unroll
+                for (int e = 0; e < L; ++e)
+                    g[i][e] = fused(h[i][e], to_h, fused(g[i][e], scale, to_g));
+                store_vec<T, P::VEC>(dx + (p.first + i * P::kStep) * P::VEC, pack<T, P::VEC>(g[i]));
+            }
     }
     if (!a.partial)
         return;
     float *const out = a.partial + (int64_t)blockIdx.x * 2 * a.dim;
-    float *const to = groups > 1 ? s_sums + (int64_t)group * 2 * a.dim : out;
+    float *const s_sums = reinterpret_cast<float *>(s_ring);
+    if (groups > 1) {
+        if constexpr (S > 0)
+            asm volatile("cp.async.wait_all;" ::: "memory");   // (the sums take the ring's place)
+        __syncthreads();
+    }
+    float *const to = groups > 1 ? s_sums + p.group * 2 * a.dim : out;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
+        if (p.has(i, chunks)) {
+            const int c = (p.first + i * P::kStep) * P::VEC;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const int c = lane + i * tpr;
-            if (c < chunks) {
-                to[c * VEC + e] = dw[i][e];
-                to[a.dim + c * VEC + e] = db[i][e];
+            for (int e = 0; e < L; ++e) {
+                *reinterpret_cast<F *>(to + c + e * (P::VEC / L)) = dw[i][e];
+                *reinterpret_cast<F *>(to + a.dim + c + e * (P::VEC / L)) = db[i][e];
             }
         }
     if (groups > 1) {
@@ -212,7 +415,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(const NormGradArgs a, i
         for (int i = threadIdx.x; i < 2 * a.dim; i += blockDim.x) {
             float s = 0.f;
             for (int g = 0; g < groups; ++g)
-                s += s_sums[(int64_t)g * 2 * a.dim + i];
+                s += s_sums[g * 2 * a.dim + i];
             out[i] = s;
         }
     }
@@ -229,6 +432,7 @@ __global__ void __launch_bounds__(256) norm_sum_kernel(const float *partial, int
     let_next_start();
     float v = 0.f;
     if (i < 2 * dim)
+#pragma unroll 8
         for (int p = warp; p < parts; p += 8)
             v += partial[(int64_t)p * 2 * dim + i];
     s[warp][lane] = v;
@@ -245,65 +449,93 @@ __global__ void __launch_bounds__(256) norm_sum_kernel(const float *partial, int
     }
 }
 
-// Threads of a row: the fewest (a power of two up to a warp, else whole
-// warps) that hold `chunks` in at most `most` chunks each.
-int threads_per_row(int chunks, int most)
-{
-    const int need = (chunks + most - 1) / most;
-    if (need > 32)
-        return (need + 31) / 32 * 32;
-    int t = 1;
-    while (t < need)
-        t *= 2;
-    return t;
-}
-
-// The smallest power of two of chunks a thread.
-int chunks_per_thread(int chunks, int tpr)
-{
-    int n = 1;
-    while (n * tpr < chunks)
-        n *= 2;
-    return n;
-}
-
-// Blocks of the persistent kernel, at most: its parts are the workspace.
+// Blocks of the backward kernel, at most: its parts are the workspace.
 int most_parts() { return 2 * num_sms(); }
+
+// Calls go(split) with the way a row of `chunks` lies over threads: a few
+// lanes with two chunks each, a warp, or a block whose warps take 32 NV
+// chunks each.
+template <typename T, int VEC, int NV, typename G>
+cudaError_t with_split(int chunks, G &&go)
+{
+    if (chunks > 32 * NV)
+        return go((Split<T, VEC, NV, 64> *)nullptr);
+    if (VEC == 1 && chunks > 128)
+        return go((Split<T, VEC, NV, 32> *)nullptr);
+    if (NV > 2 && chunks > 64)
+        return go((Split<T, VEC, (NV > 4 ? 4 : NV), 32> *)nullptr);
+    if (chunks > 32)
+        return go((Split<T, VEC, 2, 32> *)nullptr);
+    if (chunks > 16)
+        return go((Split<T, VEC, 2, 16> *)nullptr);
+    if (chunks > 8)
+        return go((Split<T, VEC, 2, 8> *)nullptr);
+    if (chunks > 2)
+        return go((Split<T, VEC, 2, 4> *)nullptr);
+    return go((Split<T, VEC, 2, 1> *)nullptr);
+}
+
+template <typename P>
+int threads_of(int chunks)
+{
+    return P::kBlock ? (chunks + 32 * P::NV - 1) / (32 * P::NV) * 32 : kThreads;
+}
 
 template <typename T, int VEC, int MOST>
 cudaError_t launch_forward(const NormArgs &a, cudaStream_t st)
 {
-    const int chunks = a.dim / VEC, tpr = threads_per_row(chunks, MOST), nv = chunks_per_thread(chunks, tpr);
-    const int groups = tpr >= kThreads ? 1 : kThreads / tpr;
-    const dim3 grid((unsigned)((a.rows + groups - 1) / groups));
-    auto go = [&](auto kern) { return launch_early(kern, grid, groups * tpr, 0, st, 1, a, tpr); };
-    switch (nv) {
-    case 1: return go(norm_kernel<T, VEC, 1>);
-    case 2: return go(norm_kernel<T, VEC, 2>);
-    case 4: return go(norm_kernel<T, VEC, 4>);
-    case 8: return go(norm_kernel<T, VEC, 8>);
-    default: return go(norm_kernel<T, VEC, 16>);
-    }
+    return with_split<T, VEC, MOST>(a.dim / VEC, [&](auto split) -> cudaError_t {
+        using P = std::remove_pointer_t<decltype(split)>;
+        const int threads = threads_of<P>(a.dim / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
+        const int64_t turns = (a.rows + groups - 1) / groups;
+        const size_t smem = Ring<P, 1, kForwardRows<P>>::bytes(threads);
+        int64_t blocks = turns;              // (loaded at once: a block for each turn)
+        if (smem > 0) {
+            static PerDevice<bool> allowed;
+            if (smem > kPlainSmem)
+                if (cudaError_t e = allow_smem((const void *)norm_kernel<P>, (int)kMostSmem, allowed))
+                    return e;
+            const int64_t most = (int64_t)num_sms() * max(1, min(1024 / threads, (int)(kMostSmem / smem)));
+            blocks = turns < most ? turns : most;
+        }
+        return launch_early(norm_kernel<P>, dim3((unsigned)blocks), threads, smem, st, 1, a);
+    });
+}
+
+template <typename P, int THREADS>
+cudaError_t launch_backward_of(const NormGradArgs &a, int threads, int blocks, cudaStream_t st)
+{
+    const int groups = P::kBlock ? 1 : threads / P::TPR;
+    const size_t parts = a.partial && groups > 1 ? (size_t)groups * 2 * a.dim * sizeof(float) : 0;
+    const size_t rows = Ring<P, 2, kBackwardRows<P, THREADS>>::bytes(threads), smem = rows > parts ? rows : parts;
+    static PerDevice<bool> allowed;
+    if (smem > kPlainSmem)
+        if (cudaError_t e = allow_smem((const void *)norm_grad_kernel<P, THREADS>, (int)kMostSmem, allowed))
+            return e;
+    return launch_early(norm_grad_kernel<P, THREADS>, dim3((unsigned)blocks), threads, smem, st, 1, a);
 }
 
 template <typename T, int VEC, int MOST>
 cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
 {
     NormGradArgs a = given;
-    const int chunks = a.dim / VEC, tpr = threads_per_row(chunks, MOST), nv = chunks_per_thread(chunks, tpr);
-    const int groups = tpr >= kThreads ? 1 : kThreads / tpr;
-    const int64_t turns = (a.rows + groups - 1) / groups;
     const bool sums = a.dweight || a.dbias;
     a.partial = sums ? static_cast<float *>(a.workspace) : nullptr;
-    const int blocks = (int)(turns < most_parts() ? turns : most_parts());
-    if (blocks > 0) {
-        const size_t smem = sums && groups > 1 ? (size_t)groups * 2 * a.dim * sizeof(float) : 0;
-        auto go = [&](auto kern) { return launch_early(kern, dim3((unsigned)blocks), groups * tpr, smem, st, 1, a, tpr); };
-        const cudaError_t e = nv == 1   ? go(norm_grad_kernel<T, VEC, 1>)
-                              : nv == 2 ? go(norm_grad_kernel<T, VEC, 2>)
-                              : nv == 4 ? go(norm_grad_kernel<T, VEC, (MOST >= 4 ? 4 : 1)>)
-                              : nv == 8 ? go(norm_grad_kernel<T, VEC, (MOST >= 8 ? 8 : 1)>)
-                                        : go(norm_grad_kernel<T, VEC, (MOST >= 16 ? 16 : 1)>);
+    int blocks = 0;
+    if (a.rows > 0) {
+        const cudaError_t e = with_split<T, VEC, MOST>(a.dim / VEC, [&](auto split) -> cudaError_t {
+            using P = std::remove_pointer_t<decltype(split)>;
+            const int threads = threads_of<P>(a.dim / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
+            const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * (threads <= 320 ? 2 : 1);
+            blocks = (int)(turns < most ? turns : most);
+            if constexpr (P::kBlock) {
+                if (threads > 512)
+                    return launch_backward_of<P, 1024>(a, threads, blocks, st);
+                if (threads > 320)
+                    return launch_backward_of<P, 512>(a, threads, blocks, st);
+            }
+            return launch_backward_of<P, 320>(a, threads, blocks, st);
+        });
         if (e != cudaSuccess)
             return e;
     }
@@ -324,15 +556,20 @@ cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
     const bool w = wide(a.x_token | a.x_head | a.y_token | a.y_head | a.dim, a.bf16);
     if (a.bf16)
         return w ? launch_forward<__nv_bfloat16, 8, 4>(a, st) : launch_forward<__nv_bfloat16, 1, 16>(a, st);
-    return w ? launch_forward<float, 4, 8>(a, st) : launch_forward<float, 1, 16>(a, st);
+    return w ? launch_forward<float, 4, 4>(a, st) : launch_forward<float, 1, 16>(a, st);
 }
 
 cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st)
 {
     const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16);
+    // (not whole 16-byte chunks: 8 elements a thread as long as 512 threads hold the row)
     if (a.bf16)
-        return w ? launch_backward<__nv_bfloat16, 8, 2>(a, st) : launch_backward<__nv_bfloat16, 1, 16>(a, st);
-    return w ? launch_backward<float, 4, 4>(a, st) : launch_backward<float, 1, 16>(a, st);
+        return w                ? launch_backward<__nv_bfloat16, 8, 2>(a, st)
+               : a.dim <= 4096 ? launch_backward<__nv_bfloat16, 1, 8>(a, st)
+                               : launch_backward<__nv_bfloat16, 1, 16>(a, st);
+    return w                ? launch_backward<float, 4, 4>(a, st)
+           : a.dim <= 4096 ? launch_backward<float, 1, 8>(a, st)
+                           : launch_backward<float, 1, 16>(a, st);
 }
 
 } // namespace rfq

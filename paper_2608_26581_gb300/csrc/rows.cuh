@@ -5,6 +5,9 @@
 
 #include <cuda_bf16.h>
 #include <cstdint>
+#include <type_traits>
+
+#include "mxfp4_math.cuh"
 
 namespace rfq {
 
@@ -39,6 +42,81 @@ __device__ __forceinline__ Vec<T, VEC> zero_vec()
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
         from_f32(v.v[e], 0.f);
+    return v;
+}
+
+// Two fp32 values in one register pair, each operation one instruction.
+struct F2 {
+    uint64_t v;
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b)
+{
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { return {fmul2(a.v, b.v)}; }
+__device__ __forceinline__ F2 fused(F2 a, F2 b, F2 c) { return {ffma2(a.v, b.v, c.v)}; }
+__device__ __forceinline__ float fused(float a, float b, float c) { return fmaf(a, b, c); }
+__device__ __forceinline__ float both(float a) { return a; }
+__device__ __forceinline__ float both(F2 a)
+{
+    float x, y;
+    f2unpack(a.v, x, y);
+    return x + y;
+}
+
+// The values of a vector of VEC elements in fp32: pairs where VEC is even,
+// single ones for VEC = 1.
+template <int VEC>
+using Lane = std::conditional_t<VEC == 1, float, F2>;
+template <int VEC>
+constexpr int kLanes = VEC == 1 ? 1 : VEC / 2;
+
+template <int VEC>
+__device__ __forceinline__ Lane<VEC> all_of(float v)
+{
+    if constexpr (VEC == 1)
+        return v;
+    else
+        return {f2pack(v, v)};
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void unpack(const Vec<T, VEC> &v, Lane<VEC> *x)
+{
+    if constexpr (VEC == 1)
+        x[0] = to_f32(v.v[0]);
+    else if constexpr (std::is_same_v<T, float>) {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i)
+            x[i] = {f2pack(v.v[2 * i], v.v[2 * i + 1])};
+    } else {
+        const uint32_t *const w = reinterpret_cast<const uint32_t *>(&v);
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i)
+            x[i] = {f2pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u))};
+    }
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> pack(const Lane<VEC> *x)
+{
+    Vec<T, VEC> v;
+    if constexpr (VEC == 1)
+        from_f32(v.v[0], x[0]);
+    else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            float a, b;
+            f2unpack(x[i].v, a, b);
+            if constexpr (std::is_same_v<T, float>) {
+                v.v[2 * i] = a;
+                v.v[2 * i + 1] = b;
+            } else
+                reinterpret_cast<__nv_bfloat162 *>(&v)[i] = __floats2bfloat162_rn(a, b);
+        }
+    }
     return v;
 }
 

@@ -612,26 +612,39 @@ def rfq_matvec(x: torch.Tensor, wq: QTensor, y: torch.Tensor, stream=None):
 
 # ---- around a mixture-of-experts block: norms, the router, rows to experts and back
 
-def _device_call(call: str, f, args, stream, *tensors):
-    """Runs f(*args, stream) on the device that every tensor (None: left out) lies on."""
-    dev = tensors[0].device
-    _want(dev.type == "cuda", call, "tensors must be on a CUDA device")
-    for t in tensors:
-        _want(t is None or t.device == dev, call, "tensors must be on one device")
-    if dev.index == torch.cuda.current_device():
-        _check(f(*args, _raw_stream(stream, tensors[0])), call)
+def _on_device(call: str, t: torch.Tensor, *others: torch.Tensor | None) -> int:
+    """The device of t, on which every other tensor lies too (None: left out)."""
+    dev = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            raise ValueError(f"{call}: tensors must be on one device")
+    if dev < 0:
+        raise ValueError(f"{call}: tensors must be on a CUDA device")
+    return dev
+
+
+def _launch(call: str, f, dev: int, stream, *args):
+    """f(*args, stream) with `dev` the current device; stream: the caller's, or the device's current one."""
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
+    if dev == torch._C._cuda_getDevice():
+        status = f(*args, int(stream))
     else:
         with torch.cuda.device(dev):
-            _check(f(*args, _raw_stream(stream, tensors[0])), call)
+            status = f(*args, int(stream))
+    if status != RFQ_OK:
+        raise RFQError(status, call)
 
 
 def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _dense(dtype, n: int, *tensors) -> bool:
-    """Every tensor (None: left out) is contiguous, of that type and of n elements."""
-    return all(t is None or (t.dtype is dtype and t.numel() == n and t.is_contiguous()) for t in tensors)
+def _is(t: torch.Tensor | None, dtype, n: int) -> bool:
+    """t is contiguous, of that type and of n elements (or None)."""
+    return t is None or (t.dtype is dtype and t.numel() == n and t.is_contiguous())
 
 
 def _rows3(t: torch.Tensor):
@@ -651,7 +664,7 @@ def _norm_params(call: str, dim: int, weight, bias) -> int:
     if w is None:
         return RFQ_OUT_F32
     dtype = _DTYPES.get(w.dtype)
-    _want(dtype is not None and _dense(w.dtype, dim, weight, bias), call,
+    _want(dtype is not None and _is(weight, w.dtype, dim) and _is(bias, w.dtype, dim), call,
           "weight and bias are contiguous [dim] tensors, fp32 or bf16 alike")
     return dtype
 
@@ -671,10 +684,11 @@ def rfq_norm(x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = Non
     (xt, xh, xd), (yt, yh, yd) = _strides(x3), _strides(y3)
     _want((xd == 1 and yd == 1) or D == 1, "rfq_norm", "the elements of a row must be contiguous")
     w_dtype = _norm_params("rfq_norm", D, weight, bias)
-    _want(_dense(torch.float32, T * H, mean, rstd), "rfq_norm", "mean and rstd are contiguous fp32, one element a row")
-    _device_call("rfq_norm", load_library().rfq_norm,
-                 (x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, dtype, T, H, D, kind, eps, _at(weight), _at(bias), w_dtype,
-                  _at(mean), _at(rstd)), stream, x, y, weight, bias, mean, rstd)
+    _want(_is(mean, torch.float32, T * H) and _is(rstd, torch.float32, T * H), "rfq_norm",
+          "mean and rstd are contiguous fp32, one element a row")
+    dev = _on_device("rfq_norm", x, y, weight, bias, mean, rstd)
+    _launch("rfq_norm", load_library().rfq_norm, dev, stream, x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, dtype,
+            T, H, D, kind, eps, _at(weight), _at(bias), w_dtype, _at(mean), _at(rstd))
 
 
 _norm_ws: dict[tuple[int, int], int] = {}     # workspace bytes by device and dim
@@ -710,8 +724,10 @@ def rfq_norm_grad(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, dx: tor
     (dt, dh, dd), (xt, xh, xd), (ot, oh, od) = _strides(_rows3(dy)), _strides(x3), _strides(_rows3(dx))
     _want((dd == 1 and xd == 1 and od == 1) or D == 1, "rfq_norm_grad", "the elements of a row must be contiguous")
     w_dtype = _norm_params("rfq_norm_grad", D, weight, None)
-    _want(_dense(torch.float32, T * H, mean, rstd), "rfq_norm_grad", "mean and rstd are contiguous fp32, one element a row")
-    _want(_dense(torch.float32, D, dweight, dbias), "rfq_norm_grad", "dweight and dbias are contiguous fp32 [dim] tensors")
+    _want(_is(mean, torch.float32, T * H) and _is(rstd, torch.float32, T * H), "rfq_norm_grad",
+          "mean and rstd are contiguous fp32, one element a row")
+    _want(_is(dweight, torch.float32, D) and _is(dbias, torch.float32, D), "rfq_norm_grad",
+          "dweight and dbias are contiguous fp32 [dim] tensors")
     if dweight is not None or dbias is not None:
         key = (x.device.index, D)
         if key not in _norm_ws and x.device.type == "cuda":
@@ -720,10 +736,10 @@ def rfq_norm_grad(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, dx: tor
         _want(workspace is not None and workspace.is_contiguous() and
               workspace.numel() * workspace.element_size() >= _norm_ws.get(key, 0), "rfq_norm_grad",
               "the workspace is smaller than rfq_norm_grad_workspace_bytes")
-    _device_call("rfq_norm_grad", load_library().rfq_norm_grad,
-                 (dy.data_ptr(), dt, dh, x.data_ptr(), xt, xh, dx.data_ptr(), ot, oh, dtype, T, H, D, kind, _at(mean),
-                  _at(rstd), _at(weight), w_dtype, _at(dweight), _at(dbias), _at(workspace)), stream, x, dy, dx, rstd,
-                 mean, weight, dweight, dbias, workspace)
+    dev = _on_device("rfq_norm_grad", x, dy, dx, rstd, mean, weight, dweight, dbias, workspace)
+    _launch("rfq_norm_grad", load_library().rfq_norm_grad, dev, stream, dy.data_ptr(), dt, dh, x.data_ptr(), xt,
+            xh, dx.data_ptr(), ot, oh, dtype, T, H, D, kind, _at(mean), _at(rstd), _at(weight), w_dtype,
+            _at(dweight), _at(dbias), _at(workspace))
 
 
 def rfq_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, normalize: bool = True, stream=None):
@@ -734,12 +750,12 @@ def rfq_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, no
     _want(dtype is not None, "rfq_route", "logits are fp32 or bf16")
     row = _rows2(logits, "rfq_route")
     T, E = logits.shape
-    _want(ids.dim() == 2 and ids.shape[0] == T and weights.shape == ids.shape and _dense(torch.int32, ids.numel(), ids) and
-          _dense(torch.float32, ids.numel(), weights), "rfq_route",
+    _want(ids.dim() == 2 and ids.shape[0] == T and weights.shape == ids.shape and _is(ids, torch.int32, ids.numel()) and
+          _is(weights, torch.float32, ids.numel()), "rfq_route",
           "ids (int32) and weights (fp32) are contiguous [tokens, top_k]")
-    _device_call("rfq_route", load_library().rfq_route,
-                 (logits.data_ptr(), row, dtype, T, E, ids.shape[1], 1 if normalize else 0, ids.data_ptr(),
-                  weights.data_ptr()), stream, logits, ids, weights)
+    dev = _on_device("rfq_route", logits, ids, weights)
+    _launch("rfq_route", load_library().rfq_route, dev, stream, logits.data_ptr(), row, dtype, T, E,
+            ids.shape[1], 1 if normalize else 0, ids.data_ptr(), weights.data_ptr())
 
 
 def rfq_route_grad(logits: torch.Tensor, ids: torch.Tensor, dweights: torch.Tensor, dlogits: torch.Tensor,
@@ -751,12 +767,13 @@ def rfq_route_grad(logits: torch.Tensor, ids: torch.Tensor, dweights: torch.Tens
           "logits and dlogits are fp32 or bf16 and of one shape")
     row, out_row = _rows2(logits, "rfq_route_grad"), _rows2(dlogits, "rfq_route_grad")
     T, E = logits.shape
-    _want(ids.dim() == 2 and ids.shape[0] == T and dweights.shape == ids.shape and _dense(torch.int32, ids.numel(), ids) and
-          _dense(torch.float32, ids.numel(), dweights), "rfq_route_grad",
+    _want(ids.dim() == 2 and ids.shape[0] == T and dweights.shape == ids.shape and _is(ids, torch.int32, ids.numel()) and
+          _is(dweights, torch.float32, ids.numel()), "rfq_route_grad",
           "ids (int32) and dweights (fp32) are contiguous [tokens, top_k]")
-    _device_call("rfq_route_grad", load_library().rfq_route_grad,
-                 (logits.data_ptr(), row, dtype, T, E, ids.shape[1], 1 if normalize else 0, ids.data_ptr(),
-                  dweights.data_ptr(), dlogits.data_ptr(), out_row), stream, logits, ids, dweights, dlogits)
+    dev = _on_device("rfq_route_grad", logits, ids, dweights, dlogits)
+    _launch("rfq_route_grad", load_library().rfq_route_grad, dev, stream, logits.data_ptr(), row, dtype, T, E,
+            ids.shape[1], 1 if normalize else 0, ids.data_ptr(), dweights.data_ptr(), dlogits.data_ptr(),
+            out_row)
 
 
 def rfq_moe_rows(tokens: int, top_k: int, experts: int, align: int = 128) -> int:
@@ -773,20 +790,20 @@ def rfq_moe_sort(ids: torch.Tensor, group_off: torch.Tensor, row_of: torch.Tenso
     256 bytes, zeroed once, for the device status (see include/rfq.h)."""
     i32 = torch.int32
     _want(ids.dim() == 2 and row_of.shape == ids.shape and group_off.numel() >= 1 and
-          _dense(i32, ids.numel(), ids, row_of) and _dense(i32, group_off.numel(), group_off) and
-          _dense(i32, pair_of.numel(), pair_of), "rfq_moe_sort",
+          _is(ids, i32, ids.numel()) and _is(row_of, i32, ids.numel()) and _is(group_off, i32, group_off.numel()) and
+          _is(pair_of, i32, pair_of.numel()), "rfq_moe_sort",
           "ids and row_of are [tokens, top_k], group_off [experts + 1], pair_of [rows], contiguous int32")
     _want(workspace.numel() * workspace.element_size() >= 256, "rfq_moe_sort", "the workspace is 256 bytes")
-    _device_call("rfq_moe_sort", load_library().rfq_moe_sort,
-                 (ids.data_ptr(), ids.shape[0], ids.shape[1], group_off.numel() - 1, align, group_off.data_ptr(),
-                  row_of.data_ptr(), pair_of.data_ptr(), pair_of.numel(), workspace.data_ptr()), stream, ids, group_off,
-                 row_of, pair_of, workspace)
+    dev = _on_device("rfq_moe_sort", ids, group_off, row_of, pair_of, workspace)
+    _launch("rfq_moe_sort", load_library().rfq_moe_sort, dev, stream, ids.data_ptr(), ids.shape[0],
+            ids.shape[1], group_off.numel() - 1, align, group_off.data_ptr(), row_of.data_ptr(),
+            pair_of.data_ptr(), pair_of.numel(), workspace.data_ptr())
 
 
 def _moe_maps(call: str, tokens: int, rows: int, row_of: torch.Tensor, pair_of: torch.Tensor | None):
-    _want(row_of.dim() == 2 and row_of.shape[0] == tokens and _dense(torch.int32, row_of.numel(), row_of), call,
+    _want(row_of.dim() == 2 and row_of.shape[0] == tokens and _is(row_of, torch.int32, row_of.numel()), call,
           "row_of is a contiguous int32 [tokens, top_k]")
-    _want(_dense(torch.int32, rows, pair_of), call, "pair_of is a contiguous int32 [rows]")
+    _want(_is(pair_of, torch.int32, rows), call, "pair_of is a contiguous int32 [rows]")
 
 
 def rfq_moe_gather(x: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, pair_of: torch.Tensor | None = None,
@@ -800,9 +817,9 @@ def rfq_moe_gather(x: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, pai
     _want(out.dim() == 2 and out.shape[1] == x.shape[1] and out.is_contiguous(), "rfq_moe_gather",
           "out is a contiguous [rows, dim]")
     _moe_maps("rfq_moe_gather", x.shape[0], out.shape[0], row_of, pair_of)
-    _device_call("rfq_moe_gather", load_library().rfq_moe_gather,
-                 (x.data_ptr(), row, dtype, x.shape[0], x.shape[1], row_of.data_ptr(), row_of.shape[1], _at(pair_of),
-                  out.data_ptr(), out.shape[0]), stream, x, row_of, pair_of, out)
+    dev = _on_device("rfq_moe_gather", x, row_of, pair_of, out)
+    _launch("rfq_moe_gather", load_library().rfq_moe_gather, dev, stream, x.data_ptr(), row, dtype, x.shape[0],
+            x.shape[1], row_of.data_ptr(), row_of.shape[1], _at(pair_of), out.data_ptr(), out.shape[0])
 
 
 def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, weights: torch.Tensor | None = None,
@@ -816,10 +833,10 @@ def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, we
     _want(y.dim() == 2 and y.shape[1] == out.shape[1] and y.is_contiguous(), "rfq_moe_combine",
           "y is a contiguous [rows, dim]")
     _moe_maps("rfq_moe_combine", out.shape[0], y.shape[0], row_of, None)
-    _want(_dense(torch.float32, row_of.numel(), weights), "rfq_moe_combine", "weights are contiguous fp32 [tokens, top_k]")
-    _device_call("rfq_moe_combine", load_library().rfq_moe_combine,
-                 (y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(weights), out.shape[0],
-                  row_of.shape[1], out.data_ptr(), row), stream, y, row_of, weights, out)
+    _want(_is(weights, torch.float32, row_of.numel()), "rfq_moe_combine", "weights are contiguous fp32 [tokens, top_k]")
+    dev = _on_device("rfq_moe_combine", y, row_of, weights, out)
+    _launch("rfq_moe_combine", load_library().rfq_moe_combine, dev, stream, y.data_ptr(), dtype, y.shape[0],
+            y.shape[1], row_of.data_ptr(), _at(weights), out.shape[0], row_of.shape[1], out.data_ptr(), row)
 
 
 def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tensor, weights: torch.Tensor,
@@ -834,12 +851,12 @@ def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tens
     _want(y.dim() == 2 and y.shape[1] == dout.shape[1] and dy.shape == y.shape and y.is_contiguous() and
           dy.is_contiguous(), "rfq_moe_combine_grad", "y and dy are contiguous [rows, dim]")
     _moe_maps("rfq_moe_combine_grad", dout.shape[0], y.shape[0], row_of, pair_of)
-    _want(_dense(torch.float32, row_of.numel(), weights, dweights), "rfq_moe_combine_grad",
-          "weights and dweights are contiguous fp32 [tokens, top_k]")
-    _device_call("rfq_moe_combine_grad", load_library().rfq_moe_combine_grad,
-                 (dout.data_ptr(), row, y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(pair_of),
-                  weights.data_ptr(), dout.shape[0], row_of.shape[1], dy.data_ptr(), dweights.data_ptr()), stream, y,
-                 dout, row_of, pair_of, weights, dy, dweights)
+    _want(_is(weights, torch.float32, row_of.numel()) and _is(dweights, torch.float32, row_of.numel()),
+          "rfq_moe_combine_grad", "weights and dweights are contiguous fp32 [tokens, top_k]")
+    dev = _on_device("rfq_moe_combine_grad", y, dout, row_of, pair_of, weights, dy, dweights)
+    _launch("rfq_moe_combine_grad", load_library().rfq_moe_combine_grad, dev, stream, dout.data_ptr(), row,
+            y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(pair_of), weights.data_ptr(),
+            dout.shape[0], row_of.shape[1], dy.data_ptr(), dweights.data_ptr())
 
 
 def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTensor | None = None,
@@ -852,7 +869,7 @@ def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTe
     _want(xq.k == x.shape[1] and (xr is None or (xr.rows == xq.rows and xr.k == xq.k)), "rfq_moe_quantize",
           "sizes do not match")
     _moe_maps("rfq_moe_quantize", x.shape[0], xq.rows, row_of, pair_of)
-    _device_call("rfq_moe_quantize", load_library().rfq_moe_quantize,
-                 (x.data_ptr(), row, x.shape[0], row_of.data_ptr(), row_of.shape[1], _at(pair_of), xq.c(),
-                  None if xr is None else xr.c()), stream, x, row_of, pair_of, xq.codes, xq.scales,
-                 None if xr is None else xr.codes, None if xr is None else xr.scales)
+    dev = _on_device("rfq_moe_quantize", x, row_of, pair_of, xq.codes, xq.scales, None if xr is None else xr.codes,
+                     None if xr is None else xr.scales)
+    _launch("rfq_moe_quantize", load_library().rfq_moe_quantize, dev, stream, x.data_ptr(), row, x.shape[0],
+            row_of.data_ptr(), row_of.shape[1], _at(pair_of), xq.c(), None if xr is None else xr.c())
