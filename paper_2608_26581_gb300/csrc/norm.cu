@@ -115,6 +115,13 @@ __device__ __forceinline__ void load_params(const void *p, bool bf16, int c, Lan
     }
 }
 
+__device__ __forceinline__ uint4 lds128(uint32_t at)
+{
+    uint4 u;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at) : "memory");
+    return u;
+}
+
 // Rows on their way, S deep, N arrays: chunks of 16 bytes copied ahead into
 // shared memory (with S = 0 a row is loaded when its turn comes).
 template <typename P, int N, int S>
@@ -134,23 +141,19 @@ struct Ring {
             if (there && p.has(i, chunks))
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * 512), "l"(x + (p.first + i * P::kStep) * P::VEC) : "memory");
     }
-    __device__ __forceinline__ void read(const P &p, int slot, int n, bool there, int chunks, typename P::F (&x)[P::NV][P::kLanesOf]) const
+    __device__ __forceinline__ void read(int slot, int n, int i, bool there, typename P::F *x) const
     {
-        const uint32_t at = base + (slot * N + n) * row;
-#pragma unroll
-        for (int i = 0; i < P::NV; ++i) {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (there && p.has(i, chunks))
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at + i * 512) : "memory");
-            unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), x[i]);
-        }
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (there)
+            u = lds128(base + (slot * N + n) * row + i * 512);
+        unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), x);
     }
 };
 __device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int S>
-__device__ __forceinline__ void ring_wait() // until the oldest of S - 1 rows has landed
+template <int N>
+__device__ __forceinline__ void ring_wait() // until no more than N rows are on their way
 {
-    asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 template <typename P>
@@ -169,9 +172,10 @@ __device__ __forceinline__ void load_row(const P &p, const typename P::T *row, b
 template <typename P>
 constexpr int kMostThreads = P::kBlock ? kNormDim / (32 * P::NV * P::VEC) * 32 : kThreads;
 
-// Rows of the forward ring: some 100 KB of an SM's copies in flight.
+// Rows of the forward ring.  (Deeper ones take L1 from the weights: with three
+// rows of 5120 elements a layer norm of 32760 takes 116 us, with two 112.)
 template <typename P>
-constexpr int kForwardRows = P::VEC == 1 ? 0 : P::NV == 2 ? 4 : 3;
+constexpr int kForwardRows = P::VEC == 1 ? 0 : P::NV == 2 ? 4 : 2;
 
 template <typename P>
 __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : kMostThreads<P> <= 512 ? 2 : 1) norm_kernel(const NormArgs a)
@@ -210,8 +214,10 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
         const bool there = P::kBlock || row < rows;
         F d[NV][L];
         if constexpr (S > 0) {
-            ring_wait<S>();
-            ring.read(p, slot, 0, there, chunks, d);
+            ring_wait<S - 2>();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                ring.read(slot, 0, i, there && p.has(i, chunks), d[i]);
             ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
             slot = slot == S - 1 ? 0 : slot + 1;
         } else
@@ -268,41 +274,64 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
                     for (int e = 0; e < L; ++e)
                         d[i][e] = d[i][e] + f[e];
                 }
-                store_vec<T, P::VEC>(y + c, pack<T, P::VEC>(d[i]));
+                store_once<T, P::VEC>(y + c, pack<T, P::VEC>(d[i]));
             }
     }
 }
 
-constexpr int rows_that_fit(size_t smem, size_t row) { return smem / row < 6 ? (int)(smem / row) : 6; }
-
-// Blocks of the backward kernel on an SM, and rows of its ring (of two arrays;
-// none where fewer than two fit), for blocks of up to THREADS threads.
-template <int THREADS>
-constexpr int kBackwardBlocks = THREADS <= 320 ? 2 : 1;
+// The backward kernel for blocks of up to THREADS threads: blocks on an SM,
+// rows of its ring (of two arrays; none without 16-byte chunks), and whether a
+// row is read from the ring a second time for dx instead of staying in
+// registers (where 64 of them have to do).
 template <typename P, int THREADS>
-constexpr int kBackwardRows = P::VEC == 1 || THREADS > 512 ? 0
-                              : rows_that_fit(kMostSmem / kBackwardBlocks<THREADS>, P::NV * 2 * 16 * THREADS);
+struct Backward {
+    static constexpr int kBlocks = THREADS <= 320 ? 2 : 1;
+    static constexpr bool kTwice = P::VEC > 1 && THREADS > 512;
+    static constexpr size_t kRow = (size_t)P::NV * 2 * 16;    // bytes of a thread
+    static constexpr int rows()
+    {
+        const size_t n = kMostSmem / kBlocks / THREADS / kRow, most = P::kBlock ? 2 : 3;
+        return P::VEC == 1 ? 0 : (int)(n < most ? n : most);
+    }
+    static constexpr int kRows = rows();
+    static_assert(P::VEC == 1 || kRows >= (kTwice ? 1 : 2), "a row on its way beside one that has been read");
+    static constexpr size_t bytes(int threads) { return kRows * kRow * threads; }
+};
+
+template <int VEC>
+__device__ __forceinline__ void store_sums(float *to, const Lane<VEC> *v)
+{
+    if constexpr (VEC == 1)
+        *to = v[0];
+    else
+#pragma unroll
+        for (int e = 0; e < kLanes<VEC>; e += 2)
+            *reinterpret_cast<ulonglong2 *>(to + 2 * e) = {v[e].v, v[e + 1].v};
+}
+
+// Columns of a part in the workspace: whole 16-byte words.
+__host__ __device__ __forceinline__ int padded_dim(int dim) { return (dim + 3) / 4 * 4; }
 
 // Blocks take rows in turn; a thread keeps its columns.  Partial sums of the
-// weight's gradient: a.partial [blocks][2][dim].
+// weight's gradient: a.partial [blocks][2][padded dim].
 template <typename P, int THREADS>
-__global__ void __launch_bounds__(THREADS, kBackwardBlocks<THREADS>) norm_grad_kernel(const NormGradArgs a)
+__global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_grad_kernel(const NormGradArgs a)
 {
     using T = typename P::T;
     using F = typename P::F;
-    constexpr int S = kBackwardRows<P, THREADS>, NV = P::NV, L = P::kLanesOf;
-    extern __shared__ __align__(16) uint8_t s_ring[];    // after the last row: [groups][2][dim] sums where a block has several groups
+    using B = Backward<P, THREADS>;
+    constexpr int S = B::kRows, NV = P::NV, L = P::kLanesOf, VEC = P::VEC;
+    constexpr bool TWICE = B::kTwice;
+    extern __shared__ __align__(16) uint8_t smem[];      // ring; after the last row: [groups][2][padded dim] sums where a block has several groups
     __shared__ Pair s_part[2][32];
     const P p;
-    const Ring<P, 2, S> ring(s_ring);
-    const int chunks = a.dim / P::VEC, groups = p.groups();
+    const Ring<P, 2, S> ring(smem);
+    const int chunks = a.dim / VEC, groups = p.groups();
     const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * groups;
     const float inv = 1.f / (float)a.dim;
-    auto row_x = [&](uint32_t r) { return row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads); };
-    auto row_dy = [&](uint32_t r) { return row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, r, a.heads); };
     auto ahead = [&](int slot, uint32_t r) {
-        ring.copy(p, slot, 0, row_x(r), r < rows, chunks);
-        ring.copy(p, slot, 1, row_dy(r), r < rows, chunks);
+        ring.copy(p, slot, 0, row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads), r < rows, chunks);
+        ring.copy(p, slot, 1, row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, r, a.heads), r < rows, chunks);
         ring_commit();
     };
     if (P::kBlock && threadIdx.x < 32)
@@ -312,14 +341,15 @@ __global__ void __launch_bounds__(THREADS, kBackwardBlocks<THREADS>) norm_grad_k
     uint32_t first = blockIdx.x * groups;
     if constexpr (S > 0)
 #pragma unroll 1
-        for (int s = 0; s < S - 1; ++s)
+        for (int s = 0; s < (TWICE ? S : S - 1); ++s)
             ahead(s, first + p.group + s * step);
     F dw[NV][L], db[NV][L];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
 #pragma unroll
         for (int e = 0; e < L; ++e)
-            dw[i][e] = db[i][e] = all_of<P::VEC>(0.f);
+            dw[i][e] = db[i][e] = all_of<VEC>(0.f);
+    }
     // (a row's statistics are loaded one row ahead)
     float next_rstd = 0.f, next_mean = 0.f;
     auto stats = [&](uint32_t r) {
@@ -337,120 +367,162 @@ __global__ void __launch_bounds__(THREADS, kBackwardBlocks<THREADS>) norm_grad_k
     for (; first < rows; first += step, turn ^= 1) {
         const uint32_t row = first + p.group;
         const bool there = P::kBlock || row < rows;
-        const F less = all_of<P::VEC>(-next_mean);
+        const F less = all_of<VEC>(-next_mean);
         const float rstd = next_rstd;
-        const F scale = all_of<P::VEC>(rstd);
+        const F scale = all_of<VEC>(rstd);
         stats(row + step);
-        F h[NV][L], g[NV][L];
-        if constexpr (S > 0) {
-            ring_wait<S>();
-            ring.read(p, slot, 0, there, chunks, h);
-            ring.read(p, slot, 1, there, chunks, g);
-            ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
-            slot = slot == S - 1 ? 0 : slot + 1;
-        } else {
-            load_row(p, row_x(row), there, chunks, h);
-            load_row(p, row_dy(row), there, chunks, g);
-        }
-        F sg = all_of<P::VEC>(0.f), sh = sg;
+        constexpr int KEPT = TWICE ? 1 : NV;
+        F h[KEPT][L], g[KEPT][L];
+        auto fetch = [&](int i) {
+            const int k = TWICE ? 0 : i;
+            const bool in = there && p.has(i, chunks);
+            if constexpr (S > 0) {
+                ring.read(slot, 0, i, in, h[k]);
+                ring.read(slot, 1, i, in, g[k]);
+            } else {
+                const int64_t c = (p.first + i * P::kStep) * VEC;
+                auto vx = zero_vec<T, VEC>(), vd = zero_vec<T, VEC>();
+                if (in) {
+                    vx = load_vec<T, VEC>(row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, row, a.heads) + c);
+                    vd = load_vec<T, VEC>(row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, row, a.heads) + c);
+                }
+                unpack<T, VEC>(vx, h[k]);
+                unpack<T, VEC>(vd, g[k]);
+            }
+        };
+        auto weighted = [&](int i) {
+            if (a.weight) {
+                F w[L];
+                load_params<VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * VEC, w);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+                for (int e = 0; e < L; ++e)
+                    g[TWICE ? 0 : i][e] = g[TWICE ? 0 : i][e] * w[e];
+            }
+        };
+        if constexpr (S > 0)
+            ring_wait<TWICE ? S - 1 : S - 2>();
+        if constexpr (!TWICE) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                fetch(i);
+            if constexpr (S > 0) {
+                ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
+                slot = slot == S - 1 ? 0 : slot + 1;
+            }
+        }
+        F sg = all_of<VEC>(0.f), sh = sg;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int k = TWICE ? 0 : i;
+            if constexpr (TWICE)
+                fetch(i);
             if (there && p.has(i, chunks)) {
 #pragma unroll
                 for (int e = 0; e < L; ++e) {
-                    h[i][e] = (h[i][e] + less) * scale;
-                    dw[i][e] = fused(g[i][e], h[i][e], dw[i][e]);
-                    db[i][e] = db[i][e] + g[i][e];
+                    h[k][e] = (h[k][e] + less) * scale;
+                    dw[i][e] = fused(g[k][e], h[k][e], dw[i][e]);
+                    db[i][e] = db[i][e] + g[k][e];
                 }
-                if (a.weight) {
-                    F w[L];
-                    load_params<P::VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * P::VEC, w);
-#pragma unroll
-                    for (int e = 0; e < L; ++e)
-                        g[i][e] = g[i][e] * w[e];
-                }
+                weighted(i);
 #pragma unroll
                 for (int e = 0; e < L; ++e) {
-                    sg = sg + g[i][e];
-                    sh = fused(g[i][e], h[i][e], sh);
+                    sg = sg + g[k][e];
+                    sh = fused(g[k][e], h[k][e], sh);
                 }
             }
+        }
         const Pair s = p.sum(Pair{both(sg), both(sh)}, s_part[turn]);
-        if (!there)
-            continue;
-        // (g - mean g - h mean(g h)) rstd
-        const F to_g = all_of<P::VEC>(a.rms ? 0.f : -(s.x * inv) * rstd), to_h = all_of<P::VEC>(-(s.y * inv) * rstd);
-        T *const dx = row_at(static_cast<T *>(a.dx), a.dx_token, a.dx_head, row, a.heads);
+        if (there) {
+            // (g - mean g - h mean(g h)) rstd
+            const F to_g = all_of<VEC>(a.rms ? 0.f : -(s.x * inv) * rstd), to_h = all_of<VEC>(-(s.y * inv) * rstd);
+            T *const dx = row_at(static_cast<T *>(a.dx), a.dx_token, a.dx_head, row, a.heads);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (p.has(i, chunks)) {
+            for (int i = 0; i < NV; ++i)
+                if (p.has(i, chunks)) {
+                    const int k = TWICE ? 0 : i;
+                    if constexpr (TWICE) {
+                        fetch(i);
+                        weighted(i);
 #pragma unroll
-                for (int e = 0; e < L; ++e)
-                    g[i][e] = fused(h[i][e], to_h, fused(g[i][e], scale, to_g));
-                store_vec<T, P::VEC>(dx + (p.first + i * P::kStep) * P::VEC, pack<T, P::VEC>(g[i]));
-            }
+                        for (int e = 0; e < L; ++e)
+                            h[k][e] = (h[k][e] + less) * scale;
+                    }
+#pragma unroll
+                    for (int e = 0; e < L; ++e)
+                        g[k][e] = fused(h[k][e], to_h, fused(g[k][e], scale, to_g));
+                    store_once<T, VEC>(dx + (p.first + i * P::kStep) * VEC, pack<T, VEC>(g[k]));
+                }
+        }
+        if constexpr (TWICE) {
+            ahead(slot, row + S * step);
+            slot = slot == S - 1 ? 0 : slot + 1;
+        }
     }
     if (!a.partial)
         return;
-    float *const out = a.partial + (int64_t)blockIdx.x * 2 * a.dim;
-    float *const s_sums = reinterpret_cast<float *>(s_ring);
+    const int padded = padded_dim(a.dim);
+    float *const out = a.partial + (int64_t)blockIdx.x * 2 * padded;
+    float *const s_sums = reinterpret_cast<float *>(smem);
     if (groups > 1) {
         if constexpr (S > 0)
             asm volatile("cp.async.wait_all;" ::: "memory");   // (the sums take the ring's place)
         __syncthreads();
     }
-    float *const to = groups > 1 ? s_sums + p.group * 2 * a.dim : out;
+    float *const to = groups > 1 ? s_sums + p.group * 2 * padded : out;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (p.has(i, chunks)) {
-            const int c = (p.first + i * P::kStep) * P::VEC;
-#pragma unroll
-            for (int e = 0; e < L; ++e) {
-                *reinterpret_cast<F *>(to + c + e * (P::VEC / L)) = dw[i][e];
-                *reinterpret_cast<F *>(to + a.dim + c + e * (P::VEC / L)) = db[i][e];
-            }
+            const int c = (p.first + i * P::kStep) * VEC;
+            store_sums<VEC>(to + c, dw[i]);
+            store_sums<VEC>(to + padded + c, db[i]);
         }
     if (groups > 1) {
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * a.dim; i += blockDim.x) {
+        for (int i = threadIdx.x; i < 2 * padded; i += blockDim.x) {
             float s = 0.f;
             for (int g = 0; g < groups; ++g)
-                s += s_sums[g * 2 * a.dim + i];
+                s += s_sums[g * 2 * padded + i];
             out[i] = s;
         }
     }
 }
 
-// dw, db: sums of the blocks' parts.  A block takes 32 columns, its warps
-// shares of the parts.
-__global__ void __launch_bounds__(256) norm_sum_kernel(const float *partial, int parts, int dim, float *dweight, float *dbias)
+// dw, db: sums of the blocks' parts.  A block takes 64 of the columns, its
+// warps shares of the parts, a lane two columns.
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(kSumWarps * 32) norm_sum_kernel(const float *partial, int parts, int dim, float *dweight, float *dbias)
 {
-    __shared__ float s[8][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int i = blockIdx.x * 32 + lane;
+    __shared__ float2 s[kSumWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, padded = padded_dim(dim);
+    const int i = (blockIdx.x * 32 + lane) * 2;
     wait_for_previous();
     let_next_start();
-    float v = 0.f;
-    if (i < 2 * dim)
-#pragma unroll 8
-        for (int p = warp; p < parts; p += 8)
-            v += partial[(int64_t)p * 2 * dim + i];
+    float2 v = {0.f, 0.f};
+    if (i < 2 * padded)
+#pragma unroll 10
+        for (int p = warp; p < parts; p += kSumWarps) {
+            const float2 u = *reinterpret_cast<const float2 *>(partial + (int64_t)p * 2 * padded + i);
+            v = {v.x + u.x, v.y + u.y};
+        }
     s[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && i < 2 * dim) {
-        v = 0.f;
-        for (int k = 0; k < 8; ++k)
-            v += s[k][lane];
-        if (i < dim) {
-            if (dweight)
-                dweight[i] = v;
-        } else if (dbias)
-            dbias[i - dim] = v;
+    if (threadIdx.x < 64) {
+        const int at = blockIdx.x * 64 + threadIdx.x;
+        const float *const column = reinterpret_cast<const float *>(s) + threadIdx.x;
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kSumWarps; ++k)
+            sum += column[k * 64];
+        if (dweight && at < dim)
+            dweight[at] = sum;
+        if (dbias && at >= padded && at < padded + dim)
+            dbias[at - padded] = sum;
     }
 }
 
-// Blocks of the backward kernel, at most: its parts are the workspace.
-int most_parts() { return 2 * num_sms(); }
+// Blocks of the backward kernel on an SM: 640 threads, or one block that is
+// larger than half of them.
+int backward_blocks(int threads) { return threads > 320 ? 1 : 640 / threads; }
 
 // Calls go(split) with the way a row of `chunks` lies over threads: a few
 // lanes with two chunks each, a warp, or a block whose warps take 32 NV
@@ -506,8 +578,8 @@ template <typename P, int THREADS>
 cudaError_t launch_backward_of(const NormGradArgs &a, int threads, int blocks, cudaStream_t st)
 {
     const int groups = P::kBlock ? 1 : threads / P::TPR;
-    const size_t parts = a.partial && groups > 1 ? (size_t)groups * 2 * a.dim * sizeof(float) : 0;
-    const size_t rows = Ring<P, 2, kBackwardRows<P, THREADS>>::bytes(threads), smem = rows > parts ? rows : parts;
+    const size_t parts = a.partial && groups > 1 ? (size_t)groups * 2 * padded_dim(a.dim) * sizeof(float) : 0;
+    const size_t rows = Backward<P, THREADS>::bytes(threads), smem = rows > parts ? rows : parts;
     static PerDevice<bool> allowed;
     if (smem > kPlainSmem)
         if (cudaError_t e = allow_smem((const void *)norm_grad_kernel<P, THREADS>, (int)kMostSmem, allowed))
@@ -526,30 +598,35 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
         const cudaError_t e = with_split<T, VEC, MOST>(a.dim / VEC, [&](auto split) -> cudaError_t {
             using P = std::remove_pointer_t<decltype(split)>;
             const int threads = threads_of<P>(a.dim / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
-            const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * (threads <= 320 ? 2 : 1);
+            const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * backward_blocks(threads);
             blocks = (int)(turns < most ? turns : most);
             if constexpr (P::kBlock) {
                 if (threads > 512)
                     return launch_backward_of<P, 1024>(a, threads, blocks, st);
                 if (threads > 320)
                     return launch_backward_of<P, 512>(a, threads, blocks, st);
-            }
-            return launch_backward_of<P, 320>(a, threads, blocks, st);
+                return launch_backward_of<P, 320>(a, threads, blocks, st);
+            } else
+                return launch_backward_of<P, 256>(a, threads, blocks, st);
         });
         if (e != cudaSuccess)
             return e;
     }
     if (!sums)
         return cudaSuccess;
-    return launch_early(norm_sum_kernel, dim3((unsigned)((2 * a.dim + 31) / 32)), 256, 0, st, 1,
-                        static_cast<const float *>(a.workspace), blocks, a.dim, a.dweight, a.dbias);
+    return launch_early(norm_sum_kernel, dim3((unsigned)((2 * padded_dim(a.dim) + 63) / 64)), kSumWarps * 32, 0, st, 1, static_cast<const float *>(a.workspace), blocks, a.dim, a.dweight, a.dbias);
 }
 
 bool wide(int64_t bits, bool bf16) { return bits % (bf16 ? 8 : 4) == 0; }
 
 } // namespace
 
-size_t norm_grad_workspace_bytes(int32_t dim) { return (size_t)most_parts() * 2 * (size_t)dim * sizeof(float); }
+size_t norm_grad_workspace_bytes(int32_t dim)
+{
+    // (whatever the type and strides: a row of a block has a warp for at most 512 elements, and two of them at least)
+    const int threads = dim > 1024 ? (dim + 511) / 512 * 32 : dim > 256 ? 64 : kThreads;
+    return (size_t)num_sms() * backward_blocks(threads) * 2 * (size_t)padded_dim(dim) * sizeof(float);
+}
 
 cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
 {

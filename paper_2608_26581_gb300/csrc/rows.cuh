@@ -35,6 +35,17 @@ __device__ __forceinline__ void store_vec(T *p, const Vec<T, VEC> &v)
     *reinterpret_cast<Vec<T, VEC> *>(p) = v;
 }
 
+// Stores that leave L1 to what is read again.
+template <typename T, int VEC>
+__device__ __forceinline__ void store_once(T *p, const Vec<T, VEC> &v)
+{
+    if constexpr (sizeof(v) == 16) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(&v);
+        asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u.x), "r"(u.y), "r"(u.z), "r"(u.w) : "memory");
+    } else
+        store_vec<T, VEC>(p, v);
+}
+
 template <typename T, int VEC>
 __device__ __forceinline__ Vec<T, VEC> zero_vec()
 {
