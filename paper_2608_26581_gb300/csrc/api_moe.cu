@@ -249,8 +249,7 @@ rfq_status rfq_moe_quantize(const void *x, int64_t x_row_stride, int64_t tokens,
     if (xq->rows == 0)
         return RFQ_OK;
     return from_cuda(launch_moe_quantize({x, x_row_stride, tokens, (int32_t)xq->k, row_of, top_k, pair_of, xq->codes,
-                                          xq->scales, xr ? xr->codes : nullptr, xr ? xr->scales : nullptr, xq->rows, 0,
-                                          0},
+                                          xq->scales, xr ? xr->codes : nullptr, xr ? xr->scales : nullptr, xq->rows, 0},
                                          static_cast<cudaStream_t>(stream)));
 }
 

@@ -430,7 +430,7 @@ struct MoeQuantizeArgs {
     const int32_t *pair_of;                       // or null
     void *m_codes, *m_scales, *r_codes, *r_scales;    // r_*: null without a residual
     int64_t rows;
-    int64_t padded, pad_from;                     // (the launcher's: rows of the scale layout, first one to clear)
+    int64_t padded;                               // (the launcher's: rows of the scale layout)
 };
 cudaError_t launch_moe_gather(const MoeGatherArgs &a, cudaStream_t st);
 cudaError_t launch_moe_combine(const MoeCombineArgs &a, cudaStream_t st);

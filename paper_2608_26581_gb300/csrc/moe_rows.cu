@@ -22,6 +22,7 @@ namespace rfq {
 namespace {
 
 constexpr int kWarps = 8;
+constexpr int kCombineBlocks = 4;            // of an SM
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 // The row of pair j of a token (lane j holds it), -1 where there is none.
@@ -31,17 +32,27 @@ __device__ __forceinline__ int token_row(const int32_t *row_of, int64_t t, int t
     return r < rows ? r : -1;
 }
 
-// Clears the columns [c0, c1) (in vectors) of those of 32 rows from r0 on that hold no pair.
-template <typename T, int VEC>
-__device__ __forceinline__ void clear_rows(T *out, const int32_t *pair_of, int64_t rows, int dim, int64_t r0, int c0, int c1, int lane)
+// Rows that a warp looks through for those of no pair.  They lie apart, by the
+// number of warps that look: long stretches of them fall to many warps.
+constexpr int kLook = 8;
+__host__ __device__ __forceinline__ int64_t lookers(int64_t rows) { return (rows + kLook - 1) / kLook; }
+
+// Calls clear(row) for each of looker i's rows that holds no pair.
+template <typename C>
+__device__ __forceinline__ void rows_of_no_pair(const int32_t *pair_of, int64_t rows, int64_t i, int lane, C &&clear)
 {
-    uint32_t none = __ballot_sync(kAll, r0 + lane < rows && pair_of[r0 + lane] < 0);
-    const Vec<T, VEC> zero = zero_vec<T, VEC>();
-    for (; none; none &= none - 1) {
-        T *const o = out + (r0 + __ffs(none) - 1) * dim;
-        for (int c = c0 + lane; c < c1; c += 32)
-            store_vec<T, VEC>(o + (int64_t)c * VEC, zero);
-    }
+    const int64_t n = lookers(rows), mine = i + lane * n;
+    for (uint32_t none = __ballot_sync(kAll, lane < kLook && mine < rows && pair_of[mine] < 0); none; none &= none - 1)
+        clear(i + (__ffs(none) - 1) * n);
+}
+
+template <typename T, int VEC>
+__device__ __forceinline__ void clear_row(T *out, int64_t row, int dim, int lane)
+{
+    T *const o = out + row * dim;
+#pragma unroll 4
+    for (int c = lane; c < dim / VEC; c += 32)
+        store_vec<T, VEC>(o + (int64_t)c * VEC, zero_vec<T, VEC>());
 }
 
 constexpr int kGatherChunks = 4;             // vectors of a lane
@@ -53,14 +64,15 @@ __global__ void __launch_bounds__(kWarps * 32) gather_kernel(const MoeGatherArgs
     const int lane = threadIdx.x & 31, chunks = a.dim / VEC;
     wait_for_previous();
     let_next_start();
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t t = item / segs;
-    const int c0 = (int)(item - t * segs) * 32 * U, c1 = min(chunks, c0 + 32 * U);
-    if (t >= a.tokens) {
-        if (a.pair_of && (t - a.tokens) * 32 < a.rows)
-            clear_rows<T, VEC>(static_cast<T *>(a.out), a.pair_of, a.rows, a.dim, (t - a.tokens) * 32, c0, c1, lane);
+    const int64_t look = a.pair_of ? lookers(a.rows) : 0, item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) - look;
+    if (item < 0) {
+        rows_of_no_pair(a.pair_of, a.rows, item + look, lane, [&](int64_t r) { clear_row<T, VEC>(static_cast<T *>(a.out), r, a.dim, lane); });
         return;
     }
+    const int64_t t = item / segs;
+    if (t >= a.tokens)
+        return;
+    const int c0 = (int)(item - t * segs) * 32 * U, c1 = min(chunks, c0 + 32 * U);
     const T *const x = static_cast<const T *>(a.x) + t * a.x_row;
     const int row = token_row(a.row_of, t, a.top_k, a.rows, lane);
     Vec<T, VEC> v[U];
@@ -80,69 +92,83 @@ __global__ void __launch_bounds__(kWarps * 32) gather_kernel(const MoeGatherArgs
     }
 }
 
+// Persistent warps take 32 vectors of a token each; the next token's rows and
+// weights are on their way while this one's are summed.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kWarps * 32) combine_kernel(const MoeCombineArgs a, int segs)
+__global__ void __launch_bounds__(kWarps * 32, kCombineBlocks) combine_kernel(const MoeCombineArgs a, int segs)
 {
     constexpr int B = 8;                     // rows in flight
     const int lane = threadIdx.x & 31, chunks = a.dim / VEC;
     wait_for_previous();
     let_next_start();
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t t = item / segs;
-    const int c = (int)(item - t * segs) * 32 + lane;
-    if (t >= a.tokens)
-        return;
-    const int row = token_row(a.row_of, t, a.top_k, a.rows, lane);
-    const float w = lane < a.top_k ? a.weights ? a.weights[t * a.top_k + lane] : 1.f : 0.f;
-    float sum[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e)
-        sum[e] = 0.f;
-    for (int j0 = 0; j0 < a.top_k; j0 += B) {
-        Vec<T, VEC> v[B];
-        int r[B];
-#pragma unroll
-        for (int j = 0; j < B; ++j) {
-            r[j] = __shfl_sync(kAll, row, (j0 + j) & 31);
-            r[j] = j0 + j < a.top_k && c < chunks ? r[j] : -1;
-            if (r[j] >= 0)
-                v[j] = load_vec<T, VEC>(static_cast<const T *>(a.y) + (int64_t)r[j] * a.dim + (int64_t)c * VEC);
+    const int64_t items = a.tokens * segs, step = (int64_t)gridDim.x * kWarps;
+    int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    int row = -1, next_row = -1;
+    float w = 0.f, next_w = 0.f;
+    auto ahead = [&](int64_t it) {
+        if (it < items) {
+            const int64_t t = it / segs;
+            next_row = token_row(a.row_of, t, a.top_k, a.rows, lane);
+            next_w = lane < a.top_k && a.weights ? a.weights[t * a.top_k + lane] : 1.f;
         }
+    };
+    ahead(item);
+#pragma unroll 1
+    for (; item < items; item += step) {
+        row = next_row;
+        w = next_w;
+        const int64_t t = item / segs;
+        const int c = (int)(item - t * segs) * 32 + lane;
+        const T *const y = static_cast<const T *>(a.y) + (int64_t)c * VEC;
+        Lane<VEC> sum[kLanes<VEC>];
 #pragma unroll
-        for (int j = 0; j < B; ++j) {
-            const float f = __shfl_sync(kAll, w, (j0 + j) & 31);
-            if (r[j] >= 0)
+        for (int e = 0; e < kLanes<VEC>; ++e)
+            sum[e] = all_of<VEC>(0.f);
+#pragma unroll 1
+        for (int j0 = 0; j0 < a.top_k; j0 += B) {
+            Vec<T, VEC> v[B];
+            int r[B];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    sum[e] += f * to_f32(v[j].v[e]);
+            for (int j = 0; j < B; ++j) {
+                r[j] = __shfl_sync(kAll, row, (j0 + j) & 31);
+                r[j] = j0 + j < a.top_k && c < chunks ? r[j] : -1;
+                if (r[j] >= 0)
+                    v[j] = load_vec<T, VEC>(y + (int64_t)r[j] * a.dim);
+            }
+            if (j0 == 0)
+                ahead(item + step);
+#pragma unroll
+            for (int j = 0; j < B; ++j) {
+                const Lane<VEC> f = all_of<VEC>(__shfl_sync(kAll, w, (j0 + j) & 31));
+                if (r[j] >= 0) {
+                    Lane<VEC> x[kLanes<VEC>];
+                    unpack<T, VEC>(v[j], x);
+#pragma unroll
+                    for (int e = 0; e < kLanes<VEC>; ++e)
+                        sum[e] = fused(f, x[e], sum[e]);
+                }
+            }
         }
-    }
-    if (c < chunks) {
-        Vec<T, VEC> o;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            from_f32(o.v[e], sum[e]);
-        store_vec<T, VEC>(static_cast<T *>(a.out) + t * a.out_row + (int64_t)c * VEC, o);
+        if (c < chunks)
+            store_once<T, VEC>(static_cast<T *>(a.out) + t * a.out_row + (int64_t)c * VEC, pack<T, VEC>(sum));
     }
 }
 
-// A warp takes a pair; then warps clear 32 rows' columns by segments.
+// Warps clear the rows of no pair; then a warp takes a pair.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kWarps * 32) combine_grad_kernel(const MoeCombineGradArgs a, int segs)
+__global__ void __launch_bounds__(kWarps * 32) combine_grad_kernel(const MoeCombineGradArgs a)
 {
     constexpr int U = 4;                     // vectors in flight
     const int lane = threadIdx.x & 31, chunks = a.dim / VEC;
     wait_for_previous();
     let_next_start();
-    const int64_t pairs = a.tokens * a.top_k;
-    const int64_t p = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (p >= pairs) {
-        const int64_t s = (p - pairs) / segs;
-        const int c0 = (int)(p - pairs - s * segs) * 128;
-        if (a.pair_of && s * 32 < a.rows)
-            clear_rows<T, VEC>(static_cast<T *>(a.dy), a.pair_of, a.rows, a.dim, s * 32, c0, min(chunks, c0 + 128), lane);
+    const int64_t look = a.pair_of ? lookers(a.rows) : 0, p = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) - look;
+    if (p < 0) {
+        rows_of_no_pair(a.pair_of, a.rows, p + look, lane, [&](int64_t r) { clear_row<T, VEC>(static_cast<T *>(a.dy), r, a.dim, lane); });
         return;
     }
+    if (p >= a.tokens * a.top_k)
+        return;
     const int row = a.row_of[p];
     float dot = 0.f;
     if (row >= 0 && row < a.rows) {
@@ -186,35 +212,39 @@ __global__ void __launch_bounds__(kWarps * 32) moe_quantize_kernel(const MoeQuan
     const int lane = threadIdx.x & 31, kblocks = a.dim / 32;
     wait_for_previous();
     let_next_start();
-    const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t t = item / segs;
-    const int b = (int)(item - t * segs) * 32 + lane;
-    const bool ok = b < kblocks;             // (dim % 128 == 0: alike for the lanes of a scale word)
     uint4 *const mc = static_cast<uint4 *>(a.m_codes), *const rc = static_cast<uint4 *>(a.r_codes);
     uint8_t *const ms = static_cast<uint8_t *>(a.m_scales), *const rs = static_cast<uint8_t *>(a.r_scales);
-    if (t >= a.tokens) {
-        // rows of no pair, and the scale layout's rows behind the last
-        const int64_t r0 = a.pad_from + (t - a.tokens) * 32, r = r0 + lane;
-        const bool pad = r >= a.rows && r < a.padded;
-        const uint32_t none = __ballot_sync(kAll, a.pair_of && r < a.rows && a.pair_of[r] < 0);
-        for (uint32_t left = none | __ballot_sync(kAll, pad); left; left &= left - 1) {
-            const int64_t row = r0 + __ffs(left) - 1;
-            if (!ok)
-                continue;
-            if (row < a.rows) {
-                mc[row * kblocks + b] = make_uint4(0, 0, 0, 0);
-                if (RES)
-                    rc[row * kblocks + b] = make_uint4(0, 0, 0, 0);
-            }
-            if ((lane & 3) == 0) {
-                const int64_t at = sf_mma_offset(row, b, kblocks >> 2);
+    // warps that clear the rows of no pair, one that clears the scale layout's rows behind the last, then the tokens'
+    const int64_t look = a.pair_of ? lookers(a.rows) : 0, item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) - look - 1;
+    if (item < 0) {
+        auto clear_scales = [&](int64_t row) {
+            for (int w = lane; w < kblocks / 4; w += 32) {
+                const int64_t at = sf_mma_offset(row, 4 * w, kblocks >> 2);
                 *reinterpret_cast<uint32_t *>(ms + at) = 0;
                 if (RES)
                     *reinterpret_cast<uint32_t *>(rs + at) = 0;
             }
-        }
+        };
+        if (item == -1)
+            for (int64_t row = a.rows; row < a.padded; ++row)
+                clear_scales(row);
+        else
+            rows_of_no_pair(a.pair_of, a.rows, item + look + 1, lane, [&](int64_t row) {
+#pragma unroll 4
+                for (int b = lane; b < kblocks; b += 32) {
+                    mc[row * kblocks + b] = make_uint4(0, 0, 0, 0);
+                    if (RES)
+                        rc[row * kblocks + b] = make_uint4(0, 0, 0, 0);
+                }
+                clear_scales(row);
+            });
         return;
     }
+    const int64_t t = item / segs;
+    if (t >= a.tokens)
+        return;
+    const int b = (int)(item - t * segs) * 32 + lane;
+    const bool ok = b < kblocks;             // (dim % 128 == 0: alike for the lanes of a scale word)
     const int row = token_row(a.row_of, t, a.top_k, a.rows, lane);
     uint32_t w[16];
 #pragma unroll
@@ -237,6 +267,7 @@ __global__ void __launch_bounds__(kWarps * 32) moe_quantize_kernel(const MoeQuan
         sr |= __shfl_xor_sync(kAll, sr, 1);
         sr |= __shfl_xor_sync(kAll, sr, 2);
     }
+    // codes: row by row; scale words: a row for each of the four lanes
     for (int j = 0; j < a.top_k; ++j) {
         const int r = __shfl_sync(kAll, row, j);
         if (r < 0 || !ok)
@@ -244,12 +275,15 @@ __global__ void __launch_bounds__(kWarps * 32) moe_quantize_kernel(const MoeQuan
         mc[(int64_t)r * kblocks + b] = q.code;
         if (RES)
             rc[(int64_t)r * kblocks + b] = q.rcode;
-        if ((lane & 3) == (j & 3)) {
-            const int64_t at = sf_mma_offset(r, b & ~3, kblocks >> 2);
-            *reinterpret_cast<uint32_t *>(ms + at) = sm;
-            if (RES)
-                *reinterpret_cast<uint32_t *>(rs + at) = sr;
-        }
+    }
+    for (int j = 0; j < a.top_k; j += 4) {
+        const int r = __shfl_sync(kAll, row, min(j + (lane & 3), 31));
+        if (r < 0 || !ok || j + (lane & 3) >= a.top_k)
+            continue;
+        const int64_t at = sf_mma_offset(r, b & ~3, kblocks >> 2);
+        *reinterpret_cast<uint32_t *>(ms + at) = sm;
+        if (RES)
+            *reinterpret_cast<uint32_t *>(rs + at) = sr;
     }
 }
 
@@ -268,7 +302,7 @@ cudaError_t gather(const MoeGatherArgs &a, cudaStream_t st)
 {
     const int per = 32 * kGatherChunks, segs = (a.dim / VEC + per - 1) / per;
     unsigned blocks;
-    if (!blocks_of((a.tokens + (a.pair_of ? (a.rows + 31) / 32 : 0)) * segs, blocks))
+    if (!blocks_of(a.tokens * segs + (a.pair_of ? lookers(a.rows) : 0), blocks))
         return cudaErrorInvalidConfiguration;
     return blocks ? launch_early(gather_kernel<T, VEC>, dim3(blocks), kWarps * 32, 0, st, 1, a, segs) : cudaSuccess;
 }
@@ -277,20 +311,17 @@ template <typename T, int VEC>
 cudaError_t combine(const MoeCombineArgs &a, cudaStream_t st)
 {
     const int segs = (a.dim / VEC + 31) / 32;
-    unsigned blocks;
-    if (!blocks_of(a.tokens * segs, blocks))
-        return cudaErrorInvalidConfiguration;
-    return launch_early(combine_kernel<T, VEC>, dim3(blocks), kWarps * 32, 0, st, 1, a, segs);
+    const int64_t blocks = (a.tokens * segs + kWarps - 1) / kWarps, most = (int64_t)num_sms() * kCombineBlocks;
+    return launch_early(combine_kernel<T, VEC>, dim3((unsigned)(blocks < most ? blocks : most)), kWarps * 32, 0, st, 1, a, segs);
 }
 
 template <typename T, int VEC>
 cudaError_t combine_grad(const MoeCombineGradArgs &a, cudaStream_t st)
 {
-    const int segs = (a.dim / VEC + 127) / 128;
     unsigned blocks;
-    if (!blocks_of(a.tokens * a.top_k + (a.pair_of ? (a.rows + 31) / 32 * segs : 0), blocks))
+    if (!blocks_of(a.tokens * a.top_k + (a.pair_of ? lookers(a.rows) : 0), blocks))
         return cudaErrorInvalidConfiguration;
-    return blocks ? launch_early(combine_grad_kernel<T, VEC>, dim3(blocks), kWarps * 32, 0, st, 1, a, segs) : cudaSuccess;
+    return blocks ? launch_early(combine_grad_kernel<T, VEC>, dim3(blocks), kWarps * 32, 0, st, 1, a) : cudaSuccess;
 }
 
 } // namespace
@@ -324,12 +355,9 @@ cudaError_t launch_moe_quantize(const MoeQuantizeArgs &a, cudaStream_t st)
     const int segs = (a.dim / 32 + 31) / 32;
     MoeQuantizeArgs b = a;
     b.padded = (a.rows + 127) / 128 * 128;
-    b.pad_from = a.pair_of ? 0 : a.rows / 32 * 32;   // (without pair_of only the layout's padding is cleared)
     unsigned blocks;
-    if (!blocks_of((a.tokens + (b.padded - b.pad_from) / 32) * segs, blocks))
+    if (!blocks_of(a.tokens * segs + (a.pair_of ? lookers(a.rows) : 0) + 1, blocks))
         return cudaErrorInvalidConfiguration;
-    if (!blocks)
-        return cudaSuccess;
     return a.r_codes ? launch_early(moe_quantize_kernel<true>, dim3(blocks), kWarps * 32, 0, st, 1, b, segs)
                      : launch_early(moe_quantize_kernel<false>, dim3(blocks), kWarps * 32, 0, st, 1, b, segs);
 }

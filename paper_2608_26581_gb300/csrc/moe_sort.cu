@@ -10,10 +10,13 @@
 //
 // Bound: latency (12 bytes a pair).  One launch of one cluster.  Each warp
 // takes a run of the pairs and counts them by expert, 32 at a time: lanes of
-// the same expert find each other with a match, the first one adds their
-// number to the warp's own counters.  The counters are summed over the warps
-// of a block and, through distributed shared memory, over the blocks; then
-// the warps go through their pairs again and give out the rows.
+// the same expert find each other by a ballot for each bit of its number (a
+// match instruction took 62 clocks of the SM, 262144 pairs 67 us in all), the
+// first one adds their number to the warp's own counters, and each pair's
+// place among the warp's is kept.  The counters are summed over the warps of a
+// block and, through distributed shared memory, over the blocks, which gives
+// the rows.  Loads that do not depend on each other (pairs of eight steps, the
+// warps' and the blocks' counters) are in flight together.
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -25,6 +28,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr int kHeld = 8;                     // steps of 32 pairs in flight
 constexpr int64_t kPairsPerCta = 4096;       // of a cluster that has room for more
 constexpr int kMostCtas = 8;
 
@@ -37,7 +41,7 @@ __device__ __forceinline__ int ld_peer(uint32_t saddr, int rank)
 
 __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
 {
-    __shared__ int s_count[kWarps][kMoeExperts];     // pairs of a warp; then those of the warps before it
+    __shared__ __align__(16) int s_count[kWarps][kMoeExperts];     // pairs of a warp; then those of the warps before it
     __shared__ int s_total[kMoeExperts];             // pairs of the block
     __shared__ int s_base[kMoeExperts];              // row of the block's first pair
     __shared__ int s_end[kMoeExperts], s_next[kMoeExperts];   // a group's end, and the next one's start
@@ -45,34 +49,64 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_ctarank(), ctas = gridDim.x;
     const int E = a.experts;
-    for (int i = tid; i < kWarps * kMoeExperts; i += kThreads)
-        (&s_count[0][0])[i] = 0;
-    __syncthreads();
-    wait_for_previous();
-    let_next_start();
-
     // this warp's pairs, whole steps of 32
     const int64_t steps = (a.pairs + 31) / 32, per = (steps + ctas * kWarps - 1) / (ctas * kWarps);
     const int64_t p0 = min(a.pairs, (rank * kWarps + warp) * per * 32), p1 = min(a.pairs, p0 + per * 32);
     int *const mine = s_count[warp];
-    auto expert = [&](int64_t p) {
-        const int e = p < p1 ? a.ids[p] : -1;
-        return e >= 0 && e < E ? e : -1;
+    int held[kHeld];                         // experts of the pairs of kHeld steps, -1 without one
+    auto hold = [&](int64_t p) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            held[i] = p + 32 * i + lane < p1 ? a.ids[p + 32 * i + lane] : -1;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            held[i] = held[i] >= 0 && held[i] < E ? held[i] : -1;
     };
-    for (int64_t p = p0; p < p1; p += 32) {
-        const int e = expert(p + lane);
-        const uint32_t same = __match_any_sync(kAll, e);
-        if (e >= 0 && (same & ((1u << lane) - 1)) == 0)
-            mine[e] += __popc(same);
-        __syncwarp();
+    wait_for_previous();
+    let_next_start();
+    hold(p0);
+    for (int i = tid; i < kWarps * kMoeExperts / 4; i += kThreads)
+        reinterpret_cast<int4 *>(s_count)[i] = make_int4(0, 0, 0, 0);
+    __syncthreads();
+    // the place of each held pair among the warp's of its expert; of pairs that
+    // are not held until the rows are given out, in the place of the row
+    int place[kHeld];
+    const bool kept = p1 - p0 <= 32 * kHeld;
+    const int bits = 32 - __clz(E - 1);
+#pragma unroll 1
+    for (int64_t p = p0; p < p1; p += 32 * kHeld) {
+        if (p > p0)
+            hold(p);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (p + 32 * i < p1) {
+                const int e = held[i];
+                uint32_t same = __ballot_sync(kAll, e >= 0);
+                for (int b = 0; b < bits; ++b) {
+                    const uint32_t set = __ballot_sync(kAll, e >> b & 1);
+                    same &= e >> b & 1 ? set : ~set;
+                }
+                const int nth = __popc(same & ((1u << lane) - 1));
+                place[i] = e >= 0 ? mine[e] + nth : 0;
+                __syncwarp();
+                if (e >= 0 && nth == 0)
+                    mine[e] = place[i] + __popc(same);
+                __syncwarp();
+                if (!kept && p + 32 * i + lane < p1)
+                    a.row_of[p + 32 * i + lane] = place[i];
+            }
     }
     __syncthreads();
     int own = 0;                             // thread e: the block's pairs of expert e
     if (tid < kMoeExperts) {
+        int n[kWarps];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            n[w] = s_count[w][tid];
+#pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const int n = s_count[w][tid];
             s_count[w][tid] = own;
-            own += n;
+            own += n[w];
         }
         s_total[tid] = own;
     }
@@ -80,11 +114,15 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
         cluster_sync();
     int before = 0, all = own;
     if (tid < kMoeExperts && ctas > 1) {
+        int n[kMostCtas];
+#pragma unroll
+        for (int r = 0; r < kMostCtas; ++r)
+            n[r] = r < ctas ? ld_peer(smem_u32(&s_total[tid]), r) : 0;
         all = 0;
-        for (int r = 0; r < ctas; ++r) {
-            const int n = ld_peer(smem_u32(&s_total[tid]), r);
-            before += r < rank ? n : 0;
-            all += n;
+#pragma unroll
+        for (int r = 0; r < kMostCtas; ++r) {
+            before += r < rank ? n[r] : 0;
+            all += n[r];
         }
     }
     // exclusive sum over the experts of the groups' sizes
@@ -118,30 +156,36 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
         }
     }
     __syncthreads();
-    for (int64_t p = p0; p < p1; p += 32) {
-        const int e = expert(p + lane);
-        const uint32_t same = __match_any_sync(kAll, e);
-        const int nth = __popc(same & ((1u << lane) - 1));
-        int row = -1;
-        if (e >= 0) {
-            row = s_base[e] + mine[e] + nth;
-            row = row < a.rows / a.align * a.align ? row : -1;
+    const int most = (int)(a.rows / a.align * a.align);
+#pragma unroll 1
+    for (int64_t p = p0; p < p1; p += 32 * kHeld) {
+        if (!kept) {
+            hold(p);
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                place[i] = p + 32 * i + lane < p1 ? a.row_of[p + 32 * i + lane] : 0;
         }
-        __syncwarp();
-        if (e >= 0 && nth == 0)
-            mine[e] += __popc(same);
-        __syncwarp();
-        if (p + lane < p1) {
-            a.row_of[p + lane] = row;
-            if (row >= 0)
-                a.pair_of[row] = (int)(p + lane);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int64_t at = p + 32 * i + lane;
+            if (at < p1) {
+                const int e = held[i];
+                int row = -1;
+                if (e >= 0) {
+                    row = s_base[e] + mine[e] + place[i];
+                    row = row < most ? row : -1;
+                }
+                a.row_of[at] = row;
+                if (row >= 0)
+                    a.pair_of[row] = (int)at;
+            }
         }
     }
     // rows of no pair: behind each group and behind the last
     for (int e = rank * kWarps + warp; e < E; e += ctas * kWarps)
         for (int64_t r = s_end[e] + lane; r < min((int64_t)s_next[e], a.rows); r += 32)
             a.pair_of[r] = -1;
-    for (int64_t r = min((int64_t)s_next[E - 1], a.rows / a.align * a.align) + rank * kThreads + tid; r < a.rows; r += ctas * kThreads)
+    for (int64_t r = min(s_next[E - 1], most) + rank * kThreads + tid; r < a.rows; r += ctas * kThreads)
         a.pair_of[r] = -1;
     if (ctas > 1)
         cluster_sync();                      // (a block's shared memory is read by the others)
