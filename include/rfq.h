@@ -756,7 +756,8 @@ RFQ_API rfq_status rfq_route(const void *logits, int64_t row_stride, int32_t dty
  * where ids[t][j] = i, 0 for experts that were not chosen, and p the softmax over
  * all experts, or with normalize != 0 over the chosen ones (0 elsewhere),
  *     dlogits[t][i] = p[i] (d[i] - sum of p d).
- * ids outside [0, experts) and their dweights are not looked at.  dlogits: device
+ * ids outside [0, experts) and their dweights are not looked at; the others of a
+ * token differ (of two that are equal one dweight counts).  dlogits: device
  * [tokens][experts] of dtype, every element written; it may be logits with the
  * same stride.  The rest as for rfq_route.
  * Errors: as rfq_route. */

@@ -4,14 +4,15 @@
 //
 // With p = softmax(l) over a token's logits and e_j its j-th largest,
 //     w_j = p[e_j],  or with normalize  w_j = p[e_j] / sum_m p[e_m],
-// which is the softmax over the chosen logits alone.  Gradient, with d_i the
-// sum of dw_j over the j that chose expert i and p restricted to the chosen
-// experts with normalize:
+// which is the softmax over the chosen logits alone.  Gradient, with d_i = dw_j
+// where e_j = i (0 elsewhere) and p restricted to the chosen experts with
+// normalize:
 //     dl_i = p_i (d_i - sum_m p_m d_m).
 //
-// A warp takes a token; lane i holds the logits of experts i, i + 32, ...  A
-// choice is the maximum over the warp of the logits as ordered integers, then
-// the lowest expert that has it.
+// A warp takes a token; a lane holds consecutive experts' logits.  A choice is
+// the maximum over the warp of the logits as ordered integers; of equal ones
+// the lowest lane's lowest is taken.  Bound: instructions of some 200 a token,
+// latency where tokens are few.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cmath>
@@ -40,27 +41,40 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// (NaN where a lane has one)
+// The logit of an ordered integer (some NaN for NaN).
+__device__ __forceinline__ float logit_of(uint32_t k)
+{
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+
+// Maximum over the warp; NaN counts as nothing (its exponential is NaN all the same).
 __device__ __forceinline__ float warp_max(float v)
 {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float u = __shfl_xor_sync(kAll, v, d);
-        v = v != v || v > u ? v : u;
-    }
-    return v;
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
 }
 
-template <typename T, int PER>
+// Lane's logits: experts PER lane .. PER lane + PER - 1, as one vector where VEC.
+template <typename T, int PER, bool VEC>
 __device__ __forceinline__ void load_logits(const void *logits, int64_t at, int experts, int lane, float (&l)[PER])
 {
-    const T *const p = static_cast<const T *>(logits) + at;
+    const T *const p = static_cast<const T *>(logits) + at + lane * PER;
+    if (VEC) {
+        if (lane * PER < experts) {
+            const Vec<T, PER> v = load_vec<T, PER>(p);
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                l[i] = to_f32(v.v[i]);
+            return;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        l[i] = lane + 32 * i < experts ? to_f32(p[lane + 32 * i]) : -INFINITY;
+        l[i] = !VEC && lane * PER + i < experts ? to_f32(p[i]) : -INFINITY;
 }
 
-template <typename T, int PER>
+template <typename T, int PER, bool VEC>
 __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
 {
     const int lane = threadIdx.x & 31;
@@ -70,19 +84,17 @@ __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
     if (t >= a.tokens)
         return;
     float l[PER];
-    load_logits<T, PER>(a.logits, t * a.row, a.experts, lane, l);
-    uint32_t key[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        key[i] = ordered(l[i]);
-    float m = l[0];
-#pragma unroll
-    for (int i = 1; i < PER; ++i)
-        m = m != m || m > l[i] ? m : l[i];
-    m = warp_max(m);
-    const bool none = m == -INFINITY;
+    load_logits<T, PER, VEC>(a.logits, t * a.row, a.experts, lane, l);
+    uint32_t key[PER], best = 0;
     float z = 0.f;
-    if (!a.normalize) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        key[i] = ordered(l[i]);
+        best = max(best, key[i]);
+    }
+    best = __reduce_max_sync(kAll, best);
+    const float m = logit_of(best);
+    if (!a.normalize && best != 0) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             z += l[i] == -INFINITY ? 0.f : expf(l[i] - m);
@@ -90,77 +102,67 @@ __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
     }
     int id = -1;
     float w = 0.f;                           // lane j: the j-th choice
-    for (int j = 0; j < a.top_k; ++j) {
-        uint32_t best = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            best = max(best, key[i]);
-        best = __reduce_max_sync(kAll, best);
-        if (best == 0)
-            break;
-        int at = INT32_MAX;
+    for (int j = 0; j < a.top_k && best != 0; ++j) {
+        int at = PER;                        // this lane's lowest expert with that logit
 #pragma unroll
         for (int i = PER - 1; i >= 0; --i)
-            if (key[i] == best)
-                at = lane + 32 * i;
-        at = __reduce_min_sync(kAll, at);
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (at == lane + 32 * i) {
-                v = l[i];
-                key[i] = 0;
-            }
-        v = __shfl_sync(kAll, v, at & 31);
+            at = key[i] == best ? i : at;
+        const int from = __ffs(__ballot_sync(kAll, at < PER)) - 1;
+        const int chosen = __shfl_sync(kAll, lane * PER + at, from);
         if (lane == j) {
-            id = at;
-            w = expf(v - m);
+            id = chosen;
+            w = expf(logit_of(best) - m);
         }
+        best = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            key[i] = chosen == lane * PER + i ? 0u : key[i];
+            best = max(best, key[i]);
+        }
+        best = __reduce_max_sync(kAll, best);
     }
     if (a.normalize)
         z = lane_sum(w);
     if (lane < a.top_k) {
         a.ids[t * a.top_k + lane] = id;
-        a.weights[t * a.top_k + lane] = none || id < 0 ? 0.f : w / z;
+        a.weights[t * a.top_k + lane] = id < 0 ? 0.f : w / z;
     }
 }
 
-template <typename T, int PER>
+template <typename T, int PER, bool VEC>
 __global__ void __launch_bounds__(kWarps * 32) route_grad_kernel(const RouteGradArgs a)
 {
+    __shared__ __align__(16) int8_t s_choice[kWarps][32 * PER];      // which choice took an expert, -1 where none
     const int lane = threadIdx.x & 31;
     const int64_t t = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    int8_t *const choice = s_choice[threadIdx.x >> 5];
     wait_for_previous();
     let_next_start();
     if (t >= a.tokens)
         return;
-    float l[PER], d[PER];
-    bool taken[PER];
-    load_logits<T, PER>(a.logits, t * a.row, a.experts, lane, l);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        d[i] = 0.f;
-        taken[i] = false;
-    }
     const bool mine = lane < a.top_k;
     const int id = mine ? a.ids[t * a.top_k + lane] : -1;
     const float dw = mine ? a.dweights[t * a.top_k + lane] : 0.f;
-    for (int j = 0; j < a.top_k; ++j) {
-        const int e = __shfl_sync(kAll, id, j);
-        const float v = __shfl_sync(kAll, dw, j);
+    float l[PER], d[PER];
+    load_logits<T, PER, VEC>(a.logits, t * a.row, a.experts, lane, l);
+    using Choices = Vec<int8_t, PER>;
+    Choices none;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (e == lane + 32 * i && e < a.experts) {
-                d[i] += v;
-                taken[i] = true;
-            }
-    }
+    for (int i = 0; i < PER; ++i)
+        none.v[i] = -1;
+    store_vec<int8_t, PER>(choice + lane * PER, none);
+    __syncwarp();
+    if (id >= 0 && id < a.experts)
+        choice[id] = (int8_t)lane;
+    __syncwarp();
+    const Choices taken = load_vec<int8_t, PER>(choice + lane * PER);
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        if (a.normalize && !taken[i])
-            l[i] = -INFINITY;
-        m = m != m || m > l[i] ? m : l[i];
+        const float v = __shfl_sync(kAll, dw, taken.v[i] & 31);
+        d[i] = taken.v[i] >= 0 ? v : 0.f;
+        l[i] = a.normalize && taken.v[i] < 0 ? -INFINITY : l[i];
+        m = fmaxf(m, l[i]);
     }
     m = warp_max(m);
     float z = 0.f, s = 0.f, p[PER];
@@ -177,11 +179,20 @@ __global__ void __launch_bounds__(kWarps * 32) route_grad_kernel(const RouteGrad
         s += p[i] * d[i];
     }
     s = lane_sum(s);
-    T *const out = static_cast<T *>(a.dlogits) + t * a.out_row;
+    T *const out = static_cast<T *>(a.dlogits) + t * a.out_row + lane * PER;
+    Vec<T, PER> o;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        if (lane + 32 * i < a.experts)
-            from_f32(out[lane + 32 * i], p[i] * (d[i] - s));
+        from_f32(o.v[i], p[i] * (d[i] - s));
+    if (VEC) {
+        if (lane * PER < a.experts)
+            store_vec<T, PER>(out, o);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (lane * PER + i < a.experts)
+                out[i] = o.v[i];
+    }
 }
 
 template <typename T, typename A>
@@ -194,14 +205,21 @@ cudaError_t launch(const A &a, cudaStream_t st)
         else
             return launch_early(bwd, grid, kWarps * 32, 0, st, 1, a);
     };
+    // vectors of a lane's logits where the rows' strides and length allow
+    int64_t strides = a.row | a.experts;
+    if constexpr (std::is_same_v<A, RouteGradArgs>)
+        strides |= a.out_row;
     static_assert(kRouteExperts == 256, "eight logits a lane");
     if (a.experts <= 32)
-        return go(route_kernel<T, 1>, route_grad_kernel<T, 1>);
+        return go(route_kernel<T, 1, false>, route_grad_kernel<T, 1, false>);
     if (a.experts <= 64)
-        return go(route_kernel<T, 2>, route_grad_kernel<T, 2>);
+        return strides % 2 == 0 ? go(route_kernel<T, 2, true>, route_grad_kernel<T, 2, true>)
+                                : go(route_kernel<T, 2, false>, route_grad_kernel<T, 2, false>);
     if (a.experts <= 128)
-        return go(route_kernel<T, 4>, route_grad_kernel<T, 4>);
-    return go(route_kernel<T, 8>, route_grad_kernel<T, 8>);
+        return strides % 4 == 0 ? go(route_kernel<T, 4, true>, route_grad_kernel<T, 4, true>)
+                                : go(route_kernel<T, 4, false>, route_grad_kernel<T, 4, false>);
+    return strides % 8 == 0 ? go(route_kernel<T, 8, true>, route_grad_kernel<T, 8, true>)
+                            : go(route_kernel<T, 8, false>, route_grad_kernel<T, 8, false>);
 }
 
 } // namespace

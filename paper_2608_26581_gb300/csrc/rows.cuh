@@ -14,7 +14,7 @@ namespace rfq {
 // VEC elements loaded or stored at once (16 bytes, or one element where
 // strides, sizes or addresses allow no more).
 template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) Vec {
+struct alignas(sizeof(T) * VEC < 16 ? sizeof(T) * VEC : 16) Vec {
     T v[VEC];
 };
 
@@ -35,7 +35,18 @@ __device__ __forceinline__ void store_vec(T *p, const Vec<T, VEC> &v)
     *reinterpret_cast<Vec<T, VEC> *>(p) = v;
 }
 
-// Stores that leave L1 to what is read again.
+// Loads and stores that leave L1 to what is read again.
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> load_once(const T *p)
+{
+    if constexpr (sizeof(T) * VEC == 16) {
+        uint4 u;
+        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+        return *reinterpret_cast<Vec<T, VEC> *>(&u);
+    } else
+        return load_vec<T, VEC>(p);
+}
+
 template <typename T, int VEC>
 __device__ __forceinline__ void store_once(T *p, const Vec<T, VEC> &v)
 {
