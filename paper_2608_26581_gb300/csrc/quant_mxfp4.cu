@@ -361,7 +361,8 @@ __global__ void dequant_mxfp4_kernel(const uint32_t *__restrict__ codes, const u
     const int64_t kchunks = k >> 3;
     for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < rows * kchunks;
          c += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t m = c / kchunks, cc = c % kchunks;
+        // (a division in 64 bits takes longer than the rest of the work)
+        const int64_t m = rows * kchunks <= UINT32_MAX ? (uint32_t)c / (uint32_t)kchunks : c / kchunks, cc = c - m * kchunks;
         const int sb = scales[scale_index<LAYOUT>(m, cc >> 2, k >> 5)];
         float q[8];
         e2m1x8_decode(codes[c], q);
@@ -379,7 +380,8 @@ __global__ void dequant_mxfp4_bf16_kernel(const uint32_t *__restrict__ codes, co
     const int64_t kchunks = k >> 3;
     for (int64_t c = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; c < rows * kchunks;
          c += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t m = c / kchunks, cc = c % kchunks;
+        // (a division in 64 bits takes longer than the rest of the work)
+        const int64_t m = rows * kchunks <= UINT32_MAX ? (uint32_t)c / (uint32_t)kchunks : c / kchunks, cc = c - m * kchunks;
         const int sb = scales[scale_index<LAYOUT>(m, cc >> 2, k >> 5)];
         float q[8];
         e2m1x8_decode(codes[c], q);
