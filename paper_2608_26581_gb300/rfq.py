@@ -611,62 +611,64 @@ def rfq_matvec(x: torch.Tensor, wq: QTensor, y: torch.Tensor, stream=None):
 
 
 # ---- around a mixture-of-experts block: norms, the router, rows to experts and back
+# (These calls are short next to what Python takes to make them: conditions are
+# written out, and sizes asked for once.)
 
-def _on_device(call: str, t: torch.Tensor, *others: torch.Tensor | None) -> int:
-    """The device of t, on which every other tensor lies too (None: left out)."""
-    dev = t.get_device()
-    for o in others:
-        if o is not None and o.get_device() != dev:
-            raise ValueError(f"{call}: tensors must be on one device")
-    if dev < 0:
-        raise ValueError(f"{call}: tensors must be on a CUDA device")
-    return dev
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _launch(call: str, f, dev: int, stream, *args):
     """f(*args, stream) with `dev` the current device; stream: the caller's, or the device's current one."""
+    if dev < 0:
+        raise ValueError(f"{call}: tensors must be on a CUDA device")
     if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(dev)
+        stream = _current_stream(dev)
     elif hasattr(stream, "cuda_stream"):
         stream = stream.cuda_stream
-    if dev == torch._C._cuda_getDevice():
-        status = f(*args, int(stream))
+    if dev == _current_device():
+        status = f(*args, stream)
     else:
         with torch.cuda.device(dev):
-            status = f(*args, int(stream))
-    if status != RFQ_OK:
+            status = f(*args, stream)
+    if status:
         raise RFQError(status, call)
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
+def _refuse(call: str, what: str):
+    raise ValueError(f"{call}: {what}")
 
 
-def _is(t: torch.Tensor | None, dtype, n: int) -> bool:
-    """t is contiguous, of that type and of n elements (or None)."""
-    return t is None or (t.dtype is dtype and t.numel() == n and t.is_contiguous())
+def _elsewhere(call: str):
+    raise ValueError(f"{call}: tensors must be on one device")
 
 
-def _rows3(t: torch.Tensor):
-    """[tokens, heads, dim] of a norm's rows: a 2-d tensor has one head."""
-    return t if t.dim() == 3 else t.unsqueeze(1)
+def _norm_rows(t: torch.Tensor):
+    """(token stride, head stride, whether the elements of a row lie together) of [rows, dim] or [tokens, heads, dim]."""
+    s, n = t.stride(), t.shape
+    if len(s) == 2:
+        return s[0] if n[0] > 1 else 0, 0, s[1] == 1 or n[1] == 1
+    return s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] == 1 or n[2] == 1
 
 
-def _rows2(t: torch.Tensor, call: str) -> int:
-    """Stride between the rows of a [rows, n] tensor, whose elements lie together."""
-    _want(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), call, "the elements of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else 0
-
-
-def _norm_params(call: str, dim: int, weight, bias) -> int:
-    """The type of weight and bias."""
-    w = weight if weight is not None else bias
-    if w is None:
-        return RFQ_OUT_F32
+def _norm_param(w, dim: int, dev: int, call: str) -> int:
+    """The type of a weight or bias."""
     dtype = _DTYPES.get(w.dtype)
-    _want(dtype is not None and _is(weight, w.dtype, dim) and _is(bias, w.dtype, dim), call,
-          "weight and bias are contiguous [dim] tensors, fp32 or bf16 alike")
+    if dtype is None or w.numel() != dim or not w.is_contiguous():
+        _refuse(call, "weight and bias are contiguous [dim] tensors, fp32 or bf16 alike")
+    if w.get_device() != dev:
+        _elsewhere(call)
     return dtype
+
+
+def _norm_sum(t, n: int, dev: int, call: str) -> int:
+    """The address of an fp32 tensor of n elements (mean, rstd, dweight, dbias)."""
+    if t.dtype is not _F32 or t.numel() != n or not t.is_contiguous():
+        _refuse(call, "mean and rstd are contiguous fp32 of one element a row, dweight and dbias of one a column")
+    if t.get_device() != dev:
+        _elsewhere(call)
+    return t.data_ptr()
 
 
 def rfq_norm(x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
@@ -676,19 +678,28 @@ def rfq_norm(x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = Non
     heads, dim] (fp32 or bf16 alike, any strides with unit stride in dim; y may
     be x); weight, bias [dim]; mean, rstd fp32 of one element a row, kept for
     rfq_norm_grad (see include/rfq.h)."""
-    dtype = _DTYPES.get(x.dtype)
-    _want(dtype is not None and y.dtype is x.dtype, "rfq_norm", "x and y are fp32 or bf16 alike")
-    _want(x.dim() in (2, 3) and y.shape == x.shape, "rfq_norm", "x and y are [rows, dim] or [tokens, heads, dim]")
-    x3, y3 = _rows3(x), _rows3(y)
-    T, H, D = x3.shape
-    (xt, xh, xd), (yt, yh, yd) = _strides(x3), _strides(y3)
-    _want((xd == 1 and yd == 1) or D == 1, "rfq_norm", "the elements of a row must be contiguous")
-    w_dtype = _norm_params("rfq_norm", D, weight, bias)
-    _want(_is(mean, torch.float32, T * H) and _is(rstd, torch.float32, T * H), "rfq_norm",
-          "mean and rstd are contiguous fp32, one element a row")
-    dev = _on_device("rfq_norm", x, y, weight, bias, mean, rstd)
-    _launch("rfq_norm", load_library().rfq_norm, dev, stream, x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, dtype,
-            T, H, D, kind, eps, _at(weight), _at(bias), w_dtype, _at(mean), _at(rstd))
+    call, shape, dev, dtype = "rfq_norm", x.shape, x.get_device(), _DTYPES.get(x.dtype)
+    if dtype is None or y.dtype is not x.dtype or y.shape != shape or len(shape) not in (2, 3):
+        _refuse(call, "x and y are [rows, dim] or [tokens, heads, dim], fp32 or bf16 alike")
+    T, H, D = shape if len(shape) == 3 else (shape[0], 1, shape[1])
+    (xt, xh, x_ok), (yt, yh, y_ok) = _norm_rows(x), _norm_rows(y)
+    if not (x_ok and y_ok):
+        _refuse(call, "the elements of a row must be contiguous")
+    w_dtype = b_dtype = None
+    if weight is not None:
+        w_dtype = _norm_param(weight, D, dev, call)
+    if bias is not None:
+        b_dtype = _norm_param(bias, D, dev, call)
+        if w_dtype is None:
+            w_dtype = b_dtype
+        elif b_dtype != w_dtype:
+            _refuse(call, "weight and bias are contiguous [dim] tensors, fp32 or bf16 alike")
+    if y.get_device() != dev:
+        _elsewhere(call)
+    _launch(call, load_library().rfq_norm, dev, stream, x.data_ptr(), xt, xh, y.data_ptr(), yt, yh, dtype, T, H, D, kind,
+            eps, None if weight is None else weight.data_ptr(), None if bias is None else bias.data_ptr(), w_dtype or 0,
+            None if mean is None else _norm_sum(mean, T * H, dev, call),
+            None if rstd is None else _norm_sum(rstd, T * H, dev, call))
 
 
 _norm_ws: dict[tuple[int, int], int] = {}     # workspace bytes by device and dim
@@ -714,66 +725,71 @@ def rfq_norm_grad(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, dx: tor
     mean, rstd as rfq_norm wrote them (mean None with RFQ_NORM_RMS); dweight,
     dbias fp32 [dim] or None, for which workspace is norm_workspace(dim) (see
     include/rfq.h)."""
-    dtype = _DTYPES.get(x.dtype)
-    _want(dtype is not None and dy.dtype is x.dtype and dx.dtype is x.dtype, "rfq_norm_grad",
-          "dy, x and dx are fp32 or bf16 alike")
-    _want(x.dim() in (2, 3) and dy.shape == x.shape and dx.shape == x.shape, "rfq_norm_grad",
-          "dy, x and dx are [rows, dim] or [tokens, heads, dim]")
-    x3 = _rows3(x)
-    T, H, D = x3.shape
-    (dt, dh, dd), (xt, xh, xd), (ot, oh, od) = _strides(_rows3(dy)), _strides(x3), _strides(_rows3(dx))
-    _want((dd == 1 and xd == 1 and od == 1) or D == 1, "rfq_norm_grad", "the elements of a row must be contiguous")
-    w_dtype = _norm_params("rfq_norm_grad", D, weight, None)
-    _want(_is(mean, torch.float32, T * H) and _is(rstd, torch.float32, T * H), "rfq_norm_grad",
-          "mean and rstd are contiguous fp32, one element a row")
-    _want(_is(dweight, torch.float32, D) and _is(dbias, torch.float32, D), "rfq_norm_grad",
-          "dweight and dbias are contiguous fp32 [dim] tensors")
+    call, shape, dev, dtype = "rfq_norm_grad", x.shape, x.get_device(), _DTYPES.get(x.dtype)
+    if (dtype is None or dy.dtype is not x.dtype or dx.dtype is not x.dtype or dy.shape != shape or dx.shape != shape or
+            len(shape) not in (2, 3)):
+        _refuse(call, "dy, x and dx are [rows, dim] or [tokens, heads, dim], fp32 or bf16 alike")
+    T, H, D = shape if len(shape) == 3 else (shape[0], 1, shape[1])
+    (dt, dh, d_ok), (xt, xh, x_ok), (ot, oh, o_ok) = _norm_rows(dy), _norm_rows(x), _norm_rows(dx)
+    if not (d_ok and x_ok and o_ok):
+        _refuse(call, "the elements of a row must be contiguous")
+    if dy.get_device() != dev or dx.get_device() != dev:
+        _elsewhere(call)
+    w_dtype = 0 if weight is None else _norm_param(weight, D, dev, call)
+    ws = None
     if dweight is not None or dbias is not None:
-        key = (x.device.index, D)
-        if key not in _norm_ws and x.device.type == "cuda":
-            with torch.cuda.device(x.device):
-                _norm_ws[key] = rfq_norm_grad_workspace_bytes(D)
-        _want(workspace is not None and workspace.is_contiguous() and
-              workspace.numel() * workspace.element_size() >= _norm_ws.get(key, 0), "rfq_norm_grad",
-              "the workspace is smaller than rfq_norm_grad_workspace_bytes")
-    dev = _on_device("rfq_norm_grad", x, dy, dx, rstd, mean, weight, dweight, dbias, workspace)
-    _launch("rfq_norm_grad", load_library().rfq_norm_grad, dev, stream, dy.data_ptr(), dt, dh, x.data_ptr(), xt,
-            xh, dx.data_ptr(), ot, oh, dtype, T, H, D, kind, _at(mean), _at(rstd), _at(weight), w_dtype,
-            _at(dweight), _at(dbias), _at(workspace))
+        need = _norm_ws.get((dev, D))
+        if need is None and dev >= 0:
+            with torch.cuda.device(dev):
+                need = _norm_ws[dev, D] = rfq_norm_grad_workspace_bytes(D)
+        if workspace is None or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < (need or 0):
+            _refuse(call, "the workspace is smaller than rfq_norm_grad_workspace_bytes")
+        if workspace.get_device() != dev:
+            _elsewhere(call)
+        ws = workspace.data_ptr()
+    _launch(call, load_library().rfq_norm_grad, dev, stream, dy.data_ptr(), dt, dh, x.data_ptr(), xt, xh, dx.data_ptr(), ot,
+            oh, dtype, T, H, D, kind, None if mean is None else _norm_sum(mean, T * H, dev, call),
+            _norm_sum(rstd, T * H, dev, call), None if weight is None else weight.data_ptr(), w_dtype,
+            None if dweight is None else _norm_sum(dweight, D, dev, call),
+            None if dbias is None else _norm_sum(dbias, D, dev, call), ws)
+
+
+def _route_sizes(call: str, logits, ids, weights):
+    """(type, row stride, tokens, experts, top_k, device) of a router's call."""
+    dtype, n, dev = _DTYPES.get(logits.dtype), ids.shape, logits.get_device()
+    T, E = logits.shape
+    row, one = logits.stride()
+    if dtype is None or (one != 1 and E > 1):
+        _refuse(call, "logits are [tokens, experts], fp32 or bf16, the elements of a row contiguous")
+    if (len(n) != 2 or n[0] != T or weights.shape != n or ids.dtype is not _I32 or weights.dtype is not _F32 or
+            not ids.is_contiguous() or not weights.is_contiguous()):
+        _refuse(call, "ids (int32) and weights (fp32) are contiguous [tokens, top_k]")
+    if ids.get_device() != dev or weights.get_device() != dev:
+        _elsewhere(call)
+    return dtype, row if T > 1 else 0, T, E, n[1], dev
 
 
 def rfq_route(logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, normalize: bool = True, stream=None):
     """The router: the top_k experts of each token and their weights from
     logits [tokens, experts] (fp32 or bf16, rows strided) into ids int32 and
     weights fp32 [tokens, top_k] (see include/rfq.h)."""
-    dtype = _DTYPES.get(logits.dtype)
-    _want(dtype is not None, "rfq_route", "logits are fp32 or bf16")
-    row = _rows2(logits, "rfq_route")
-    T, E = logits.shape
-    _want(ids.dim() == 2 and ids.shape[0] == T and weights.shape == ids.shape and _is(ids, torch.int32, ids.numel()) and
-          _is(weights, torch.float32, ids.numel()), "rfq_route",
-          "ids (int32) and weights (fp32) are contiguous [tokens, top_k]")
-    dev = _on_device("rfq_route", logits, ids, weights)
-    _launch("rfq_route", load_library().rfq_route, dev, stream, logits.data_ptr(), row, dtype, T, E,
-            ids.shape[1], 1 if normalize else 0, ids.data_ptr(), weights.data_ptr())
+    dtype, row, T, E, k, dev = _route_sizes("rfq_route", logits, ids, weights)
+    _launch("rfq_route", load_library().rfq_route, dev, stream, logits.data_ptr(), row, dtype, T, E, k,
+            1 if normalize else 0, ids.data_ptr(), weights.data_ptr())
 
 
 def rfq_route_grad(logits: torch.Tensor, ids: torch.Tensor, dweights: torch.Tensor, dlogits: torch.Tensor,
                    normalize: bool = True, stream=None):
     """Gradient of rfq_route's weights: dweights fp32 [tokens, top_k] into
     dlogits like logits (see include/rfq.h)."""
-    dtype = _DTYPES.get(logits.dtype)
-    _want(dtype is not None and dlogits.dtype is logits.dtype and dlogits.shape == logits.shape, "rfq_route_grad",
-          "logits and dlogits are fp32 or bf16 and of one shape")
-    row, out_row = _rows2(logits, "rfq_route_grad"), _rows2(dlogits, "rfq_route_grad")
-    T, E = logits.shape
-    _want(ids.dim() == 2 and ids.shape[0] == T and dweights.shape == ids.shape and _is(ids, torch.int32, ids.numel()) and
-          _is(dweights, torch.float32, ids.numel()), "rfq_route_grad",
-          "ids (int32) and dweights (fp32) are contiguous [tokens, top_k]")
-    dev = _on_device("rfq_route_grad", logits, ids, dweights, dlogits)
-    _launch("rfq_route_grad", load_library().rfq_route_grad, dev, stream, logits.data_ptr(), row, dtype, T, E,
-            ids.shape[1], 1 if normalize else 0, ids.data_ptr(), dweights.data_ptr(), dlogits.data_ptr(),
-            out_row)
+    dtype, row, T, E, k, dev = _route_sizes("rfq_route_grad", logits, ids, dweights)
+    out_row, one = dlogits.stride() if dlogits.dim() == 2 else (0, 0)
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or (one != 1 and E > 1):
+        _refuse("rfq_route_grad", "dlogits is like logits, the elements of a row contiguous")
+    if dlogits.get_device() != dev:
+        _elsewhere("rfq_route_grad")
+    _launch("rfq_route_grad", load_library().rfq_route_grad, dev, stream, logits.data_ptr(), row, dtype, T, E, k,
+            1 if normalize else 0, ids.data_ptr(), dweights.data_ptr(), dlogits.data_ptr(), out_row if T > 1 else 0)
 
 
 def rfq_moe_rows(tokens: int, top_k: int, experts: int, align: int = 128) -> int:
@@ -788,22 +804,54 @@ def rfq_moe_sort(ids: torch.Tensor, group_off: torch.Tensor, row_of: torch.Tenso
     """Pairs of ids [tokens, top_k] sorted by expert: group_off [experts + 1],
     row_of [tokens, top_k], pair_of [rows], all int32 and contiguous; workspace:
     256 bytes, zeroed once, for the device status (see include/rfq.h)."""
-    i32 = torch.int32
-    _want(ids.dim() == 2 and row_of.shape == ids.shape and group_off.numel() >= 1 and
-          _is(ids, i32, ids.numel()) and _is(row_of, i32, ids.numel()) and _is(group_off, i32, group_off.numel()) and
-          _is(pair_of, i32, pair_of.numel()), "rfq_moe_sort",
-          "ids and row_of are [tokens, top_k], group_off [experts + 1], pair_of [rows], contiguous int32")
-    _want(workspace.numel() * workspace.element_size() >= 256, "rfq_moe_sort", "the workspace is 256 bytes")
-    dev = _on_device("rfq_moe_sort", ids, group_off, row_of, pair_of, workspace)
-    _launch("rfq_moe_sort", load_library().rfq_moe_sort, dev, stream, ids.data_ptr(), ids.shape[0],
-            ids.shape[1], group_off.numel() - 1, align, group_off.data_ptr(), row_of.data_ptr(),
-            pair_of.data_ptr(), pair_of.numel(), workspace.data_ptr())
+    n, dev, experts, rows = ids.shape, ids.get_device(), group_off.numel() - 1, pair_of.numel()
+    if (len(n) != 2 or row_of.shape != n or experts < 0 or ids.dtype is not _I32 or row_of.dtype is not _I32 or
+            group_off.dtype is not _I32 or pair_of.dtype is not _I32 or not ids.is_contiguous() or
+            not row_of.is_contiguous() or not group_off.is_contiguous() or not pair_of.is_contiguous()):
+        _refuse("rfq_moe_sort", "ids and row_of are [tokens, top_k], group_off [experts + 1], pair_of [rows], contiguous int32")
+    if workspace.numel() * workspace.element_size() < 256:
+        _refuse("rfq_moe_sort", "the workspace is 256 bytes")
+    if (row_of.get_device() != dev or group_off.get_device() != dev or pair_of.get_device() != dev or
+            workspace.get_device() != dev):
+        _elsewhere("rfq_moe_sort")
+    _launch("rfq_moe_sort", load_library().rfq_moe_sort, dev, stream, ids.data_ptr(), n[0], n[1], experts, align,
+            group_off.data_ptr(), row_of.data_ptr(), pair_of.data_ptr(), rows, workspace.data_ptr())
 
 
-def _moe_maps(call: str, tokens: int, rows: int, row_of: torch.Tensor, pair_of: torch.Tensor | None):
-    _want(row_of.dim() == 2 and row_of.shape[0] == tokens and _is(row_of, torch.int32, row_of.numel()), call,
-          "row_of is a contiguous int32 [tokens, top_k]")
-    _want(_is(pair_of, torch.int32, rows), call, "pair_of is a contiguous int32 [rows]")
+def _moe_rows(call: str, tokens, stacked, row_of, pair_of):
+    """(type, row stride of the tokens, tokens, dim, rows, top_k, device) of a call that moves rows."""
+    dtype, n, dev, S = _DTYPES.get(tokens.dtype), row_of.shape, tokens.get_device(), stacked.shape
+    T, D = tokens.shape
+    row, one = tokens.stride()
+    if dtype is None or stacked.dtype is not tokens.dtype or len(S) != 2 or S[1] != D or not stacked.is_contiguous():
+        _refuse(call, "the tokens' rows and the stacked ones are fp32 or bf16 alike, of one length, the stacked contiguous")
+    if one != 1 and D > 1:
+        _refuse(call, "the elements of a row must be contiguous")
+    if stacked.get_device() != dev:
+        _elsewhere(call)
+    _moe_maps(call, T, S[0], row_of, pair_of, n, dev)
+    return dtype, row if T > 1 else 0, T, D, S[0], n[1], dev
+
+
+def _moe_maps(call: str, tokens: int, rows: int, row_of, pair_of, n, dev: int):
+    if len(n) != 2 or n[0] != tokens or row_of.dtype is not _I32 or not row_of.is_contiguous():
+        _refuse(call, "row_of is a contiguous int32 [tokens, top_k]")
+    if row_of.get_device() != dev:
+        _elsewhere(call)
+    if pair_of is not None:
+        if pair_of.dtype is not _I32 or pair_of.numel() != rows or not pair_of.is_contiguous():
+            _refuse(call, "pair_of is a contiguous int32 [rows]")
+        if pair_of.get_device() != dev:
+            _elsewhere(call)
+
+
+def _moe_weights(call: str, w, n, dev: int) -> int:
+    """The address of weights or their gradients."""
+    if w.dtype is not _F32 or w.shape != n or not w.is_contiguous():
+        _refuse(call, "weights and dweights are contiguous fp32 [tokens, top_k]")
+    if w.get_device() != dev:
+        _elsewhere(call)
+    return w.data_ptr()
 
 
 def rfq_moe_gather(x: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, pair_of: torch.Tensor | None = None,
@@ -811,15 +859,9 @@ def rfq_moe_gather(x: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, pai
     """out[row_of[t, j]] = x[t]: x [tokens, dim] (fp32 or bf16, rows strided),
     out [rows, dim] contiguous; rows of no pair are cleared with pair_of, left
     alone without (see include/rfq.h)."""
-    dtype = _DTYPES.get(x.dtype)
-    _want(dtype is not None and out.dtype is x.dtype, "rfq_moe_gather", "x and out are fp32 or bf16 alike")
-    row = _rows2(x, "rfq_moe_gather")
-    _want(out.dim() == 2 and out.shape[1] == x.shape[1] and out.is_contiguous(), "rfq_moe_gather",
-          "out is a contiguous [rows, dim]")
-    _moe_maps("rfq_moe_gather", x.shape[0], out.shape[0], row_of, pair_of)
-    dev = _on_device("rfq_moe_gather", x, row_of, pair_of, out)
-    _launch("rfq_moe_gather", load_library().rfq_moe_gather, dev, stream, x.data_ptr(), row, dtype, x.shape[0],
-            x.shape[1], row_of.data_ptr(), row_of.shape[1], _at(pair_of), out.data_ptr(), out.shape[0])
+    dtype, row, T, D, rows, k, dev = _moe_rows("rfq_moe_gather", x, out, row_of, pair_of)
+    _launch("rfq_moe_gather", load_library().rfq_moe_gather, dev, stream, x.data_ptr(), row, dtype, T, D, row_of.data_ptr(),
+            k, None if pair_of is None else pair_of.data_ptr(), out.data_ptr(), rows)
 
 
 def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, weights: torch.Tensor | None = None,
@@ -827,16 +869,10 @@ def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, we
     """out[t] = sum_j weights[t, j] y[row_of[t, j]]: y [rows, dim] contiguous,
     out [tokens, dim] (fp32 or bf16 alike, rows strided), weights fp32 [tokens,
     top_k] or None (1; see include/rfq.h)."""
-    dtype = _DTYPES.get(y.dtype)
-    _want(dtype is not None and out.dtype is y.dtype, "rfq_moe_combine", "y and out are fp32 or bf16 alike")
-    row = _rows2(out, "rfq_moe_combine")
-    _want(y.dim() == 2 and y.shape[1] == out.shape[1] and y.is_contiguous(), "rfq_moe_combine",
-          "y is a contiguous [rows, dim]")
-    _moe_maps("rfq_moe_combine", out.shape[0], y.shape[0], row_of, None)
-    _want(_is(weights, torch.float32, row_of.numel()), "rfq_moe_combine", "weights are contiguous fp32 [tokens, top_k]")
-    dev = _on_device("rfq_moe_combine", y, row_of, weights, out)
-    _launch("rfq_moe_combine", load_library().rfq_moe_combine, dev, stream, y.data_ptr(), dtype, y.shape[0],
-            y.shape[1], row_of.data_ptr(), _at(weights), out.shape[0], row_of.shape[1], out.data_ptr(), row)
+    dtype, row, T, D, rows, k, dev = _moe_rows("rfq_moe_combine", out, y, row_of, None)
+    _launch("rfq_moe_combine", load_library().rfq_moe_combine, dev, stream, y.data_ptr(), dtype, rows, D, row_of.data_ptr(),
+            None if weights is None else _moe_weights("rfq_moe_combine", weights, row_of.shape, dev), T, k, out.data_ptr(),
+            row)
 
 
 def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tensor, weights: torch.Tensor,
@@ -844,19 +880,16 @@ def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tens
     """Gradients of rfq_moe_combine: dout [tokens, dim] (rows strided) into dy
     like y (may be y) and dweights fp32 [tokens, top_k]; rows of no pair are
     cleared with pair_of, left alone without (see include/rfq.h)."""
-    dtype = _DTYPES.get(y.dtype)
-    _want(dtype is not None and dout.dtype is y.dtype and dy.dtype is y.dtype, "rfq_moe_combine_grad",
-          "dout, y and dy are fp32 or bf16 alike")
-    row = _rows2(dout, "rfq_moe_combine_grad")
-    _want(y.dim() == 2 and y.shape[1] == dout.shape[1] and dy.shape == y.shape and y.is_contiguous() and
-          dy.is_contiguous(), "rfq_moe_combine_grad", "y and dy are contiguous [rows, dim]")
-    _moe_maps("rfq_moe_combine_grad", dout.shape[0], y.shape[0], row_of, pair_of)
-    _want(_is(weights, torch.float32, row_of.numel()) and _is(dweights, torch.float32, row_of.numel()),
-          "rfq_moe_combine_grad", "weights and dweights are contiguous fp32 [tokens, top_k]")
-    dev = _on_device("rfq_moe_combine_grad", y, dout, row_of, pair_of, weights, dy, dweights)
-    _launch("rfq_moe_combine_grad", load_library().rfq_moe_combine_grad, dev, stream, dout.data_ptr(), row,
-            y.data_ptr(), dtype, y.shape[0], y.shape[1], row_of.data_ptr(), _at(pair_of), weights.data_ptr(),
-            dout.shape[0], row_of.shape[1], dy.data_ptr(), dweights.data_ptr())
+    call = "rfq_moe_combine_grad"
+    dtype, row, T, D, rows, k, dev = _moe_rows(call, dout, y, row_of, pair_of)
+    if dy.dtype is not y.dtype or dy.shape != y.shape or not dy.is_contiguous():
+        _refuse(call, "dy is like y")
+    if dy.get_device() != dev:
+        _elsewhere(call)
+    n = row_of.shape
+    _launch(call, load_library().rfq_moe_combine_grad, dev, stream, dout.data_ptr(), row, y.data_ptr(), dtype, rows, D,
+            row_of.data_ptr(), None if pair_of is None else pair_of.data_ptr(), _moe_weights(call, weights, n, dev), T, k,
+            dy.data_ptr(), _moe_weights(call, dweights, n, dev))
 
 
 def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTensor | None = None,
@@ -864,12 +897,16 @@ def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTe
     """rfq_moe_gather that quantizes x (bf16 [tokens, k], rows strided) into
     the MXFP4 operands of rfq_linear_grouped, X~ into xq and X^ into xr (see
     include/rfq.h)."""
-    _want(x.dtype is torch.bfloat16, "rfq_moe_quantize", "x is bf16")
-    row = _rows2(x, "rfq_moe_quantize")
-    _want(xq.k == x.shape[1] and (xr is None or (xr.rows == xq.rows and xr.k == xq.k)), "rfq_moe_quantize",
-          "sizes do not match")
-    _moe_maps("rfq_moe_quantize", x.shape[0], xq.rows, row_of, pair_of)
-    dev = _on_device("rfq_moe_quantize", x, row_of, pair_of, xq.codes, xq.scales, None if xr is None else xr.codes,
-                     None if xr is None else xr.scales)
-    _launch("rfq_moe_quantize", load_library().rfq_moe_quantize, dev, stream, x.data_ptr(), row, x.shape[0],
-            row_of.data_ptr(), row_of.shape[1], _at(pair_of), xq.c(), None if xr is None else xr.c())
+    call, n, dev = "rfq_moe_quantize", row_of.shape, x.get_device()
+    T, D = x.shape
+    row, one = x.stride()
+    if x.dtype is not _BF16 or one != 1:
+        _refuse(call, "x is bf16 [tokens, k], the elements of a row contiguous")
+    if xq.k != D or (xr is not None and (xr.rows != xq.rows or xr.k != D)):
+        _refuse(call, "sizes do not match")
+    _moe_maps(call, T, xq.rows, row_of, pair_of, n, dev)
+    for q in (xq,) if xr is None else (xq, xr):
+        if q.codes.get_device() != dev or q.scales.get_device() != dev:
+            _elsewhere(call)
+    _launch(call, load_library().rfq_moe_quantize, dev, stream, x.data_ptr(), row if T > 1 else 0, T, row_of.data_ptr(), n[1],
+            None if pair_of is None else pair_of.data_ptr(), xq.c(), None if xr is None else xr.c())
