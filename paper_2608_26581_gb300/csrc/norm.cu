@@ -91,15 +91,47 @@ struct Split {
     }
 };
 
-// Where rows lie: [tokens][heads] with two strides in elements.
-template <typename T>
-__device__ __forceinline__ T *row_at(T *p, int64_t token, int64_t head, uint32_t row, uint32_t heads)
-{
-    if (heads == 1)
-        return p + row * token;
-    const uint32_t t = row / heads;
-    return p + t * token + (row - t * heads) * head;
-}
+// Rows in steps, as (token, head): rows lie [tokens][heads] with two strides in
+// elements.  (A division for each row costs as much as its 8 elements.)
+struct Walk {
+    uint32_t token, head, tokens_on, heads_on, heads;
+    __device__ __forceinline__ Walk(uint32_t row, uint32_t step, uint32_t h)
+        : token(row / h), head(row - token * h), tokens_on(step / h), heads_on(step - tokens_on * h), heads(h)
+    {
+    }
+    __device__ __forceinline__ void next()
+    {
+        token += tokens_on;
+        head += heads_on;
+        if (head >= heads) {
+            head -= heads;
+            ++token;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ T *at(T *p, int64_t token_stride, int64_t head_stride) const
+    {
+        return p + token * token_stride + head * head_stride;
+    }
+};
+
+// The same without a state, for rows of a whole block.
+struct Place {
+    uint32_t row, step, heads;
+    __device__ __forceinline__ Place(uint32_t r, uint32_t s, uint32_t h) : row(r), step(s), heads(h) {}
+    __device__ __forceinline__ void next() { row += step; }
+    template <typename T>
+    __device__ __forceinline__ T *at(T *p, int64_t token_stride, int64_t head_stride) const
+    {
+        if (heads == 1)
+            return p + row * token_stride;
+        const uint32_t t = row / heads;
+        return p + t * token_stride + (row - t * heads) * head_stride;
+    }
+};
+template <typename P>
+using Rows = std::conditional_t<P::kBlock, Place, Walk>;
+
 
 // VEC parameters from column c on, in fp32.
 template <int VEC>
@@ -178,7 +210,7 @@ template <typename P>
 constexpr int kForwardRows = P::VEC == 1 ? 0 : P::NV == 2 ? 4 : 2;
 
 template <typename P>
-__global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : kMostThreads<P> <= 512 ? 2 : 1) norm_kernel(const NormArgs a)
+__global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> <= 512 ? 2 : 1) : 4) norm_kernel(const NormArgs a)
 {
     using T = typename P::T;
     using F = typename P::F;
@@ -190,26 +222,35 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
     const int chunks = a.dim / P::VEC;
     const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * p.groups();
     const float inv = 1.f / (float)a.dim;
-    auto row_x = [&](uint32_t r) { return row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads); };
+    uint32_t first = blockIdx.x * p.groups();
+    Rows<P> here(first + p.group, step, a.heads), there_at = here;       // this turn's row; the one that is copied next
     auto ahead = [&](int slot, uint32_t r) {
-        ring.copy(p, slot, 0, row_x(r), r < rows, chunks);
+        ring.copy(p, slot, 0, there_at.at(static_cast<const T *>(a.x), a.x_token, a.x_head), r < rows, chunks);
         ring_commit();
+        there_at.next();
     };
     if (P::kBlock && threadIdx.x < 32)
         s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = 0.f;
     wait_for_previous();
     let_next_start();
-    uint32_t first = blockIdx.x * p.groups();
     if constexpr (S > 0)
 #pragma unroll 1
         for (int s = 0; s < S - 1; ++s)
             ahead(s, first + p.group + s * step);
     if (P::kBlock)
         __syncthreads();
+    // (few lanes a row: many rows for the same few weights)
+    constexpr bool HELD = !P::kBlock && P::VEC > 1 && NV == 2;
+    F held[HELD ? NV : 1][L];
+    if (HELD && a.weight)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (p.has(i, chunks))
+                load_params<P::VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * P::VEC, held[HELD ? i : 0]);
     int slot = 0, turn = 0;
     // (every thread of the block takes part in the sums of every turn)
 #pragma unroll 1
-    for (; first < rows; first += step, turn ^= 1) {
+    for (; first < rows; first += step, turn ^= 1, here.next()) {
         const uint32_t row = first + p.group;
         const bool there = P::kBlock || row < rows;
         F d[NV][L];
@@ -221,7 +262,7 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
             ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
             slot = slot == S - 1 ? 0 : slot + 1;
         } else
-            load_row(p, row_x(row), there, chunks, d);
+            load_row(p, here.at(static_cast<const T *>(a.x), a.x_token, a.x_head), there, chunks, d);
         float mean = 0.f;
         if (!a.rms) {
             F s = all_of<P::VEC>(0.f);
@@ -253,7 +294,7 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
                 a.rstd[row] = rstd;
         }
         const F scale = all_of<P::VEC>(rstd);
-        T *const y = row_at(static_cast<T *>(a.y), a.y_token, a.y_head, row, a.heads);
+        T *const y = here.at(static_cast<T *>(a.y), a.y_token, a.y_head);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (p.has(i, chunks)) {
@@ -263,10 +304,11 @@ __global__ void __launch_bounds__(kMostThreads<P>, kMostThreads<P> <= 256 ? 4 : 
                 for (int e = 0; e < L; ++e)
                     d[i][e] = d[i][e] * scale;
                 if (a.weight) {
-                    load_params<P::VEC>(a.weight, a.w_bf16, c, f);
+                    if (!HELD)
+                        load_params<P::VEC>(a.weight, a.w_bf16, c, f);
 #pragma unroll
                     for (int e = 0; e < L; ++e)
-                        d[i][e] = d[i][e] * f[e];
+                        d[i][e] = d[i][e] * (HELD ? held[HELD ? i : 0][e] : f[e]);
                 }
                 if (a.bias) {
                     load_params<P::VEC>(a.bias, a.w_bf16, c, f);
@@ -329,16 +371,18 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
     const int chunks = a.dim / VEC, groups = p.groups();
     const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * groups;
     const float inv = 1.f / (float)a.dim;
+    uint32_t first = blockIdx.x * groups;
+    Rows<P> here(first + p.group, step, a.heads), there_at = here;       // this turn's row; the one that is copied next
     auto ahead = [&](int slot, uint32_t r) {
-        ring.copy(p, slot, 0, row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, r, a.heads), r < rows, chunks);
-        ring.copy(p, slot, 1, row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, r, a.heads), r < rows, chunks);
+        ring.copy(p, slot, 0, there_at.at(static_cast<const T *>(a.x), a.x_token, a.x_head), r < rows, chunks);
+        ring.copy(p, slot, 1, there_at.at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head), r < rows, chunks);
         ring_commit();
+        there_at.next();
     };
     if (P::kBlock && threadIdx.x < 32)
         s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = {0.f, 0.f};
     wait_for_previous();
     let_next_start();
-    uint32_t first = blockIdx.x * groups;
     if constexpr (S > 0)
 #pragma unroll 1
         for (int s = 0; s < (TWICE ? S : S - 1); ++s)
@@ -364,7 +408,7 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
     int slot = 0, turn = 0;
     // (every thread of the block takes part in the sums of every turn)
 #pragma unroll 1
-    for (; first < rows; first += step, turn ^= 1) {
+    for (; first < rows; first += step, turn ^= 1, here.next()) {
         const uint32_t row = first + p.group;
         const bool there = P::kBlock || row < rows;
         const F less = all_of<VEC>(-next_mean);
@@ -383,8 +427,8 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
                 const int64_t c = (p.first + i * P::kStep) * VEC;
                 auto vx = zero_vec<T, VEC>(), vd = zero_vec<T, VEC>();
                 if (in) {
-                    vx = load_vec<T, VEC>(row_at(static_cast<const T *>(a.x), a.x_token, a.x_head, row, a.heads) + c);
-                    vd = load_vec<T, VEC>(row_at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head, row, a.heads) + c);
+                    vx = load_vec<T, VEC>(here.at(static_cast<const T *>(a.x), a.x_token, a.x_head) + c);
+                    vd = load_vec<T, VEC>(here.at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head) + c);
                 }
                 unpack<T, VEC>(vx, h[k]);
                 unpack<T, VEC>(vd, g[k]);
@@ -399,16 +443,16 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
                     g[TWICE ? 0 : i][e] = g[TWICE ? 0 : i][e] * w[e];
             }
         };
+        if constexpr (S > 0 && !TWICE)
+            ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
         if constexpr (S > 0)
-            ring_wait<TWICE ? S - 1 : S - 2>();
+            ring_wait<S - 1>();
         if constexpr (!TWICE) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 fetch(i);
-            if constexpr (S > 0) {
-                ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
+            if constexpr (S > 0)
                 slot = slot == S - 1 ? 0 : slot + 1;
-            }
         }
         F sg = all_of<VEC>(0.f), sh = sg;
 #pragma unroll
@@ -435,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
         if (there) {
             // (g - mean g - h mean(g h)) rstd
             const F to_g = all_of<VEC>(a.rms ? 0.f : -(s.x * inv) * rstd), to_h = all_of<VEC>(-(s.y * inv) * rstd);
-            T *const dx = row_at(static_cast<T *>(a.dx), a.dx_token, a.dx_head, row, a.heads);
+            T *const dx = here.at(static_cast<T *>(a.dx), a.dx_token, a.dx_head);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (p.has(i, chunks)) {
