@@ -785,6 +785,7 @@ RFQ_API int64_t rfq_moe_rows(int64_t tokens, int32_t top_k, int32_t experts, int
  *     group_off is cut there, and the device status becomes RFQ_ERR_SHAPE.
  *   workspace: device, 256 bytes zeroed by the caller once, for the device status
  *     (rfq_workspace_status).
+ * No two of the arrays overlap.
  * 1 <= experts <= 256, 1 <= top_k <= 32, 1 <= align <= 4096,
  * tokens * top_k + experts * align < 2^31, rows < 2^31.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
@@ -802,8 +803,7 @@ RFQ_API rfq_status rfq_moe_sort(const int32_t *ids, int64_t tokens, int32_t top_
  *   out: device [rows][dim] of dtype, contiguous; not x.
  * A row that two pairs name gets either token.  Its gradient in x is
  * rfq_moe_combine without weights.
- * 1 <= dim <= 65536, 1 <= top_k <= 32, tokens * top_k < 2^31, rows < 2^31 and
- * (tokens * top_k + rows) ceil(dim / 32) < 2^34.
+ * 1 <= dim <= 65536, 1 <= top_k <= 32, tokens * top_k < 2^31, rows < 2^31.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
  * RFQ_ERR_DEVICE. */
 RFQ_API rfq_status rfq_moe_gather(const void *x, int64_t x_row_stride, int32_t dtype, int64_t tokens, int32_t dim,

