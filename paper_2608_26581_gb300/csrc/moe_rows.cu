@@ -292,7 +292,23 @@ __global__ void __launch_bounds__(kWarps * 32) moe_quantize_kernel(const MoeQuan
     }
 }
 
-bool wide(int64_t bits, bool bf16) { return bits % (bf16 ? 8 : 4) == 0; }
+template <typename T_, int VEC_>
+struct Width {
+    using T = T_;
+    static constexpr int VEC = VEC_;
+};
+
+// Calls go with the widest vectors, of up to 16 bytes, that divide strides and length (`bits`: all of them or'ed).
+template <typename G>
+cudaError_t by_width(int64_t bits, bool bf16, G &&go)
+{
+    if (bf16)
+        return bits % 8 == 0   ? go(Width<__nv_bfloat16, 8>())
+               : bits % 4 == 0 ? go(Width<__nv_bfloat16, 4>())
+               : bits % 2 == 0 ? go(Width<__nv_bfloat16, 2>())
+                               : go(Width<__nv_bfloat16, 1>());
+    return bits % 4 == 0 ? go(Width<float, 4>()) : bits % 2 == 0 ? go(Width<float, 2>()) : go(Width<float, 1>());
+}
 
 // Blocks of kWarps warps for so many items (pairs and stacked rows are counted in 31 bits: no more than a grid holds).
 unsigned blocks_of(int64_t items) { return (unsigned)((items + kWarps - 1) / kWarps); }
@@ -324,26 +340,17 @@ cudaError_t combine_grad(const MoeCombineGradArgs &a, cudaStream_t st)
 
 cudaError_t launch_moe_gather(const MoeGatherArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.x_row | a.dim, a.bf16);
-    if (a.bf16)
-        return w ? gather<__nv_bfloat16, 8>(a, st) : gather<__nv_bfloat16, 1>(a, st);
-    return w ? gather<float, 4>(a, st) : gather<float, 1>(a, st);
+    return by_width(a.x_row | a.dim, a.bf16, [&](auto v) { return gather<typename decltype(v)::T, decltype(v)::VEC>(a, st); });
 }
 
 cudaError_t launch_moe_combine(const MoeCombineArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.out_row | a.dim, a.bf16);
-    if (a.bf16)
-        return w ? combine<__nv_bfloat16, 8>(a, st) : combine<__nv_bfloat16, 1>(a, st);
-    return w ? combine<float, 4>(a, st) : combine<float, 1>(a, st);
+    return by_width(a.out_row | a.dim, a.bf16, [&](auto v) { return combine<typename decltype(v)::T, decltype(v)::VEC>(a, st); });
 }
 
 cudaError_t launch_moe_combine_grad(const MoeCombineGradArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.dout_row | a.dim, a.bf16);
-    if (a.bf16)
-        return w ? combine_grad<__nv_bfloat16, 8>(a, st) : combine_grad<__nv_bfloat16, 1>(a, st);
-    return w ? combine_grad<float, 4>(a, st) : combine_grad<float, 1>(a, st);
+    return by_width(a.dout_row | a.dim, a.bf16, [&](auto v) { return combine_grad<typename decltype(v)::T, decltype(v)::VEC>(a, st); });
 }
 
 cudaError_t launch_moe_quantize(const MoeQuantizeArgs &a, cudaStream_t st)

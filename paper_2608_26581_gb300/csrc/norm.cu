@@ -12,22 +12,25 @@
 // in registers, so the mean and the squared distances from it are two passes
 // over registers.  Rows that come next are on their way to shared memory: a
 // thread copies (cp.async) and reads its own 16-byte chunks alone, so the ring
-// needs no barrier.  (Rows that are not whole 16-byte chunks are loaded when
-// their turn comes.)  A thread's chunks lie a fixed distance apart, which
+// needs no barrier.  Where strides and sizes allow no more, chunks are words, and
+// the next row's are loaded into registers (a row of bf16 that starts in the
+// middle of a word takes two words for each chunk, and joins them).  A thread's chunks lie a fixed distance apart, which
 // leaves one address a row; arithmetic is on pairs of fp32 values.  The
 // weight's gradient is summed in fp32 in registers by threads that keep their
 // columns over all their rows; the blocks' sums go through the workspace and a
 // second kernel adds them, both in a fixed order.
 //
 // 32760 rows of 5120 bf16: forward 112 us, 6.0 TB/s, 89% of the copy rate;
-// backward 166 us with both sums, 90% (155 us without weights and sums: the
-// partial sums of 304 blocks, 12 MB, and their kernel are 8 of the 11).  Heads
-// of 128: forward 87%, backward 95%.  fp32 rows of 4096: 87 and 89%.  Issue
+// backward 166 us with both sums, 89% (148 us without weights and sums: the
+// partial sums of 304 blocks, 12 MB there and back, and their kernel take 8 of
+// the 18, the weights' loads the rest).  Heads of 128: forward 87%, backward 95%.
+// fp32 rows of 4096: 87 and 89%.  Issue
 // slots are 65% busy at that.  Rows beyond 8192 elements backwards are slower (13824: 50%): a thread
 // has 64 registers there, and the row is read from shared memory twice.
 // (Measured and not kept: tiles of several rows gone through twice, first by
 // rows, then by columns, 188 us backwards; weights in shared memory, 197; the
-// next row asked for after this one's sums, 184 to 220.)
+// next row asked for after this one's sums, 184 to 220; weights loaded ahead of
+// the row or held, 183.)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -57,6 +60,8 @@ template <typename T_, int VEC_, int NV_, int TPR_>
 struct Split {
     using T = T_;
     static constexpr int VEC = VEC_, NV = NV_, TPR = TPR_;
+    static constexpr int kChunk = VEC * (int)sizeof(T);               // bytes: 16, or 4
+    static constexpr bool kNarrow = kChunk == 4, kHalves = kNarrow && VEC == 2;
     static constexpr bool kBlock = TPR > 32;
     static constexpr int kStep = kBlock ? 32 : TPR;                   // chunks between a thread's
     static constexpr int kLanesOf = kLanes<VEC>;
@@ -139,14 +144,32 @@ struct Place {
         return p + t * token_stride + (row - t * heads) * head_stride;
     }
 };
+// The end of an array of rows (for chunks that are words of two elements).
+template <typename P, typename T>
+__device__ __forceinline__ const T *array_end(const T *p, int64_t token_stride, int64_t head_stride, uint32_t rows, uint32_t heads, int dim)
+{
+    return P::kHalves ? p + (int64_t)(rows / heads - 1) * token_stride + (int64_t)(heads - 1) * head_stride + dim : nullptr;
+}
+
+__device__ __forceinline__ F2 first_only(F2 v)
+{
+    float a, b;
+    f2unpack(v.v, a, b);
+    return {f2pack(a, 0.f)};
+}
+
 template <typename P>
 using Rows = std::conditional_t<P::kBlock, Place, Walk>;
 
-// VEC parameters from column c on, in fp32.
+// VEC parameters from column c on (of dim), in fp32.
 template <int VEC>
-__device__ __forceinline__ void load_params(const void *p, bool bf16, int c, Lane<VEC> *v)
+__device__ __forceinline__ void load_params(const void *p, bool bf16, int c, int dim, Lane<VEC> *v)
 {
-    if (bf16)
+    if (VEC == 2 && c + 1 == dim) {          // (the last of an odd number)
+        const float one = bf16 ? to_f32(static_cast<const __nv_bfloat16 *>(p)[c]) : static_cast<const float *>(p)[c];
+        if constexpr (VEC == 2)
+            v[0] = {f2pack(one, 0.f)};
+    } else if (bf16)
         unpack<__nv_bfloat16, VEC>(load_vec<__nv_bfloat16, VEC>(static_cast<const __nv_bfloat16 *>(p) + c), v);
     else {
         constexpr int F = VEC < 4 ? VEC : 4;
@@ -163,8 +186,7 @@ __device__ __forceinline__ uint4 lds128(uint32_t at)
     return u;
 }
 
-// Rows on their way, S deep, N arrays: chunks of 16 bytes copied ahead into
-// shared memory (with S = 0 a row is loaded when its turn comes).
+// Rows on their way, S deep, N arrays: 16-byte chunks copied ahead into shared memory.
 template <typename P, int N, int S>
 struct Ring {
     using T = typename P::T;
@@ -190,6 +212,54 @@ struct Ring {
         unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), x);
     }
 };
+
+// A row that starts in the middle of a word (of bf16 elements).
+__device__ __forceinline__ uint32_t half_off(const void *row) { return (uint32_t)reinterpret_cast<uintptr_t>(row) & 2u; }
+
+// A thread's words of a row.
+template <typename P>
+struct Words {
+    using T = typename P::T;
+    uint32_t low[P::NV], high[P::kHalves ? P::NV : 1], off;
+    // The word of bf16 elements at `from`, or its first half alone.
+    static __device__ __forceinline__ uint32_t halves(const char *from, bool both)
+    {
+        return both ? *reinterpret_cast<const uint32_t *>(from) : (uint32_t)*reinterpret_cast<const uint16_t *>(from);
+    }
+    // x: the row; end: of its array (which a word that holds the last element may pass)
+    __device__ __forceinline__ void load(const P &p, const T *x, const T *end, bool there, int chunks, int dim)
+    {
+        off = P::kHalves ? half_off(x) : 0;
+        const int most = P::kHalves && x + dim == end ? dim : INT32_MAX;      // elements that may be read, from x on
+        const char *const word = reinterpret_cast<const char *>(x + p.first * P::VEC) - off;
+        const int e = p.first * 2 - (off ? 1 : 0);                             // the first word's first element
+#pragma unroll
+        for (int i = 0; i < P::NV; ++i) {
+            low[i] = 0;
+            if constexpr (P::kHalves)
+                high[i] = 0;
+            if (there && p.has(i, chunks)) {
+                if constexpr (P::kHalves) {
+                    low[i] = halves(word + i * P::kStep * 4, e + i * P::kStep * 2 + 1 < most);
+                    if (off && 2 * (p.first + i * P::kStep) + 1 < dim)
+                        high[i] = halves(word + i * P::kStep * 4 + 4, e + i * P::kStep * 2 + 3 < most);
+                } else
+                    low[i] = *reinterpret_cast<const uint32_t *>(word + i * P::kStep * 4);
+            }
+        }
+    }
+    __device__ __forceinline__ void get(const P &p, int i, int dim, typename P::F *v) const
+    {
+        uint32_t u = low[i];
+        if constexpr (P::kHalves) {
+            if (off)
+                u = __funnelshift_r(u, high[i], 16);
+            if (2 * (p.first + i * P::kStep) + 1 == dim)
+                u &= 0xFFFFu;                // (zero behind the last of an odd number)
+        }
+        unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), v);
+    }
+};
 __device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void ring_wait() // until no more than N rows are on their way
@@ -197,26 +267,31 @@ __device__ __forceinline__ void ring_wait() // until no more than N rows are on 
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// Chunk i of a result's row.
 template <typename P>
-__device__ __forceinline__ void load_row(const P &p, const typename P::T *row, bool there, int chunks, typename P::F (&x)[P::NV][P::kLanesOf])
+__device__ __forceinline__ void store_chunk(const P &p, typename P::T *row, int i, int dim, const typename P::F *v)
 {
-#pragma unroll
-    for (int i = 0; i < P::NV; ++i) {
-        auto v = zero_vec<typename P::T, P::VEC>();
-        if (there && p.has(i, chunks))
-            v = load_vec<typename P::T, P::VEC>(row + (p.first + i * P::kStep) * P::VEC);
-        unpack<typename P::T, P::VEC>(v, x[i]);
+    const int c = (p.first + i * P::kStep) * P::VEC;
+    const auto u = pack<typename P::T, P::VEC>(v);
+    if constexpr (P::kHalves) {
+        if (half_off(row) || c + 1 == dim) {
+            row[c] = u.v[0];
+            if (c + 1 < dim)
+                row[c + 1] = u.v[1];
+            return;
+        }
     }
+    store_once<typename P::T, P::VEC>(row + c, u);
 }
-
-// The most threads of a block.
+// The most threads of a block (with 8 elements each it takes rows of up to kFewElements).
+constexpr int kFewElements = 8192;
 template <typename P>
-constexpr int kMostThreads = P::kBlock ? kNormDim / (32 * P::NV * P::VEC) * 32 : kThreads;
+constexpr int kMostThreads = P::kBlock ? (P::NV * P::VEC == 8 ? kFewElements : kNormDim) / (P::NV * P::VEC) : kThreads;
 
 // Rows of the forward ring.  (Deeper ones take L1 from the weights: with three
 // rows of 5120 elements a layer norm of 32760 takes 116 us, with two 112.)
 template <typename P>
-constexpr int kForwardRows = P::VEC == 1 ? 0 : P::NV == 2 ? 4 : 2;
+constexpr int kForwardRows = P::kNarrow ? 0 : P::NV == 2 ? 4 : 2;
 
 template <typename P>
 __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> <= 512 ? 2 : 1) : 4) norm_kernel(const NormArgs a)
@@ -228,34 +303,39 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
     __shared__ float s_part[2][32];
     const P p;
     const Ring<P, 1, S> ring(s_ring);
-    const int chunks = a.dim / P::VEC;
+    const int chunks = (a.dim + P::VEC - 1) / P::VEC;
     const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * p.groups();
     const float inv = 1.f / (float)a.dim;
     uint32_t first = blockIdx.x * p.groups();
     Rows<P> here(first + p.group, step, a.heads), next = here;        // this turn's row; the one that is copied next
+    const T *const x = static_cast<const T *>(a.x), *const x_end = array_end<P>(x, a.x_token, a.x_head, rows, a.heads, a.dim);
+    Words<P> words;                          // of the next row
     auto ahead = [&](int slot, uint32_t r) {
-        ring.copy(p, slot, 0, next.at(static_cast<const T *>(a.x), a.x_token, a.x_head), r < rows, chunks);
-        ring_commit();
+        if constexpr (P::kNarrow)
+            words.load(p, next.at(x, a.x_token, a.x_head), x_end, r < rows, chunks, a.dim);
+        else {
+            ring.copy(p, slot, 0, next.at(x, a.x_token, a.x_head), r < rows, chunks);
+            ring_commit();
+        }
         next.next();
     };
     if (P::kBlock && threadIdx.x < 32)
         s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = 0.f;
     wait_for_previous();
     let_next_start();
-    if constexpr (S > 0)
 #pragma unroll 1
-        for (int s = 0; s < S - 1; ++s)
-            ahead(s, first + p.group + s * step);
+    for (int s = 0; s < (P::kNarrow ? 1 : S - 1); ++s)
+        ahead(s, first + p.group + s * step);
     if (P::kBlock)
         __syncthreads();
     // (few lanes a row: many rows for the same few weights)
-    constexpr bool HELD = !P::kBlock && P::VEC > 1 && NV == 2;
+    constexpr bool HELD = P::kNarrow ? NV * P::VEC <= 8 : !P::kBlock && NV == 2;
     F held[HELD ? NV : 1][L];
     if (HELD && a.weight)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (p.has(i, chunks))
-                load_params<P::VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * P::VEC, held[HELD ? i : 0]);
+                load_params<P::VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * P::VEC, a.dim, held[HELD ? i : 0]);
     int slot = 0, turn = 0;
     // (every thread of the block takes part in the sums of every turn)
 #pragma unroll 1
@@ -263,15 +343,19 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
         const uint32_t row = first + p.group;
         const bool there = P::kBlock || row < rows;
         F d[NV][L];
-        if constexpr (S > 0) {
+        if constexpr (P::kNarrow) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                words.get(p, i, a.dim, d[i]);
+            ahead(0, row + step);
+        } else {
             ring_wait<S - 2>();
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 ring.read(slot, 0, i, there && p.has(i, chunks), d[i]);
             ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
             slot = slot == S - 1 ? 0 : slot + 1;
-        } else
-            load_row(p, here.at(static_cast<const T *>(a.x), a.x_token, a.x_head), there, chunks, d);
+        }
         float mean = 0.f;
         if (!a.rms) {
             F s = all_of<P::VEC>(0.f);
@@ -290,6 +374,9 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
 #pragma unroll
                 for (int e = 0; e < L; ++e) {
                     d[i][e] = d[i][e] + less;
+                    if constexpr (P::kHalves)
+                        if (2 * (p.first + i * P::kStep) + 1 == a.dim)
+                            d[i][e] = first_only(d[i][e]);
                     q = fused(d[i][e], d[i][e], q);
                 }
         // (two sums a turn, or with RMS one; rsqrtf is off by two steps of fp32 at most)
@@ -314,47 +401,48 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
                     d[i][e] = d[i][e] * scale;
                 if (a.weight) {
                     if (!HELD)
-                        load_params<P::VEC>(a.weight, a.w_bf16, c, f);
+                        load_params<P::VEC>(a.weight, a.w_bf16, c, a.dim, f);
 #pragma unroll
                     for (int e = 0; e < L; ++e)
                         d[i][e] = d[i][e] * (HELD ? held[HELD ? i : 0][e] : f[e]);
                 }
                 if (a.bias) {
-                    load_params<P::VEC>(a.bias, a.w_bf16, c, f);
+                    load_params<P::VEC>(a.bias, a.w_bf16, c, a.dim, f);
 #pragma unroll
                     for (int e = 0; e < L; ++e)
                         d[i][e] = d[i][e] + f[e];
                 }
-                store_once<T, P::VEC>(y + c, pack<T, P::VEC>(d[i]));
+                store_chunk(p, y, i, a.dim, d[i]);
             }
     }
 }
 
 // The backward kernel for blocks of up to THREADS threads: blocks on an SM,
-// rows of its ring (of two arrays; none without 16-byte chunks), and whether a
-// row is read from the ring a second time for dx instead of staying in
-// registers (where 64 of them have to do).
+// rows of its ring (of two arrays), and whether a row is read from the ring a
+// second time for dx instead of staying in registers (where 64 of them have to
+// do).
 template <typename P, int THREADS>
 struct Backward {
     static constexpr int kBlocks = THREADS <= 320 ? 2 : 1;
-    static constexpr bool kTwice = P::VEC > 1 && THREADS > 512;
+    static constexpr bool kTwice = !P::kNarrow && THREADS > 512;
+    static constexpr bool kAhead = P::kNarrow && P::NV * P::VEC <= 8;    // the next row's words in registers
     static constexpr size_t kRow = (size_t)P::NV * 2 * 16;    // bytes of a thread
     // (three rows of a block's: 189 us instead of 166)
     static constexpr int rows()
     {
         const size_t n = kMostSmem / kBlocks / THREADS / kRow, most = P::kBlock ? 2 : 3;
-        return P::VEC == 1 ? 0 : (int)(n < most ? n : most);
+        return P::kNarrow ? 0 : (int)(n < most ? n : most);
     }
     static constexpr int kRows = rows();
-    static_assert(P::VEC == 1 || kRows >= (kTwice ? 1 : 2), "a row on its way beside one that has been read");
+    static_assert(P::kNarrow || kRows >= (kTwice ? 1 : 2), "a row on its way beside one that has been read");
     static constexpr size_t bytes(int threads) { return kRows * kRow * threads; }
 };
 
 template <int VEC>
 __device__ __forceinline__ void store_sums(float *to, const Lane<VEC> *v)
 {
-    if constexpr (VEC == 1)
-        *to = v[0];
+    if constexpr (VEC <= 2)
+        *reinterpret_cast<Lane<VEC> *>(to) = v[0];
     else
 #pragma unroll
         for (int e = 0; e < kLanes<VEC>; e += 2)
@@ -378,25 +466,32 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
     __shared__ Pair s_part[2][32];
     const P p;
     const Ring<P, 2, S> ring(smem);
-    const int chunks = a.dim / VEC, groups = p.groups();
+    const int chunks = (a.dim + VEC - 1) / VEC, groups = p.groups();
     const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * groups;
     const float inv = 1.f / (float)a.dim;
     uint32_t first = blockIdx.x * groups;
     Rows<P> here(first + p.group, step, a.heads), next = here;        // this turn's row; the one that is copied next
+    const T *const x = static_cast<const T *>(a.x), *const x_end = array_end<P>(x, a.x_token, a.x_head, rows, a.heads, a.dim);
+    const T *const dy = static_cast<const T *>(a.dy), *const dy_end = array_end<P>(dy, a.dy_token, a.dy_head, rows, a.heads, a.dim);
+    Words<P> words_x, words_dy;              // of the next row
     auto ahead = [&](int slot, uint32_t r) {
-        ring.copy(p, slot, 0, next.at(static_cast<const T *>(a.x), a.x_token, a.x_head), r < rows, chunks);
-        ring.copy(p, slot, 1, next.at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head), r < rows, chunks);
-        ring_commit();
+        if constexpr (P::kNarrow) {
+            words_x.load(p, next.at(x, a.x_token, a.x_head), x_end, r < rows, chunks, a.dim);
+            words_dy.load(p, next.at(dy, a.dy_token, a.dy_head), dy_end, r < rows, chunks, a.dim);
+        } else {
+            ring.copy(p, slot, 0, next.at(x, a.x_token, a.x_head), r < rows, chunks);
+            ring.copy(p, slot, 1, next.at(dy, a.dy_token, a.dy_head), r < rows, chunks);
+            ring_commit();
+        }
         next.next();
     };
     if (P::kBlock && threadIdx.x < 32)
         s_part[0][threadIdx.x] = s_part[1][threadIdx.x] = {0.f, 0.f};
     wait_for_previous();
     let_next_start();
-    if constexpr (S > 0)
 #pragma unroll 1
-        for (int s = 0; s < (TWICE ? S : S - 1); ++s)
-            ahead(s, first + p.group + s * step);
+    for (int s = 0; s < (P::kNarrow ? B::kAhead : TWICE ? S : S - 1); ++s)
+        ahead(s, first + p.group + s * step);
     F dw[NV][L], db[NV][L];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -404,6 +499,12 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
         for (int e = 0; e < L; ++e)
             dw[i][e] = db[i][e] = all_of<VEC>(0.f);
     }
+    F held[B::kAhead ? NV : 1][L];           // weights, where there is room for them
+    if (B::kAhead && a.weight)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (p.has(i, chunks))
+                load_params<VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * VEC, a.dim, held[B::kAhead ? i : 0]);
     // (a row's statistics are loaded one row ahead)
     float next_rstd = 0.f, next_mean = 0.f;
     auto stats = [&](uint32_t r) {
@@ -430,39 +531,43 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
         auto fetch = [&](int i) {
             const int k = TWICE ? 0 : i;
             const bool in = there && p.has(i, chunks);
-            if constexpr (S > 0) {
+            if constexpr (P::kNarrow) {
+                words_x.get(p, i, a.dim, h[k]);
+                words_dy.get(p, i, a.dim, g[k]);
+            } else {
                 ring.read(slot, 0, i, in, h[k]);
                 ring.read(slot, 1, i, in, g[k]);
-            } else {
-                const int64_t c = (p.first + i * P::kStep) * VEC;
-                auto vx = zero_vec<T, VEC>(), vd = zero_vec<T, VEC>();
-                if (in) {
-                    vx = load_vec<T, VEC>(here.at(static_cast<const T *>(a.x), a.x_token, a.x_head) + c);
-                    vd = load_vec<T, VEC>(here.at(static_cast<const T *>(a.dy), a.dy_token, a.dy_head) + c);
-                }
-                unpack<T, VEC>(vx, h[k]);
-                unpack<T, VEC>(vd, g[k]);
             }
         };
         auto weighted = [&](int i) {
             if (a.weight) {
                 F w[L];
-                load_params<VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * VEC, w);
+                if (B::kAhead) {
+#pragma unroll
+                    for (int e = 0; e < L; ++e)
+                        w[e] = held[B::kAhead ? i : 0][e];
+                } else
+                    load_params<VEC>(a.weight, a.w_bf16, (p.first + i * P::kStep) * VEC, a.dim, w);
 #pragma unroll
                 for (int e = 0; e < L; ++e)
                     g[TWICE ? 0 : i][e] = g[TWICE ? 0 : i][e] * w[e];
             }
         };
-        if constexpr (S > 0 && !TWICE)
-            ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
-        if constexpr (S > 0)
+        if constexpr (P::kNarrow) {
+            if constexpr (!B::kAhead)
+                ahead(0, row);
+        } else {
+            if constexpr (!TWICE)
+                ahead(slot == 0 ? S - 1 : slot - 1, row + (S - 1) * step);
             ring_wait<S - 1>();
+        }
         if constexpr (!TWICE) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 fetch(i);
-            if constexpr (S > 0)
-                slot = slot == S - 1 ? 0 : slot + 1;
+            slot = slot == S - 1 ? 0 : slot + 1;
+            if constexpr (B::kAhead)
+                ahead(0, row + step);
         }
         F sg = all_of<VEC>(0.f), sh = sg;
 #pragma unroll
@@ -504,7 +609,7 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
 #pragma unroll
                     for (int e = 0; e < L; ++e)
                         g[k][e] = fused(h[k][e], to_h, fused(g[k][e], scale, to_g));
-                    store_once<T, VEC>(dx + (p.first + i * P::kStep) * VEC, pack<T, VEC>(g[k]));
+                    store_chunk(p, dx, i, a.dim, g[k]);
                 }
         }
         if constexpr (TWICE) {
@@ -518,7 +623,7 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
     float *const out = a.partial + (int64_t)blockIdx.x * 2 * padded;
     float *const s_sums = reinterpret_cast<float *>(smem);
     if (groups > 1) {
-        if constexpr (S > 0)
+        if constexpr (!P::kNarrow)
             asm volatile("cp.async.wait_all;" ::: "memory");   // (the sums take the ring's place)
         __syncthreads();
     }
@@ -586,10 +691,12 @@ cudaError_t with_split(int chunks, G &&go)
 {
     if (chunks > 32 * NV)
         return go((Split<T, VEC, NV, 64> *)nullptr);
-    if (VEC == 1 && chunks > 128)
-        return go((Split<T, VEC, NV, 32> *)nullptr);
-    if (NV > 2 && chunks > 64)
-        return go((Split<T, VEC, (NV > 4 ? 4 : NV), 32> *)nullptr);
+    if (NV >= 16 && chunks > 256)
+        return go((Split<T, VEC, (NV < 16 ? 2 : 16), 32> *)nullptr);
+    if (NV >= 8 && chunks > 128)
+        return go((Split<T, VEC, (NV < 8 ? 2 : 8), 32> *)nullptr);
+    if (NV >= 4 && chunks > 64)
+        return go((Split<T, VEC, (NV < 4 ? 2 : 4), 32> *)nullptr);
     if (chunks > 32)
         return go((Split<T, VEC, 2, 32> *)nullptr);
     if (chunks > 16)
@@ -610,20 +717,18 @@ int threads_of(int chunks)
 template <typename T, int VEC, int MOST>
 cudaError_t launch_forward(const NormArgs &a, cudaStream_t st)
 {
-    return with_split<T, VEC, MOST>(a.dim / VEC, [&](auto split) -> cudaError_t {
+    const int chunks = (a.dim + VEC - 1) / VEC;
+    return with_split<T, VEC, MOST>(chunks, [&](auto split) -> cudaError_t {
         using P = std::remove_pointer_t<decltype(split)>;
-        const int threads = threads_of<P>(a.dim / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
+        const int threads = threads_of<P>(chunks), groups = P::kBlock ? 1 : threads / P::TPR;
         const int64_t turns = (a.rows + groups - 1) / groups;
         const size_t smem = Ring<P, 1, kForwardRows<P>>::bytes(threads);
-        int64_t blocks = turns;              // (loaded at once: a block for each turn)
-        if (smem > 0) {
-            static PerDevice<bool> allowed;
-            if (smem > kPlainSmem)
-                if (cudaError_t e = allow_smem((const void *)norm_kernel<P>, (int)kMostSmem, allowed))
-                    return e;
-            const int64_t most = (int64_t)num_sms() * max(1, min(1024 / threads, (int)(kMostSmem / smem)));
-            blocks = turns < most ? turns : most;
-        }
+        static PerDevice<bool> allowed;
+        if (smem > kPlainSmem)
+            if (cudaError_t e = allow_smem((const void *)norm_kernel<P>, (int)kMostSmem, allowed))
+                return e;
+        const int64_t most = (int64_t)num_sms() * max(1, min(1024 / threads, (int)(kMostSmem / max(smem, (size_t)1))));
+        const int64_t blocks = turns < most ? turns : most;
         return launch_early(norm_kernel<P>, dim3((unsigned)blocks), threads, smem, st, 1, a);
     });
 }
@@ -649,9 +754,9 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
     a.partial = sums ? static_cast<float *>(a.workspace) : nullptr;
     int blocks = 0;
     if (a.rows > 0) {
-        const cudaError_t e = with_split<T, VEC, MOST>(a.dim / VEC, [&](auto split) -> cudaError_t {
+        const cudaError_t e = with_split<T, VEC, MOST>((a.dim + VEC - 1) / VEC, [&](auto split) -> cudaError_t {
             using P = std::remove_pointer_t<decltype(split)>;
-            const int threads = threads_of<P>(a.dim / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
+            const int threads = threads_of<P>((a.dim + VEC - 1) / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
             const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * backward_blocks(threads);
             blocks = (int)(turns < most ? turns : most);
             if constexpr (P::kBlock) {
@@ -684,23 +789,18 @@ size_t norm_grad_workspace_bytes(int32_t dim)
 
 cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.x_token | a.x_head | a.y_token | a.y_head | a.dim, a.bf16);
+    const bool w = wide(a.x_token | a.x_head | a.y_token | a.y_head | a.dim, a.bf16), few = a.dim <= kFewElements / 2;
     if (a.bf16)
-        return w ? launch_forward<__nv_bfloat16, 8, 4>(a, st) : launch_forward<__nv_bfloat16, 1, 16>(a, st);
-    return w ? launch_forward<float, 4, 4>(a, st) : launch_forward<float, 1, 16>(a, st);
+        return w ? launch_forward<__nv_bfloat16, 8, 4>(a, st) : few ? launch_forward<__nv_bfloat16, 2, 4>(a, st) : launch_forward<__nv_bfloat16, 2, 8>(a, st);
+    return w ? launch_forward<float, 4, 4>(a, st) : few ? launch_forward<float, 1, 8>(a, st) : launch_forward<float, 1, 16>(a, st);
 }
 
 cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16);
-    // (not whole 16-byte chunks: 8 elements a thread as long as 512 threads hold the row)
+    const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16), few = a.dim <= kFewElements;
     if (a.bf16)
-        return w                ? launch_backward<__nv_bfloat16, 8, 2>(a, st)
-               : a.dim <= 4096 ? launch_backward<__nv_bfloat16, 1, 8>(a, st)
-                               : launch_backward<__nv_bfloat16, 1, 16>(a, st);
-    return w                ? launch_backward<float, 4, 4>(a, st)
-           : a.dim <= 4096 ? launch_backward<float, 1, 8>(a, st)
-                           : launch_backward<float, 1, 16>(a, st);
+        return w ? launch_backward<__nv_bfloat16, 8, 2>(a, st) : few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st);
+    return w ? launch_backward<float, 4, 4>(a, st) : few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st);
 }
 
 } // namespace rfq

@@ -94,7 +94,7 @@ CASES = [(1, 1, 1, 1, "spread"), (1, 8, 16, 128, "spread"), (5, 3, 4, 1, "holes"
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("dim", [1, 8, 33, 100, 128, 1000, 2048, 4104])
+@pytest.mark.parametrize("dim", [1, 2, 6, 8, 12, 33, 100, 128, 130, 1000, 1030, 2048, 4104])
 @pytest.mark.parametrize("T,k,E,align,kind", CASES)
 def test_rows_there_and_back(T, k, E, align, kind, dim, dtype):
     rows, row_of, pair_of = _maps(T + dim, T, k, E, align, kind, extra=3)

@@ -73,6 +73,44 @@ def test_rows(kind, dtype, wtype, tokens, dim):
     _check(tokens, 1, 1, dim, kind, "both", dtype, wtype, seed=dim)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,dim", [(5, 2), (40, 3), (9, 10), (33, 17), (70, 31), (300, 65), (50, 131), (29, 257), (31, 258), (17, 511), (9, 513), (700, 620),
+                                        (7, 2047), (3, 4095), (3, 4097), (5, 4098), (400, 5121), (2, 8193), (3, 10001), (3, 16382)])
+def test_rows_of_no_convenient_length(dtype, tokens, dim):
+    """Rows that start inside a 16-byte word, or of bf16 inside a 4-byte one."""
+    _check(tokens, 1, 1, dim, "layer" if dim % 2 else "rms", "both", dtype, F32 if dim % 3 else dtype, seed=dim)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [1, 6, 33, 75, 300, 1001, 6000])
+@pytest.mark.parametrize("heads,row", [(1, 1), (3, 5)])
+def test_odd_strides_in_place(dtype, dim, heads, row):
+    """Rows of odd strides, the result in the place of its input: what lies
+    between the rows stays as it was."""
+    g = _gen(dim)
+    T, pad = 11, 3
+    base = _x(g, (T, row * dim + pad), dtype).to(DEV)
+    x = base[:, :row * dim].unflatten(1, (row, dim))[:, :heads]
+    dy0 = torch.randn(T, row * dim + pad, generator=g).to(dtype).to(DEV)
+    want, before = torch.empty(T, heads, dim, dtype=dtype, device=DEV), base.clone()
+    mean, rstd = torch.empty(T, heads, device=DEV), torch.empty(T, heads, device=DEV)
+    rfq.rfq_norm(x.contiguous(), want, mean=mean, rstd=rstd)
+    x64 = x.double().cpu()
+    bound = moe_ref.norm_bound(x64, None, None, 1e-6, False, dtype)[0]
+    _within(want, moe_ref.norm(x64, None, None, 1e-6, False)[0], bound)
+    keep = torch.ones(T, row * dim + pad, dtype=torch.bool, device=DEV)
+    keep[:, :row * dim].unflatten(1, (row, dim))[:, :heads] = False
+    dx = dy0.clone()
+    there = dx[:, :row * dim].unflatten(1, (row, dim))[:, :heads]
+    rfq.rfq_norm_grad(there, x, rstd, there, mean=mean)
+    args = dy0[:, :row * dim].unflatten(1, (row, dim))[:, :heads].double().cpu(), x64, mean.double().cpu(), rstd.double().cpu(), None, False
+    _within(there, moe_ref.norm_grad(*args)[0], moe_ref.norm_grad_bound(*args, dtype)[0])
+    assert torch.equal(dx[keep], dy0[keep])
+    rfq.rfq_norm(x, x)
+    _within(x, moe_ref.norm(x64, None, None, 1e-6, False)[0], bound)
+    assert torch.equal(base[keep], before[keep])
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("tokens,heads,row,dim", [(1, 1, 3, 128), (37, 5, 9, 128), (11, 40, 48, 64), (5, 3, 4, 80), (4, 3, 5, 33), (2000, 4, 6, 24)])
