@@ -97,8 +97,12 @@ __global__ void __launch_bounds__(kWarps * 32) gather_kernel(const MoeGatherArgs
     }
 }
 
-// Persistent warps take 32 vectors of a token each; the next token's rows and
-// weights are on their way while this one's are summed.
+// Vectors of a lane that are in flight together: more of them where they are short.
+template <typename T, int VEC>
+constexpr int kVectors = VEC * sizeof(T) >= 16 ? 1 : VEC * sizeof(T) >= 8 ? 2 : 4;
+
+// Persistent warps take 32 vectors (of each kind of a lane's) of a token each; the
+// next token's rows and weights are on their way while this one's are summed.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kWarps * 32, kCombineBlocks) combine_kernel(const MoeCombineArgs a)
 {
@@ -107,8 +111,8 @@ __global__ void __launch_bounds__(kWarps * 32, kCombineBlocks) combine_kernel(co
     wait_for_previous();
     let_next_start();
     const uint32_t tokens = (uint32_t)a.tokens, step = gridDim.x * kWarps;
-    const int c = blockIdx.y * 32 + lane;
-    const bool in = c < chunks;
+    constexpr int U = kVectors<T, VEC>, L = kLanes<VEC>;
+    const int c = blockIdx.y * 32 * U + lane;
     const T *const y = static_cast<const T *>(a.y) + (int64_t)c * VEC;
     int row = -1, next_row = -1;
     float w = 0.f, next_w = 0.f;
@@ -124,37 +128,46 @@ __global__ void __launch_bounds__(kWarps * 32, kCombineBlocks) combine_kernel(co
     for (; t < tokens; t += step) {
         row = next_row;
         w = next_w;
-        Lane<VEC> sum[kLanes<VEC>];
+        Lane<VEC> sum[U][L];
 #pragma unroll
-        for (int e = 0; e < kLanes<VEC>; ++e)
-            sum[e] = all_of<VEC>(0.f);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < L; ++e)
+                sum[u][e] = all_of<VEC>(0.f);
 #pragma unroll 1
         for (int j0 = 0; j0 < a.top_k; j0 += B) {
-            Vec<T, VEC> v[B];
+            Vec<T, VEC> v[B][U];
             int r[B];
 #pragma unroll
             for (int j = 0; j < B; ++j) {
                 r[j] = __shfl_sync(kAll, row, (j0 + j) & 31);
-                r[j] = j0 + j < a.top_k && in ? r[j] : -1;
-                if (r[j] >= 0)
-                    v[j] = load_once<T, VEC>(y + (int64_t)r[j] * a.dim);
+                r[j] = j0 + j < a.top_k ? r[j] : -1;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (r[j] >= 0 && c + 32 * u < chunks)
+                        v[j][u] = load_once<T, VEC>(y + (int64_t)r[j] * a.dim + 32 * u * VEC);
             }
             if (j0 == 0)
                 ahead(t + step);
 #pragma unroll
             for (int j = 0; j < B; ++j) {
                 const Lane<VEC> f = all_of<VEC>(__shfl_sync(kAll, w, (j0 + j) & 31));
-                if (r[j] >= 0) {
-                    Lane<VEC> x[kLanes<VEC>];
-                    unpack<T, VEC>(v[j], x);
+                if (r[j] >= 0)
 #pragma unroll
-                    for (int e = 0; e < kLanes<VEC>; ++e)
-                        sum[e] = fused(f, x[e], sum[e]);
-                }
+                    for (int u = 0; u < U; ++u)
+                        if (c + 32 * u < chunks) {
+                            Lane<VEC> x[L];
+                            unpack<T, VEC>(v[j][u], x);
+#pragma unroll
+                            for (int e = 0; e < L; ++e)
+                                sum[u][e] = fused(f, x[e], sum[u][e]);
+                        }
             }
         }
-        if (in)
-            store_once<T, VEC>(static_cast<T *>(a.out) + t * a.out_row + (int64_t)c * VEC, pack<T, VEC>(sum));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c + 32 * u < chunks)
+                store_once<T, VEC>(static_cast<T *>(a.out) + t * a.out_row + (int64_t)(c + 32 * u) * VEC, pack<T, VEC>(sum[u]));
     }
 }
 
@@ -162,7 +175,7 @@ __global__ void __launch_bounds__(kWarps * 32, kCombineBlocks) combine_kernel(co
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kWarps * 32) combine_grad_kernel(const MoeCombineGradArgs a)
 {
-    constexpr int U = 4;                     // vectors in flight
+    constexpr int U = 4 * kVectors<T, VEC>;  // vectors in flight
     const int lane = threadIdx.x & 31, chunks = a.dim / VEC;
     wait_for_previous();
     let_next_start();
@@ -324,7 +337,7 @@ cudaError_t gather(const MoeGatherArgs &a, cudaStream_t st)
 template <typename T, int VEC>
 cudaError_t combine(const MoeCombineArgs &a, cudaStream_t st)
 {
-    const int segs = (a.dim / VEC + 31) / 32;
+    const int per = 32 * kVectors<T, VEC>, segs = (a.dim / VEC + per - 1) / per;
     const int64_t blocks = (a.tokens + kWarps - 1) / kWarps, most = max((int64_t)1, (int64_t)num_sms() * kCombineBlocks / segs);
     return launch_early(combine_kernel<T, VEC>, dim3((unsigned)(blocks < most ? blocks : most), (unsigned)segs), kWarps * 32, 0, st, 1, a);
 }
