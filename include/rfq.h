@@ -684,8 +684,8 @@ RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows,
  * counterpart for them; the format is its own (Sec. 3.2.2, Sec. 4.3).  Arrays
  * of int32 and fp32 results need their natural alignment only; every other
  * device pointer must be 16-byte aligned.  Rows whose strides and sizes are
- * multiples of 16 bytes are read and written 16 bytes at a time, others element
- * by element.  The same inputs give the same bits. */
+ * multiples of 16 bytes are read and written 16 bytes at a time, others in
+ * smaller steps.  The same inputs give the same bits. */
 
 /* RFQ_NORM_LAYER  y = (x - mean) rstd w + b,  rstd = 1 / sqrt(variance + eps)
  * RFQ_NORM_RMS    y = x rstd w + b,           rstd = 1 / sqrt(mean x^2 + eps) */

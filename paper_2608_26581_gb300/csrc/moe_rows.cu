@@ -13,7 +13,8 @@
 // gather 35.5 us (91% of the copy rate), combine 26 us (86%), quantize with its
 // residual 26 us (70%: a scale word of four bytes takes a transaction of its
 // own; without those stores it takes 22).  combine_grad of 3001 tokens of 6
-// pairs, 1000 fp32: 25.9 us (91%).
+// pairs, 1000 fp32: 25.9 us (91%).  Rows of no whole 16-byte words go in 8-, 4-
+// or 2-byte vectors (combine of 4096 x 4 x 1023 in fp32 57%, in bf16 25%).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

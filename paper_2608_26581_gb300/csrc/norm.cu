@@ -23,10 +23,12 @@
 // 32760 rows of 5120 bf16: forward 112 us, 6.0 TB/s, 89% of the copy rate;
 // backward 166 us with both sums, 89% (148 us without weights and sums: the
 // partial sums of 304 blocks, 12 MB there and back, and their kernel take 8 of
-// the 18, the weights' loads the rest).  Heads of 128: forward 87%, backward 95%.
-// fp32 rows of 4096: 87 and 89%.  Issue
-// slots are 65% busy at that.  Rows beyond 8192 elements backwards are slower (13824: 50%): a thread
-// has 64 registers there, and the row is read from shared memory twice.
+// the 18, the weights' loads the rest).  Issue slots are 65% busy at that.
+// Heads of 128: forward 87%, backward 95%.  fp32 rows of 4096: 87 and 89%.
+// Slower are rows beyond 8192 elements backwards (13824: 50%): a thread has 64
+// registers there, and the row is read from shared memory twice; and rows of
+// words, through instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and 39%;
+// words by cp.async took longer, 45 us instead of 29 for the first).
 // (Measured and not kept: tiles of several rows gone through twice, first by
 // rows, then by columns, 188 us backwards; weights in shared memory, 197; the
 // next row asked for after this one's sums, 184 to 220; weights loaded ahead of
@@ -144,6 +146,7 @@ struct Place {
         return p + t * token_stride + (row - t * heads) * head_stride;
     }
 };
+
 // The end of an array of rows (for chunks that are words of two elements).
 template <typename P, typename T>
 __device__ __forceinline__ const T *array_end(const T *p, int64_t token_stride, int64_t head_stride, uint32_t rows, uint32_t heads, int dim)
@@ -260,6 +263,7 @@ struct Words {
         unpack<T, P::VEC>(*reinterpret_cast<Vec<T, P::VEC> *>(&u), v);
     }
 };
+
 __device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void ring_wait() // until no more than N rows are on their way
@@ -283,6 +287,7 @@ __device__ __forceinline__ void store_chunk(const P &p, typename P::T *row, int 
     }
     store_once<typename P::T, P::VEC>(row + c, u);
 }
+
 // The most threads of a block (with 8 elements each it takes rows of up to kFewElements).
 constexpr int kFewElements = 8192;
 template <typename P>

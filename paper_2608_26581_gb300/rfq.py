@@ -809,7 +809,7 @@ def rfq_moe_sort(ids: torch.Tensor, group_off: torch.Tensor, row_of: torch.Tenso
             group_off.dtype is not _I32 or pair_of.dtype is not _I32 or not ids.is_contiguous() or
             not row_of.is_contiguous() or not group_off.is_contiguous() or not pair_of.is_contiguous()):
         _refuse("rfq_moe_sort", "ids and row_of are [tokens, top_k], group_off [experts + 1], pair_of [rows], contiguous int32")
-    if workspace.numel() * workspace.element_size() < 256:
+    if workspace.numel() * workspace.element_size() < 256 or not workspace.is_contiguous():
         _refuse("rfq_moe_sort", "the workspace is 256 bytes")
     if (row_of.get_device() != dev or group_off.get_device() != dev or pair_of.get_device() != dev or
             workspace.get_device() != dev):
@@ -906,6 +906,9 @@ def rfq_moe_quantize(x: torch.Tensor, row_of: torch.Tensor, xq: QTensor, xr: QTe
         _refuse(call, "sizes do not match")
     _moe_maps(call, T, xq.rows, row_of, pair_of, n, dev)
     for q in (xq,) if xr is None else (xq, xr):
+        if (q.codes.numel() * q.codes.element_size() < q.rows * D // 2 or
+                q.scales.numel() * q.scales.element_size() < (q.rows + 127) // 128 * 4 * D):
+            _refuse(call, "codes and scales are smaller than rfq_qtensor_bytes")
         if q.codes.get_device() != dev or q.scales.get_device() != dev:
             _elsewhere(call)
     _launch(call, load_library().rfq_moe_quantize, dev, stream, x.data_ptr(), row if T > 1 else 0, T, row_of.data_ptr(), n[1],

@@ -129,7 +129,9 @@ def test_binding_refuses(lib):
            lambda: rfq.rfq_moe_combine(torch.zeros(8, 8)[::2], i32, f32),
            lambda: rfq.rfq_moe_combine_grad(f32, f32, i32, w, torch.zeros(5, 8), w), lambda: rfq.rfq_moe_combine_grad(f32, f32, i32, w, f32, w[:3]),
            lambda: rfq.rfq_moe_quantize(f32, i32, rfq.QTensor(0, 1, 8, 8, f32, f32)),
-           lambda: rfq.rfq_moe_quantize(b16, i32, rfq.QTensor(0, 1, 8, 16, f32, f32))]
+           lambda: rfq.rfq_moe_quantize(b16, i32, rfq.QTensor(0, 1, 8, 16, f32, f32)),
+           lambda: rfq.rfq_moe_quantize(torch.zeros(4, 128, dtype=torch.bfloat16), i32, rfq.QTensor(0, 1, 8, 128, f32, torch.zeros(128))),
+           lambda: rfq.rfq_moe_quantize(torch.zeros(4, 128, dtype=torch.bfloat16), i32, rfq.QTensor(0, 1, 8, 128, torch.zeros(128), f32))]
     for f in bad:
         with pytest.raises(ValueError):
             f()
