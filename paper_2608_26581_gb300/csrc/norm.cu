@@ -14,21 +14,22 @@
 // thread copies (cp.async) and reads its own 16-byte chunks alone, so the ring
 // needs no barrier.  Where strides and sizes allow no more, chunks are words, and
 // the next row's are loaded into registers (a row of bf16 that starts in the
-// middle of a word takes two words for each chunk, and joins them).  A thread's chunks lie a fixed distance apart, which
-// leaves one address a row; arithmetic is on pairs of fp32 values.  The
-// weight's gradient is summed in fp32 in registers by threads that keep their
-// columns over all their rows; the blocks' sums go through the workspace and a
-// second kernel adds them, both in a fixed order.
+// middle of a word takes two words for each chunk, and joins them).  A thread's
+// chunks lie a fixed distance apart, which leaves one address a row; arithmetic
+// is on pairs of fp32 values.  The weight's gradient is summed in fp32 in
+// registers by threads that keep their columns over all their rows; the blocks'
+// sums go through the workspace and a second kernel adds them, both in a fixed
+// order.
 //
 // 32760 rows of 5120 bf16: forward 112 us, 6.0 TB/s, 89% of the copy rate;
 // backward 166 us with both sums, 89% (148 us without weights and sums: the
 // partial sums of 304 blocks, 12 MB there and back, and their kernel take 8 of
 // the 18, the weights' loads the rest).  Issue slots are 65% busy at that.
 // Heads of 128: forward 87%, backward 95%.  fp32 rows of 4096: 87 and 89%.
-// Slower are rows beyond 8192 elements backwards (13824: 50%): a thread has 64
-// registers there, and the row is read from shared memory twice; and rows of
-// words, through instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and 39%;
-// words by cp.async took longer, 45 us instead of 29 for the first).
+// Slower are rows beyond 5120 elements backwards (8192: 77%, 13824: 61%: one
+// block on an SM, beyond 8192 the row is read from shared memory twice), and rows
+// of words, through instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and
+// 39%; words by cp.async took longer, 45 us instead of 29 for the first).
 // (Measured and not kept: tiles of several rows gone through twice, first by
 // rows, then by columns, 188 us backwards; weights in shared memory, 197; the
 // next row asked for after this one's sums, 184 to 220; weights loaded ahead of
@@ -422,14 +423,16 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
     }
 }
 
-// The backward kernel for blocks of up to THREADS threads: blocks on an SM,
-// rows of its ring (of two arrays), and whether a row is read from the ring a
-// second time for dx instead of staying in registers (where 64 of them have to
-// do).
+// Whether a row is read from the ring a second time for dx instead of staying
+// in registers (32 elements a thread).
+template <typename P>
+constexpr bool kTwice = P::NV * P::VEC > 16;
+
+// The backward kernel for blocks of up to THREADS threads: blocks on an SM and
+// rows of its ring (of two arrays).
 template <typename P, int THREADS>
 struct Backward {
     static constexpr int kBlocks = THREADS <= 320 ? 2 : 1;
-    static constexpr bool kTwice = !P::kNarrow && THREADS > 512;
     static constexpr bool kAhead = P::kNarrow && P::NV * P::VEC <= 8;    // the next row's words in registers
     static constexpr size_t kRow = (size_t)P::NV * 2 * 16;    // bytes of a thread
     // (three rows of a block's: 189 us instead of 166)
@@ -439,7 +442,7 @@ struct Backward {
         return P::kNarrow ? 0 : (int)(n < most ? n : most);
     }
     static constexpr int kRows = rows();
-    static_assert(P::kNarrow || kRows >= (kTwice ? 1 : 2), "a row on its way beside one that has been read");
+    static_assert(P::kNarrow || kRows >= (kTwice<P> ? 1 : 2), "a row on its way beside one that has been read");
     static constexpr size_t bytes(int threads) { return kRows * kRow * threads; }
 };
 
@@ -466,7 +469,7 @@ __global__ void __launch_bounds__(THREADS, Backward<P, THREADS>::kBlocks) norm_g
     using F = typename P::F;
     using B = Backward<P, THREADS>;
     constexpr int S = B::kRows, NV = P::NV, L = P::kLanesOf, VEC = P::VEC;
-    constexpr bool TWICE = B::kTwice;
+    constexpr bool TWICE = kTwice<P>;
     extern __shared__ __align__(16) uint8_t smem[];      // ring; after the last row: [groups][2][padded dim] sums where a block has several groups
     __shared__ Pair s_part[2][32];
     const P p;
@@ -762,14 +765,19 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
         const cudaError_t e = with_split<T, VEC, MOST>((a.dim + VEC - 1) / VEC, [&](auto split) -> cudaError_t {
             using P = std::remove_pointer_t<decltype(split)>;
             const int threads = threads_of<P>((a.dim + VEC - 1) / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
-            const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * backward_blocks(threads);
+            const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * (kTwice<P> ? 1 : backward_blocks(threads));
             blocks = (int)(turns < most ? turns : most);
             if constexpr (P::kBlock) {
-                if (threads > 512)
-                    return launch_backward_of<P, 1024>(a, threads, blocks, st);
-                if (threads > 320)
+                if constexpr (kTwice<P>)
                     return launch_backward_of<P, 512>(a, threads, blocks, st);
-                return launch_backward_of<P, 320>(a, threads, blocks, st);
+                else {
+                    if constexpr (P::kNarrow)
+                        if (threads > 512)
+                            return launch_backward_of<P, 1024>(a, threads, blocks, st);
+                    if (threads > 320)
+                        return launch_backward_of<P, 512>(a, threads, blocks, st);
+                    return launch_backward_of<P, 320>(a, threads, blocks, st);
+                }
             } else
                 return launch_backward_of<P, 256>(a, threads, blocks, st);
         });
@@ -803,9 +811,16 @@ cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
 cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st)
 {
     const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16), few = a.dim <= kFewElements;
+    // (16-byte chunks of 32 elements a thread where 16 would take more than 512 threads: 13824 bf16 98 us instead of 119, the floor is 59.5
+    // at the copy rate; with 5632 to 8192 elements 16 are faster)
+    const bool many = a.dim > 512 * 16;
     if (a.bf16)
-        return w ? launch_backward<__nv_bfloat16, 8, 2>(a, st) : few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st);
-    return w ? launch_backward<float, 4, 4>(a, st) : few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st);
+        return !w     ? (few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st))
+               : many ? launch_backward<__nv_bfloat16, 8, 4>(a, st)
+                      : launch_backward<__nv_bfloat16, 8, 2>(a, st);
+    return !w     ? (few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st))
+           : many ? launch_backward<float, 4, 8>(a, st)
+                  : launch_backward<float, 4, 4>(a, st);
 }
 
 } // namespace rfq
