@@ -185,9 +185,9 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
     }
     // rows of no pair: behind each group and behind the last
     for (int e = rank * kWarps + warp; e < E; e += ctas * kWarps)
-        for (int64_t r = s_end[e] + lane; r < min((int64_t)s_next[e], a.rows); r += 32)
+        for (int64_t r = (int64_t)s_end[e] + lane; r < min((int64_t)s_next[e], a.rows); r += 32)
             a.pair_of[r] = -1;
-    for (int64_t r = min(s_next[E - 1], most) + rank * kThreads + tid; r < a.rows; r += ctas * kThreads)
+    for (int64_t r = (int64_t)min(s_next[E - 1], most) + rank * kThreads + tid; r < a.rows; r += ctas * kThreads)
         a.pair_of[r] = -1;
     if (ctas > 1)
         cluster_sync();                      // (a block's shared memory is read by the others)

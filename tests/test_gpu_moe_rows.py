@@ -51,6 +51,23 @@ def test_sort(T, k, E, kind, align):
         assert torch.equal(a.cpu(), b)
 
 
+def test_sort_up_to_31_bits():
+    """As many pairs as are taken: the rows behind the last group start just below 2^31."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    T = 2 ** 31 - 2
+    # (one array, pair_of last: 2^31 elements before a row of pair_of lies row_of)
+    words = torch.zeros(3 * (2 ** 31 + 64), dtype=I32, device=DEV)
+    ids, row_of, pair_of = (w[:n] for w, n in zip(words.view(3, -1), (T, T, T + 1)))
+    off, ws = torch.zeros(2, dtype=I32, device=DEV), torch.zeros(64, dtype=I32, device=DEV)
+    rfq.rfq_moe_sort(ids.view(T, 1), off, row_of.view(T, 1), pair_of, ws, align=1)
+    assert rfq.rfq_workspace_status(ws) == rfq.RFQ_OK and off.tolist() == [0, T] and pair_of[T].item() == -1
+    for a in range(0, T, 2 ** 28):
+        want = torch.arange(a, min(T, a + 2 ** 28), dtype=I32, device=DEV)
+        assert torch.equal(row_of[a:a + 2 ** 28], want) and torch.equal(pair_of[a:min(T, a + 2 ** 28)], want)
+    assert (words.view(3, -1)[1, T:] == 0).all() and (words.view(3, -1)[2, T + 1:] == 0).all()
+
+
 def test_sort_of_many_pairs():
     """262144 pairs over one cluster, against a stable sort."""
     T, k, E = 32768, 8, 128
