@@ -26,10 +26,11 @@
 // partial sums of 304 blocks, 12 MB there and back, and their kernel take 8 of
 // the 18, the weights' loads the rest).  Issue slots are 65% busy at that.
 // Heads of 128: forward 87%, backward 95%.  fp32 rows of 4096: 87 and 89%.
-// Slower are rows beyond 5120 elements backwards (8192: 77%, 13824: 61%: one
-// block on an SM, beyond 8192 the row is read from shared memory twice), and rows
-// of words, through instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and
-// 39%; words by cp.async took longer, 45 us instead of 29 for the first).
+// Slower are rows beyond 5120 elements backwards (bf16 8192: 77%, 9216: 70%,
+// 13824: 61%, fp32 8192: 92%, 9216: 88%, 13824: 69%: one block on an SM, beyond
+// 8192 the row is read from shared memory twice), and rows of words, through
+// instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and 39%; words by
+// cp.async took longer, 45 us instead of 29 for the first).
 // (Measured and not kept: tiles of several rows gone through twice, first by
 // rows, then by columns, 188 us backwards; weights in shared memory, 197; the
 // next row asked for after this one's sums, 184 to 220; weights loaded ahead of
@@ -424,7 +425,8 @@ __global__ void __launch_bounds__(kMostThreads<P>, P::kBlock ? (kMostThreads<P> 
 }
 
 // Whether a row is read from the ring a second time for dx instead of staying
-// in registers (32 elements a thread).
+// in registers (24 elements a thread or more; 9216 bf16 in registers: 96 us
+// instead of 85, 8192 bf16, which stays there, from the ring: 90 instead of 77).
 template <typename P>
 constexpr bool kTwice = P::NV * P::VEC > 16;
 
@@ -811,16 +813,18 @@ cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
 cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st)
 {
     const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16), few = a.dim <= kFewElements;
-    // (16-byte chunks of 32 elements a thread where 16 would take more than 512 threads: 13824 bf16 98 us instead of 119, the floor is 59.5
-    // at the copy rate; with 5632 to 8192 elements 16 are faster)
-    const bool many = a.dim > 512 * 16;
+    // (Elements of a thread: the fewest that need no more than 512 threads.  At 2^26 elements, of which copies take 59.5 us: rows of
+    // 9216 bf16 with 16 take 133 us, with 24 85, with 32 130; 13824 with 16 119, with 24 119, with 32 98.)
+    const int of_thread = a.dim <= 512 * 16 ? 16 : a.dim <= 512 * 24 ? 24 : 32;
     if (a.bf16)
-        return !w     ? (few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st))
-               : many ? launch_backward<__nv_bfloat16, 8, 4>(a, st)
-                      : launch_backward<__nv_bfloat16, 8, 2>(a, st);
-    return !w     ? (few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st))
-           : many ? launch_backward<float, 4, 8>(a, st)
-                  : launch_backward<float, 4, 4>(a, st);
+        return !w                ? (few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st))
+               : of_thread == 16 ? launch_backward<__nv_bfloat16, 8, 2>(a, st)
+               : of_thread == 24 ? launch_backward<__nv_bfloat16, 8, 3>(a, st)
+                                 : launch_backward<__nv_bfloat16, 8, 4>(a, st);
+    return !w                ? (few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st))
+           : of_thread == 16 ? launch_backward<float, 4, 4>(a, st)
+           : of_thread == 24 ? launch_backward<float, 4, 6>(a, st)
+                             : launch_backward<float, 4, 8>(a, st);
 }
 
 } // namespace rfq

@@ -148,7 +148,7 @@ def test_launch_shapes(fake):
     for device in (0, 1):
         fake.device(device)
         sms = 76 if device == 1 else 152
-        for dim in (1, 2, 7, 8, 31, 64, 80, 120, 128, 256, 264, 512, 1000, 1023, 1024, 2048, 4096, 4100, 5120, 5128, 8192, 8200, 8201, 8288, 9216, 10001, 11264, 12288, 13824, 16383, 16384):
+        for dim in (1, 2, 7, 8, 31, 64, 80, 120, 128, 256, 264, 512, 1000, 1023, 1024, 2048, 4096, 4100, 5120, 5128, 8192, 8200, 8201, 8288, 9216, 10001, 11264, 12288, 12296, 13824, 16383, 16384):
             for dtype in (0, 1):
                 for rows in (1, 5, 32760):
                     before = len(fake.launches())
