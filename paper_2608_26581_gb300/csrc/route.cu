@@ -11,9 +11,11 @@
 //
 // A warp takes a token; a lane holds consecutive experts' logits.  A choice is
 // the maximum over the warp of the logits as ordered integers; of equal ones
-// the lowest lane's lowest is taken.  Bound: instructions of some 200 a token
-// (32768 tokens of 128 experts in fp32, gradient: 9.6 us, 55% of the copy rate,
-// issue slots 68% busy), latency where tokens are few (61 tokens, top 8: 2.4 us).
+// the lowest expert is taken.  Bound: latency where tokens are few (61 tokens of
+// 128 experts, top 8: 1.8 us), else instructions: some 350 a token forward (32768
+// tokens 12.6 us; without the experts in the keys, or a lane's logits in order,
+// 19.6), backwards less (32768 tokens in fp32 8.4 us, 63% of the copy rate; with
+// a persistent grid 8.6, with 4 warps a block 9.0).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cmath>
@@ -42,10 +44,13 @@ __device__ __forceinline__ uint32_t ordered(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The logit of an ordered integer (some NaN for NaN).
+// The logit of a key (some NaN for NaN): an ordered integer, of bf16 logits the
+// upper half alone.
+template <typename T>
 __device__ __forceinline__ float logit_of(uint32_t k)
 {
-    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+    const uint32_t b = k & 0x80000000u ? k ^ 0x80000000u : ~k;
+    return __uint_as_float(std::is_same_v<T, float> ? b : b & 0xFFFF0000u);
 }
 
 // Maximum over the warp; NaN counts as nothing (its exponential is NaN all the same).
@@ -75,6 +80,84 @@ __device__ __forceinline__ void load_logits(const void *logits, int64_t at, int 
         l[i] = !VEC && lane * PER + i < experts ? to_f32(p[i]) : -INFINITY;
 }
 
+// The warp's choices: best() is the key of the largest logit left (0 where none
+// is), take(best) its expert, which is left out from then on.  A key of a bf16
+// logit holds the expert as well, so one maximum over the warp finds both, and
+// equal logits follow by their experts.
+template <typename T, int PER>
+struct Choices {
+    uint32_t key[PER];
+    __device__ __forceinline__ Choices(const float (&l)[PER], int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t k = ordered(l[i]);
+            key[i] = k ? (k & 0xFFFF0000u) | (0xFFFFu - (lane * PER + i)) : 0u;
+        }
+    }
+    __device__ __forceinline__ uint32_t best() const
+    {
+        uint32_t k = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i)
+            k = max(k, key[i]);
+        return __reduce_max_sync(kAll, k);
+    }
+    __device__ __forceinline__ int take(uint32_t best)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            key[i] = key[i] == best ? 0u : key[i];
+        return 0xFFFF - (best & 0xFFFFu);
+    }
+};
+
+// fp32: a lane's keys in order (equal ones by expert), the first of them left is
+// compared with the others'.
+template <int PER>
+struct Choices<float, PER> {
+    uint32_t key[PER], order = 0;            // order: the experts' places in the lane, 4 bits each
+    int from;
+    __device__ __forceinline__ Choices(const float (&l)[PER], int lane) : from(lane * PER)
+    {
+        uint32_t at[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            key[i] = ordered(l[i]);
+            at[i] = i;
+        }
+        // (neighbours alone change places: equal ones never pass each other)
+#pragma unroll
+        for (int pass = 0; pass < PER; ++pass)
+#pragma unroll
+            for (int i = pass & 1; i + 1 < PER; i += 2) {
+                const bool swap = key[i + 1] > key[i];
+                const uint32_t k = key[i], n = at[i];
+                key[i] = max(k, key[i + 1]);
+                key[i + 1] = min(k, key[i + 1]);
+                at[i] = swap ? at[i + 1] : n;
+                at[i + 1] = swap ? n : at[i + 1];
+            }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            order |= at[i] << 4 * i;
+    }
+    __device__ __forceinline__ uint32_t best() const { return __reduce_max_sync(kAll, key[0]); }
+    __device__ __forceinline__ int take(uint32_t best)
+    {
+        const uint32_t first = from + (order & 15);
+        const uint32_t chosen = __reduce_min_sync(kAll, key[0] == best ? first : 0xFFFFu);
+        if (first == chosen) {
+#pragma unroll
+            for (int i = 0; i + 1 < PER; ++i)
+                key[i] = key[i + 1];
+            key[PER - 1] = 0;
+            order >>= 4;
+        }
+        return (int)chosen;
+    }
+};
+
 template <typename T, int PER, bool VEC>
 __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
 {
@@ -86,15 +169,10 @@ __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
         return;
     float l[PER];
     load_logits<T, PER, VEC>(a.logits, t * a.row, a.experts, lane, l);
-    uint32_t key[PER], best = 0;
+    Choices<T, PER> choices(l, lane);
+    uint32_t best = choices.best();
+    const float m = logit_of<T>(best);
     float z = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        key[i] = ordered(l[i]);
-        best = max(best, key[i]);
-    }
-    best = __reduce_max_sync(kAll, best);
-    const float m = logit_of(best);
     if (!a.normalize && best != 0) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -102,26 +180,15 @@ __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
         z = lane_sum(z);
     }
     int id = -1;
-    float w = 0.f;                           // lane j: the j-th choice
-    for (int j = 0; j < a.top_k && best != 0; ++j) {
-        int at = PER;                        // this lane's lowest expert with that logit
-#pragma unroll
-        for (int i = PER - 1; i >= 0; --i)
-            at = key[i] == best ? i : at;
-        const int from = __ffs(__ballot_sync(kAll, at < PER)) - 1;
-        const int chosen = __shfl_sync(kAll, lane * PER + at, from);
-        if (lane == j) {
-            id = chosen;
-            w = expf(logit_of(best) - m);
-        }
-        best = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            key[i] = chosen == lane * PER + i ? 0u : key[i];
-            best = max(best, key[i]);
-        }
-        best = __reduce_max_sync(kAll, best);
+    uint32_t key = 0;                        // lane j: the j-th choice
+    for (int j = 0; best != 0; best = choices.best()) {
+        const int chosen = choices.take(best);
+        id = lane == j ? chosen : id;
+        key = lane == j ? best : key;
+        if (++j == a.top_k)
+            break;
     }
+    const float w = id < 0 ? 0.f : expf(logit_of<T>(key) - m);
     if (a.normalize)
         z = lane_sum(w);
     if (lane < a.top_k) {
@@ -130,61 +197,66 @@ __global__ void __launch_bounds__(kWarps * 32) route_kernel(const RouteArgs a)
     }
 }
 
+// What an expert that was not chosen has in the place of its dweight (a NaN
+// that no dweight is scattered as).
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
 template <typename T, int PER, bool VEC>
 __global__ void __launch_bounds__(kWarps * 32) route_grad_kernel(const RouteGradArgs a)
 {
-    __shared__ __align__(16) int8_t s_choice[kWarps][32 * PER];      // which choice took an expert, -1 where none
+    __shared__ __align__(16) uint32_t s_dw[kWarps][32 * PER];        // each expert's dweight
     const int lane = threadIdx.x & 31;
     const int64_t t = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    int8_t *const choice = s_choice[threadIdx.x >> 5];
+    uint32_t *const of = s_dw[threadIdx.x >> 5];
     wait_for_previous();
     let_next_start();
     if (t >= a.tokens)
         return;
     const bool mine = lane < a.top_k;
     const int id = mine ? a.ids[t * a.top_k + lane] : -1;
-    const float dw = mine ? a.dweights[t * a.top_k + lane] : 0.f;
+    const uint32_t dw = mine ? __float_as_uint(a.dweights[t * a.top_k + lane]) : 0;
     float l[PER], d[PER];
     load_logits<T, PER, VEC>(a.logits, t * a.row, a.experts, lane, l);
-    using Choices = Vec<int8_t, PER>;
-    Choices none;
+    using All = Vec<uint32_t, PER>;
+    All all;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        none.v[i] = -1;
-    store_vec<int8_t, PER>(choice + lane * PER, none);
+        all.v[i] = kNone;
+    store_vec<uint32_t, PER>(of + lane * PER, all);
     __syncwarp();
     if (id >= 0 && id < a.experts)
-        choice[id] = (int8_t)lane;
+        of[id] = dw == kNone ? 0x7FFFFFFFu : dw;
     __syncwarp();
-    const Choices taken = load_vec<int8_t, PER>(choice + lane * PER);
+    all = load_vec<uint32_t, PER>(of + lane * PER);
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const float v = __shfl_sync(kAll, dw, taken.v[i] & 31);
-        d[i] = taken.v[i] >= 0 ? v : 0.f;
-        l[i] = a.normalize && taken.v[i] < 0 ? -INFINITY : l[i];
+        const bool taken = all.v[i] != kNone;
+        d[i] = taken ? __uint_as_float(all.v[i]) : 0.f;
+        l[i] = a.normalize && !taken ? -INFINITY : l[i];
         m = fmaxf(m, l[i]);
     }
     m = warp_max(m);
+    m = m == -INFINITY ? 0.f : m;            // (no logit at all: every exponential is 0)
     float z = 0.f, s = 0.f, p[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        p[i] = l[i] == -INFINITY ? 0.f : expf(l[i] - m);
+        p[i] = expf(l[i] - m);
         z += p[i];
-    }
-    z = lane_sum(z);
-    const float inv = z == 0.f ? 0.f : 1.f / z;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        p[i] *= inv;
         s += p[i] * d[i];
     }
-    s = lane_sum(s);
+    // both sums over the warp: half of it takes z, the other s
+    float half = (lane < 16 ? z : s) + __shfl_xor_sync(kAll, lane < 16 ? s : z, 16);
+    half = lane_sum(half, 16);
+    z = __shfl_sync(kAll, half, 0);
+    s = __shfl_sync(kAll, half, 16);
+    const float inv = z == 0.f ? 0.f : 1.f / z;
+    s *= inv;
     T *const out = static_cast<T *>(a.dlogits) + t * a.out_row + lane * PER;
     Vec<T, PER> o;
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-        from_f32(o.v[i], p[i] * (d[i] - s));
+        from_f32(o.v[i], p[i] * inv * (d[i] - s));
     if (VEC) {
         if (lane * PER < a.experts)
             store_vec<T, PER>(out, o);

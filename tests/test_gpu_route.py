@@ -80,6 +80,30 @@ def test_logits_far_apart(normalize):
     _check(torch.stack((l, -l, l * 1e-36)), 5, normalize)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("E", [5, 33, 64, 100, 129, 256])
+def test_few_values(dtype, E):
+    """Rows of few different logits, equal ones in one lane and across lanes: by their experts."""
+    g = torch.Generator().manual_seed(E)
+    values = torch.tensor([-INF, torch.finfo(dtype).min, -1.0, -0.0, 0.0, torch.finfo(dtype).smallest_normal, 1.0, 1.0078125], dtype=dtype)
+    for k in (1, min(7, E), min(32, E)):
+        _check(values[torch.randint(0, 8, (70, E), generator=g)], k, True)
+        _check(values[torch.randint(3, 5, (3, E), generator=g)], k, False)
+
+
+def test_nan_among_bf16():
+    """NaN of either sign counts as the largest, then +inf."""
+    l = torch.randn(4, 64, generator=torch.Generator().manual_seed(1)).to(BF16)
+    l[1, 9], l[2, 5], l[3, 60] = float("nan"), INF, INF
+    l[3, 7] = torch.tensor([0xFFC0 - 0x10000], dtype=torch.int16).view(BF16)[0]
+    l[3, 3] = float("nan")
+    ids, w = torch.empty(4, 3, dtype=torch.int32, device=DEV), torch.empty(4, 3, device=DEV)
+    for normalize in (False, True):
+        rfq.rfq_route(l.to(DEV), ids, w, normalize=normalize)
+        assert ids[1, 0].item() == 9 and ids[2, 0].item() == 5 and ids[3].tolist() == [3, 7, 60]
+        assert w[1].isnan().all() and w[2].isnan().any() and w[3].isnan().all() and w[0].isfinite().all()
+
+
 def test_nan_and_inf():
     l = torch.randn(4, 64, generator=torch.Generator().manual_seed(1))
     l[1, 9] = float("nan")
