@@ -17,8 +17,9 @@
 // block and, through distributed shared memory, over the blocks, which gives
 // the rows.  Loads that do not depend on each other (pairs of eight steps, the
 // warps' and the blocks' counters) are in flight together.
-// 256 pairs of 128 experts: 4.0 us; 32768: 8.8 us, of which 1.3 are the ballots,
-// 1.3 the scattered stores of pair_of and 1 the rows of no pair; 262144: 42 us.
+// 256 pairs of 128 experts: 2.5 us (4.1 with groups on 128 rows, 16512 in all);
+// 32768: 8.5 us, of which 1.3 are the ballots, 1.3 the scattered stores of
+// pair_of and 1 the rows of no pair; 262144: 42 us.
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -28,10 +29,10 @@
 namespace rfq {
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 constexpr int kHeld = 8;                     // steps of 32 pairs in flight
-constexpr int64_t kPairsPerCta = 1024;       // of a cluster that has room for more (with 4096, 16384 pairs take 9.2 us instead of 7.2)
+constexpr int64_t kPairsPerCta = 512;        // of a cluster that has room for more; four rows count like a pair, most of a small call's hold
+                                             // none (32 tokens of 8 pairs, 16512 rows: 4.1 us, with one block 6.4)
 constexpr int kMostCtas = 8;
 
 __device__ __forceinline__ int ld_peer(uint32_t saddr, int rank)
@@ -41,8 +42,11 @@ __device__ __forceinline__ int ld_peer(uint32_t saddr, int rank)
     return v;
 }
 
-__global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) moe_sort_kernel(const MoeSortArgs a)
 {
+    static_assert(THREADS >= kMoeExperts, "a thread for each expert");
+    constexpr int kWarps = THREADS / 32;
     __shared__ __align__(16) int s_count[kWarps][kMoeExperts];     // pairs of a warp; then those of the warps before it
     __shared__ int s_total[kMoeExperts];             // pairs of the block
     __shared__ int s_base[kMoeExperts];              // row of the block's first pair
@@ -67,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
     wait_for_previous();
     let_next_start();
     hold(p0);
-    for (int i = tid; i < kWarps * kMoeExperts / 4; i += kThreads)
+    for (int i = tid; i < kWarps * kMoeExperts / 4; i += THREADS)
         reinterpret_cast<int4 *>(s_count)[i] = make_int4(0, 0, 0, 0);
     __syncthreads();
     // the place of each held pair among the warp's of its expert; of pairs that
@@ -184,10 +188,16 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
         }
     }
     // rows of no pair: behind each group and behind the last
-    for (int e = rank * kWarps + warp; e < E; e += ctas * kWarps)
-        for (int64_t r = (int64_t)s_end[e] + lane; r < min((int64_t)s_next[e], a.rows); r += 32)
-            a.pair_of[r] = -1;
-    for (int64_t r = (int64_t)min(s_next[E - 1], most) + rank * kThreads + tid; r < a.rows; r += ctas * kThreads)
+    const int w = rank * kWarps + warp, warps = ctas * kWarps;
+    for (int e0 = w; e0 < E; e0 += 32 * warps) {
+        const int e = e0 + lane * warps, end = e < E ? s_end[e] : 0, next = e < E ? s_next[e] : 0;
+        for (uint32_t some = __ballot_sync(kAll, end < next); some; some &= some - 1) {
+            const int64_t from = __shfl_sync(kAll, end, __ffs(some) - 1), to = __shfl_sync(kAll, next, __ffs(some) - 1);
+            for (int64_t r = from + lane; r < min(to, a.rows); r += 32)
+                a.pair_of[r] = -1;
+        }
+    }
+    for (int64_t r = (int64_t)min(s_next[E - 1], most) + rank * THREADS + tid; r < a.rows; r += ctas * THREADS)
         a.pair_of[r] = -1;
     if (ctas > 1)
         cluster_sync();                      // (a block's shared memory is read by the others)
@@ -198,9 +208,13 @@ __global__ void __launch_bounds__(kThreads) moe_sort_kernel(const MoeSortArgs a)
 cudaError_t launch_moe_sort(const MoeSortArgs &a, cudaStream_t st)
 {
     int ctas = 1;
-    while (ctas < kMostCtas && ctas * kPairsPerCta < a.pairs)
+    while (ctas < kMostCtas && ctas * kPairsPerCta < a.pairs + a.rows / 4)
         ctas *= 2;
-    return launch_early(moe_sort_kernel, dim3(ctas), kThreads, 0, st, ctas, a);
+    // (fewer threads pass barriers sooner, more have more pairs in flight: 256 pairs take 4.1 us with 256 threads, 5.7 with 1024;
+    // 32768 pairs 8.5 with 512, 9.1 with 1024; 131072 pairs 24.7 and 23.1)
+    return a.pairs <= 4096    ? launch_early(moe_sort_kernel<256>, dim3(ctas), 256, 0, st, ctas, a)
+           : a.pairs <= 32768 ? launch_early(moe_sort_kernel<512>, dim3(ctas), 512, 0, st, ctas, a)
+                              : launch_early(moe_sort_kernel<1024>, dim3(ctas), 1024, 0, st, ctas, a);
 }
 
 } // namespace rfq

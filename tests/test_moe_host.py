@@ -177,7 +177,7 @@ def test_launch_shapes(fake):
             before = len(fake.launches())
             assert fake.lib.rfq_moe_sort(256, tokens, 8, 128, 128, 256, 256, 256, 2 ** 31 - 1, 256, None) == rfq.RFQ_OK
             (x, _, _, threads, cluster, _), = fake.launches()[before:]
-            assert threads == 1024 and x == cluster <= 8
+            assert threads in (256, 512, 1024) and x == cluster <= 8
 
 
 def test_references_against_autograd():
