@@ -768,7 +768,11 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
             using P = std::remove_pointer_t<decltype(split)>;
             const int threads = threads_of<P>((a.dim + VEC - 1) / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
             const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * (kTwice<P> ? 1 : backward_blocks(threads));
-            blocks = (int)(turns < most ? turns : most);
+            // (all blocks take as many turns; four of them, if each SM has that many, halve the partial sums and more: 1531 rows of
+            // 1024 bf16 take 7.8 us instead of 11.9)
+            const int64_t few = turns / num_sms() < 4 ? turns / num_sms() : 4, least = sums && few > 1 ? few : 1;
+            const int64_t each = (turns + most - 1) / most > least ? (turns + most - 1) / most : least;
+            blocks = (int)((turns + each - 1) / each);
             if constexpr (P::kBlock) {
                 if constexpr (kTwice<P>)
                     return launch_backward_of<P, 512>(a, threads, blocks, st);
