@@ -24,6 +24,13 @@ bool choices_fit(int64_t tokens, int32_t top_k)
     return tokens >= 0 && top_k >= 1 && top_k <= kRouteTopK && tokens <= INT32_MAX / top_k;
 }
 
+// Sizes of pairs sorted into groups: every row that a group can have is counted in 31 bits.
+bool groups_fit(int64_t tokens, int32_t top_k, int32_t experts, int32_t align)
+{
+    return choices_fit(tokens, top_k) && experts >= 1 && experts <= kMoeExperts && align >= 1 && align <= kMoeAlign &&
+           tokens * top_k + (int64_t)experts * align <= INT32_MAX;
+}
+
 // Sizes shared by the calls that move rows.
 bool rows_fit(int64_t tokens, int32_t top_k, int64_t rows, int64_t dim, int64_t stride)
 {
@@ -138,7 +145,7 @@ rfq_status rfq_route_grad(const void *logits, int64_t row_stride, int32_t dtype,
 
 int64_t rfq_moe_rows(int64_t tokens, int32_t top_k, int32_t experts, int32_t align)
 {
-    if (!choices_fit(tokens, top_k) || experts < 1 || experts > kMoeExperts || align < 1 || align > kMoeAlign)
+    if (!groups_fit(tokens, top_k, experts, align))
         return -1;
     const int64_t pairs = tokens * top_k, groups = pairs < experts ? pairs : experts;
     return (pairs + groups * (align - 1)) / align * align;
@@ -148,8 +155,7 @@ rfq_status rfq_moe_sort(const int32_t *ids, int64_t tokens, int32_t top_k, int32
                         int32_t *group_off, int32_t *row_of, int32_t *pair_of, int64_t rows, void *workspace,
                         void *stream)
 {
-    if (!choices_fit(tokens, top_k) || experts < 1 || experts > kMoeExperts || align < 1 || align > kMoeAlign ||
-        rows < 0 || rows > INT32_MAX || tokens * top_k + (int64_t)experts * align > INT32_MAX)
+    if (!groups_fit(tokens, top_k, experts, align) || rows < 0 || rows > INT32_MAX)
         return RFQ_ERR_SHAPE;
     if (!group_off || !workspace || (tokens > 0 && (!ids || !row_of)) || (rows > 0 && !pair_of))
         return RFQ_ERR_INVALID_ARG;
