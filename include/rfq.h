@@ -685,7 +685,9 @@ RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows,
  * of int32 and fp32 results need their natural alignment only; every other
  * device pointer must be 16-byte aligned.  Rows whose strides and sizes are
  * multiples of 16 bytes are read and written 16 bytes at a time, others in
- * smaller steps.  The same inputs give the same bits. */
+ * smaller steps.  A stride along an axis of one element is not looked at.  The
+ * same call on the same inputs and device gives the same bits; sizes, types and
+ * strides choose the order of sums. */
 
 /* RFQ_NORM_LAYER  y = (x - mean) rstd w + b,  rstd = 1 / sqrt(variance + eps)
  * RFQ_NORM_RMS    y = x rstd w + b,           rstd = 1 / sqrt(mean x^2 + eps) */
@@ -724,8 +726,9 @@ RFQ_API size_t rfq_norm_grad_workspace_bytes(int32_t dim);
  *     NULL with RFQ_NORM_RMS).
  *   weight: as rfq_norm got it, or NULL.
  *   dweight, dbias: device fp32 [dim], or NULL; written also when there are no
- *     rows (zeros).  The sums are fp32 in an order that the sizes and the device
- *     alone decide.
+ *     rows (zeros).  The sums are fp32 in an order that the sizes, the type, the
+ *     strides and the device decide, and nothing else: rows whose strides allow
+ *     no 16-byte access are shared out in another way than those that do.
  *   workspace: rfq_norm_grad_workspace_bytes bytes, needed for dweight or dbias;
  *     calls that overlap on the GPU must not share it.  Its contents do not
  *     matter.

@@ -18,6 +18,9 @@ rfq_status from_cuda(cudaError_t e) { return e == cudaSuccess ? RFQ_OK : RFQ_ERR
 
 bool is_dtype(int32_t d) { return d == RFQ_OUT_F32 || d == RFQ_OUT_BF16; }
 
+// A stride along an axis of n elements: of one element it means nothing, and takes no part in any choice.
+int64_t used(int64_t stride, int64_t n) { return n > 1 ? stride : 0; }
+
 // Sizes of tokens' choices of experts.
 bool choices_fit(int64_t tokens, int32_t top_k)
 {
@@ -46,6 +49,10 @@ rfq_status rfq_norm(const void *x, int64_t x_token_stride, int64_t x_head_stride
                     float eps, const void *weight, const void *bias, int32_t w_dtype, float *mean, float *rstd,
                     void *stream)
 {
+    x_token_stride = used(x_token_stride, tokens);
+    x_head_stride = used(x_head_stride, heads);
+    y_token_stride = used(y_token_stride, tokens);
+    y_head_stride = used(y_head_stride, heads);
     if (!is_dtype(dtype) || !is_dtype(w_dtype) || (kind != RFQ_NORM_LAYER && kind != RFQ_NORM_RMS) || !(eps >= 0.f))
         return RFQ_ERR_INVALID_ARG;
     if (tokens < 0 || heads < 1 || tokens > INT32_MAX / heads || dim < 1 || dim > kNormDim || x_token_stride < 0 ||
@@ -77,6 +84,12 @@ rfq_status rfq_norm_grad(const void *dy, int64_t dy_token_stride, int64_t dy_hea
                          int32_t kind, const float *mean, const float *rstd, const void *weight, int32_t w_dtype,
                          float *dweight, float *dbias, void *workspace, void *stream)
 {
+    dy_token_stride = used(dy_token_stride, tokens);
+    dy_head_stride = used(dy_head_stride, heads);
+    x_token_stride = used(x_token_stride, tokens);
+    x_head_stride = used(x_head_stride, heads);
+    dx_token_stride = used(dx_token_stride, tokens);
+    dx_head_stride = used(dx_head_stride, heads);
     if (!is_dtype(dtype) || !is_dtype(w_dtype) || (kind != RFQ_NORM_LAYER && kind != RFQ_NORM_RMS))
         return RFQ_ERR_INVALID_ARG;
     if (tokens < 0 || heads < 1 || tokens > INT32_MAX / heads || dim < 1 || dim > kNormDim || dy_token_stride < 0 ||
@@ -104,6 +117,7 @@ rfq_status rfq_norm_grad(const void *dy, int64_t dy_token_stride, int64_t dy_hea
 rfq_status rfq_route(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens, int32_t experts,
                      int32_t top_k, int32_t normalize, int32_t *ids, float *weights, void *stream)
 {
+    row_stride = used(row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!choices_fit(tokens, top_k) || experts < 1 || experts > kRouteExperts || top_k > experts || row_stride < 0)
@@ -125,6 +139,8 @@ rfq_status rfq_route_grad(const void *logits, int64_t row_stride, int32_t dtype,
                           int32_t top_k, int32_t normalize, const int32_t *ids, const float *dweights, void *dlogits,
                           int64_t dlogits_row_stride, void *stream)
 {
+    row_stride = used(row_stride, tokens);
+    dlogits_row_stride = used(dlogits_row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!choices_fit(tokens, top_k) || experts < 1 || experts > kRouteExperts || top_k > experts || row_stride < 0 ||
@@ -173,6 +189,7 @@ rfq_status rfq_moe_gather(const void *x, int64_t x_row_stride, int32_t dtype, in
                           const int32_t *row_of, int32_t top_k, const int32_t *pair_of, void *out, int64_t rows,
                           void *stream)
 {
+    x_row_stride = used(x_row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!rows_fit(tokens, top_k, rows, dim, x_row_stride))
@@ -194,6 +211,7 @@ rfq_status rfq_moe_combine(const void *y, int32_t dtype, int64_t rows, int32_t d
                            const float *weights, int64_t tokens, int32_t top_k, void *out, int64_t out_row_stride,
                            void *stream)
 {
+    out_row_stride = used(out_row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!rows_fit(tokens, top_k, rows, dim, out_row_stride))
@@ -215,6 +233,7 @@ rfq_status rfq_moe_combine_grad(const void *dout, int64_t dout_row_stride, const
                                 int32_t dim, const int32_t *row_of, const int32_t *pair_of, const float *weights,
                                 int64_t tokens, int32_t top_k, void *dy, float *dweights, void *stream)
 {
+    dout_row_stride = used(dout_row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!rows_fit(tokens, top_k, rows, dim, dout_row_stride))
@@ -234,6 +253,7 @@ rfq_status rfq_moe_combine_grad(const void *dout, int64_t dout_row_stride, const
 rfq_status rfq_moe_quantize(const void *x, int64_t x_row_stride, int64_t tokens, const int32_t *row_of, int32_t top_k,
                             const int32_t *pair_of, rfq_qtensor *xq, rfq_qtensor *xr, void *stream)
 {
+    x_row_stride = used(x_row_stride, tokens);
     if (!xq)
         return RFQ_ERR_INVALID_ARG;
     rfq_status s = check_qtensor(xq, xq->rows, xq->k);
