@@ -806,8 +806,8 @@ RFQ_API rfq_status rfq_moe_sort(const int32_t *ids, int64_t tokens, int32_t top_
  *     pair_of is negative are cleared, so that every row of out is written;
  *     without (NULL), rows of no pair are left as they were.
  *   out: device [rows][dim] of dtype, contiguous; not x.
- * A row that two pairs name gets either token.  Its gradient in x is
- * rfq_moe_combine without weights.
+ * rfq_moe_sort gives no row to two pairs; of a row that two name each element is
+ * either token's.  Its gradient in x is rfq_moe_combine without weights.
  * 1 <= dim <= 65536, 1 <= top_k <= 32, tokens * top_k < 2^31, rows < 2^31.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
  * RFQ_ERR_DEVICE. */
@@ -832,9 +832,11 @@ RFQ_API rfq_status rfq_moe_combine(const void *y, int32_t dtype, int64_t rows, i
  * and dweights[t][j] = 0 for the others.  With pair_of, rows of dy whose pair_of is
  * negative are cleared; without (NULL), rows of no pair are left as they were.
  *   dout: device [tokens][dim] of dtype, dout_row_stride in elements.
- *   y, dy: device [rows][dim] of dtype, contiguous; dy may be y.
+ *   y, dy: device [rows][dim] of dtype, contiguous; dy may be y if no two pairs
+ *     name a row (rfq_moe_sort gives none to two: the second would multiply dout
+ *     with the first one's gradient).
  *   dweights: device fp32 [tokens][top_k].
- * A row that two pairs name gets either one's gradient.
+ * Of a row that two pairs name each element of dy is either one's gradient.
  * Sizes and errors: as rfq_moe_gather. */
 RFQ_API rfq_status rfq_moe_combine_grad(const void *dout, int64_t dout_row_stride, const void *y, int32_t dtype,
                                         int64_t rows, int32_t dim, const int32_t *row_of, const int32_t *pair_of,
@@ -849,7 +851,8 @@ RFQ_API rfq_status rfq_moe_combine_grad(const void *dout, int64_t dout_row_strid
  *     rfq_linear_grouped; xr may be NULL.  Scale bytes of the layout's padding
  *     rows (from xq->rows on) are zero.
  *   row_of, pair_of: as for rfq_moe_gather; a cleared row has zero codes and
- *     scales.
+ *     scales, and of a row that two pairs name the codes of 32 elements are one
+ *     token's and the scales of 128 one token's, not the same one's.
  * k <= 65536; the other sizes as for rfq_moe_gather.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT,
  * RFQ_ERR_UNSUPPORTED (other formats or layouts), RFQ_ERR_CUDA, RFQ_ERR_DEVICE. */

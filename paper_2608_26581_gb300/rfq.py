@@ -878,8 +878,9 @@ def rfq_moe_combine(y: torch.Tensor, row_of: torch.Tensor, out: torch.Tensor, we
 def rfq_moe_combine_grad(dout: torch.Tensor, y: torch.Tensor, row_of: torch.Tensor, weights: torch.Tensor,
                          dy: torch.Tensor, dweights: torch.Tensor, pair_of: torch.Tensor | None = None, stream=None):
     """Gradients of rfq_moe_combine: dout [tokens, dim] (rows strided) into dy
-    like y (may be y) and dweights fp32 [tokens, top_k]; rows of no pair are
-    cleared with pair_of, left alone without (see include/rfq.h)."""
+    like y (may be y if no two pairs name a row) and dweights fp32 [tokens,
+    top_k]; rows of no pair are cleared with pair_of, left alone without (see
+    include/rfq.h)."""
     call = "rfq_moe_combine_grad"
     dtype, row, T, D, rows, k, dev = _moe_rows(call, dout, y, row_of, pair_of)
     if dy.dtype is not y.dtype or dy.shape != y.shape or not dy.is_contiguous():
