@@ -640,6 +640,13 @@ def _refuse(call: str, what: str):
     raise ValueError(f"{call}: {what}")
 
 
+_MOST = 2 ** 31 - 1                           # (ctypes takes larger numbers modulo 2^32)
+
+
+def _too_large(call: str):
+    raise RFQError(RFQ_ERR_SHAPE, call)
+
+
 def _elsewhere(call: str):
     raise ValueError(f"{call}: tensors must be on one device")
 
@@ -682,6 +689,8 @@ def rfq_norm(x: torch.Tensor, y: torch.Tensor, weight: torch.Tensor | None = Non
     if dtype is None or y.dtype is not x.dtype or y.shape != shape or len(shape) not in (2, 3):
         _refuse(call, "x and y are [rows, dim] or [tokens, heads, dim], fp32 or bf16 alike")
     T, H, D = shape if len(shape) == 3 else (shape[0], 1, shape[1])
+    if D > _MOST or H > _MOST:
+        _too_large(call)
     (xt, xh, x_ok), (yt, yh, y_ok) = _norm_rows(x), _norm_rows(y)
     if not (x_ok and y_ok):
         _refuse(call, "the elements of a row must be contiguous")
@@ -706,7 +715,7 @@ _norm_ws: dict[tuple[int, int], int] = {}     # workspace bytes by device and di
 
 
 def rfq_norm_grad_workspace_bytes(dim: int) -> int:
-    return load_library().rfq_norm_grad_workspace_bytes(dim)
+    return load_library().rfq_norm_grad_workspace_bytes(dim) if 0 < dim <= _MOST else 0
 
 
 def norm_workspace(dim: int, device="cuda") -> torch.Tensor:
@@ -730,6 +739,8 @@ def rfq_norm_grad(dy: torch.Tensor, x: torch.Tensor, rstd: torch.Tensor, dx: tor
             len(shape) not in (2, 3)):
         _refuse(call, "dy, x and dx are [rows, dim] or [tokens, heads, dim], fp32 or bf16 alike")
     T, H, D = shape if len(shape) == 3 else (shape[0], 1, shape[1])
+    if D > _MOST or H > _MOST:
+        _too_large(call)
     (dt, dh, d_ok), (xt, xh, x_ok), (ot, oh, o_ok) = _norm_rows(dy), _norm_rows(x), _norm_rows(dx)
     if not (d_ok and x_ok and o_ok):
         _refuse(call, "the elements of a row must be contiguous")
@@ -766,6 +777,8 @@ def _route_sizes(call: str, logits, ids, weights):
         _refuse(call, "ids (int32) and weights (fp32) are contiguous [tokens, top_k]")
     if ids.get_device() != dev or weights.get_device() != dev:
         _elsewhere(call)
+    if E > _MOST or n[1] > _MOST:
+        _too_large(call)
     return dtype, row if T > 1 else 0, T, E, n[1], dev
 
 
@@ -794,7 +807,8 @@ def rfq_route_grad(logits: torch.Tensor, ids: torch.Tensor, dweights: torch.Tens
 
 def rfq_moe_rows(tokens: int, top_k: int, experts: int, align: int = 128) -> int:
     """Rows that hold the groups of tokens * top_k pairs whatever the ids."""
-    n = load_library().rfq_moe_rows(tokens, top_k, experts, align)
+    sizes = tokens, top_k, experts, align
+    n = load_library().rfq_moe_rows(*sizes) if max(sizes) <= _MOST and min(sizes) >= 0 else -1
     _want(n >= 0, "rfq_moe_rows", "sizes out of range")
     return n
 
@@ -814,6 +828,8 @@ def rfq_moe_sort(ids: torch.Tensor, group_off: torch.Tensor, row_of: torch.Tenso
     if (row_of.get_device() != dev or group_off.get_device() != dev or pair_of.get_device() != dev or
             workspace.get_device() != dev):
         _elsewhere("rfq_moe_sort")
+    if n[1] > _MOST or experts > _MOST or not 0 <= align <= _MOST:
+        _too_large("rfq_moe_sort")
     _launch("rfq_moe_sort", load_library().rfq_moe_sort, dev, stream, ids.data_ptr(), n[0], n[1], experts, align,
             group_off.data_ptr(), row_of.data_ptr(), pair_of.data_ptr(), rows, workspace.data_ptr())
 
@@ -830,12 +846,16 @@ def _moe_rows(call: str, tokens, stacked, row_of, pair_of):
     if stacked.get_device() != dev:
         _elsewhere(call)
     _moe_maps(call, T, S[0], row_of, pair_of, n, dev)
+    if D > _MOST:
+        _too_large(call)
     return dtype, row if T > 1 else 0, T, D, S[0], n[1], dev
 
 
 def _moe_maps(call: str, tokens: int, rows: int, row_of, pair_of, n, dev: int):
     if len(n) != 2 or n[0] != tokens or row_of.dtype is not _I32 or not row_of.is_contiguous():
         _refuse(call, "row_of is a contiguous int32 [tokens, top_k]")
+    if n[1] > _MOST:
+        _too_large(call)
     if row_of.get_device() != dev:
         _elsewhere(call)
     if pair_of is not None:

@@ -3,6 +3,7 @@ without a GPU: sizes that are taken and refused, launches of unusual calls."""
 import ctypes
 
 import pytest
+import torch
 
 from fake_kernels import FakeKernels
 from paper_2608_26581_gb300 import rfq
@@ -52,3 +53,32 @@ def test_strides_along_one_element(fake):
         want = fake.call(f, *even)
         assert want[0] == rfq.RFQ_OK and want[1]
         assert fake.call(f, *odd) == want, (f, odd)
+
+
+def test_binding_refuses_sizes_past_31_bits():
+    """A size that C's int32 does not hold is refused, not taken modulo 2^32."""
+    far = 2 ** 32
+    new = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device="meta")  # noqa: E731
+    i32 = lambda *s: new(*s, t=torch.int32)  # noqa: E731
+    wide, few, ws = new(1, far + 128), new(3, 8), i32(64)
+    q = rfq.QTensor(0, 1, 8, 128, new(512, t=torch.uint8), new(512, t=torch.uint8))
+    calls = [lambda: rfq.rfq_norm(wide, wide), lambda: rfq.rfq_norm(new(1, far + 4, 8), new(1, far + 4, 8)),
+             lambda: rfq.rfq_norm_grad(wide, wide, new(1), wide, mean=new(1)),
+             lambda: rfq.rfq_norm_grad(new(1, far + 4, 8), new(1, far + 4, 8), new(far + 4), new(1, far + 4, 8)),
+             lambda: rfq.rfq_route(wide, i32(1, 8), new(1, 8)), lambda: rfq.rfq_route(new(1, 8), i32(1, far + 2), new(1, far + 2)),
+             lambda: rfq.rfq_route_grad(wide, i32(1, 8), new(1, 8), wide),
+             lambda: rfq.rfq_moe_sort(i32(1, far + 2), i32(9), i32(1, far + 2), i32(16), ws), lambda: rfq.rfq_moe_sort(i32(3, 2), i32(far + 9), i32(3, 2), i32(16), ws),
+             lambda: rfq.rfq_moe_sort(i32(3, 2), i32(9), i32(3, 2), i32(16), ws, align=far + 1), lambda: rfq.rfq_moe_sort(i32(3, 2), i32(9), i32(3, 2), i32(16), ws, align=1 - far),
+             lambda: rfq.rfq_moe_gather(wide, i32(1, 2), new(2, far + 128)), lambda: rfq.rfq_moe_gather(few, i32(3, far + 2), few),
+             lambda: rfq.rfq_moe_combine(new(2, far + 128), i32(1, 2), wide), lambda: rfq.rfq_moe_combine(few, i32(3, far + 2), few),
+             lambda: rfq.rfq_moe_combine_grad(wide, new(2, far + 128), i32(1, 2), new(1, 2), new(2, far + 128), new(1, 2)),
+             lambda: rfq.rfq_moe_combine_grad(few, few, i32(3, far + 2), new(3, far + 2), few, new(3, far + 2)),
+             lambda: rfq.rfq_moe_quantize(new(3, 128, t=torch.bfloat16), i32(3, far + 2), q)]
+    for i, f in enumerate(calls):
+        with pytest.raises(rfq.RFQError) as e:
+            f()
+        assert e.value.status == rfq.RFQ_ERR_SHAPE, i
+    assert rfq.rfq_norm_grad_workspace_bytes(far + 128) == 0
+    for sizes in ((2 ** 64 + 4, 2, 8, 1), (4, far + 2, 8, 1), (4, 2, far + 8, 1), (4, 2, 8, far + 1), (4, 2, 8, 1 - far)):
+        with pytest.raises(ValueError):
+            rfq.rfq_moe_rows(*sizes)
