@@ -685,9 +685,11 @@ RFQ_API rfq_status rfq_matvec(const void *x, int64_t x_row_stride, int64_t rows,
  * of int32 and fp32 results need their natural alignment only; every other
  * device pointer must be 16-byte aligned.  Rows whose strides and sizes are
  * multiples of 16 bytes are read and written 16 bytes at a time, others in
- * smaller steps.  A stride along an axis of one element is not looked at.  The
- * same call on the same inputs and device gives the same bits; sizes, types and
- * strides choose the order of sums. */
+ * smaller steps.  A stride along an axis of one element is not looked at; along
+ * others the rows of a result do not overlap (strides below their length are
+ * refused, RFQ_ERR_SHAPE), while rows that are only read may.  The same call on
+ * the same inputs and device gives the same bits; sizes, types and strides
+ * choose the order of sums. */
 
 /* RFQ_NORM_LAYER  y = (x - mean) rstd w + b,  rstd = 1 / sqrt(variance + eps)
  * RFQ_NORM_RMS    y = x rstd w + b,           rstd = 1 / sqrt(mean x^2 + eps) */

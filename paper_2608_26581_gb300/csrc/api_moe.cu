@@ -21,6 +21,9 @@ bool is_dtype(int32_t d) { return d == RFQ_OUT_F32 || d == RFQ_OUT_BF16; }
 // A stride along an axis of n elements: of one element it means nothing, and takes no part in any choice.
 int64_t used(int64_t stride, int64_t n) { return n > 1 ? stride : 0; }
 
+// n rows of a result, of dim elements, do not lie on top of each other.
+bool apart(int64_t stride, int64_t n, int64_t dim) { return n <= 1 || stride >= dim; }
+
 // Sizes of tokens' choices of experts.
 bool choices_fit(int64_t tokens, int32_t top_k)
 {
@@ -56,7 +59,8 @@ rfq_status rfq_norm(const void *x, int64_t x_token_stride, int64_t x_head_stride
     if (!is_dtype(dtype) || !is_dtype(w_dtype) || (kind != RFQ_NORM_LAYER && kind != RFQ_NORM_RMS) || !(eps >= 0.f))
         return RFQ_ERR_INVALID_ARG;
     if (tokens < 0 || heads < 1 || tokens > INT32_MAX / heads || dim < 1 || dim > kNormDim || x_token_stride < 0 ||
-        x_head_stride < 0 || y_token_stride < 0 || y_head_stride < 0)
+        x_head_stride < 0 || y_token_stride < 0 || y_head_stride < 0 || !apart(y_token_stride, tokens, dim) ||
+        !apart(y_head_stride, heads, dim))
         return RFQ_ERR_SHAPE;
     if (tokens > 0 && (!x || !y))
         return RFQ_ERR_INVALID_ARG;
@@ -93,7 +97,8 @@ rfq_status rfq_norm_grad(const void *dy, int64_t dy_token_stride, int64_t dy_hea
     if (!is_dtype(dtype) || !is_dtype(w_dtype) || (kind != RFQ_NORM_LAYER && kind != RFQ_NORM_RMS))
         return RFQ_ERR_INVALID_ARG;
     if (tokens < 0 || heads < 1 || tokens > INT32_MAX / heads || dim < 1 || dim > kNormDim || dy_token_stride < 0 ||
-        dy_head_stride < 0 || x_token_stride < 0 || x_head_stride < 0 || dx_token_stride < 0 || dx_head_stride < 0)
+        dy_head_stride < 0 || x_token_stride < 0 || x_head_stride < 0 || dx_token_stride < 0 || dx_head_stride < 0 ||
+        !apart(dx_token_stride, tokens, dim) || !apart(dx_head_stride, heads, dim))
         return RFQ_ERR_SHAPE;
     if (tokens > 0 && (!dy || !x || !dx || !rstd || (kind == RFQ_NORM_LAYER && !mean)))
         return RFQ_ERR_INVALID_ARG;
@@ -144,7 +149,7 @@ rfq_status rfq_route_grad(const void *logits, int64_t row_stride, int32_t dtype,
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
     if (!choices_fit(tokens, top_k) || experts < 1 || experts > kRouteExperts || top_k > experts || row_stride < 0 ||
-        dlogits_row_stride < 0)
+        dlogits_row_stride < 0 || !apart(dlogits_row_stride, tokens, experts))
         return RFQ_ERR_SHAPE;
     if (tokens > 0 && (!logits || !ids || !dweights || !dlogits))
         return RFQ_ERR_INVALID_ARG;
@@ -214,7 +219,7 @@ rfq_status rfq_moe_combine(const void *y, int32_t dtype, int64_t rows, int32_t d
     out_row_stride = used(out_row_stride, tokens);
     if (!is_dtype(dtype))
         return RFQ_ERR_INVALID_ARG;
-    if (!rows_fit(tokens, top_k, rows, dim, out_row_stride))
+    if (!rows_fit(tokens, top_k, rows, dim, out_row_stride) || !apart(out_row_stride, tokens, dim))
         return RFQ_ERR_SHAPE;
     if (tokens > 0 && (!row_of || !out || (rows > 0 && !y)))
         return RFQ_ERR_INVALID_ARG;

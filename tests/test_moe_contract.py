@@ -82,3 +82,19 @@ def test_binding_refuses_sizes_past_31_bits():
     for sizes in ((2 ** 64 + 4, 2, 8, 1), (4, far + 2, 8, 1), (4, 2, far + 8, 1), (4, 2, 8, far + 1), (4, 2, 8, 1 - far)):
         with pytest.raises(ValueError):
             rfq.rfq_moe_rows(*sizes)
+
+
+def test_results_whose_rows_overlap(fake):
+    """Several rows of a result in one place are refused (inputs may share rows)."""
+    for t, h in ((0, 64), (63, 64), (256, 0), (256, 63)):
+        for x in ((256, 64), (0, 64), (256, 0), (0, 0)):
+            assert fake.call("rfq_norm", 256, *x, 256, t, h, 1, 3, 4, 64, 0, 1e-6, None, None, 0, None, None, None) == (rfq.RFQ_ERR_SHAPE, [])
+            assert fake.call("rfq_norm", 256, *x, 256, 256, 64, 1, 3, 4, 64, 0, 1e-6, None, None, 0, None, None, None)[0] == rfq.RFQ_OK
+            assert fake.call("rfq_norm_grad", 256, *x, 256, *x, 256, t, h, 1, 3, 4, 64, 0, 256, 256, None, 0, None, None, None, None) == (rfq.RFQ_ERR_SHAPE, [])
+            assert fake.call("rfq_norm_grad", 256, *x, 256, *x, 256, 256, 64, 1, 3, 4, 64, 0, 256, 256, None, 0, None, None, None, None)[0] == rfq.RFQ_OK
+    # heads before tokens
+    assert fake.call("rfq_norm", 256, 64, 192, 256, 64, 192, 1, 3, 4, 64, 0, 1e-6, None, None, 0, None, None, None)[0] == rfq.RFQ_OK
+    for row, status in ((0, rfq.RFQ_ERR_SHAPE), (127, rfq.RFQ_ERR_SHAPE), (128, rfq.RFQ_OK)):
+        assert fake.call("rfq_route_grad", 256, 0, 0, 3, 128, 8, 1, 256, 256, 256, row, None)[0] == status
+        assert fake.call("rfq_moe_combine", 256, 1, 24, 128, 256, 256, 3, 8, 256, row, None)[0] == status
+    assert fake.call("rfq_moe_gather", 256, 0, 1, 3, 128, 256, 8, 256, 256, 24, None)[0] == rfq.RFQ_OK
