@@ -291,10 +291,12 @@ __device__ __forceinline__ void store_chunk(const P &p, typename P::T *row, int 
     store_once<typename P::T, P::VEC>(row + c, u);
 }
 
-// The most threads of a block (with 8 elements each it takes rows of up to kFewElements).
-constexpr int kFewElements = 8192;
+// Narrow rows of up to so many elements go with 8 elements a thread, longer ones with 16.
+constexpr int kFewForward = 4096, kFewBackward = 8192;
+
+// The most threads of a forward block.
 template <typename P>
-constexpr int kMostThreads = P::kBlock ? (P::NV * P::VEC == 8 ? kFewElements : kNormDim) / (P::NV * P::VEC) : kThreads;
+constexpr int kMostThreads = P::kBlock ? (P::NV * P::VEC == 8 ? kFewForward : kNormDim) / (P::NV * P::VEC) : kThreads;
 
 // Rows of the forward ring.  (Deeper ones take L1 from the weights: with three
 // rows of 5120 elements a layer norm of 32760 takes 116 us, with two 112.)
@@ -696,27 +698,30 @@ int backward_blocks(int threads) { return threads > 320 ? 1 : 640 / threads; }
 
 // Calls go(split) with the way a row of `chunks` lies over threads: a few
 // lanes with two chunks each, a warp, or a block whose warps take 32 NV
-// chunks each.
-template <typename T, int VEC, int NV, typename G>
+// chunks each.  LONG: rows that always take a block.
+template <typename T, int VEC, int NV, bool LONG, typename G>
 cudaError_t with_split(int chunks, G &&go)
 {
-    if (chunks > 32 * NV)
-        return go((Split<T, VEC, NV, 64> *)nullptr);
-    if (NV >= 16 && chunks > 256)
-        return go((Split<T, VEC, (NV < 16 ? 2 : 16), 32> *)nullptr);
-    if (NV >= 8 && chunks > 128)
-        return go((Split<T, VEC, (NV < 8 ? 2 : 8), 32> *)nullptr);
-    if (NV >= 4 && chunks > 64)
-        return go((Split<T, VEC, (NV < 4 ? 2 : 4), 32> *)nullptr);
-    if (chunks > 32)
-        return go((Split<T, VEC, 2, 32> *)nullptr);
-    if (chunks > 16)
-        return go((Split<T, VEC, 2, 16> *)nullptr);
-    if (chunks > 8)
-        return go((Split<T, VEC, 2, 8> *)nullptr);
-    if (chunks > 2)
-        return go((Split<T, VEC, 2, 4> *)nullptr);
-    return go((Split<T, VEC, 2, 1> *)nullptr);
+    if constexpr (!LONG) {
+        static_assert(NV == 2 || NV == 4 || NV == 8, "a warp's splits below");
+        if (chunks <= 2)
+            return go((Split<T, VEC, 2, 1> *)nullptr);
+        if (chunks <= 8)
+            return go((Split<T, VEC, 2, 4> *)nullptr);
+        if (chunks <= 16)
+            return go((Split<T, VEC, 2, 8> *)nullptr);
+        if (chunks <= 32)
+            return go((Split<T, VEC, 2, 16> *)nullptr);
+        if (chunks <= 64)
+            return go((Split<T, VEC, 2, 32> *)nullptr);
+        if constexpr (NV >= 4)
+            if (chunks <= 128)
+                return go((Split<T, VEC, 4, 32> *)nullptr);
+        if constexpr (NV >= 8)
+            if (chunks <= 256)
+                return go((Split<T, VEC, 8, 32> *)nullptr);
+    }
+    return go((Split<T, VEC, NV, 64> *)nullptr);
 }
 
 template <typename P>
@@ -725,11 +730,11 @@ int threads_of(int chunks)
     return P::kBlock ? (chunks + 32 * P::NV - 1) / (32 * P::NV) * 32 : kThreads;
 }
 
-template <typename T, int VEC, int MOST>
+template <typename T, int VEC, int MOST, bool LONG = false>
 cudaError_t launch_forward(const NormArgs &a, cudaStream_t st)
 {
     const int chunks = (a.dim + VEC - 1) / VEC;
-    return with_split<T, VEC, MOST>(chunks, [&](auto split) -> cudaError_t {
+    return with_split<T, VEC, MOST, LONG>(chunks, [&](auto split) -> cudaError_t {
         using P = std::remove_pointer_t<decltype(split)>;
         const int threads = threads_of<P>(chunks), groups = P::kBlock ? 1 : threads / P::TPR;
         const int64_t turns = (a.rows + groups - 1) / groups;
@@ -757,7 +762,7 @@ cudaError_t launch_backward_of(const NormGradArgs &a, int threads, int blocks, c
     return launch_early(norm_grad_kernel<P, THREADS>, dim3((unsigned)blocks), threads, smem, st, 1, a);
 }
 
-template <typename T, int VEC, int MOST>
+template <typename T, int VEC, int MOST, bool LONG = false>
 cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
 {
     NormGradArgs a = given;
@@ -765,7 +770,7 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
     a.partial = sums ? static_cast<float *>(a.workspace) : nullptr;
     int blocks = 0;
     if (a.rows > 0) {
-        const cudaError_t e = with_split<T, VEC, MOST>((a.dim + VEC - 1) / VEC, [&](auto split) -> cudaError_t {
+        const cudaError_t e = with_split<T, VEC, MOST, LONG>((a.dim + VEC - 1) / VEC, [&](auto split) -> cudaError_t {
             using P = std::remove_pointer_t<decltype(split)>;
             const int threads = threads_of<P>((a.dim + VEC - 1) / VEC), groups = P::kBlock ? 1 : threads / P::TPR;
             const int64_t turns = (a.rows + groups - 1) / groups, most = (int64_t)num_sms() * (kTwice<P> ? 1 : backward_blocks(threads));
@@ -774,17 +779,15 @@ cudaError_t launch_backward(const NormGradArgs &given, cudaStream_t st)
             const int64_t few = turns / num_sms() < 4 ? turns / num_sms() : 4, least = sums && few > 1 ? few : 1;
             const int64_t each = (turns + most - 1) / most > least ? (turns + most - 1) / most : least;
             blocks = (int)((turns + each - 1) / each);
-            if constexpr (P::kBlock) {
-                if constexpr (kTwice<P>)
+            if constexpr (LONG)
+                return launch_backward_of<P, P::kNarrow ? 1024 : 512>(a, threads, blocks, st);
+            else if constexpr (P::kBlock) {
+                if constexpr (P::kNarrow)
+                    if (threads > 512)
+                        return launch_backward_of<P, 1024>(a, threads, blocks, st);
+                if (threads > 320)
                     return launch_backward_of<P, 512>(a, threads, blocks, st);
-                else {
-                    if constexpr (P::kNarrow)
-                        if (threads > 512)
-                            return launch_backward_of<P, 1024>(a, threads, blocks, st);
-                    if (threads > 320)
-                        return launch_backward_of<P, 512>(a, threads, blocks, st);
-                    return launch_backward_of<P, 320>(a, threads, blocks, st);
-                }
+                return launch_backward_of<P, 320>(a, threads, blocks, st);
             } else
                 return launch_backward_of<P, 256>(a, threads, blocks, st);
         });
@@ -802,34 +805,35 @@ bool wide(int64_t bits, bool bf16) { return bits % (bf16 ? 8 : 4) == 0; }
 
 size_t norm_grad_workspace_bytes(int32_t dim)
 {
-    // (whatever the type and strides: a row of a block has a warp for at most 512 elements, and two of them at least)
+    // (whatever the type and strides: a row of a block has a warp for at most 512 elements, and two of them at least; rows beyond
+    // 8192, which can have fewer warps, take one block an SM)
     const int threads = dim > 1024 ? (dim + 511) / 512 * 32 : dim > 256 ? 64 : kThreads;
     return (size_t)num_sms() * backward_blocks(threads) * 2 * (size_t)padded_dim(dim) * sizeof(float);
 }
 
 cudaError_t launch_norm(const NormArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.x_token | a.x_head | a.y_token | a.y_head | a.dim, a.bf16), few = a.dim <= kFewElements / 2;
+    const bool w = wide(a.x_token | a.x_head | a.y_token | a.y_head | a.dim, a.bf16), few = a.dim <= kFewForward;
     if (a.bf16)
-        return w ? launch_forward<__nv_bfloat16, 8, 4>(a, st) : few ? launch_forward<__nv_bfloat16, 2, 4>(a, st) : launch_forward<__nv_bfloat16, 2, 8>(a, st);
-    return w ? launch_forward<float, 4, 4>(a, st) : few ? launch_forward<float, 1, 8>(a, st) : launch_forward<float, 1, 16>(a, st);
+        return w ? launch_forward<__nv_bfloat16, 8, 4>(a, st) : few ? launch_forward<__nv_bfloat16, 2, 4>(a, st) : launch_forward<__nv_bfloat16, 2, 8, true>(a, st);
+    return w ? launch_forward<float, 4, 4>(a, st) : few ? launch_forward<float, 1, 8>(a, st) : launch_forward<float, 1, 16, true>(a, st);
 }
 
 cudaError_t launch_norm_grad(const NormGradArgs &a, cudaStream_t st)
 {
-    const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16), few = a.dim <= kFewElements;
+    const bool w = wide(a.dy_token | a.dy_head | a.x_token | a.x_head | a.dx_token | a.dx_head | a.dim, a.bf16), few = a.dim <= kFewBackward;
     // (Elements of a thread: the fewest that need no more than 512 threads.  At 2^26 elements, of which copies take 59.5 us: rows of
     // 9216 bf16 with 16 take 133 us, with 24 85, with 32 130; 13824 with 16 119, with 24 119, with 32 98.)
     const int of_thread = a.dim <= 512 * 16 ? 16 : a.dim <= 512 * 24 ? 24 : 32;
     if (a.bf16)
-        return !w                ? (few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8>(a, st))
+        return !w                ? (few ? launch_backward<__nv_bfloat16, 2, 4>(a, st) : launch_backward<__nv_bfloat16, 2, 8, true>(a, st))
                : of_thread == 16 ? launch_backward<__nv_bfloat16, 8, 2>(a, st)
-               : of_thread == 24 ? launch_backward<__nv_bfloat16, 8, 3>(a, st)
-                                 : launch_backward<__nv_bfloat16, 8, 4>(a, st);
-    return !w                ? (few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16>(a, st))
+               : of_thread == 24 ? launch_backward<__nv_bfloat16, 8, 3, true>(a, st)
+                                 : launch_backward<__nv_bfloat16, 8, 4, true>(a, st);
+    return !w                ? (few ? launch_backward<float, 1, 8>(a, st) : launch_backward<float, 1, 16, true>(a, st))
            : of_thread == 16 ? launch_backward<float, 4, 4>(a, st)
-           : of_thread == 24 ? launch_backward<float, 4, 6>(a, st)
-                             : launch_backward<float, 4, 8>(a, st);
+           : of_thread == 24 ? launch_backward<float, 4, 6, true>(a, st)
+                             : launch_backward<float, 4, 8, true>(a, st);
 }
 
 } // namespace rfq

@@ -1,6 +1,7 @@
 """What the header says of the entry points around a mixture-of-experts block,
 without a GPU: sizes that are taken and refused, launches of unusual calls."""
 import ctypes
+import re
 
 import pytest
 import torch
@@ -98,3 +99,29 @@ def test_results_whose_rows_overlap(fake):
         assert fake.call("rfq_route_grad", 256, 0, 0, 3, 128, 8, 1, 256, 256, 256, row, None)[0] == status
         assert fake.call("rfq_moe_combine", 256, 1, 24, 128, 256, 256, 3, 8, 256, row, None)[0] == status
     assert fake.call("rfq_moe_gather", 256, 0, 1, 3, 128, 256, 8, 256, 256, 24, None)[0] == rfq.RFQ_OK
+
+
+def test_every_norm_kernel_is_reached(fake):
+    """Some length and stride launches each kernel of the norms that is compiled,
+    and the threads of a row hold all of its chunks."""
+    compiled = {k for k in fake.kernels() if "norm_kernel" in k or "norm_grad_kernel" in k or "norm_sum_kernel" in k}
+    start, n = fake.lib.fake_launched(), fake.lib.fake_launches()
+    made = []                                # (dim, whether rows are narrow) of each launch
+    for dim in range(1, 16385):
+        for dtype, words in ((0, 4), (1, 8)):
+            for stride in {-(-dim // words) * words, -(-dim // words) * words + 1}:
+                narrow = (stride | dim) % words != 0
+                assert fake.lib.rfq_norm(256, stride, 0, 256, stride, 0, dtype, 2, 1, dim, 0, 1e-6, 256, 256, 0, 256, 256, None) == rfq.RFQ_OK
+                assert fake.lib.rfq_norm_grad(256, stride, 0, 256, stride, 0, 256, stride, 0, dtype, 2, 1, dim, 0, 256, 256, 256, 0, 256, 256, 256,
+                                              None) == rfq.RFQ_OK
+                made += [(dim, dtype, narrow)] * 3
+    reached = [fake.lib.fake_launched_kernel(start + i).decode() for i in range(len(made))]
+    assert compiled == set(reached), sorted(compiled - set(reached))
+    v = (ctypes.c_uint * 6)()
+    for i, (kernel, (dim, dtype, narrow)) in enumerate(zip(reached, made)):
+        split = re.search(r"SplitI(?:f|14__nv_bfloat16)Li(\d+)ELi(\d+)ELi(\d+)E", kernel)
+        if split:
+            vec, chunks, lanes = map(int, split.groups())
+            fake.lib.fake_launch(n + i, v)
+            assert vec == (1 + dtype if narrow else 4 + 4 * dtype)
+            assert (v[3] if lanes > 32 else lanes) * chunks * vec >= dim, (kernel, dim)
