@@ -54,3 +54,67 @@ def test_rows_that_two_pairs_name(dim, dtype):
     # a lane's own products and additions, then five over lanes
     e = (2 * -(-dim // 32) + 8) * moe_ref.U * dots.abs().sum(-1)
     assert ((dw.double().cpu()[:, 0] - dots.sum(-1)).abs() <= e).all()
+
+
+def _rows_and_back(x, dy, w, rms, rstd_mean, dx, dw, db, ws):
+    mean, rstd = rstd_mean
+    kind = rfq.RFQ_NORM_RMS if rms else rfq.RFQ_NORM_LAYER
+    rfq.rfq_norm(x, torch.empty(x.shape, dtype=x.dtype, device=DEV), weight=w, kind=kind, mean=mean, rstd=rstd)
+    rfq.rfq_norm_grad(dy, x, rstd, dx, mean=mean, weight=w, dweight=dw, dbias=db, workspace=ws, kind=kind)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,dim,bf16_groups,f32_groups", [(60000, 16, 256, 64), (40001, 128, 32, 16), (9120, 257, 1, 1), (9001, 300, 1, 8), (9120, 511, 1, 1),
+                                                              (32760, 512, 8, 8), (12160, 1024, 1, 1), (8001, 1023, 1, 1), (912, 8288, 1, 1), (608, 8193, 1, 1),
+                                                              (608, 16384, 1, 1)])
+def test_weight_gradients_of_many_rows(rows, dim, bf16_groups, f32_groups, dtype):
+    """dweight and dbias over as many rows as the blocks go through in several
+    turns, within a bound counted from their chains of additions; nothing is
+    written behind a workspace that such a call can fill to its end.
+
+    A block takes `groups` rows at once, and four turns or as many as the rows of
+    an SM need: a thread adds the rows of its turns, then the block its groups'
+    sums; the second kernel adds a 32nd of at most ten blocks an SM, then 32 sums."""
+    g, sms = torch.Generator().manual_seed(dim), torch.cuda.get_device_properties(0).multi_processor_count
+    x, dy = (torch.randn(rows, dim, generator=g) + 0.3).to(dtype), torch.randn(rows, dim, generator=g).to(dtype)
+    w = 1 + 0.3 * torch.randn(dim, generator=g)
+    groups = bf16_groups if dtype is BF16 else f32_groups
+    chain = max(4, -(-rows // (groups * sms))) + groups + -(-10 * sms // 32) + 32
+    size = rfq.rfq_norm_grad_workspace_bytes(dim)
+    for rms in (False, True):
+        stats, dw, db = (torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)), guarded_full((dim,), float("nan"), F32), guarded_full((dim,), float("nan"), F32)
+        dx = guarded_full((rows, dim), float("nan"), dtype)
+        _rows_and_back(x.to(DEV), dy.to(DEV), w.to(DEV), rms, stats, dx, dw, db, guarded_full((size // 4,), float("nan"), F32))
+        args = dy.double(), x.double(), *(s.double().cpu() for s in stats), w.double(), rms
+        ex, want = moe_ref.norm_grad_bound(*args, dtype)[0], moe_ref.norm_grad(*args)
+        h = (args[1] - (0 if rms else args[2][:, None])) * args[3][:, None]
+        # (a term's own roundings: the difference, the product with rstd, and room for products of errors)
+        bounds = ex, (chain + 4) * moe_ref.U * (args[0] * h).abs().sum(0), (chain + 1) * moe_ref.U * args[0].abs().sum(0)
+        for got, c, e in zip((dx, dw, db), want, bounds):
+            assert ((got.double().cpu() - c).abs() <= e).all(), ((got.double().cpu() - c).abs() / e.clamp_min(1e-300)).max()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [128, 33, 600])
+def test_strides_in_any_order(dim, dtype):
+    """Heads that lie before tokens, and rows that are read several times
+    (expanded: strides of 0), give the bits of the same rows lying in order."""
+    g = torch.Generator().manual_seed(dim)
+    T, H = 37, 5
+    heads_first = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    new = lambda *s: torch.full(s, float("nan"), device=DEV)  # noqa: E731
+    x, dy = torch.randn(T, H, dim, generator=g).to(dtype).to(DEV), torch.randn(T, H, dim, generator=g).to(dtype).to(DEV)
+    w = (1 + 0.3 * torch.randn(dim, generator=g)).to(DEV)
+    ws = rfq.norm_workspace(dim)
+    assert heads_first(x).stride() == (dim, T * dim, 1)
+
+    def run(x, dy, place):
+        stats, dw, db = (new(T * H), new(T * H)), new(dim), new(dim)
+        y, dx = place(torch.full((T, H, dim), float("nan"), dtype=dtype, device=DEV)), place(torch.full((T, H, dim), float("nan"), dtype=dtype, device=DEV))
+        rfq.rfq_norm(x, y, weight=w, mean=stats[0], rstd=stats[1])
+        rfq.rfq_norm_grad(dy, x, stats[1], dx, mean=stats[0], weight=w, dweight=dw, dbias=db, workspace=ws)
+        return y, *stats, dx, dw, db
+    for a, b in ((x, dy), (x[:1].expand(T, H, dim), dy), (x[:, :1].expand(T, H, dim), dy), (x, dy[:1, :1].expand(T, H, dim))):
+        want = run(a.contiguous(), b.contiguous(), lambda t: t)
+        for got in (run(a, b, lambda t: t), run(a, b, heads_first), run(heads_first(a), heads_first(b), heads_first)):
+            assert all(torch.equal(p, q) for p, q in zip(got, want))

@@ -125,3 +125,31 @@ def test_every_norm_kernel_is_reached(fake):
             fake.lib.fake_launch(n + i, v)
             assert vec == (1 + dtype if narrow else 4 + 4 * dtype)
             assert (v[3] if lanes > 32 else lanes) * chunks * vec >= dim, (kernel, dim)
+
+
+def test_workspace_of_the_norms_gradient(fake):
+    """Rows enough for every block: the blocks' partial sums fit the workspace for
+    each length, wide and narrow, and fill it exactly for some of each; a block's
+    shared memory is within what an SM's blocks have."""
+    launch = (ctypes.c_uint * 6)()
+    for device in (0, 1):
+        fake.device(device)
+        full = set()
+        for dim in [*range(1, 1100), *range(1100, 16385, 61), 8192, 8193, 8200, 12288, 12289, 12296, 16383, 16384]:
+            padded, have = -(-dim // 4) * 4, fake.lib.rfq_norm_grad_workspace_bytes(dim)
+            for dtype, words in ((0, 4), (1, 8)):
+                for stride in {-(-dim // words) * words, dim + 1 - dim % 2}:
+                    n = fake.lib.fake_launches()
+                    assert fake.lib.rfq_norm_grad(256, stride, 0, 256, stride, 0, 256, stride, 0, dtype, 2 ** 20, 1, dim, 0, 256, 256, 256, 0, 256, 256, 256,
+                                                  None) == rfq.RFQ_OK
+                    assert fake.lib.fake_launches() == n + 2
+                    fake.lib.fake_launch(n, launch)
+                    blocks, threads, smem = launch[0], launch[3], launch[5]
+                    assert blocks * 2 * padded * 4 <= have, (dim, dtype, stride)
+                    # (512 static bytes beside the dynamic ones; 228 KB an SM)
+                    assert threads <= 1024 and smem <= 200 * 1024
+                    if blocks * 2 * padded * 4 == have:
+                        full.add((dim > 8192, 256 < dim <= 512, (stride | dim) % words != 0))
+        # (wide rows of 257 to 512 elements take a warp each, and two blocks an SM where the workspace has ten)
+        assert {(False, False, False), (False, False, True), (False, True, True), (True, False, False), (True, False, True)} <= full
+    fake.device(0)
