@@ -48,7 +48,7 @@ class MoELayer:
         bf16, i32 = dict(dtype=torch.bfloat16, device="cuda"), dict(dtype=torch.int32, device="cuda")
         rows = rfq.rfq_moe_rows(tokens, self.top_k, self.experts, 128)
         new = lambda k: [rfq.empty_qtensor(rfq.RFQ_FMT_MXFP4, rfq.RFQ_SCALE_MMA, rows, k) for _ in range(2)]  # noqa: E731
-        # (the grouped product leaves the rows behind the last group alone: they stay zero)
+        # (the grouped product leaves the rows behind the last group alone: zeros, or what a step with more rows left, which no pair reads)
         return {"n": torch.empty(tokens, self.hidden, **bf16), "logits": torch.empty(tokens, self.experts, **bf16),
                 "ids": torch.empty(tokens, self.top_k, **i32), "weights": torch.empty(tokens, self.top_k, device="cuda"),
                 "off": torch.empty(self.experts + 1, **i32), "row_of": torch.empty(tokens, self.top_k, **i32),

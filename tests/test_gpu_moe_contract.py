@@ -1,9 +1,13 @@
 """What the header says of the entry points around a mixture-of-experts block,
 in calls that lie at the edge of it."""
+import importlib.util
+import os
+
 import pytest
 import torch
 
 import moe_ref
+from conftest import ROOT
 from gpu_util import DEV, guarded_full
 from paper_2608_26581_gb300 import rfq
 
@@ -118,3 +122,21 @@ def test_strides_in_any_order(dim, dtype):
         want = run(a.contiguous(), b.contiguous(), lambda t: t)
         for got in (run(a, b, lambda t: t), run(a, b, heads_first), run(heads_first(a), heads_first(b), heads_first)):
             assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_steps_of_other_routings_in_one_set_of_buffers():
+    """What a step with more rows left behind the last group of the next one's
+    is not seen by it."""
+    spec = importlib.util.spec_from_file_location("moe_layer", os.path.join(ROOT, "examples", "moe_layer.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    layer = m.MoELayer(hidden=256, width=128, experts=16, top_k=2)
+    g = torch.Generator().manual_seed(4)
+    spread, alike = torch.randn(60, 256, generator=g).bfloat16().to(DEV), torch.randn(1, 256, generator=g).bfloat16().to(DEV).expand(60, 256).contiguous()
+    fresh, used = layer.buffers(60), layer.buffers(60)
+    want = layer.step(alike, fresh).clone()
+    layer.step(spread, used)
+    many = used["off"][-1].item()
+    got = layer.step(alike, used)
+    layer.check()
+    assert used["off"][-1].item() == 256 < many and (used["gu"][256:many] != 0).any() and torch.equal(got, want)
