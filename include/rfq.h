@@ -705,9 +705,10 @@ typedef enum { RFQ_NORM_LAYER = 0, RFQ_NORM_RMS = 1 } rfq_norm_kind;
  *     (with RFQ_NORM_RMS mean gets 0).
  * Mean, variance (from the differences to the mean) and everything between are
  * fp32; y is rounded once.  Squares that pass fp32 (elements beyond 1e18) give
- * rstd = 0.  A NaN makes its whole row NaN, and so does an Inf in a layer norm; in
- * an RMS norm the squares' mean is then Inf and rstd = 0, which gives NaN in the
- * Inf's own place and b in the others.  No other row is affected.
+ * rstd = 0.  A NaN makes its whole row NaN; in a layer norm so does an Inf, or a
+ * sum of the row that passes fp32 (elements beyond 1e34 of one sign).  In an RMS
+ * norm an Inf makes the squares' mean Inf and rstd = 0, which gives NaN in its own
+ * place and b in the others.  No other row is affected.
  * 1 <= dim <= 16384, tokens * heads < 2^31, eps >= 0.
  * Errors: RFQ_ERR_INVALID_ARG, RFQ_ERR_SHAPE, RFQ_ERR_ALIGNMENT, RFQ_ERR_CUDA,
  * RFQ_ERR_DEVICE. */

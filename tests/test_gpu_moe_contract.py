@@ -140,3 +140,18 @@ def test_steps_of_other_routings_in_one_set_of_buffers():
     got = layer.step(alike, used)
     layer.check()
     assert used["off"][-1].item() == 256 < many and (used["gu"][256:many] != 0).any() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dim", [64, 1023])
+def test_rows_whose_sum_passes_fp32(dim):
+    """Finite elements whose sum is none in fp32: NaN in a layer norm, rstd = 0 in
+    an RMS norm, and the rows beside them as ever."""
+    x = torch.randn(3, dim, generator=torch.Generator().manual_seed(1))
+    x[1] = 3e38
+    for dtype in (BF16, F32):
+        xs, y, rstd = x.to(dtype).to(DEV), torch.empty(3, dim, dtype=dtype, device=DEV), torch.empty(3, device=DEV)
+        assert xs.isfinite().all()
+        rfq.rfq_norm(xs, y, rstd=rstd)
+        assert y[1].isnan().all() and y[[0, 2]].isfinite().all()
+        rfq.rfq_norm(xs, y, kind=rfq.RFQ_NORM_RMS, rstd=rstd)
+        assert rstd[1].item() == 0 and (y[1] == 0).all() and y[[0, 2]].isfinite().all()
