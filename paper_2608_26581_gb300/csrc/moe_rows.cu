@@ -13,8 +13,13 @@
 // gather 35.5 us (91% of the copy rate), combine 26 us (86%), quantize with its
 // residual 26 us (70%: a scale word of four bytes takes a transaction of its
 // own; without those stores it takes 22).  combine_grad of 3001 tokens of 6
-// pairs, 1000 fp32: 25.9 us (91%).  Rows of no whole 16-byte words go in 8-, 4-
-// or 2-byte vectors (combine of 4096 x 4 x 1023 in fp32 57%, in bf16 25%).
+// pairs, 1000 fp32: 25.9 us (91%); of the 4096 tokens, bf16, 59.6 (87%).
+// Combine of 32 tokens: 2.1 us, latency.
+// Rows of no whole 16-byte words go in 8-, 4- or 2-byte vectors: 4096 tokens of 4
+// pairs, groups on 16 rows, gather of 1023 fp32 17.7 us (77%), bf16 13.4 (51%), of
+// 1020 bf16 9.0 (76%); combine of 1023 fp32 32.7 us (38%), 1022 fp32 18.8 (66%),
+// 1023 bf16 25.0 (25%), 1020 bf16 11.6 (54%); combine_grad of 1023 fp32 28.1 us
+// (84%), bf16 20.6 (57%).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

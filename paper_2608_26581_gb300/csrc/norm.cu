@@ -25,12 +25,23 @@
 // backward 166 us with both sums, 89% (148 us without weights and sums: the
 // partial sums of 304 blocks, 12 MB there and back, and their kernel take 8 of
 // the 18, the weights' loads the rest).  Issue slots are 65% busy at that.
-// Heads of 128: forward 87%, backward 95%.  fp32 rows of 4096: 87 and 89%.
-// Slower are rows beyond 5120 elements backwards (bf16 8192: 77%, 9216: 70%,
-// 13824: 61%, fp32 8192: 92%, 9216: 88%, 13824: 69%: one block on an SM, beyond
-// 8192 the row is read from shared memory twice), and rows of words, through
-// instructions (1023 elements, fp32: 67 and 73%, bf16: 35 and 39%; words by
-// cp.async took longer, 45 us instead of 29 for the first).
+// At 16384 rows: 32 heads of 128 bf16 forward 83%, backward 92% (fp32 89 and
+// 98%); 4096 elements bf16 80 and 81% (fp32 83 and 89%).
+// Slower are, at floors of 59.5 us (2^26 elements of bf16, 2^25 of fp32), rows
+// beyond 5120 elements backwards: bf16 8192 77%, 9216 70%, 13824 61%, fp32 8192
+// 92%, 9216 88%, 13824 69%: one block on an SM, beyond 8192 the row is read from
+// shared memory twice.  And backwards, calls as large as a prompt: the partial
+// sums are 7 to 12 MB whatever the rows, their kernel has a block for 64 columns,
+// and both sums are kept where one is asked for.  RMS with a weight, bf16: 4096
+// rows of 2048 17.3 us of 7.4, 8192 of 1024 18.7 of 7.5, 1531 of 4096 15.5 of 5.6,
+// 2000 of 5120 20.0 of 9.1; 700 of 5120 fp32 17.5 of 6.4; 4096 of 32 heads of 128
+// 22.0 of 15.0.  (Forward, 4096 of 2048: 5.7 of 5.0; one to 32 rows: 2.3, latency.)
+// Rows of words are bound by instructions: 65536 rows of 1023 fp32 78% forward
+// and 89% backward, bf16 38 and 41%, 54123 of 620 bf16 37 and 33%; 16384 rows of
+// 1023 fp32 72 and 73%, bf16 35 and 36% (words by cp.async took longer, 45 us
+// instead of 29 for the first of these).
+// The narrow backward kernels of blocks of 1024 threads (64 registers) spill 56 to
+// 192 bytes, and the forward one of 16-byte bf16 rows that take a block 8.
 // (Measured and not kept: tiles of several rows gone through twice, first by
 // rows, then by columns, 188 us backwards; weights in shared memory, 197; the
 // next row asked for after this one's sums, 184 to 220; weights loaded ahead of
