@@ -10,6 +10,10 @@ from fake_kernels import FakeKernels
 from paper_2608_26581_gb300 import rfq
 
 
+# lengths of rows: all short ones, a spread of the others, and those at which a kernel changes
+LENGTHS = [*range(1, 1100), *range(1100, 16385, 61), 2048, 2049, 2560, 2561, 4096, 4097, 4104, 5120, 5121, 5128, 8192, 8193, 8200, 12288, 12289, 12296, 16383, 16384]
+
+
 @pytest.fixture(scope="module")
 def fake(tmp_path_factory):
     return FakeKernels(tmp_path_factory.mktemp("fake"))
@@ -107,7 +111,7 @@ def test_every_norm_kernel_is_reached(fake):
     compiled = {k for k in fake.kernels() if "norm_kernel" in k or "norm_grad_kernel" in k or "norm_sum_kernel" in k}
     start, n = fake.lib.fake_launched(), fake.lib.fake_launches()
     made = []                                # (dim, whether rows are narrow) of each launch
-    for dim in range(1, 16385):
+    for dim in LENGTHS:
         for dtype, words in ((0, 4), (1, 8)):
             for stride in {-(-dim // words) * words, -(-dim // words) * words + 1}:
                 narrow = (stride | dim) % words != 0
@@ -135,7 +139,7 @@ def test_workspace_of_the_norms_gradient(fake):
     for device in (0, 1):
         fake.device(device)
         full = set()
-        for dim in [*range(1, 1100), *range(1100, 16385, 61), 8192, 8193, 8200, 12288, 12289, 12296, 16383, 16384]:
+        for dim in LENGTHS:
             padded, have = -(-dim // 4) * 4, fake.lib.rfq_norm_grad_workspace_bytes(dim)
             for dtype, words in ((0, 4), (1, 8)):
                 for stride in {-(-dim // words) * words, dim + 1 - dim % 2}:
